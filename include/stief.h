@@ -47,7 +47,8 @@ enum stief_status {
   STIEF_ERR_CUDA = 4,         /* a CUDA runtime/driver call failed (cudaGetLastError is left readable) */
   STIEF_ERR_BOUNDS = 5,       /* device-side: page id or position out of range (status word only)      */
   STIEF_ERR_TIMEOUT = 6,      /* device-side: a bounded wait on an async copy ran out (status word)    */
-  STIEF_ERR_INFEASIBLE = 7    /* rank selection: no candidate pair fits the budget at some layer       */
+  STIEF_ERR_INFEASIBLE = 7,   /* rank selection: no candidate pair fits the budget at some layer       */
+  STIEF_ERR_NO_PAGES = 8      /* device-side: fewer free pages than a page call needs (status word only) */
 };
 
 #define STIEF_PAGE 64
@@ -384,6 +385,102 @@ int stief_mq_attention(const stief_layer* layer, const stief_batch* batch, const
                        int64_t q_stride_t, int32_t n_q, const int32_t* q_lens, void* workspace, size_t workspace_bytes,
                        int32_t num_splits, uint16_t* out, int64_t out_stride_b, int64_t out_stride_t, float* out_lse,
                        uint32_t flags, int32_t* status, void* stream);
+
+/* ---- attention of a tree of drafted tokens over the cache (speculative decode) ---------------------------------
+ * Like stief_mq_attention, but the new tokens form a tree instead of a run: node i of sequence b attends the whole
+ * context, positions 0 .. seq_lens[b] - 1, and those drafted nodes whose bit is set in its mask row (its ancestors and
+ * itself, for a tree; any set of nodes is allowed).  seq_lens counts the context only; node j's compressed row sits at
+ * position seq_lens[b] + j (stief_append_chunk with ends_at_len = 0 puts it there, and the pages must be assigned).  A row
+ * that sees nothing (empty context and empty mask row) gives zeros and lse = -inf.
+ *   q          device bf16 [B][n_q][Hq][d_q], strides as in stief_mq_attention
+ *   n_q        nodes per sequence in q, the mask and out (1 .. STIEF_TREE_MAX_NODES)
+ *   n_nodes    device int32 [B] or NULL: how many of them are real (clamped to 0 .. n_q); rows behind are neither read,
+ *              computed nor written, and nobody attends them.  NULL = n_q everywhere
+ *   tree_mask  device uint32 [B][n_q][mask_words], mask_words >= ceil(n_q / 32): bit j % 32 of word j / 32 of row i = node i
+ *              attends node j; bits of nodes that are not real are ignored
+ *   workspace  device, 128-byte aligned, stief_tree_workspace_bytes(...) bytes, contents irrelevant on entry; calls that share
+ *              it must not overlap on the GPU
+ *   out        device bf16 [B][n_q][Hq][d_out];  out_lse optional fp32 [B][n_q][Hq];  flags must be 0
+ * Any number of query heads per KV head.  q' = q U_k and the probabilities pass through bf16, scores, sums and the mix keep
+ * fp32 accuracy.  A sequence whose context and nodes do not fit its block table sets STIEF_ERR_BOUNDS and is skipped. */
+#define STIEF_TREE_MAX_NODES 1024
+size_t stief_tree_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t r_v);
+int stief_tree_attention(const stief_layer* layer, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b,
+                         int64_t q_stride_t, int32_t n_q, const int32_t* n_nodes, const uint32_t* tree_mask,
+                         int32_t mask_words, void* workspace, size_t workspace_bytes, uint16_t* out, int64_t out_stride_b,
+                         int64_t out_stride_t, float* out_lse, uint32_t flags, int32_t* status, void* stream);
+
+/* Keeps the accepted nodes of every sequence's tree: row accepted[b][j] of the draft moves to position seq_lens[b] + j, for
+ * j < n_accepted[b], in the key and value pools of all layers (layers_host: HOST array of descriptors with the same Hkv and
+ * num_pages; bases are not used).  accepted: device int32 [B][max_accept], strictly increasing in j (a path from the root
+ * is, when nodes are numbered parents first); n_accepted: device int32 [B].  A sequence whose list is not increasing or
+ * leaves the block table sets STIEF_ERR_BOUNDS and keeps its rows.  The caller then advances its lengths
+ * (stief_advance_seq_lens_by); rejected rows lie behind the new end and are overwritten by the next draft. */
+int stief_tree_accept(const stief_layer* layers_host, int32_t n_layers, const stief_batch* batch, const int32_t* accepted,
+                      int32_t max_accept, const int32_t* n_accepted, int32_t* status, void* stream);
+
+/* seq_lens[b] += deltas[b] on the device. */
+int stief_advance_seq_lens_by(int32_t* seq_lens, const int32_t* deltas, int32_t B, void* stream);
+
+/* ---- causal attention over whole prompts, before they are compressed --------------------------------------------
+ * B prompts of different lengths packed behind one another: tokens cu_seqlens[b] .. cu_seqlens[b+1] - 1 are prompt b
+ * (device int32 [B + 1]; empty prompts are allowed).  out_i = softmax(q_i K[first .. i]^T / sqrt(128)) V[first .. i] per query
+ * head, query head g reading KV head g / (Hq / Hkv).  The K and V given here are what stief_prefill_compress takes next.
+ *   q, k, v    device bf16 [total_tokens][heads][128]: heads and elements contiguous, element strides between tokens free
+ *              (multiples of 8, rows 16-byte aligned), so views of one fused projection serve as they are
+ *   out        device bf16 [total_tokens][Hq][128]; rows of tokens that belong to no prompt are left as they are, and
+ *              whatever such rows of q, k, v hold (NaN included) influences nothing
+ *   out_lse    optional device fp32 [total_tokens][Hq]: natural-log sum-exp of each row's scaled scores
+ * The probabilities pass through bf16; scores, sums and the mix are fp32.  A prompt with a negative length or outside
+ * 0 .. total_tokens sets STIEF_ERR_BOUNDS and is skipped.  B <= 1024; flags must be 0.  A NaN or infinity in a value row
+ * reaches every row of its prompt that attends it, and may reach up to 127 rows before it. */
+int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tokens, const int32_t* cu_seqlens,
+                           const uint16_t* q, int64_t q_stride_t, const uint16_t* k, int64_t k_stride_t, const uint16_t* v,
+                           int64_t v_stride_t, uint16_t* out, int64_t out_stride_t, float* out_lse, uint32_t flags,
+                           int32_t* status, void* stream);
+
+/* ---- pages of the cache: taking, forking, reordering, copying, freeing ---------------------------------------------
+ * The other entry points only read block_table and seq_lens; these calls write them, on the device, so that a captured step
+ * can take and give back pages.  Slot b of the batch holds pages block_table[b][0 .. page_counts[b]); ref_counts[p] is the
+ * number of slots that hold page p, and a page is free when that is 0.  The lowest-numbered free page is always taken first,
+ * for the lowest slot first.  Only full pages are ever shared, so appending never writes a page of another slot.
+ * Table entries at or behind page_counts[b] are left as they are. */
+typedef struct stief_page_table {
+  int32_t B, max_pages_per_seq, num_pages;
+  int32_t* block_table; /* [B][max_pages_per_seq] */
+  int32_t* seq_lens;    /* [B] */
+  int32_t* page_counts; /* [B] */
+  int32_t* ref_counts;  /* [num_pages] */
+} stief_page_table;
+
+/* One pool whose pages lie page_bytes apart (a multiple of 16), page 0 at base (16-byte aligned): a key or value pool of any
+ * layer, the code pools and v_params of a quantised layer.  k_params have no pages. */
+typedef struct stief_page_pool {
+  void* base;
+  int64_t page_bytes;
+} stief_page_pool;
+
+/* Gives every slot the pages it lacks to take extra[b] more tokens (device int32 [B], or NULL: extra_all for every slot)
+ * behind seq_lens[b].  Too few free pages: STIEF_ERR_NO_PAGES in the status word, the lowest slots having got theirs.  A slot
+ * that would outgrow max_pages_per_seq gets none and sets STIEF_ERR_BOUNDS. */
+int stief_pages_reserve(const stief_page_table* table, const int32_t* extra, int32_t extra_all, int32_t* status, void* stream);
+
+/* Slot b becomes a copy of what slot parent[b] is at the time of the call (device int32 [B]; parent[b] = b: it stays as it is,
+ * -1: it becomes empty and its pages are released), for all slots at once: the reordering of a beam search, a fork into
+ * empty slots, and the freeing of finished sequences.  Full pages are shared.  One child takes the parent's pages over as
+ * they are, reserved ones included: the parent itself if it stays, else the lowest-numbered; every other child gets a
+ * page of its own for a partial last page, copied in all n_pools pools (pools_host: HOST array).  When pages run out
+ * (STIEF_ERR_NO_PAGES) such a child ends at its last full page.  A parent outside -1 .. B - 1: STIEF_ERR_BOUNDS, the slot stays.
+ * workspace: device, 128-byte aligned, stief_pages_workspace_bytes(B, max_pages_per_seq) bytes, contents irrelevant; calls that
+ * share it must not overlap on the GPU. */
+size_t stief_pages_workspace_bytes(int32_t B, int32_t max_pages_per_seq);
+int stief_pages_fork(const stief_page_table* table, const stief_page_pool* pools_host, int32_t n_pools, const int32_t* parent,
+                     void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* Page src[i] -> page dst[i] for i < n in every pool (device int32 [n] each).  No page may be written twice, nor read and
+ * written, in one call.  An id outside 0 .. num_pages - 1 sets STIEF_ERR_BOUNDS and that pair is skipped. */
+int stief_pages_copy(const stief_page_pool* pools_host, int32_t n_pools, int32_t num_pages, const int32_t* src,
+                     const int32_t* dst, int32_t n, int32_t* status, void* stream);
 
 /* ---- rank selection (host only) --------------------------------------------------------------------------
  * Sequential budgeted rank selection, Algorithm 2 of the paper (Sec. 3.4, Eq. 15-17; cost c = (r_K + r_V) / (2 d_h),

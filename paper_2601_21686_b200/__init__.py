@@ -19,7 +19,9 @@ LIB_PATH = os.path.join(_PKG, "libstief.so")
 
 STIEF_OK, STIEF_ERR_INVALID_ARG, STIEF_ERR_UNSUPPORTED, STIEF_ERR_WORKSPACE = 0, 1, 2, 3
 STIEF_ERR_CUDA, STIEF_ERR_BOUNDS, STIEF_ERR_TIMEOUT, STIEF_ERR_INFEASIBLE = 4, 5, 6, 7
+STIEF_ERR_NO_PAGES = 8
 PAGE = 64
+TREE_MAX_NODES = 1024
 D_HEAD = 128
 STIEF_DECODE_OVERLAP_PREVIOUS = 1
 STIEF_PREFILL_OVERLAP_PREVIOUS = 1
@@ -53,6 +55,16 @@ class _CBatch(ctypes.Structure):
                 ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
 
 
+class _CPageTable(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("page_counts", ctypes.c_void_p),
+                ("ref_counts", ctypes.c_void_p)]
+
+
+class _CPagePool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
+
+
 _SURFACE_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32),
                                ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_double))
 
@@ -69,6 +81,7 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         P, I32, I64, SZ, U32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_uint32
         LP, BP, QP = ctypes.POINTER(_CLayer), ctypes.POINTER(_CBatch), ctypes.POINTER(_CQLayer)
+        TP = ctypes.POINTER(_CPageTable)
         sig = {
             "stief_prefill_compress": (ctypes.c_int, [LP, BP, P, P, I64, I64, I64, I64, I32, U32, P, P]),
             "stief_append": (ctypes.c_int, [LP, BP, P, P, P, P]),
@@ -95,6 +108,15 @@ def lib() -> ctypes.CDLL:
             "stief_mq_attention": (ctypes.c_int, [LP, BP, P, I64, I64, I32, P, P, SZ, I32, P, I64, I64, P, U32, P, P]),
             "stief_mq_num_splits": (I32, [I32, I32, I32, I32, I32]),
             "stief_mq_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
+            "stief_tree_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
+            "stief_tree_attention": (ctypes.c_int, [LP, BP, P, I64, I64, I32, P, P, I32, P, SZ, P, I64, I64, P, U32, P, P]),
+            "stief_tree_accept": (ctypes.c_int, [P, I32, BP, P, I32, P, P, P]),
+            "stief_advance_seq_lens_by": (ctypes.c_int, [P, P, I32, P]),
+            "stief_prompt_attention": (ctypes.c_int, [I32, I32, I32, I32, P, P, I64, P, I64, P, I64, P, I64, P, U32, P, P]),
+            "stief_pages_workspace_bytes": (SZ, [I32, I32]),
+            "stief_pages_reserve": (ctypes.c_int, [TP, P, I32, P, P]),
+            "stief_pages_fork": (ctypes.c_int, [TP, P, I32, P, P, SZ, P, P]),
+            "stief_pages_copy": (ctypes.c_int, [P, I32, I32, P, P, I32, P, P]),
             "stief_select_ranks": (ctypes.c_int, [I32, I32, P, I32, P, I32, ctypes.c_double, P, _SURFACE_FN, P, P, P, P, P]),
             "stief_selftest_wait_limit": (ctypes.c_int, [P, P, I32, P]),
             "stief_trace_next_decode_kernel": (ctypes.c_int, [P, SZ]),
@@ -193,6 +215,54 @@ class Batch:
         st = _CBatch(self.block_table.shape[0], self.block_table.shape[1], _ptr(self.block_table), _ptr(self.seq_lens))
         self.__dict__["_c"] = (key, st)
         return st
+
+
+@dataclass
+class PageTable:
+    """Paging state that the page calls write (device int32 tensors): block_table [B, max_pages_per_seq], seq_lens [B],
+    page_counts [B] (pages each slot holds), ref_counts [num_pages] (slots that hold each page, 0 = free).  The
+    ``batch`` of the attention and append calls shares block_table and seq_lens with it."""
+    block_table: torch.Tensor
+    seq_lens: torch.Tensor
+    page_counts: torch.Tensor
+    ref_counts: torch.Tensor
+
+    @property
+    def batch(self) -> "Batch":
+        return Batch(self.block_table, self.seq_lens)
+
+    def c(self) -> _CPageTable:
+        key = (_ptr(self.block_table), _ptr(self.seq_lens), _ptr(self.page_counts), _ptr(self.ref_counts),
+               tuple(self.block_table.shape), self.ref_counts.shape[0])
+        cached = self.__dict__.get("_c")
+        if cached is not None and cached[0] == key:
+            return cached[1]
+        for t in (self.block_table, self.seq_lens, self.page_counts, self.ref_counts):
+            _int32(t, "page table")
+        B = self.block_table.shape[0]
+        if self.block_table.dim() != 2 or self.seq_lens.shape != (B,) or self.page_counts.shape != (B,):
+            raise ValueError("block_table [B, max_pages], seq_lens [B] and page_counts [B] disagree")
+        st = _CPageTable(B, self.block_table.shape[1], self.ref_counts.shape[0], _ptr(self.block_table), _ptr(self.seq_lens),
+                         _ptr(self.page_counts), _ptr(self.ref_counts))
+        self.__dict__["_c"] = (key, st)
+        return st
+
+
+def _here(t: torch.Tensor, name: str) -> torch.Tensor:
+    """The kernels run on torch's current device and stream: a tensor of another device is refused."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
+    return t
+
+
+def _int32(t: torch.Tensor, name: str, shape=None) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must be a contiguous int32 tensor" + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return _here(t, name)
+
+
+def _status(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else _int32(t, "status").data_ptr()
 
 
 def _check(rc: int, where: str):
@@ -416,6 +486,140 @@ def stief_mq_attention(layer: Layer, batch: Batch, q: torch.Tensor, out: torch.T
     _check(lib().stief_mq_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), _ptr(q), q.stride(0), q.stride(1),
                                     q.shape[1], _ptr(q_lens), _ptr(workspace), ws_bytes, num_splits, _ptr(out), out.stride(0),
                                     out.stride(1), _ptr(out_lse), flags, _ptr(status), _stream()), "stief_mq_attention")
+
+
+def stief_tree_workspace_bytes(B: int, n_q: int, Hq: int, Hkv: int, r_v: int) -> int:
+    return lib().stief_tree_workspace_bytes(B, n_q, Hq, Hkv, r_v)
+
+
+def stief_tree_attention(layer: Layer, batch: Batch, q: torch.Tensor, tree_mask: torch.Tensor, workspace: torch.Tensor,
+                         out: torch.Tensor, n_nodes: Optional[torch.Tensor] = None, out_lse: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None, flags: int = 0):
+    """A tree of drafted tokens over the cache: q [B, n_q, Hq, d_q] bf16 -> out [B, n_q, Hq, d_out] bf16 (strides over b and t
+    free).  seq_lens is the context; node j is cached at position seq_lens[b] + j.  tree_mask [B, n_q, words] int32: bit j of
+    row i = node i attends node j.  n_nodes [B] int32: real nodes per sequence (default n_q)."""
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.dim() != 4 or out.dim() != 4:
+        raise ValueError("q and out must be bf16 [B, n_q, Hq, d]")
+    B, n_q, Hq, d_q = q.shape
+    d_out = D_HEAD if layer.U_v is not None else layer.r_v
+    if Hq != layer.Hq or d_q != (D_HEAD if layer.U_k is not None else layer.r_k) or tuple(out.shape) != (B, n_q, Hq, d_out) or B != batch.block_table.shape[0]:
+        raise ValueError("q, out, layer and batch disagree in shape")
+    if q.stride(3) != 1 or q.stride(2) != d_q or out.stride(3) != 1 or out.stride(2) != d_out:
+        raise ValueError("heads and elements of q and out must be contiguous")
+    _int32(tree_mask, "tree_mask")
+    if tree_mask.dim() != 3 or tuple(tree_mask.shape[:2]) != (B, n_q):
+        raise ValueError("tree_mask must be [B, n_q, words]")
+    if n_nodes is not None:
+        _int32(n_nodes, "n_nodes", (B,))
+    if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (B, n_q, Hq)):
+        raise ValueError("out_lse must be contiguous fp32 [B, n_q, Hq]")
+    for t, name in ((q, "q"), (out, "out"), (workspace, "workspace"), (layer.k_pool, "k_pool"), (batch.block_table, "block_table")):
+        _here(t, name)
+    _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), _ptr(q), _row_stride(q, 0), _row_stride(q, 1), n_q,
+                                      _ptr(n_nodes), _ptr(tree_mask), tree_mask.shape[2], _ptr(workspace),
+                                      workspace.numel() * workspace.element_size(), _ptr(out), _row_stride(out, 0), _row_stride(out, 1),
+                                      _ptr(out_lse), flags, _status(status), _stream()), "stief_tree_attention")
+
+
+def _row_stride(t: torch.Tensor, dim: int) -> int:
+    """Element stride of a leading dimension; one of extent 1 may carry any stride and gets the packed one."""
+    return t.stride(dim) if t.shape[dim] > 1 else max(t.stride(dim), t.stride(dim + 1) * t.shape[dim + 1])
+
+
+def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Tensor, n_accepted: torch.Tensor,
+                      status: Optional[torch.Tensor] = None):
+    """Moves the cache rows of the accepted nodes to the end of the context, in all layers: node accepted[b, j] goes to
+    position seq_lens[b] + j for j < n_accepted[b].  accepted [B, max_accept] int32, strictly increasing along j."""
+    B = batch.block_table.shape[0]
+    _int32(n_accepted, "n_accepted", (B,))
+    _int32(accepted, "accepted")
+    if accepted.dim() != 2 or accepted.shape[0] != B:
+        raise ValueError("accepted must be [B, max_accept]")
+    _here(batch.block_table, "block_table")
+    arr = (_CLayer * max(len(layers), 1))(*[_here_layer(l).c() for l in layers])
+    _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), _ptr(accepted), accepted.shape[1], _ptr(n_accepted),
+                                   _status(status), _stream()), "stief_tree_accept")
+
+
+def _here_layer(layer):
+    for t in _page_tensors(layer):
+        _here(t, "pool")
+    return layer
+
+
+def stief_advance_seq_lens_by(seq_lens: torch.Tensor, deltas: torch.Tensor):
+    _int32(deltas, "deltas", _int32(seq_lens, "seq_lens").shape)
+    _check(lib().stief_advance_seq_lens_by(_ptr(seq_lens), _ptr(deltas), seq_lens.numel(), _stream()), "stief_advance_seq_lens_by")
+
+
+def stief_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
+                           out_lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, flags: int = 0):
+    """Causal attention over packed prompts: q [total, Hq, 128], k, v [total, Hkv, 128], out [total, Hq, 128] bf16 (strides
+    over tokens free), cu_seqlens [B + 1] int32, out_lse [total, Hq] fp32."""
+    total, Hq, Hkv = q.shape[0], q.shape[1], k.shape[1]
+    for t, name, heads in ((q, "q", Hq), (k, "k", Hkv), (v, "v", Hkv), (out, "out", Hq)):
+        if t.dtype != torch.bfloat16 or tuple(t.shape) != (total, heads, D_HEAD) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D_HEAD):
+            raise ValueError(f"{name} must be bf16 [{total}, {heads}, {D_HEAD}] with contiguous heads and elements")
+        _here(t, name)
+    _int32(cu_seqlens, "cu_seqlens")
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+        raise ValueError("cu_seqlens must be [B + 1]")
+    if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (total, Hq)):
+        raise ValueError("out_lse must be contiguous fp32 [total, Hq]")
+    row = lambda t: t.stride(0) if total > 1 else max(t.stride(0), t.shape[1] * D_HEAD)
+    _check(lib().stief_prompt_attention(Hq, Hkv, cu_seqlens.numel() - 1, total, _ptr(cu_seqlens), _ptr(q), row(q), _ptr(k), row(k), _ptr(v),
+                                        row(v), _ptr(out), row(out), _ptr(out_lse), flags, _status(status), _stream()),
+           "stief_prompt_attention")
+
+
+def _page_tensors(layer):
+    if isinstance(layer, QLayer):
+        return (layer.k_codes, layer.v_codes, layer.v_params)
+    return (layer.k_pool, layer.v_pool)
+
+
+def _page_pools(layers):
+    """C array of every pool of the layers (Layer or QLayer), checked to hold the same pages."""
+    tensors = [t for l in layers for t in _page_tensors(l)]
+    for t in tensors:
+        if not t.is_contiguous() or t.shape[0] != tensors[0].shape[0]:
+            raise ValueError("pools must be contiguous and have the same number of pages")
+        _here(t, "pool")
+    arr = (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
+    return arr, len(tensors), tensors[0].shape[0] if tensors else 0
+
+
+def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:
+    return lib().stief_pages_workspace_bytes(B, max_pages_per_seq)
+
+
+def stief_pages_reserve(table: PageTable, extra, status: Optional[torch.Tensor] = None):
+    """Pages for ``extra`` more tokens behind every slot's sequence: an int for all, or an int32 tensor [B]."""
+    per_slot = isinstance(extra, torch.Tensor)
+    if per_slot:
+        _int32(extra, "extra", (table.block_table.shape[0],))
+    _check(lib().stief_pages_reserve(ctypes.byref(table.c()), _ptr(extra) if per_slot else None, 0 if per_slot else int(extra),
+                                     _status(status), _stream()), "stief_pages_reserve")
+
+
+def stief_pages_fork(table: PageTable, layers, parent: torch.Tensor, workspace: torch.Tensor, status: Optional[torch.Tensor] = None):
+    """Slot b becomes a copy of slot parent[b] (int32 [B]; b = unchanged, -1 = emptied).  ``layers``: every Layer / QLayer whose
+    pools this table pages."""
+    _int32(parent, "parent", (table.block_table.shape[0],))
+    arr, n, num_pages = _page_pools(layers)
+    if n and num_pages < table.ref_counts.shape[0]:
+        raise ValueError("the table counts more pages than the pools hold")
+    _here(workspace, "workspace")
+    _check(lib().stief_pages_fork(ctypes.byref(table.c()), arr, n, _ptr(parent), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _status(status), _stream()), "stief_pages_fork")
+
+
+def stief_pages_copy(layers, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None):
+    """Page src[i] -> page dst[i] (int32 [n]) in every pool of the layers."""
+    _int32(src, "src")
+    _int32(dst, "dst", src.shape)
+    arr, n, num_pages = _page_pools(layers)
+    _check(lib().stief_pages_copy(arr, n, num_pages, _ptr(src), _ptr(dst), src.numel(), _status(status), _stream()), "stief_pages_copy")
 
 
 def stief_append_chunk(layer: Layer, batch: Batch, K: torch.Tensor, V: torch.Tensor, chunk_lens: Optional[torch.Tensor] = None,

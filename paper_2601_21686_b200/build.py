@@ -31,7 +31,8 @@ def _nvcc() -> str:
 def _units():
     """(source, object, extra flags) for every translation unit."""
     units = [(os.path.join(CSRC, f + ".cu"), os.path.join(OBJ, f + ".o"), [])
-             for f in ("stief_api", "stief_small", "stief_prefill", "stief_prefill_tc", "stief_noalloc", "stief_quant", "stief_rank_select", "stief_mq", "stief_selftest")
+             for f in ("stief_api", "stief_small", "stief_prefill", "stief_prefill_tc", "stief_noalloc", "stief_quant", "stief_rank_select", "stief_mq", "stief_selftest",
+                       "stief_tree", "stief_prompt", "stief_pages")
              if os.path.exists(os.path.join(CSRC, f + ".cu"))]
     for rk in KEY_RANKS:
         units.append((os.path.join(CSRC, "stief_decode_inst.cu"), os.path.join(OBJ, f"stief_decode_rk{rk}.o"),

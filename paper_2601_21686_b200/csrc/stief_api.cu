@@ -451,6 +451,7 @@ const char* stief_status_string(int status) {
     case STIEF_ERR_BOUNDS: return "page id or position out of range (device)";
     case STIEF_ERR_TIMEOUT: return "bounded device-side wait ran out";
     case STIEF_ERR_INFEASIBLE: return "no candidate rank pair fits the budget";
+    case STIEF_ERR_NO_PAGES: return "not enough free pages (device)";
     default: return "unknown status";
   }
 }
