@@ -39,7 +39,7 @@
 #include <type_traits>
 
 #include "stief_kernels.h"
-#include "stief_tc.cuh"
+#include "stief_softmax.cuh"
 
 #ifndef STIEF_MQ_POLY_EVERY
 #define STIEF_MQ_POLY_EVERY 4
@@ -142,53 +142,6 @@ __device__ __forceinline__ Unit decode_unit(const Args& a, int u, int TT) {
   }
   w.valid = w.cnt != 0;                          // a part may be empty when there are fewer pages than parts
   return w;
-}
-
-// packed fp32 pairs (sm_100): one instruction for two lanes of arithmetic
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-// 2^x for a pair of x in [-125, 16] on the FMA pipe: x = n + f with n = rint(x) (the 1.5 * 2^23 trick leaves n in the low
-// mantissa bits of t), 2^f by a cubic fitted to [-0.5, 0.5] (relative error 7.5e-5, far below the bf16 rounding of
-// the probabilities), 2^n by adding n to the exponent field.  The special-function pipe does 16 ex2 per clock and SM,
-// which at 64 of them per score row and page is this kernel's tightest unit; a quarter of the exponentials go here.
-__device__ __forceinline__ void exp2_pair_fma(uint64_t x2, float& e0, float& e1) {
-  const uint64_t magic = pack2(12582912.f, 12582912.f), neg_magic = pack2(-12582912.f, -12582912.f);
-  const uint64_t t = add2(x2, magic);
-  const uint64_t n = add2(t, neg_magic);
-  const uint64_t f = fma2(n, pack2(-1.f, -1.f), x2);
-  uint64_t q = fma2(f, pack2(0.05517145f, 0.05517145f), pack2(0.24261084f, 0.24261084f));
-  q = fma2(q, f, pack2(0.69326097f, 0.69326097f));
-  q = fma2(q, f, pack2(0.99992812f, 0.99992812f));
-  float t0, t1, q0, q1;
-  unpack2(t, t0, t1);
-  unpack2(q, q0, q1);
-  e0 = __int_as_float(__float_as_int(q0) + (__float_as_int(t0) << 23));
-  e1 = __int_as_float(__float_as_int(q1) + (__float_as_int(t1) << 23));
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
-// 16 fp32 values of a row -> 8 packed bf16 words
-__device__ __forceinline__ void pack16(const uint32_t (&v)[16], float scale, uint32_t (&w)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]) * scale, __uint_as_float(v[2 * i + 1]) * scale);
 }
 
 // The ranks are template parameters: the descriptor offsets and K-step counts of the MMA role are then constants,
