@@ -1,0 +1,499 @@
+// Attention of a tree of drafted tokens over the compressed cache (stief_tree_attention).  Node i of sequence b attends the
+// context, positions 0 .. ctx_b - 1, and the drafted nodes in its mask row, whose rows are cached behind the context:
+//   out_i = softmax(q_i' K_down[S_i]^T / sqrt(128)) V_down[S_i] U_v^T,   q_i' = q_i U_k.
+// A tree has few query rows (nodes x heads of the group) and a long cache, so the cache is what has to be streamed: every
+// row of it once per (sequence, KV head).  Three launches, each started while the one before it still runs:
+//   project_kernel   q' = q U_k in fp32, rounded once to bf16, rows packed per (sequence, KV head)
+//   tree_kernel      one persistent CTA per SM.  A unit is (sequence, KV head, up to 256 query rows); the units' blocks of 128
+//                    positions lie end to end on one axis (each unit preceded by kPad blocks' worth of start-up cost) and
+//                    every CTA takes an equal range of it, so that ragged lengths and few units fill the GPU alike.  What a
+//                    CTA finds in one unit, a segment, leaves a partial result: unnormalised mix, reference, sum.
+//   combine_kernel   joins the segments of 16 rows (log-sum-exp), normalises, back-projects and writes them.
+//
+// tree_kernel, 384 threads: two row tiles of 128 rows.  With at most 128 rows both tiles hold the SAME rows and take
+// alternate blocks (two independent softmax streams, joined like segments): one stream is bound by the latency of its chain
+// scores -> softmax -> P V.  With more, each tile has its own rows and both use every block.
+//   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
+//   warp 8          cache pages by TMA into a ring, a stage = K page | V page of one KV head
+//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page), O += P V (N = r_v), P in TMEM over S
+//   warp 11         Q' tiles
+// TMEM (512 columns): per tile 128 for S and 128 for O.  Everything else follows the prompt kernel (stief_prompt.cu).
+#pragma once
+
+#include "stief_softmax.cuh"
+#include "stief_tree.h"
+#include "stief_umma.cuh"
+
+namespace stief {
+namespace tree {
+
+using namespace tc;
+
+constexpr int kThreads = 384;
+constexpr int kRows = 128;                      // rows of a tile
+constexpr int kBlock = 128;                     // positions of a block: two pages
+constexpr int kSmemLimit = 232448;
+constexpr int kHeadBytes = 5120;                // prefix sums (4112), barriers (512)
+constexpr int kMaxStages = 12;
+constexpr int kTmemCols = 512;
+constexpr float kRescaleLog2 = 8.0f;
+
+// Sequence b as every kernel sees it
+struct Seq {
+  int ctx, n, blocks, units;                    // context, nodes, blocks of positions, units per KV head (0: nothing to do)
+};
+__device__ __forceinline__ Seq sequence(const Args& a, int b) {
+  Seq s;
+  s.ctx = a.Bt.seq_lens[b];
+  s.n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.n_q) : a.n_q;
+  const bool fits = s.ctx >= 0 && ((long long)s.ctx + s.n + kPage - 1) / kPage <= a.Bt.max_pages;
+  if (!fits && s.n > 0) report(a.status, STIEF_ERR_BOUNDS);
+  if (!fits) s.n = 0;
+  s.blocks = s.n > 0 ? (s.ctx + s.n + kBlock - 1) / kBlock : 0;
+  s.units = (s.n * a.L.G + kUnitRows - 1) / kUnitRows;
+  return s;
+}
+__device__ __forceinline__ int sequence_cost(const Args& a, const Seq& s) { return a.L.Hkv * s.units * (s.blocks + kPad); }
+// First position of the axis that CTA i of n takes
+__device__ __forceinline__ int range_start(int i, int n, int total) { return (int)((long long)i * total / n); }
+__device__ __forceinline__ int cta_count(const Args& a, int total) { return min(a.n_cta, total); }
+
+struct Segment {
+  int b, h, unit, slot;                         // unit: row block within the (sequence, KV head)
+  int ctx, n, rows;                             // rows of the unit
+  int j0, cnt;                                  // blocks [j0, j0 + cnt)
+  bool dual, valid;
+};
+
+struct Walk {
+  int pos, hi, b, cta;
+  __device__ __forceinline__ void start(const Args& a, const int* pref) {
+    const int total = pref[a.Bt.B], n = cta_count(a, total);
+    cta = blockIdx.x;
+    pos = hi = b = 0;
+    if (cta < n) {
+      pos = range_start(cta, n, total);
+      hi = range_start(cta + 1, n, total);
+    }
+  }
+  __device__ __forceinline__ Segment next(const Args& a, const int* pref) {
+    Segment g;
+    g.valid = false;
+    g.cnt = 0;
+    while (pos < hi) {
+      while (pref[b + 1] <= pos) ++b;
+      const Seq s = sequence(a, b);
+      const int len = s.blocks + kPad, r = pos - pref[b], u = r / len, first = pref[b] + u * len;
+      const int end = min(hi, first + len);
+      g.j0 = max(pos - first - kPad, 0);
+      g.cnt = end - first - kPad - g.j0;
+      pos = end;
+      if (g.cnt <= 0) continue;
+      g.b = b;
+      g.h = u / s.units;
+      g.unit = u - g.h * s.units;
+      g.slot = cta + (b * a.L.Hkv + g.h) * a.max_units + g.unit;
+      g.ctx = s.ctx;
+      g.n = s.n;
+      g.rows = min(s.n * a.L.G - g.unit * kUnitRows, kUnitRows);
+      g.dual = g.rows <= kRows;
+      g.valid = true;
+      break;
+    }
+    return g;
+  }
+};
+
+// Blocks of a segment that tile t works on
+__device__ __forceinline__ int tile_blocks(const Segment& g, int t) { return g.dual ? (g.cnt + 1 - t) >> 1 : g.cnt; }
+
+// 32 positions from node index s on (negative: context): which of them a row with mask words `m` sees
+__device__ __forceinline__ uint32_t seen32(const uint32_t* m, int s, int n) {
+  if (s <= -32) return ~0u;
+  if (s >= n) return 0u;
+  uint32_t w;
+  if (s < 0) {
+    w = m[0] << -s;
+  } else {
+    const int i = s >> 5;
+    w = __funnelshift_r(m[i], (i + 1) * 32 < n ? m[i + 1] : 0u, s & 31);
+  }
+  if (n - s < 32) w &= (1u << (n - s)) - 1u;
+  return s < 0 ? w | ((1u << -s) - 1u) : w;
+}
+
+template <int RK, int RV>
+__global__ void __launch_bounds__(kThreads, 1)
+tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Args a) {
+  constexpr Blocks bk{(RK % 64 == 0) ? 64 : (RK % 32 == 0) ? 32 : 16, 0, 0, 0}, bv{(RV % 64 == 0) ? 64 : (RV % 32 == 0) ? 32 : 16, 0, 0, 0};
+  constexpr int kSpanK = 2 * bk.bw, kSpanV = 2 * bv.bw, kNbK = RK / bk.bw, kNbV = RV / bv.bw;       // see Blocks in stief_tc.cuh
+  constexpr int kLayK = kSpanK == 128 ? 2 : kSpanK == 64 ? 4 : 6, kLayV = kSpanV == 128 ? 2 : kSpanV == 64 ? 4 : 6;
+  constexpr int kPageK = kPage * RK * 2, kStageBytes = kPage * (RK + RV) * 2, kQBytes = kRows * RK * 2;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int* pref = reinterpret_cast<int*>(smem);
+  uint8_t* ctrl_ptr = smem + 4352;
+  const uint32_t ctrl = smem_u32(ctrl_ptr);
+  const uint32_t q_smem = smem_u32(smem) + kHeadBytes, ring = q_smem + 2 * kQBytes;
+  uint8_t* ring_ptr = smem + kHeadBytes + 2 * kQBytes;
+  const int nst = a.nst;
+  auto full_bar = [&](int s) { return ctrl + s * 8; };
+  auto empty_bar = [&](int s) { return ctrl + (12 + s) * 8; };
+  auto q_full = [&](int t) { return ctrl + (24 + t) * 8; };
+  auto q_empty = [&](int t) { return ctrl + (26 + t) * 8; };
+  auto s_full = [&](int t) { return ctrl + (28 + t) * 8; };
+  auto p_full = [&](int t, int half) { return ctrl + (30 + 2 * t + half) * 8; };
+  auto o_full = [&](int t) { return ctrl + (34 + t) * 8; };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + 36 * 8);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 36 * 8 + 4);
+  int32_t* status = a.status;
+  launch_dependents();
+  if (q_smem & 1023u) {                         // the swizzled tiles need it; dynamic shared memory starts there
+    report(status, STIEF_ERR_CUDA);
+    return;
+  }
+
+  for (int b = tid; b < a.Bt.B; b += kThreads) pref[b + 1] = sequence_cost(a, sequence(a, b));
+  if (tid == 0) {
+    pref[0] = 0;
+    for (int s = 0; s < kMaxStages; ++s) {
+      mbar_init(full_bar(s), 1);
+      mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer, or two from the only one that uses the page
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(q_full(t), 1);
+      mbar_init(q_empty(t), 1);
+      mbar_init(s_full(t), 1);
+      mbar_init(p_full(t, 0), 4);
+      mbar_init(p_full(t, 1), 4);
+      mbar_init(o_full(t), 1);
+    }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
+  __syncthreads();
+  if (warp == 0) {                              // running sums of the costs
+    int carry = 0;
+    for (int b0 = 0; b0 < a.Bt.B; b0 += 32) {
+      int x = b0 + lane < a.Bt.B ? pref[b0 + lane + 1] : 0;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (b0 + lane < a.Bt.B) pref[b0 + lane + 1] = carry + x;
+      carry += __shfl_sync(0xffffffffu, x, 31);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  if (blockIdx.x == 0)                          // for the combine kernel
+    for (int b = tid; b <= a.Bt.B; b += kThreads) a.prefix[b] = pref[b];
+
+  Walk walk;
+  walk.start(a, pref);
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");      // 384 x 168 registers at launch = 256 x 200 + 128 x 104
+    if (warp == 8) {
+      // ---------------------------------------------------------------------------------------- cache pages
+      if (lane == 0) {
+        tma_prefetch_desc(&tmK);
+        tma_prefetch_desc(&tmV);
+      }
+      int st = 0, use = 0;
+      for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
+        const int first = 2 * g.j0, pages = min(2 * g.cnt, (g.ctx + g.n + kPage - 1) / kPage - first);
+        const int* bt = a.Bt.block_table + (size_t)g.b * a.Bt.max_pages + first;
+        int ids = lane < pages ? bt[lane] : 0;
+        for (int j0 = 0; j0 < pages; j0 += 32) {
+          const int nxt = j0 + 32 + lane < pages ? bt[j0 + 32 + lane] : 0;     // a batch of page ids ahead
+          const int cnt = min(32, pages - j0);
+          for (int jj = 0; jj < cnt; ++jj) {
+            int pg = __shfl_sync(0xffffffffu, ids, jj);
+            if (lane == 0) {
+              if (pg < 0 || pg >= a.L.num_pages) {
+                report(status, STIEF_ERR_BOUNDS);
+                pg = 0;
+              }
+              if (use > 0) mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
+              const int row = (pg * a.L.Hkv + g.h) * kPage;
+              const uint32_t dst = ring + st * kStageBytes;
+              mbar_arrive_expect_tx(full_bar(st), kStageBytes);
+#pragma unroll
+              for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
+#pragma unroll
+              for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + kPageK + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+              if (++st == nst) {
+                st = 0;
+                ++use;
+              }
+            }
+          }
+          ids = nxt;
+        }
+      }
+    } else if (warp == 11) {
+      // ---------------------------------------------------------------------------------------- Q' tiles
+      grid_dependency_wait();                                   // project_kernel has written them, with ordinary stores
+      asm volatile("fence.proxy.async;" ::: "memory");
+      if (lane == 0) {
+        tma_prefetch_desc(&tmQ);
+        int kt[2] = {0, 0};
+        for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
+          const int row0 = (g.b * a.L.Hkv + g.h) * (a.n_q * a.L.G) + g.unit * kUnitRows;
+          for (int t = 0; t < 2; ++t) {
+            if (tile_blocks(g, t) == 0) continue;
+            if (kt[t] > 0) mbar_wait(q_empty(t), (kt[t] - 1) & 1, abort_flag, status);
+            ++kt[t];
+            mbar_arrive_expect_tx(q_full(t), kQBytes);
+#pragma unroll
+            for (int i = 0; i < kNbK; ++i)
+              tma_load_2d(q_smem + t * kQBytes + i * kRows * kSpanK, &tmQ, i * bk.bw, row0 + (g.dual ? 0 : t * kRows), q_full(t));
+          }
+        }
+      }
+    } else {
+      // ---------------------------------------------------------------------------------------- MMA issue, tile t
+      const int t = uniform(warp) - 9;
+      const uint32_t tmem_u = uniform(tmem_base) + t * 256, ring_u = uniform(ring), ctrl_u = uniform(ctrl);
+      const uint32_t qa = desc_lo(16, uniform(q_smem) + t * kQBytes);
+      constexpr uint32_t kHiK = (uint32_t)((((uint64_t)(8 * kSpanK >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayK << 61)) >> 32);
+      constexpr uint32_t kHiV = (uint32_t)((((uint64_t)(8 * kSpanV >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayV << 61)) >> 32);
+      const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_pv = idesc_bf16_f32_bmn(kRows, RV);
+      auto bar = [&](int i) { return ctrl_u + i * 8; };                        // as numbered above
+      int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next page
+      auto step = [&](int pages) {
+        st += pages;
+        if (st >= nst) {
+          st -= nst;
+          ++use;
+        }
+      };
+      // the pages of a block, and S = Q' K^T of each
+      int page_st[2];
+      auto score = [&](int pages, bool last) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          if (p < pages) {
+            mbar_wait_warp(bar(st), use & 1, abort_flag, status);
+            page_st[p] = st;
+            const uint32_t ka = desc_lo(16, ring_u + st * kStageBytes);
+            step(1);
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < RK / 16; ++k) {
+              constexpr int kPer = bk.bw / 16;                                 // K steps per swizzled block
+              const uint32_t qo = (uint32_t)((k / kPer) * kRows * kSpanK + (k % kPer) * 32) >> 4, ko = (uint32_t)((k / kPer) * kPage * kSpanK + (k % kPer) * 32) >> 4;
+              umma_ss(tmem_u + 64 * p, qa + qo, kHiK, ka + ko, kHiK, id_qk, k > 0 ? 1u : 0u);
+            }
+          }
+        }
+        umma_commit_warp(bar(28 + t));
+        if (last) umma_commit_warp(bar(26 + t));
+      };
+      for (Segment g = walk.next(a, pref); uniform((int)g.valid); g = walk.next(a, pref)) {
+        const int cnt = uniform(g.cnt), j0 = uniform(g.j0), len = uniform(g.ctx + g.n);
+        const bool dual = uniform((int)g.dual) != 0;
+        const int pages = min(2 * cnt, (len + kPage - 1) / kPage - 2 * j0);    // pages of the segment
+        const int steps = dual ? (cnt + 1 - t) >> 1 : cnt, stride = dual ? 2 : 1, at = dual ? t : 0;
+        if (steps == 0) {
+          for (int i = 0; i < pages; ++i) step(1);                             // a lone block: the other tile's
+          continue;
+        }
+        mbar_wait_warp(bar(24 + t), kt & 1, abort_flag, status);
+        if (at) step(2);
+        score(min(2, pages - 2 * at), steps == 1);
+        for (int s = 0; s < steps; ++s) {
+          const int here = min(2, pages - 2 * (at + s * stride)), cur[2] = {page_st[0], page_st[1]};
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
+            tc_fence_after();
+            if (p < here) {
+              const uint32_t va = desc_lo(kPage * kSpanV, ring_u + cur[p] * kStageBytes + kPageK);
+#pragma unroll
+              for (int k = 0; k < kPage / 16; ++k)
+                umma_ts(tmem_u + 128, tmem_u + 32 * p + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || p > 0 || k > 0 ? 1u : 0u);
+            }
+          }
+          ++n;
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (p < here) {
+              umma_commit_warp(bar(12 + cur[p]));
+              if (dual) umma_commit_warp(bar(12 + cur[p]));
+            }
+          if (s + 1 < steps) {
+            if (dual) step(2);                                                 // the other tile's block between
+            score(min(2, pages - 2 * (at + (s + 1) * stride)), s + 2 == steps);
+          } else {
+            umma_commit_warp(bar(34 + t));
+          }
+        }
+        if (dual) {                                                            // blocks behind this tile's last
+          const int done = 2 * (at + (steps - 1) * 2) + 2;
+          for (int i = done; i < pages; ++i) step(1);
+        }
+        ++kt;
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------------------------------ softmax, partial results
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    const int t = warp >> 2, q4 = warp & 3, row = 32 * q4 + lane;
+    const uint32_t t_s = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256, t_o = t_s + 128;
+    const float c = kLog2e * rsqrtf((float)kD);
+    int n = 0, kt = 0, ring_page = 0;                           // blocks and segments of this tile so far; pages of both
+    auto arrive_warp = [&](uint32_t bar) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
+      const int len = g.ctx + g.n, page0 = ring_page;
+      ring_page += min(2 * g.cnt, (len + kPage - 1) / kPage - 2 * g.j0);
+      const int steps = tile_blocks(g, t);
+      if (steps == 0) continue;
+      const int base_row = g.dual ? 0 : t * kRows, urow = base_row + row;
+      const bool row_valid = urow < g.rows, warp_live = base_row + 32 * q4 < g.rows;
+      const int node = min(g.unit * kUnitRows + urow, g.n * a.L.G - 1) / a.L.G;
+      const uint32_t* mask = a.mask + ((size_t)g.b * a.n_q + node) * a.mask_words;
+      float m_ref = 0.f, l = 0.f;
+      for (int s_i = 0; s_i < steps; ++s_i, ++n) {
+        const int j = g.dual ? 2 * s_i + t : s_i, p0 = (g.j0 + j) * kBlock;
+        mbar_wait(s_full(t), n & 1, abort_flag, status);
+        tc_fence_after();
+        if (p0 + kBlock > len) {
+          // Rows behind the sequence's end: whatever bits they have (NaN included) must not reach the accumulator through
+          // 0 * x.  Every tile that uses the page zeroes them.
+          for (int p = 0; p < 2 && p0 + p * kPage < len; ++p) {
+            const int dead = len - p0 - p * kPage;              // first dead row of the page
+            const int idx = page0 + 2 * j + p, stg = idx % nst;
+            mbar_wait(full_bar(stg), (idx / nst) & 1, abort_flag, status);
+            uint8_t* v = ring_ptr + stg * kStageBytes + kPageK;
+            constexpr int kCpr = kSpanV / 16, kPerRow = RV / 8;
+            for (int e = row; e < (kPage - dead) * kPerRow; e += kRows) {
+              const int r = dead + e / kPerRow, ch = e % kPerRow;
+              *reinterpret_cast<uint4*>(v + (ch / kCpr) * kPage * kSpanV + r * kSpanV + (ch % kCpr) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        if (!warp_live) {                                       // none of the warp's rows exists
+          arrive_warp(p_full(t, 0));
+          arrive_warp(p_full(t, 1));
+          continue;
+        }
+        uint32_t sv[128];
+        float* s = reinterpret_cast<float*>(sv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32 * i, sv + 32 * i);
+        tmem_ld_wait();
+        if (p0 + kBlock > g.ctx) {                              // the drafted nodes, and what lies behind them
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t seen = seen32(mask, p0 + 32 * w - g.ctx, g.n);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!((seen >> i) & 1u)) s[32 * w + i] = -INFINITY;
+          }
+        }
+        float mx;
+        {
+          float m[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+          for (int i = 4; i < 124; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = max3(m[e], s[i + 2 * e], s[i + 2 * e + 1]);
+          mx = fmaxf(max3(max3(m[0], s[124], s[125]), m[1], m[2]), max3(m[3], s[126], s[127]));
+        }
+        if (s_i == 0) {
+          m_ref = fmaxf(mx, -1e30f);                            // a row that sees nothing here keeps p = 0 and l = 0
+          l = 0.f;
+        } else if (const bool grown = (mx - m_ref) * c > kRescaleLog2; __any_sync(0xffffffffu, grown)) {
+          const float f = grown ? fast_exp2((m_ref - mx) * c) : 1.0f;       // a row's bits do not depend on its neighbours
+          if (grown) m_ref = mx;
+          l *= f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < RV; c0 += 16) {                 // the product of the block before is complete: S is
+            uint32_t v[16];
+            tmem_ld16(t_o + c0, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_st16(t_o + c0, v);
+          }
+        }
+        const uint64_t c2 = pack2(c, c), neg2 = pack2(-m_ref * c, -m_ref * c);
+        uint64_t sum[2] = {0ull, 0ull};                         // pairs of +0
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                           // a page: probabilities as bf16 pairs over the scores
+#pragma unroll
+          for (int q = 2 * h; q < 2 * h + 2; ++q) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x0, x1;
+              unpack2(fma2(pack2(s[32 * q + 2 * i], s[32 * q + 2 * i + 1]), c2, neg2), x0, x1);
+              const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
+              sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+              pk[i] = pack_bf16(e0, e1);
+            }
+            tmem_st16(t_s + 16 * q, pk);
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          arrive_warp(p_full(t, h));
+        }
+        float a0, a1;
+        unpack2(add2(sum[0], sum[1]), a0, a1);
+        l += a0 + a1;
+      }
+      // ---- the segment's partial result, [slot][RV / 4][slot rows] float4: a warp writes 512 contiguous bytes
+      mbar_wait(o_full(t), kt & 1, abort_flag, status);
+      ++kt;
+      tc_fence_after();
+      if (warp_live) {
+        const size_t slot = (size_t)g.slot * 2 + t;
+        float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * a.slot_rows + row;
+#pragma unroll 1
+        for (int c0 = 0; c0 < RV; c0 += 16) {
+          uint32_t v[16];
+          tmem_ld16(t_o + c0, v);
+          tmem_ld_wait();
+          if (row_valid) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              po[(size_t)(c0 / 4 + i) * a.slot_rows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+          }
+        }
+        if (row_valid) reinterpret_cast<float2*>(a.part_ml)[slot * a.slot_rows + row] = make_float2(m_ref * c, l);
+      }
+      tc_fence_before();                                        // ordered before this tile's next P by the arrival that publishes it
+    }
+  }
+
+  if (*abort_flag) let_copies_land();           // a wait ran out: nobody has waited for the ring's last copies
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) tmem_dealloc(tmem_base, kTmemCols);
+}
+
+struct Launch {
+  Args a;
+  CUtensorMap tmQ, tmK, tmV;
+  int grid, smem;
+};
+
+}  // namespace tree
+
+// One launcher per key rank (each its own translation unit)
+cudaError_t launch_tree_rk32(const tree::Launch& l, cudaStream_t st);
+cudaError_t launch_tree_rk48(const tree::Launch& l, cudaStream_t st);
+cudaError_t launch_tree_rk64(const tree::Launch& l, cudaStream_t st);
+cudaError_t launch_tree_rk96(const tree::Launch& l, cudaStream_t st);
+cudaError_t launch_tree_rk128(const tree::Launch& l, cudaStream_t st);
+
+}  // namespace stief
