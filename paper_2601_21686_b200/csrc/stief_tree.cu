@@ -5,78 +5,106 @@
 namespace stief {
 namespace tree {
 
-// ---------------------------------------------------------------------------------------------
-// project_kernel: q' = q U_k for 16 rows (node, head of the group) of one (sequence, KV head).  A group of r_k threads owns
-// the columns for a share of the rows; a row of U_k is read by neighbouring threads, the queries are broadcast from shared
-// memory.  128 r_k MACs per row, next to 2 T (r_k + r_v) of the attention.
-// ---------------------------------------------------------------------------------------------
 constexpr int kSmallThreads = 128, kSmallRows = 16;
 
+// ---------------------------------------------------------------------------------------------
+// project_kernel: q' = q U_k for 16 rows (node, head of the group) of one (sequence, KV head), by mma.sync (16 rows are too few
+// for a tcgen05 tile).  Its time is the latency of its loads, so all of them are issued before the first is used.
+// ---------------------------------------------------------------------------------------------
 template <int RK>
 __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
-  constexpr int kGroups = kSmallThreads / RK, kPer = kSmallRows / kGroups;
-  __shared__ __align__(16) float x[kD][kSmallRows];
+  constexpr int kQRow = kD + 8, kURow = RK + 8;                 // padded rows: ldmatrix without bank conflicts
+  __shared__ __align__(16) __nv_bfloat16 xq[kSmallRows * kQRow];
+  __shared__ __align__(16) __nv_bfloat16 xu[kD * kURow];
   launch_dependents();
   const int h = blockIdx.y, b = blockIdx.z, G = a.L.G, rows = a.n_q * G, r0 = blockIdx.x * kSmallRows;
   const int n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.n_q) : a.n_q;
-  if (r0 >= n * G) return;
   const bool fold = a.L.U_k == nullptr;
   const int dq = fold ? RK : kD;
   const int live = min(kSmallRows, n * G - r0);
   __nv_bfloat16* dst = a.qp + (((size_t)b * a.L.Hkv + h) * rows + r0) * RK;
   auto src = [&](int r) {
     const int node = (r0 + r) / G, g = r0 + r - node * G;
-    return a.q + (size_t)b * a.q_stride_b + (size_t)node * a.q_stride_t + (size_t)(h * G + g) * dq;
+    return reinterpret_cast<const uint4*>(a.q + (size_t)b * a.q_stride_b + (size_t)node * a.q_stride_t + (size_t)(h * G + g) * dq);
   };
   if (fold) {                                                   // the queries arrive projected: rows are only packed
-    for (int e = threadIdx.x; e < live * (RK / 8); e += kSmallThreads)
-      reinterpret_cast<uint4*>(dst)[e] = reinterpret_cast<const uint4*>(src(e / (RK / 8)))[e % (RK / 8)];
+    for (int e = threadIdx.x; e < live * (RK / 8); e += kSmallThreads) reinterpret_cast<uint4*>(dst)[e] = src(e / (RK / 8))[e % (RK / 8)];
     return;
   }
-  for (int e = threadIdx.x; e < kSmallRows * (kD / 8); e += kSmallThreads) {
-    const int r = e % kSmallRows, d = e / kSmallRows * 8;
-    const uint4 v = r < live ? reinterpret_cast<const uint4*>(src(r))[d / 8] : make_uint4(0u, 0u, 0u, 0u);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  constexpr int kULoads = kD * (RK / 8) / kSmallThreads;
+  uint4 u[kULoads], q[2];
+  const uint4* U = reinterpret_cast<const uint4*>(a.L.U_k + (size_t)h * a.L.uk_stride);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[d + 2 * i][r] = bf16_lo(w[i]);
-      x[d + 2 * i + 1][r] = bf16_hi(w[i]);
-    }
+  for (int i = 0; i < kULoads; ++i) u[i] = U[i * kSmallThreads + threadIdx.x];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int e = i * kSmallThreads + threadIdx.x;
+    q[i] = e / 16 < live ? src(e / 16)[e % 16] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  if (live <= 0) return;
+#pragma unroll
+  for (int i = 0; i < kULoads; ++i) {
+    const int e = i * kSmallThreads + threadIdx.x;
+    *reinterpret_cast<uint4*>(xu + e / (RK / 8) * kURow + e % (RK / 8) * 8) = u[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int e = i * kSmallThreads + threadIdx.x;
+    *reinterpret_cast<uint4*>(xq + e / 16 * kQRow + e % 16 * 8) = q[i];
   }
   __syncthreads();
-  const int grp = threadIdx.x / RK, j = threadIdx.x - grp * RK;
-  if (grp >= kGroups) return;
-  const __nv_bfloat16* U = a.L.U_k + (size_t)h * a.L.uk_stride + j;
-  float acc[kPer] = {};
-#pragma unroll 8
-  for (int d = 0; d < kD; ++d) {
-    const float u = __bfloat162float(U[d * RK]);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int p = warp; p < RK / 16; p += kSmallThreads / 32) {    // 16 columns at a time
+    float acc[2][4] = {};
 #pragma unroll
-    for (int i = 0; i < kPer; i += 4) {
-      const float4 q = *reinterpret_cast<const float4*>(&x[d][grp * kPer + i]);
-      acc[i] = fmaf(q.x, u, acc[i]);
-      acc[i + 1] = fmaf(q.y, u, acc[i + 1]);
-      acc[i + 2] = fmaf(q.z, u, acc[i + 2]);
-      acc[i + 3] = fmaf(q.w, u, acc[i + 3]);
+    for (int k = 0; k < kD; k += 16) {
+      uint32_t A[4], b0, b1, b2, b3;
+      ldsm_x4(smem_u32(xq + (lane & 15) * kQRow + k + (lane >> 4) * 8), A[0], A[1], A[2], A[3]);
+      ldsm_x4_t(smem_u32(xu + (k + (lane & 15)) * kURow + p * 16 + (lane >> 4) * 8), b0, b1, b2, b3);
+      mma_bf16(acc[0], A, b0, b1);
+      mma_bf16(acc[1], A, b2, b3);
     }
-  }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i)
-    if (grp * kPer + i < live) dst[(grp * kPer + i) * RK + j] = __float2bfloat16_rn(acc[i]);
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = (lane >> 2) + 8 * i;
+        if (r < live) *reinterpret_cast<uint32_t*>(dst + r * RK + p * 16 + t * 8 + (lane & 3) * 2) = pack_bf16(acc[t][2 * i], acc[t][2 * i + 1]);
+      }
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
 // combine_kernel: 16 rows of one (sequence, KV head).  The segments of the rows' unit follow from the running costs; each left
-// one partial result per tile that had a block.
+// one partial result per tile that had a block.  The weights of all parts are found first, by all threads; the back-projection
+// runs on mma.sync with the joined rows as bf16 value + remainder (16 significant bits) and U_v fetched before the wait for
+// the kernel that makes the parts.
 // ---------------------------------------------------------------------------------------------
+constexpr int kMaxParts = 2 * 256;                              // two tiles of every CTA: more than any device of this kind has
+
 template <int RV>
 __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
-  __shared__ __align__(16) float od[RV][kSmallRows];
-  __shared__ float lse[kSmallRows];
-  grid_dependency_wait();
+  constexpr int kRow = RV + 8;
+  __shared__ __align__(16) __nv_bfloat16 hi[kSmallRows * kRow], lo[kSmallRows * kRow];
+  __shared__ float weight[kMaxParts][kSmallRows];
+  __shared__ int part_slot[kMaxParts];                          // -1: no such part
+  __shared__ float red[kSmallThreads / kSmallRows][kSmallRows];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z, G = a.L.G, r0 = blockIdx.x * kSmallRows;
+  const bool fold = a.L.U_v == nullptr;
+  uint32_t u[4][RV / 16][2];                                    // B fragments of this warp's 32 output channels
+  if (!fold) {
+    const __nv_bfloat16* U = a.L.U_v + (size_t)h * a.L.uv_stride + (size_t)(warp * 32 + (lane >> 2)) * RV + (lane & 3) * 2;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < RV / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) u[t][k][i] = *reinterpret_cast<const uint32_t*>(U + t * 8 * RV + k * 16 + i * 8);
+  }
   const Seq s = sequence(a, b);
   const int live = min(kSmallRows, s.n * G - r0);
+  grid_dependency_wait();
   if (live <= 0) return;
   const int unit = r0 / kUnitRows, rows = min(s.n * G - unit * kUnitRows, kUnitRows), in_unit = r0 - unit * kUnitRows;
   const bool dual = rows <= kRows;
@@ -85,87 +113,100 @@ __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
   const int first = a.prefix[b] + (h * s.units + unit) * (s.blocks + kPad) + kPad, end = first + s.blocks;     // real blocks
   // the CTA whose range holds position p is the last one that starts at or before it
   auto owner = [&](int p) { return (int)((((long long)p + 1) * n - 1) / total); };
-  const int c0 = owner(first), c1 = owner(end - 1);
-  const int slot0 = (b * a.L.Hkv + h) * a.max_units + unit;
-  auto blocks_of_cta = [&](int i) { return min(end, range_start(i + 1, n, total)) - max(first, range_start(i, n, total)); };
-  for (int e = threadIdx.x; e < kSmallRows * (RV / 4); e += kSmallThreads) {
-    const int r = e % kSmallRows, c4 = e / kSmallRows;
-    if (r >= live) continue;
-    const size_t at = (size_t)row0 + r;
-    auto ml = [&](size_t slot) { return reinterpret_cast<const float2*>(a.part_ml)[slot * a.slot_rows + at]; };
-    auto parts = [&](auto use) {
-      for (int i = c0; i <= c1; ++i) {
-        const int cnt = blocks_of_cta(i);
-        const size_t slot = (size_t)(i + slot0) * 2;
-        if (cnt <= 0) continue;
-        use(slot + tile);
-        if (dual && cnt > 1) use(slot + 1);
-      }
-    };
-    float M = -INFINITY, den = 0.f;
-    parts([&](size_t slot) { M = fmaxf(M, ml(slot).x); });
-    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-    parts([&](size_t slot) {
-      const float2 x = ml(slot);
-      const float w = fast_exp2(x.x - M);
-      const float4 o = reinterpret_cast<const float4*>(a.part_o)[(slot * (RV / 4) + c4) * a.slot_rows + at];
-      den = fmaf(x.y, w, den);
-      num.x = fmaf(o.x, w, num.x);
-      num.y = fmaf(o.y, w, num.y);
-      num.z = fmaf(o.z, w, num.z);
-      num.w = fmaf(o.w, w, num.w);
-    });
-    const float inv = den > 0.f ? 1.0f / den : 0.f;             // a row that saw nothing: zeros
-    od[4 * c4][r] = num.x * inv;
-    od[4 * c4 + 1][r] = num.y * inv;
-    od[4 * c4 + 2][r] = num.z * inv;
-    od[4 * c4 + 3][r] = num.w * inv;
-    if (c4 == 0) lse[r] = den > 0.f ? kLn2 * (M + log2f(den)) : -INFINITY;
+  const int c0 = owner(first), parts = 2 * (owner(end - 1) - c0 + 1), slot0 = (b * a.L.Hkv + h) * a.max_units + unit;
+  for (int p = tid; p < parts; p += kSmallThreads) {
+    const int i = c0 + (p >> 1), cnt = min(end, range_start(i + 1, n, total)) - max(first, range_start(i, n, total));
+    const bool there = (p & 1) ? (dual ? cnt > 1 : cnt > 0 && tile == 1) : cnt > 0 && (dual || tile == 0);
+    part_slot[p] = there ? (i + slot0) * 2 + (p & 1) : -1;
   }
   __syncthreads();
-  auto where = [&](int r, int& node, int& hq) {
-    node = (r0 + r) / G;
-    hq = h * G + r0 + r - node * G;
+  const int r = tid % kSmallRows, grp = tid / kSmallRows;
+  constexpr int kGroups = kSmallThreads / kSmallRows;
+  const size_t at = (size_t)row0 + min(r, live - 1);
+  float M = -INFINITY, den = 0.f;
+  for (int p = grp; p < parts; p += kGroups)
+    if (part_slot[p] >= 0) M = fmaxf(M, reinterpret_cast<const float2*>(a.part_ml)[(size_t)part_slot[p] * a.slot_rows + at].x);
+  red[grp][r] = M;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) M = fmaxf(M, red[i][r]);
+  __syncthreads();
+  for (int p = grp; p < parts; p += kGroups) {
+    float w = 0.f;
+    if (part_slot[p] >= 0) {
+      const float2 ml = reinterpret_cast<const float2*>(a.part_ml)[(size_t)part_slot[p] * a.slot_rows + at];
+      w = fast_exp2(ml.x - M);
+      den = fmaf(ml.y, w, den);
+    }
+    weight[p][r] = w;
+  }
+  red[grp][r] = den;
+  __syncthreads();
+  den = 0.f;
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) den += red[i][r];
+  const float inv = den > 0.f ? 1.0f / den : 0.f;               // a row that saw nothing: zeros
+  auto where = [&](int row, int& node, int& hq) {
+    node = (r0 + row) / G;
+    hq = h * G + r0 + row - node * G;
   };
-  if (a.out_lse && threadIdx.x < live) {
+  if (a.out_lse && grp == 0 && r < live) {
     int node, hq;
-    where(threadIdx.x, node, hq);
-    a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = lse[threadIdx.x];
+    where(r, node, hq);
+    a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = den > 0.f ? kLn2 * (M + log2f(den)) : -INFINITY;
   }
-  const bool fold = a.L.U_v == nullptr;
-  const int d_out = fold ? RV : kD, d = threadIdx.x;
-  if (d >= d_out) return;
-  float acc[kSmallRows] = {};
-  if (fold) {
 #pragma unroll
-    for (int r = 0; r < kSmallRows; ++r) acc[r] = od[d][r];
-  } else {                                                      // one output channel per thread: row d of U_v
-    const uint4* U = reinterpret_cast<const uint4*>(a.L.U_v + (size_t)h * a.L.uv_stride + (size_t)d * RV);
-#pragma unroll 2
-    for (int c8 = 0; c8 < RV / 8; ++c8) {
-      const uint4 u = U[c8];
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float uv = i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
-#pragma unroll
-        for (int r = 0; r < kSmallRows; r += 4) {
-          const float4 o = *reinterpret_cast<const float4*>(&od[c8 * 8 + i][r]);
-          acc[r] = fmaf(o.x, uv, acc[r]);
-          acc[r + 1] = fmaf(o.y, uv, acc[r + 1]);
-          acc[r + 2] = fmaf(o.z, uv, acc[r + 2]);
-          acc[r + 3] = fmaf(o.w, uv, acc[r + 3]);
-        }
+  for (int c4 = grp; c4 < RV / 4; c4 += kGroups) {              // four channels of a row; neighbouring rows side by side
+    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p)
+      if (part_slot[p] >= 0) {
+        const float w = weight[p][r];
+        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)part_slot[p] * (RV / 4) + c4) * a.slot_rows + at];
+        num.x = fmaf(o.x, w, num.x);
+        num.y = fmaf(o.y, w, num.y);
+        num.z = fmaf(o.z, w, num.z);
+        num.w = fmaf(o.w, w, num.w);
       }
+    uint32_t v[2], x[2];
+    split_bf16(num.x * inv, num.y * inv, v[0], x[0]);
+    split_bf16(num.z * inv, num.w * inv, v[1], x[1]);
+    *reinterpret_cast<uint2*>(hi + r * kRow + c4 * 4) = make_uint2(v[0], v[1]);
+    *reinterpret_cast<uint2*>(lo + r * kRow + c4 * 4) = make_uint2(x[0], x[1]);
+  }
+  __syncthreads();
+  if (fold) {
+    for (int e = tid; e < live * (RV / 2); e += kSmallThreads) {
+      const int row = e / (RV / 2), c = e % (RV / 2) * 2;
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(hi + row * kRow + c);
+      int node, hq;
+      where(row, node, hq);
+      *reinterpret_cast<uint32_t*>(a.out + (size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * RV + c) = v;
+    }
+    return;
+  }
+  float acc[4][4] = {};
+#pragma unroll
+  for (int k = 0; k < RV / 16; ++k) {
+    uint32_t A[4], B[4];
+    ldsm_x4(smem_u32(hi + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), A[0], A[1], A[2], A[3]);
+    ldsm_x4(smem_u32(lo + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), B[0], B[1], B[2], B[3]);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      mma_bf16(acc[t], A, u[t][k][0], u[t][k][1]);
+      mma_bf16(acc[t], B, u[t][k][0], u[t][k][1]);
     }
   }
 #pragma unroll
-  for (int r = 0; r < kSmallRows; ++r)
-    if (r < live) {
-      int node, hq;
-      where(r, node, hq);
-      a.out[(size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * d_out + d] = __float2bfloat16_rn(acc[r]);
-    }
+  for (int i = 0; i < 2; ++i) {
+    const int row = (lane >> 2) + 8 * i;
+    if (row >= live) continue;
+    int node, hq;
+    where(row, node, hq);
+    __nv_bfloat16* o = a.out + (size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * kD + warp * 32 + (lane & 3) * 2;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(o + t * 8) = pack_bf16(acc[t][2 * i], acc[t][2 * i + 1]);
+  }
 }
 
 cudaError_t launch_project(const Args& a, dim3 grid, cudaStream_t st) {

@@ -158,7 +158,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     pref[0] = 0;
     for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(full_bar(s), 1);
-      mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer, or two from the only one that uses the page
+      mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer, or from the only one that uses the page and the producer
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full(t), 1);
@@ -226,6 +226,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
 #pragma unroll
               for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + kPageK + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+              if (g.dual) mbar_arrive(empty_bar(st));
               if (++st == nst) {
                 st = 0;
                 ++use;
@@ -272,17 +273,20 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           ++use;
         }
       };
-      // the pages of a block, and S = Q' K^T of each
-      int page_st[2];
-      auto score = [&](int pages, bool last) {
+      auto fetch = [&](int pages, int (&at)[2]) {                              // the next block's pages, once they have landed
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
+        for (int p = 0; p < 2; ++p)
           if (p < pages) {
             mbar_wait_warp(bar(st), use & 1, abort_flag, status);
-            page_st[p] = st;
-            const uint32_t ka = desc_lo(16, ring_u + st * kStageBytes);
+            at[p] = st;
             step(1);
-            tc_fence_after();
+          }
+      };
+      auto score = [&](int pages, const int (&at)[2], bool last) {             // S = Q' K^T, 64 columns per page
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          if (p < pages) {
+            const uint32_t ka = desc_lo(16, ring_u + at[p] * kStageBytes);
 #pragma unroll
             for (int k = 0; k < RK / 16; ++k) {
               constexpr int kPer = bk.bw / 16;                                 // K steps per swizzled block
@@ -290,26 +294,41 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               umma_ss(tmem_u + 64 * p, qa + qo, kHiK, ka + ko, kHiK, id_qk, k > 0 ? 1u : 0u);
             }
           }
-        }
         umma_commit_warp(bar(28 + t));
         if (last) umma_commit_warp(bar(26 + t));
       };
       for (Segment g = walk.next(a, pref); uniform((int)g.valid); g = walk.next(a, pref)) {
         const int cnt = uniform(g.cnt), j0 = uniform(g.j0), len = uniform(g.ctx + g.n);
-        const bool dual = uniform((int)g.dual) != 0;
+        const bool dual = uniform((int)g.dual) != 0, ahead = !dual || nst >= 6;
         const int pages = min(2 * cnt, (len + kPage - 1) / kPage - 2 * j0);    // pages of the segment
         const int steps = dual ? (cnt + 1 - t) >> 1 : cnt, stride = dual ? 2 : 1, at = dual ? t : 0;
         if (steps == 0) {
           for (int i = 0; i < pages; ++i) step(1);                             // a lone block: the other tile's
           continue;
         }
-        mbar_wait_warp(bar(24 + t), kt & 1, abort_flag, status);
+        int here = min(2, pages - 2 * at), next = 0, cur[2], nxt[2];
         if (at) step(2);
-        score(min(2, pages - 2 * at), steps == 1);
+        fetch(here, cur);
+        mbar_wait_warp(bar(24 + t), kt & 1, abort_flag, status);
+        tc_fence_after();
+        score(here, cur, steps == 1);
         for (int s = 0; s < steps; ++s) {
-          const int here = min(2, pages - 2 * (at + s * stride)), cur[2] = {page_st[0], page_st[1]};
+          // What the step needs besides P is waited for ahead of it, so that from P to the next scores only products are
+          // issued.  Two tiles on blocks of their own hold four pages and ask for two more: a shorter ring asks later.
+          auto fetch_next = [&]() {
+            if (s + 1 == steps) return;
+            if (dual) step(2);                                                 // the other tile's block between
+            next = min(2, pages - 2 * (at + (s + 1) * stride));
+            fetch(next, nxt);
+          };
+          auto release = [&]() {
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
+            for (int p = 0; p < 2; ++p)
+              if (p < here) umma_commit_warp(bar(12 + cur[p]));
+          };
+          if (ahead) fetch_next();
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {                                        // O += P V
             mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
             tc_fence_after();
             if (p < here) {
@@ -320,18 +339,16 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             }
           }
           ++n;
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            if (p < here) {
-              umma_commit_warp(bar(12 + cur[p]));
-              if (dual) umma_commit_warp(bar(12 + cur[p]));
-            }
-          if (s + 1 < steps) {
-            if (dual) step(2);                                                 // the other tile's block between
-            score(min(2, pages - 2 * (at + (s + 1) * stride)), s + 2 == steps);
-          } else {
-            umma_commit_warp(bar(34 + t));
+          if (!ahead) {
+            release();
+            fetch_next();
           }
+          if (s + 1 < steps) score(next, nxt, s + 2 == steps);
+          else umma_commit_warp(bar(34 + t));
+          if (ahead) release();
+          here = next;
+          cur[0] = nxt[0];
+          cur[1] = nxt[1];
         }
         if (dual) {                                                            // blocks behind this tile's last
           const int done = 2 * (at + (steps - 1) * 2) + 2;

@@ -154,6 +154,15 @@ def test_long_contexts_are_cut_and_joined(lens, n):
     assert int(c.status) == 0
 
 
+@pytest.mark.parametrize("r_k", [32, 48, 64, 96, 128])
+@pytest.mark.parametrize("r_v", [32, 48, 64, 96, 128])
+@pytest.mark.parametrize("n", [8, 50])
+def test_many_blocks_per_segment_at_every_rank_pair(r_k, r_v, n):
+    c = TreeCase(r_k + 3 * r_v + n, [150 * 128 * 6 + 77, 40], n, [n, 3], Hq=8, Hkv=1, r_k=r_k, r_v=r_v)
+    c.check(*c.run())
+    assert int(c.status) == 0
+
+
 def test_many_sequences():
     lens = [(37 * i) % 450 for i in range(200)]
     c = TreeCase(5, lens, 6, [(i % 7) for i in range(200)], Hq=8, Hkv=2)
