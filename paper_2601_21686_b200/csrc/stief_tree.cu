@@ -75,32 +75,35 @@ __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// combine_kernel: 16 rows of one (sequence, KV head).  The segments of the rows' unit follow from the running costs; each left
-// one partial result per tile that had a block.  The weights of all parts are found first, by all threads; the back-projection
-// runs on mma.sync with the joined rows as bf16 value + remainder (16 significant bits) and U_v fetched before the wait for
-// the kernel that makes the parts.
+// combine_kernel: 16 rows of one (sequence, KV head).  The segments of the rows' unit follow from the running costs and the CTAs'
+// ranges; each left one partial result per tile that had a block and per copy of the rows.  All its time is the latency of
+// loads, hence the many threads for 16 rows: the weights of all parts are found first, then every thread sums four channels of a
+// row over a share of the parts.  The back-projection runs on mma.sync with the joined rows as bf16 value + remainder (16
+// significant bits) and U_v fetched before the wait for the kernel that makes the parts.
 // ---------------------------------------------------------------------------------------------
-constexpr int kMaxParts = 2 * 256;                              // two tiles of every CTA: more than any device of this kind has
+constexpr int kJoinThreads = 512;
+constexpr int kPartChunk = 256;                                 // parts whose weights are held at a time
 
 template <int RV>
-__global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
-  constexpr int kRow = RV + 8;
+__global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
+  constexpr int kRow = RV + 8, kGroups = kJoinThreads / kSmallRows, kItems = kSmallRows * RV / 4, kSplit = kJoinThreads / kItems > 0 ? kJoinThreads / kItems : 1;
+  static_assert(kItems <= kJoinThreads, "an item per thread");
   __shared__ __align__(16) __nv_bfloat16 hi[kSmallRows * kRow], lo[kSmallRows * kRow];
-  __shared__ float weight[kMaxParts][kSmallRows];
-  __shared__ int part_slot[kMaxParts];                          // -1: no such part
-  __shared__ float red[kSmallThreads / kSmallRows][kSmallRows];
+  __shared__ float weight[kPartChunk][kSmallRows];
+  __shared__ int part_at[kPartChunk];                           // (slot, copy) of the part as its first lane, -1: no such part
+  __shared__ float red[kJoinThreads / 32][kSmallRows];
+  __shared__ float4 share[kSplit > 1 ? (kSplit - 1) * kItems : 1];
+  __shared__ int range_of[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z, G = a.L.G, r0 = blockIdx.x * kSmallRows;
   const bool fold = a.L.U_v == nullptr;
-  uint32_t u[4][RV / 16][2];                                    // B fragments of this warp's 32 output channels
+  uint32_t u[RV / 16][2];                                       // B fragments of this warp's 8 output channels
   if (!fold) {
-    const __nv_bfloat16* U = a.L.U_v + (size_t)h * a.L.uv_stride + (size_t)(warp * 32 + (lane >> 2)) * RV + (lane & 3) * 2;
+    const __nv_bfloat16* U = a.L.U_v + (size_t)h * a.L.uv_stride + (size_t)(warp * 8 + (lane >> 2)) * RV + (lane & 3) * 2;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int k = 0; k < RV / 16; ++k)
 #pragma unroll
-      for (int k = 0; k < RV / 16; ++k)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) u[t][k][i] = *reinterpret_cast<const uint32_t*>(U + t * 8 * RV + k * 16 + i * 8);
+      for (int i = 0; i < 2; ++i) u[k][i] = *reinterpret_cast<const uint32_t*>(U + k * 16 + i * 8);
   }
   const Seq s = sequence(a, b);
   const int live = min(kSmallRows, s.n * G - r0);
@@ -108,44 +111,80 @@ __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
   if (live <= 0) return;
   const int unit = r0 / kUnitRows, rows = min(s.n * G - unit * kUnitRows, kUnitRows), in_unit = r0 - unit * kUnitRows;
   const bool dual = rows <= kRows;
+  const int copies = replicas_of(rows), wrap = kRows / copies;
   const int tile = dual ? 0 : in_unit / kRows, row0 = in_unit - tile * kRows;
   const int total = a.prefix[a.Bt.B], n = cta_count(a, total);
   const int first = a.prefix[b] + (h * s.units + unit) * (s.blocks + kPad) + kPad, end = first + s.blocks;     // real blocks
-  // the CTA whose range holds position p is the last one that starts at or before it
-  auto owner = [&](int p) { return (int)((((long long)p + 1) * n - 1) / total); };
-  const int c0 = owner(first), parts = 2 * (owner(end - 1) - c0 + 1), slot0 = (b * a.L.Hkv + h) * a.max_units + unit;
-  for (int p = tid; p < parts; p += kSmallThreads) {
-    const int i = c0 + (p >> 1), cnt = min(end, range_start(i + 1, n, total)) - max(first, range_start(i, n, total));
-    const bool there = (p & 1) ? (dual ? cnt > 1 : cnt > 0 && tile == 1) : cnt > 0 && (dual || tile == 0);
-    part_slot[p] = there ? (i + slot0) * 2 + (p & 1) : -1;
+  for (int i = tid; i < n; i += kJoinThreads) {                 // the CTAs that hold the unit's first and last block
+    const int lo_i = a.ranges[i], hi_i = a.ranges[i + 1];
+    if (lo_i <= first && first < hi_i) range_of[0] = i;
+    if (lo_i < end && end <= hi_i) range_of[1] = i;
   }
   __syncthreads();
-  const int r = tid % kSmallRows, grp = tid / kSmallRows;
-  constexpr int kGroups = kSmallThreads / kSmallRows;
-  const size_t at = (size_t)row0 + min(r, live - 1);
-  float M = -INFINITY, den = 0.f;
-  for (int p = grp; p < parts; p += kGroups)
-    if (part_slot[p] >= 0) M = fmaxf(M, reinterpret_cast<const float2*>(a.part_ml)[(size_t)part_slot[p] * a.slot_rows + at].x);
-  red[grp][r] = M;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kGroups; ++i) M = fmaxf(M, red[i][r]);
-  __syncthreads();
-  for (int p = grp; p < parts; p += kGroups) {
-    float w = 0.f;
-    if (part_slot[p] >= 0) {
-      const float2 ml = reinterpret_cast<const float2*>(a.part_ml)[(size_t)part_slot[p] * a.slot_rows + at];
-      w = fast_exp2(ml.x - M);
-      den = fmaf(ml.y, w, den);
+  const int c0 = range_of[0], per_cta = 2 * copies, parts = per_cta * (range_of[1] - c0 + 1), slot0 = (b * a.L.Hkv + h) * a.max_units + unit;
+  const int r = tid % kSmallRows, grp = tid / kSmallRows, at = row0 + min(r, live - 1);
+  auto list_parts = [&](int p0) {                               // parts [p0, p0 + kPartChunk): CTA, tile, copy
+    __syncthreads();
+    if (tid < kPartChunk) {
+      int x = -1;
+      if (p0 + tid < parts) {
+        const int i = (p0 + tid) / per_cta, rest = p0 + tid - i * per_cta, t = rest / copies, cta = c0 + i;
+        const int cnt = min(end, a.ranges[cta + 1]) - max(first, a.ranges[cta]);
+        if (t ? (dual ? cnt > 1 : cnt > 0 && tile == 1) : cnt > 0 && (dual || tile == 0)) x = ((cta + slot0) * 2 + t) * kRows + (rest - t * copies) * wrap;
+      }
+      part_at[tid] = x;
     }
-    weight[p][r] = w;
-  }
-  red[grp][r] = den;
-  __syncthreads();
-  den = 0.f;
+    __syncthreads();
+  };
+  auto over_groups = [&](float v, auto join) {                  // over the threads that share a row
+    v = join(v, __shfl_xor_sync(0xffffffffu, v, 16));
+    __syncthreads();
+    if (lane < kSmallRows) red[warp][lane] = v;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) den += red[i][r];
-  const float inv = den > 0.f ? 1.0f / den : 0.f;               // a row that saw nothing: zeros
+    for (int i = 1; i < kJoinThreads / 32; ++i) v = join(i > 1 ? v : red[0][r], red[i][r]);
+    return v;
+  };
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float M = -INFINITY;
+  for (int p0 = 0; p0 < parts; p0 += kPartChunk) {
+    list_parts(p0);
+    for (int p = grp; p < min(parts - p0, kPartChunk); p += kGroups)
+      if (part_at[p] >= 0) M = fmaxf(M, ml[(size_t)part_at[p] + at].x);
+  }
+  M = over_groups(M, [](float x, float y) { return fmaxf(x, y); });
+  float den = 0.f;
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int item = tid % kItems, share_i = tid / kItems, ir = item % kSmallRows, c4 = item / kSmallRows, iat = row0 + min(ir, live - 1);
+  for (int p0 = 0; p0 < parts; p0 += kPartChunk) {
+    if (parts > kPartChunk) list_parts(p0);                     // else the list still stands
+    const int cnt = min(parts - p0, kPartChunk);
+    for (int p = grp; p < cnt; p += kGroups) {
+      float w = 0.f;
+      if (part_at[p] >= 0) {
+        const float2 x = ml[(size_t)part_at[p] + at];
+        w = fast_exp2(x.x - M);
+        den = fmaf(x.y, w, den);
+      }
+      weight[p][r] = w;
+    }
+    __syncthreads();
+    if (share_i < kSplit) {
+#pragma unroll 8
+      for (int p = share_i; p < cnt; p += kSplit) {             // neighbouring threads, neighbouring rows
+        const int x = part_at[p];
+        if (x < 0) continue;
+        const float w = weight[p][ir];
+        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)(x / kRows) * (RV / 4) + c4) * kRows + x % kRows + iat];
+        num.x = fmaf(o.x, w, num.x);
+        num.y = fmaf(o.y, w, num.y);
+        num.z = fmaf(o.z, w, num.z);
+        num.w = fmaf(o.w, w, num.w);
+      }
+    }
+  }
+  den = over_groups(den, [](float x, float y) { return x + y; });
+  if (kSplit > 1 && share_i > 0 && share_i < kSplit) share[(share_i - 1) * kItems + item] = num;
   auto where = [&](int row, int& node, int& hq) {
     node = (r0 + row) / G;
     hq = h * G + r0 + row - node * G;
@@ -155,28 +194,26 @@ __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
     where(r, node, hq);
     a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = den > 0.f ? kLn2 * (M + log2f(den)) : -INFINITY;
   }
+  __syncthreads();
+  if (share_i == 0) {                                           // r == ir here: kItems is a multiple of 16
 #pragma unroll
-  for (int c4 = grp; c4 < RV / 4; c4 += kGroups) {              // four channels of a row; neighbouring rows side by side
-    float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p)
-      if (part_slot[p] >= 0) {
-        const float w = weight[p][r];
-        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)part_slot[p] * (RV / 4) + c4) * a.slot_rows + at];
-        num.x = fmaf(o.x, w, num.x);
-        num.y = fmaf(o.y, w, num.y);
-        num.z = fmaf(o.z, w, num.z);
-        num.w = fmaf(o.w, w, num.w);
-      }
+    for (int i = 0; i + 1 < kSplit; ++i) {
+      const float4 o = share[i * kItems + item];
+      num.x += o.x;
+      num.y += o.y;
+      num.z += o.z;
+      num.w += o.w;
+    }
+    const float inv = den > 0.f ? 1.0f / den : 0.f;             // a row that saw nothing: zeros
     uint32_t v[2], x[2];
     split_bf16(num.x * inv, num.y * inv, v[0], x[0]);
     split_bf16(num.z * inv, num.w * inv, v[1], x[1]);
-    *reinterpret_cast<uint2*>(hi + r * kRow + c4 * 4) = make_uint2(v[0], v[1]);
-    *reinterpret_cast<uint2*>(lo + r * kRow + c4 * 4) = make_uint2(x[0], x[1]);
+    *reinterpret_cast<uint2*>(hi + ir * kRow + c4 * 4) = make_uint2(v[0], v[1]);
+    *reinterpret_cast<uint2*>(lo + ir * kRow + c4 * 4) = make_uint2(x[0], x[1]);
   }
   __syncthreads();
   if (fold) {
-    for (int e = tid; e < live * (RV / 2); e += kSmallThreads) {
+    for (int e = tid; e < live * (RV / 2); e += kJoinThreads) {
       const int row = e / (RV / 2), c = e % (RV / 2) * 2;
       const uint32_t v = *reinterpret_cast<const uint32_t*>(hi + row * kRow + c);
       int node, hq;
@@ -185,17 +222,14 @@ __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
     }
     return;
   }
-  float acc[4][4] = {};
+  float acc[4] = {};
 #pragma unroll
   for (int k = 0; k < RV / 16; ++k) {
     uint32_t A[4], B[4];
     ldsm_x4(smem_u32(hi + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), A[0], A[1], A[2], A[3]);
     ldsm_x4(smem_u32(lo + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), B[0], B[1], B[2], B[3]);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      mma_bf16(acc[t], A, u[t][k][0], u[t][k][1]);
-      mma_bf16(acc[t], B, u[t][k][0], u[t][k][1]);
-    }
+    mma_bf16(acc, A, u[k][0], u[k][1]);
+    mma_bf16(acc, B, u[k][0], u[k][1]);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -203,9 +237,8 @@ __global__ void __launch_bounds__(kSmallThreads) combine_kernel(const Args a) {
     if (row >= live) continue;
     int node, hq;
     where(row, node, hq);
-    __nv_bfloat16* o = a.out + (size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * kD + warp * 32 + (lane & 3) * 2;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) *reinterpret_cast<uint32_t*>(o + t * 8) = pack_bf16(acc[t][2 * i], acc[t][2 * i + 1]);
+    __nv_bfloat16* o = a.out + (size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * kD + warp * 8 + (lane & 3) * 2;
+    *reinterpret_cast<uint32_t*>(o) = pack_bf16(acc[2 * i], acc[2 * i + 1]);
   }
 }
 
@@ -223,7 +256,7 @@ cudaError_t launch_project(const Args& a, dim3 grid, cudaStream_t st) {
 
 cudaError_t launch_combine(const Args& a, dim3 grid, cudaStream_t st) {
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = after_previous(attr, grid, kSmallThreads, 0, st);
+  const cudaLaunchConfig_t cfg = after_previous(attr, grid, kJoinThreads, 0, st);
   switch (a.L.r_v) {
     case 32: return cudaLaunchKernelEx(&cfg, combine_kernel<32>, a);
     case 48: return cudaLaunchKernelEx(&cfg, combine_kernel<48>, a);
@@ -263,7 +296,7 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
                            b.span == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : b.span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
   };
   const unsigned long long pool_rows = (unsigned long long)layer->num_pages * layer->Hkv * kPage;
-  if (!rows_map(&L.tmQ, a.qp, RK, (unsigned long long)batch->B * layer->Hkv * n_q * G, tree::kRows, bk) ||
+  if (!rows_map(&L.tmQ, a.qp, RK, (unsigned long long)batch->B * layer->Hkv * n_q * G, 32u, bk) ||
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
   const int fixed = tree::kHeadBytes + 2 * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;

@@ -13,11 +13,14 @@
 // tree_kernel, 384 threads: two row tiles of 128 rows.  With at most 128 rows both tiles hold the SAME rows and take
 // alternate blocks (two independent softmax streams, joined like segments): one stream is bound by the latency of its chain
 // scores -> softmax -> P V.  With more, each tile has its own rows and both use every block.
+// TMEM gives a warp 32 lanes, so 32 rows would keep one warp of four at work; with at most 64 or 32 rows a tile therefore holds
+// them twice or four times, each copy takes its half or quarter of a block's columns (P is zero elsewhere, the wasted products
+// cost nothing here) and is one more partial result to join.
 //   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
-//   warp 8          cache pages by TMA into a ring, a stage = K page | V page of one KV head
-//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page), O += P V (N = r_v), P in TMEM over S
-//   warp 11         Q' tiles
-// TMEM (512 columns): per tile 128 for S and 128 for O.  Everything else follows the prompt kernel (stief_prompt.cu).
+//   warps 8, 11     cache pages by TMA into a ring, a stage = K page | V page of one KV head; Q' tiles
+//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page), O += P V (N = r_v)
+// TMEM (512 columns): per tile 128 for S and 128 for O; with r_v <= 64 half of O's are free and hold P, and the next scores are
+// made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
 #pragma once
 
 #include "stief_softmax.cuh"
@@ -58,10 +61,13 @@ __device__ __forceinline__ int sequence_cost(const Args& a, const Seq& s) { retu
 __device__ __forceinline__ int range_start(int i, int n, int total) { return (int)((long long)i * total / n); }
 __device__ __forceinline__ int cta_count(const Args& a, int total) { return min(a.n_cta, total); }
 
+__device__ __forceinline__ int replicas_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+
 struct Segment {
   int b, h, unit, slot;                         // unit: row block within the (sequence, KV head)
   int ctx, n, rows;                             // rows of the unit
   int j0, cnt;                                  // blocks [j0, j0 + cnt)
+  int replicas;                                 // copies of the rows in a tile (see tree_kernel): 1, 2 or 4
   bool dual, valid;
 };
 
@@ -97,6 +103,7 @@ struct Walk {
       g.n = s.n;
       g.rows = min(s.n * a.L.G - g.unit * kUnitRows, kUnitRows);
       g.dual = g.rows <= kRows;
+      g.replicas = replicas_of(g.rows);
       g.valid = true;
       break;
     }
@@ -128,6 +135,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   constexpr Blocks bk{(RK % 64 == 0) ? 64 : (RK % 32 == 0) ? 32 : 16, 0, 0, 0}, bv{(RV % 64 == 0) ? 64 : (RV % 32 == 0) ? 32 : 16, 0, 0, 0};
   constexpr int kSpanK = 2 * bk.bw, kSpanV = 2 * bv.bw, kNbK = RK / bk.bw, kNbV = RV / bv.bw;       // see Blocks in stief_tc.cuh
   constexpr int kLayK = kSpanK == 128 ? 2 : kSpanK == 64 ? 4 : 6, kLayV = kSpanV == 128 ? 2 : kSpanV == 64 ? 4 : 6;
+  constexpr bool kOwnP = RV <= 64;              // P has TMEM columns of its own: 192 .. 255 of the tile's
+  constexpr int kColP = kOwnP ? 192 : 0;
   constexpr int kPageK = kPage * RK * 2, kStageBytes = kPage * (RK + RV) * 2, kQBytes = kRows * RK * 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -144,8 +153,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   auto s_full = [&](int t) { return ctrl + (28 + t) * 8; };
   auto p_full = [&](int t, int half) { return ctrl + (30 + 2 * t + half) * 8; };
   auto o_full = [&](int t) { return ctrl + (34 + t) * 8; };
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + 36 * 8);
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 36 * 8 + 4);
+  auto s_free = [&](int t) { return ctrl + (36 + t) * 8; };
+  auto p_free = [&](int t) { return ctrl + (38 + t) * 8; };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + 40 * 8);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 40 * 8 + 4);
   int32_t* status = a.status;
   launch_dependents();
   if (q_smem & 1023u) {                         // the swizzled tiles need it; dynamic shared memory starts there
@@ -157,7 +168,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   if (tid == 0) {
     pref[0] = 0;
     for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(full_bar(s), 1);
+      mbar_init(full_bar(s), 2);                // the K half and the V half of a page
       mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer, or from the only one that uses the page and the producer
     }
     for (int t = 0; t < 2; ++t) {
@@ -167,6 +178,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       mbar_init(p_full(t, 0), 4);
       mbar_init(p_full(t, 1), 4);
       mbar_init(o_full(t), 1);
+      mbar_init(s_free(t), 4);
+      mbar_init(p_free(t), 1);
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -190,23 +203,54 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  if (blockIdx.x == 0)                          // for the combine kernel
+  if (blockIdx.x == 0) {                        // for the combine kernel
+    const int total = pref[a.Bt.B], n = cta_count(a, total);
     for (int b = tid; b <= a.Bt.B; b += kThreads) a.prefix[b] = pref[b];
+    for (int i = tid; i <= n && total > 0; i += kThreads) a.ranges[i] = range_start(i, n, total);
+  }
 
   Walk walk;
   walk.start(a, pref);
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");      // 384 x 168 registers at launch = 256 x 200 + 128 x 104
-    if (warp == 8) {
-      // ---------------------------------------------------------------------------------------- cache pages
+    if (warp == 8 || warp == 11) {
+      // ---------------------------------------------------------------------------------------- cache pages, Q' tiles
+      // One warp fetches the K halves of the pages, the other the V halves (a warp needs some 500 cycles per page for both,
+      // which is what a page of ranks 48/48 may take in all) and the queries, which it must not wait for before the ring
+      // is on its way: they come from a kernel that may still run, or their place is in use by the segment before.
+      const bool keys = warp == 8;
       if (lane == 0) {
-        tma_prefetch_desc(&tmK);
-        tma_prefetch_desc(&tmV);
+        tma_prefetch_desc(keys ? &tmK : &tmV);
+        if (!keys) tma_prefetch_desc(&tmQ);
       }
-      int st = 0, use = 0;
+      int st = 0, use = 0, kt[2] = {0, 0};
+      bool first_q = true;
       for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
         const int first = 2 * g.j0, pages = min(2 * g.cnt, (g.ctx + g.n + kPage - 1) / kPage - first);
         const int* bt = a.Bt.block_table + (size_t)g.b * a.Bt.max_pages + first;
+        int q_due = keys ? 0 : (tile_blocks(g, 0) > 0) | (tile_blocks(g, 1) > 0) << 1;         // tiles whose queries are still to be sent
+        auto send_queries = [&](bool wait) {                    // lane 0
+          if (first_q) {
+            grid_dependency_wait();                             // project_kernel has written them, with ordinary stores
+            asm volatile("fence.proxy.async;" ::: "memory");
+            first_q = false;
+          }
+          const int row0 = (g.b * a.L.Hkv + g.h) * (a.n_q * a.L.G) + g.unit * kUnitRows, wrap = kRows / g.replicas;
+          for (int t = 0; t < 2; ++t) {
+            if (!(q_due >> t & 1)) continue;
+            if (kt[t] > 0) {
+              if (wait) mbar_wait(q_empty(t), (kt[t] - 1) & 1, abort_flag, status);
+              else if (!mbar_test_wait(q_empty(t), (kt[t] - 1) & 1)) continue;
+            }
+            ++kt[t];
+            q_due &= ~(1 << t);
+            mbar_arrive_expect_tx(q_full(t), kQBytes);
+#pragma unroll
+            for (int i = 0; i < kNbK; ++i)
+              for (int r = 0; r < kRows; r += 32)
+                tma_load_2d(q_smem + t * kQBytes + (i * kRows + r) * kSpanK, &tmQ, i * bk.bw, row0 + (g.dual ? r % wrap : t * kRows + r), q_full(t));
+          }
+        };
         int ids = lane < pages ? bt[lane] : 0;
         for (int j0 = 0; j0 < pages; j0 += 32) {
           const int nxt = j0 + 32 + lane < pages ? bt[j0 + 32 + lane] : 0;     // a batch of page ids ahead
@@ -218,15 +262,22 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 report(status, STIEF_ERR_BOUNDS);
                 pg = 0;
               }
-              if (use > 0) mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
+              if (use > 0) {
+                if (q_due) send_queries(!mbar_test_wait(empty_bar(st), (use - 1) & 1));        // no page to fetch: wait for the queries' place
+                mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
+              }
               const int row = (pg * a.L.Hkv + g.h) * kPage;
               const uint32_t dst = ring + st * kStageBytes;
-              mbar_arrive_expect_tx(full_bar(st), kStageBytes);
+              if (keys) {
+                mbar_arrive_expect_tx(full_bar(st), kPageK);
 #pragma unroll
-              for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
+                for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
+                if (g.dual) mbar_arrive(empty_bar(st));
+              } else {
+                mbar_arrive_expect_tx(full_bar(st), kStageBytes - kPageK);
 #pragma unroll
-              for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + kPageK + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
-              if (g.dual) mbar_arrive(empty_bar(st));
+                for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + kPageK + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+              }
               if (++st == nst) {
                 st = 0;
                 ++use;
@@ -235,27 +286,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           }
           ids = nxt;
         }
+        if (lane == 0 && q_due) send_queries(true);
+        __syncwarp();
       }
-    } else if (warp == 11) {
-      // ---------------------------------------------------------------------------------------- Q' tiles
-      grid_dependency_wait();                                   // project_kernel has written them, with ordinary stores
-      asm volatile("fence.proxy.async;" ::: "memory");
-      if (lane == 0) {
-        tma_prefetch_desc(&tmQ);
-        int kt[2] = {0, 0};
-        for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
-          const int row0 = (g.b * a.L.Hkv + g.h) * (a.n_q * a.L.G) + g.unit * kUnitRows;
-          for (int t = 0; t < 2; ++t) {
-            if (tile_blocks(g, t) == 0) continue;
-            if (kt[t] > 0) mbar_wait(q_empty(t), (kt[t] - 1) & 1, abort_flag, status);
-            ++kt[t];
-            mbar_arrive_expect_tx(q_full(t), kQBytes);
-#pragma unroll
-            for (int i = 0; i < kNbK; ++i)
-              tma_load_2d(q_smem + t * kQBytes + i * kRows * kSpanK, &tmQ, i * bk.bw, row0 + (g.dual ? 0 : t * kRows), q_full(t));
-          }
-        }
-      }
+      if (!keys && first_q) grid_dependency_wait();             // a CTA without work, too, ends after the kernel before it
     } else {
       // ---------------------------------------------------------------------------------------- MMA issue, tile t
       const int t = uniform(warp) - 9;
@@ -327,6 +361,11 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               if (p < here) umma_commit_warp(bar(12 + cur[p]));
           };
           if (ahead) fetch_next();
+          if (kOwnP && ahead && s + 1 < steps) {                               // the next scores do not wait for P: S is free once it has been read
+            mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
+            tc_fence_after();
+            score(next, nxt, s + 2 == steps);
+          }
 #pragma unroll
           for (int p = 0; p < 2; ++p) {                                        // O += P V
             mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
@@ -335,16 +374,18 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               const uint32_t va = desc_lo(kPage * kSpanV, ring_u + cur[p] * kStageBytes + kPageK);
 #pragma unroll
               for (int k = 0; k < kPage / 16; ++k)
-                umma_ts(tmem_u + 128, tmem_u + 32 * p + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || p > 0 || k > 0 ? 1u : 0u);
+                umma_ts(tmem_u + 128, tmem_u + kColP + 32 * p + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || p > 0 || k > 0 ? 1u : 0u);
             }
           }
-          ++n;
+          umma_commit_warp(bar(38 + t));
           if (!ahead) {
             release();
             fetch_next();
+            if (kOwnP && s + 1 < steps) mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);     // S has been read long ago
           }
-          if (s + 1 < steps) score(next, nxt, s + 2 == steps);
-          else umma_commit_warp(bar(34 + t));
+          ++n;
+          if (s + 1 == steps) umma_commit_warp(bar(34 + t));
+          else if (!kOwnP || !ahead) score(next, nxt, s + 2 == steps);
           if (ahead) release();
           here = next;
           cur[0] = nxt[0];
@@ -360,8 +401,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   } else {
     // ------------------------------------------------------------------------------------------ softmax, partial results
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-    const int t = warp >> 2, q4 = warp & 3, row = 32 * q4 + lane;
-    const uint32_t t_s = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256, t_o = t_s + 128;
+    const int t = warp >> 2, q4 = warp & 3, lane_row = 32 * q4 + lane;
+    const uint32_t t_s = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256, t_o = t_s + 128, t_p = t_s + kColP;
     const float c = kLog2e * rsqrtf((float)kD);
     int n = 0, kt = 0, ring_page = 0;                           // blocks and segments of this tile so far; pages of both
     auto arrive_warp = [&](uint32_t bar) {
@@ -373,11 +414,99 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       ring_page += min(2 * g.cnt, (len + kPage - 1) / kPage - 2 * g.j0);
       const int steps = tile_blocks(g, t);
       if (steps == 0) continue;
+      const int wrap = kRows / g.replicas, replica = lane_row / wrap, row = lane_row - replica * wrap;
       const int base_row = g.dual ? 0 : t * kRows, urow = base_row + row;
-      const bool row_valid = urow < g.rows, warp_live = base_row + 32 * q4 < g.rows;
+      const bool row_valid = urow < g.rows, warp_live = base_row + row - lane < g.rows;
       const int node = min(g.unit * kUnitRows + urow, g.n * a.L.G - 1) / a.L.G;
       const uint32_t* mask = a.mask + ((size_t)g.b * a.n_q + node) * a.mask_words;
       float m_ref = 0.f, l = 0.f;
+      // One block, of whose 128 columns this thread takes kCols: all of them, or with the rows there twice or four times
+      // its copy's half or quarter, P being zero elsewhere.
+      auto block = [&](auto cols_tag, int s_i, int p0) {
+        constexpr int kCols = decltype(cols_tag)::value, kWords = kCols / 2;
+        const int col0 = kCols == 128 ? 0 : replica * kCols;
+        uint32_t sv[kCols];
+        float* s = reinterpret_cast<float*>(sv);
+#pragma unroll
+        for (int i = 0; i < kCols / 32; ++i) tmem_ld32(t_s + col0 + 32 * i, sv + 32 * i);
+        tmem_ld_wait();
+        if (kOwnP) {
+          tc_fence_before();
+          arrive_warp(s_free(t));
+        }
+        if (p0 + kBlock > g.ctx) {                              // the drafted nodes, and what lies behind them
+#pragma unroll
+          for (int w = 0; w < kCols / 32; ++w) {
+            const uint32_t seen = seen32(mask, p0 + col0 + 32 * w - g.ctx, g.n);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!((seen >> i) & 1u)) s[32 * w + i] = -INFINITY;
+          }
+        }
+        float mx;
+        {
+          float m[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+          for (int i = 4; i < kCols - 4; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m[e] = max3(m[e], s[i + 2 * e], s[i + 2 * e + 1]);
+          mx = fmaxf(max3(max3(m[0], s[kCols - 4], s[kCols - 3]), m[1], m[2]), max3(m[3], s[kCols - 2], s[kCols - 1]));
+        }
+        if (kOwnP && n > 0) {                                   // the product of the block before is complete
+          mbar_wait(p_free(t), (n - 1) & 1, abort_flag, status);
+          tc_fence_after();
+        }
+        if (s_i == 0) {
+          m_ref = fmaxf(mx, -1e30f);                            // a row that sees nothing here keeps p = 0 and l = 0
+          l = 0.f;
+        } else if (const bool grown = (mx - m_ref) * c > kRescaleLog2; __any_sync(0xffffffffu, grown)) {
+          const float f = grown ? fast_exp2((m_ref - mx) * c) : 1.0f;       // a row's bits do not depend on its neighbours
+          if (grown) m_ref = mx;
+          l *= f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < RV; c0 += 16) {                 // (where P lies over S, S implies that product)
+            uint32_t v[16];
+            tmem_ld16(t_o + c0, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_st16(t_o + c0, v);
+          }
+        }
+        if (kCols < 128 && (!kOwnP || s_i == 0)) {              // the other copies' columns: once, or wherever S has been
+          const uint32_t zero[16] = {};
+#pragma unroll 1
+          for (int w = 0; w < 64; w += 16)
+            if (w / kWords != replica) tmem_st16(t_p + w, zero);
+        }
+        const uint64_t c2 = pack2(c, c), neg2 = pack2(-m_ref * c, -m_ref * c);
+        uint64_t sum[2] = {0ull, 0ull};                         // pairs of +0
+#pragma unroll
+        for (int q = 0; q < kCols / 32; ++q) {                  // probabilities as bf16 pairs
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float x0, x1;
+            unpack2(fma2(pack2(s[32 * q + 2 * i], s[32 * q + 2 * i + 1]), c2, neg2), x0, x1);
+            const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
+            sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
+            pk[i] = pack_bf16(e0, e1);
+          }
+          tmem_st16(t_p + col0 / 2 + 16 * q, pk);
+          if (kCols == 128 && q == 1) {                         // the first page's may be used already
+            tmem_st_wait();
+            tc_fence_before();
+            arrive_warp(p_full(t, 0));
+          }
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        if (kCols < 128) arrive_warp(p_full(t, 0));
+        arrive_warp(p_full(t, 1));
+        float a0, a1;
+        unpack2(add2(sum[0], sum[1]), a0, a1);
+        l += a0 + a1;
+      };
       for (int s_i = 0; s_i < steps; ++s_i, ++n) {
         const int j = g.dual ? 2 * s_i + t : s_i, p0 = (g.j0 + j) * kBlock;
         mbar_wait(s_full(t), n & 1, abort_flag, status);
@@ -391,7 +520,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             mbar_wait(full_bar(stg), (idx / nst) & 1, abort_flag, status);
             uint8_t* v = ring_ptr + stg * kStageBytes + kPageK;
             constexpr int kCpr = kSpanV / 16, kPerRow = RV / 8;
-            for (int e = row; e < (kPage - dead) * kPerRow; e += kRows) {
+            for (int e = lane_row; e < (kPage - dead) * kPerRow; e += kRows) {
               const int r = dead + e / kPerRow, ch = e % kPerRow;
               *reinterpret_cast<uint4*>(v + (ch / kCpr) * kPage * kSpanV + r * kSpanV + (ch % kCpr) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
@@ -399,82 +528,27 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           fence_proxy_async_smem();
         }
         if (!warp_live) {                                       // none of the warp's rows exists
+          if (kOwnP) {                                          // not before the others have published the block before
+            arrive_warp(s_free(t));
+            if (n > 0) mbar_wait(p_free(t), (n - 1) & 1, abort_flag, status);
+          }
           arrive_warp(p_full(t, 0));
           arrive_warp(p_full(t, 1));
-          continue;
+        } else if (g.replicas == 1) {
+          block(std::integral_constant<int, 128>{}, s_i, p0);
+        } else if (g.replicas == 2) {
+          block(std::integral_constant<int, 64>{}, s_i, p0);
+        } else {
+          block(std::integral_constant<int, 32>{}, s_i, p0);
         }
-        uint32_t sv[128];
-        float* s = reinterpret_cast<float*>(sv);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32 * i, sv + 32 * i);
-        tmem_ld_wait();
-        if (p0 + kBlock > g.ctx) {                              // the drafted nodes, and what lies behind them
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t seen = seen32(mask, p0 + 32 * w - g.ctx, g.n);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!((seen >> i) & 1u)) s[32 * w + i] = -INFINITY;
-          }
-        }
-        float mx;
-        {
-          float m[4] = {s[0], s[1], s[2], s[3]};
-#pragma unroll
-          for (int i = 4; i < 124; i += 8)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m[e] = max3(m[e], s[i + 2 * e], s[i + 2 * e + 1]);
-          mx = fmaxf(max3(max3(m[0], s[124], s[125]), m[1], m[2]), max3(m[3], s[126], s[127]));
-        }
-        if (s_i == 0) {
-          m_ref = fmaxf(mx, -1e30f);                            // a row that sees nothing here keeps p = 0 and l = 0
-          l = 0.f;
-        } else if (const bool grown = (mx - m_ref) * c > kRescaleLog2; __any_sync(0xffffffffu, grown)) {
-          const float f = grown ? fast_exp2((m_ref - mx) * c) : 1.0f;       // a row's bits do not depend on its neighbours
-          if (grown) m_ref = mx;
-          l *= f;
-#pragma unroll 1
-          for (int c0 = 0; c0 < RV; c0 += 16) {                 // the product of the block before is complete: S is
-            uint32_t v[16];
-            tmem_ld16(t_o + c0, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            tmem_st16(t_o + c0, v);
-          }
-        }
-        const uint64_t c2 = pack2(c, c), neg2 = pack2(-m_ref * c, -m_ref * c);
-        uint64_t sum[2] = {0ull, 0ull};                         // pairs of +0
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {                           // a page: probabilities as bf16 pairs over the scores
-#pragma unroll
-          for (int q = 2 * h; q < 2 * h + 2; ++q) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              float x0, x1;
-              unpack2(fma2(pack2(s[32 * q + 2 * i], s[32 * q + 2 * i + 1]), c2, neg2), x0, x1);
-              const float e0 = fast_exp2(x0), e1 = fast_exp2(x1);
-              sum[i & 1] = add2(sum[i & 1], pack2(e0, e1));
-              pk[i] = pack_bf16(e0, e1);
-            }
-            tmem_st16(t_s + 16 * q, pk);
-          }
-          tmem_st_wait();
-          tc_fence_before();
-          arrive_warp(p_full(t, h));
-        }
-        float a0, a1;
-        unpack2(add2(sum[0], sum[1]), a0, a1);
-        l += a0 + a1;
       }
-      // ---- the segment's partial result, [slot][RV / 4][slot rows] float4: a warp writes 512 contiguous bytes
+      // ---- the segment's partial result, [slot][RV / 4][128 lanes] float4: a warp writes 512 contiguous bytes
       mbar_wait(o_full(t), kt & 1, abort_flag, status);
       ++kt;
       tc_fence_after();
       if (warp_live) {
         const size_t slot = (size_t)g.slot * 2 + t;
-        float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * a.slot_rows + row;
+        float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * kRows + lane_row;
 #pragma unroll 1
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16];
@@ -483,10 +557,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           if (row_valid) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              po[(size_t)(c0 / 4 + i) * a.slot_rows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+              po[(size_t)(c0 / 4 + i) * kRows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
           }
         }
-        if (row_valid) reinterpret_cast<float2*>(a.part_ml)[slot * a.slot_rows + row] = make_float2(m_ref * c, l);
+        if (row_valid) reinterpret_cast<float2*>(a.part_ml)[slot * kRows + lane_row] = make_float2(m_ref * c, l);
       }
       tc_fence_before();                                        // ordered before this tile's next P by the arrival that publishes it
     }

@@ -25,19 +25,18 @@ struct Args {
   int32_t* status;
   // planning and workspace (see carve)
   int n_cta, max_units;                    // CTAs; units per (sequence, KV head) at most
-  int slot_rows;                           // rows of one partial result
   int nst;                                 // ring stages
   __nv_bfloat16* qp;                       // [B][Hkv][n_q G][r_k]  projected queries, rows (node, head of the group)
   int* prefix;                             // [B + 1] running cost of the sequences
-  float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][slot_rows] float4
-  float* part_ml;                          // [(n_cta + units)][2 tiles][slot_rows] float2: reference (base 2), sum
+  int* ranges;                             // [n_cta + 1] first position of every CTA
+  float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][128 lanes] float4
+  float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (base 2), sum
 };
 
 // Workspace: a segment is found by (CTA + unit), so there are at most n_cta + units of them
 inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_v, Args* a) {
   const int G = Hq / Hkv, rows = n_q * G, n_cta = host::sm_count();
   const int max_units = (rows + kUnitRows - 1) / kUnitRows;
-  const int slot_rows = rows >= 128 ? 128 : (rows + 31) / 32 * 32;
   const size_t slots = 2 * ((size_t)n_cta + (size_t)B * Hkv * max_units);
   uint8_t* p = static_cast<uint8_t*>(base);
   size_t off = 0;
@@ -46,13 +45,13 @@ inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_
     off += host::align_up(bytes, 128);
     return at;
   };
-  uint8_t *prefix = take((size_t)(B + 1) * 4), *qp = take((size_t)B * Hkv * rows * r_k * 2);
-  uint8_t *po = take(slots * slot_rows * r_v * 4), *ml = take(slots * slot_rows * 8);
+  uint8_t *prefix = take((size_t)(B + 1) * 4), *ranges = take((size_t)(n_cta + 1) * 4), *qp = take((size_t)B * Hkv * rows * r_k * 2);
+  uint8_t *po = take(slots * 128 * r_v * 4), *ml = take(slots * 128 * 8);
   if (a) {
     a->n_cta = n_cta;
     a->max_units = max_units;
-    a->slot_rows = slot_rows;
     a->prefix = reinterpret_cast<int*>(prefix);
+    a->ranges = reinterpret_cast<int*>(ranges);
     a->qp = reinterpret_cast<__nv_bfloat16*>(qp);
     a->part_o = reinterpret_cast<float*>(po);
     a->part_ml = reinterpret_cast<float*>(ml);
@@ -95,7 +94,9 @@ inline int check(const stief_layer* l, const stief_batch* batch, const uint16_t*
   if ((long long)l->num_pages * l->Hkv * kPage >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;   // pool rows are counted in int
   // rows of the projected queries and positions of the work axis are counted in int
   const long long rows = (long long)n_q * (l->Hq / l->Hkv), units = (long long)batch->B * l->Hkv * ((rows + kUnitRows - 1) / kUnitRows);
-  if ((long long)batch->B * l->Hkv * rows >= (1ll << 31) || units * (batch->max_pages_per_seq / 2 + 1 + kPad) >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;
+  if ((long long)batch->B * l->Hkv * rows >= (1ll << 31) || units * (batch->max_pages_per_seq / 2 + 1 + kPad) >= (1ll << 31) ||
+      (units + host::sm_count()) * 256 >= (1ll << 31))
+    return STIEF_ERR_INVALID_ARG;
   if (!workspace || !host::aligned(workspace, 128)) return STIEF_ERR_INVALID_ARG;
   if (workspace_bytes < stief_tree_workspace_bytes(batch->B, n_q, l->Hq, l->Hkv, l->r_v)) return STIEF_ERR_WORKSPACE;
   a->L.Hq = l->Hq; a->L.Hkv = l->Hkv; a->L.G = l->Hq / l->Hkv; a->L.r_k = l->r_k; a->L.r_v = l->r_v; a->L.num_pages = l->num_pages;
