@@ -76,9 +76,8 @@ __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
 
 // ---------------------------------------------------------------------------------------------
 // combine_kernel: 16 rows of one (sequence, KV head).  The segments of the rows' unit follow from the running costs and the CTAs'
-// ranges; each left one partial result per tile that had a block and per copy of the rows.  All its time is the latency of
-// loads, hence the many threads for 16 rows: the weights of all parts are found first, then every thread sums four channels of a
-// row over a share of the parts.  The back-projection runs on mma.sync with the joined rows as bf16 value + remainder (16
+// ranges; each left one partial result.  All its time is the latency of loads, hence the many threads for 16 rows: the
+// weights of all parts are found first, then every thread sums four channels of a row over a share of the parts.  The back-projection runs on mma.sync with the joined rows as bf16 value + remainder (16
 // significant bits) and U_v fetched before the wait for the kernel that makes the parts.
 // ---------------------------------------------------------------------------------------------
 constexpr int kJoinThreads = 512;
@@ -90,7 +89,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   static_assert(kItems <= kJoinThreads, "an item per thread");
   __shared__ __align__(16) __nv_bfloat16 hi[kSmallRows * kRow], lo[kSmallRows * kRow];
   __shared__ float weight[kPartChunk][kSmallRows];
-  __shared__ int part_at[kPartChunk];                           // (slot, copy) of the part as its first lane, -1: no such part
+  __shared__ int slot_of[kPartChunk];
   __shared__ float red[kJoinThreads / 32][kSmallRows];
   __shared__ float4 share[kSplit > 1 ? (kSplit - 1) * kItems : 1];
   __shared__ int range_of[2];
@@ -111,7 +110,6 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   if (live <= 0) return;
   const int unit = r0 / kUnitRows, rows = min(s.n * G - unit * kUnitRows, kUnitRows), in_unit = r0 - unit * kUnitRows;
   const bool dual = rows <= kRows;
-  const int copies = replicas_of(rows), wrap = kRows / copies;
   const int tile = dual ? 0 : in_unit / kRows, row0 = in_unit - tile * kRows;
   const int total = a.prefix[a.Bt.B], n = cta_count(a, total);
   const int first = a.prefix[b] + (h * s.units + unit) * (s.blocks + kPad) + kPad, end = first + s.blocks;     // real blocks
@@ -121,21 +119,17 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     if (lo_i < end && end <= hi_i) range_of[1] = i;
   }
   __syncthreads();
-  const int c0 = range_of[0], per_cta = 2 * copies, parts = per_cta * (range_of[1] - c0 + 1), slot0 = (b * a.L.Hkv + h) * a.max_units + unit;
-  const int r = tid % kSmallRows, grp = tid / kSmallRows, at = row0 + min(r, live - 1);
-  auto list_parts = [&](int p0) {                               // parts [p0, p0 + kPartChunk): CTA, tile, copy
-    __syncthreads();
-    if (tid < kPartChunk) {
-      int x = -1;
-      if (p0 + tid < parts) {
-        const int i = (p0 + tid) / per_cta, rest = p0 + tid - i * per_cta, t = rest / copies, cta = c0 + i;
-        const int cnt = min(end, a.ranges[cta + 1]) - max(first, a.ranges[cta]);
-        if (t ? (dual ? cnt > 1 : cnt > 0 && tile == 1) : cnt > 0 && (dual || tile == 0)) x = ((cta + slot0) * 2 + t) * kRows + (rest - t * copies) * wrap;
-      }
-      part_at[tid] = x;
-    }
-    __syncthreads();
+  // Every CTA from the first to the last has a block of the unit, and so a part of tile 0 (or of the rows' own tile, when the
+  // tiles hold different rows); tile 1 has one too where it had a block, else tile 0's part stands in with weight 0.
+  const int c0 = range_of[0], parts = (dual ? 2 : 1) * (range_of[1] - c0 + 1), slot0 = (c0 + (b * a.L.Hkv + h) * a.max_units + unit) * 2;
+  auto part_slot = [&](int p, bool& there) {
+    there = true;
+    if (!dual) return slot0 + 2 * p + tile;
+    const int cta = c0 + (p >> 1);
+    there = !(p & 1) || min(end, a.ranges[cta + 1]) - max(first, a.ranges[cta]) > 1;
+    return slot0 + p - (there ? 0 : 1);
   };
+  const int r = tid % kSmallRows, grp = tid / kSmallRows, at = row0 + min(r, live - 1);
   auto over_groups = [&](float v, auto join) {                  // over the threads that share a row
     v = join(v, __shfl_xor_sync(0xffffffffu, v, 16));
     __syncthreads();
@@ -145,37 +139,34 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     for (int i = 1; i < kJoinThreads / 32; ++i) v = join(i > 1 ? v : red[0][r], red[i][r]);
     return v;
   };
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at;
   float M = -INFINITY;
-  for (int p0 = 0; p0 < parts; p0 += kPartChunk) {
-    list_parts(p0);
-    for (int p = grp; p < min(parts - p0, kPartChunk); p += kGroups)
-      if (part_at[p] >= 0) M = fmaxf(M, ml[(size_t)part_at[p] + at].x);
+  for (int p = grp; p < parts; p += kGroups) {
+    bool there;
+    M = fmaxf(M, ml[(size_t)part_slot(p, there) * kRows].x);
   }
   M = over_groups(M, [](float x, float y) { return fmaxf(x, y); });
   float den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
   const int item = tid % kItems, share_i = tid / kItems, ir = item % kSmallRows, c4 = item / kSmallRows, iat = row0 + min(ir, live - 1);
   for (int p0 = 0; p0 < parts; p0 += kPartChunk) {
-    if (parts > kPartChunk) list_parts(p0);                     // else the list still stands
+    if (p0) __syncthreads();                                    // the weights of the chunk before have been read
     const int cnt = min(parts - p0, kPartChunk);
     for (int p = grp; p < cnt; p += kGroups) {
-      float w = 0.f;
-      if (part_at[p] >= 0) {
-        const float2 x = ml[(size_t)part_at[p] + at];
-        w = fast_exp2(x.x - M);
-        den = fmaf(x.y, w, den);
-      }
+      bool there;
+      const int slot = part_slot(p0 + p, there);
+      const float2 x = ml[(size_t)slot * kRows];
+      const float w = there ? fast_exp2(x.x - M) : 0.f;
+      if (r == 0) slot_of[p] = slot;
+      den = fmaf(x.y, w, den);
       weight[p][r] = w;
     }
     __syncthreads();
     if (share_i < kSplit) {
 #pragma unroll 8
       for (int p = share_i; p < cnt; p += kSplit) {             // neighbouring threads, neighbouring rows
-        const int x = part_at[p];
-        if (x < 0) continue;
         const float w = weight[p][ir];
-        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)(x / kRows) * (RV / 4) + c4) * kRows + x % kRows + iat];
+        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)slot_of[p] * (RV / 4) + c4) * kRows + iat];
         num.x = fmaf(o.x, w, num.x);
         num.y = fmaf(o.y, w, num.y);
         num.z = fmaf(o.z, w, num.z);
@@ -299,7 +290,7 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
   if (!rows_map(&L.tmQ, a.qp, RK, (unsigned long long)batch->B * layer->Hkv * n_q * G, 32u, bk) ||
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
-  const int fixed = tree::kHeadBytes + 2 * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
+  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + 2 * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
   a.nst = (tree::kSmemLimit - fixed) / stage;
   if (a.nst > tree::kMaxStages) a.nst = tree::kMaxStages;
   L.smem = fixed + a.nst * stage;

@@ -15,7 +15,7 @@
 // scores -> softmax -> P V.  With more, each tile has its own rows and both use every block.
 // TMEM gives a warp 32 lanes, so 32 rows would keep one warp of four at work; with at most 64 or 32 rows a tile therefore holds
 // them twice or four times, each copy takes its half or quarter of a block's columns (P is zero elsewhere, the wasted products
-// cost nothing here) and is one more partial result to join.
+// cost nothing here) and is joined with the others when the segment ends.
 //   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
 //   warps 8, 11     cache pages by TMA into a ring, a stage = K page | V page of one KV head; Q' tiles
 //   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page), O += P V (N = r_v)
@@ -36,7 +36,9 @@ constexpr int kThreads = 384;
 constexpr int kRows = 128;                      // rows of a tile
 constexpr int kBlock = 128;                     // positions of a block: two pages
 constexpr int kSmemLimit = 232448;
-constexpr int kHeadBytes = 5120;                // prefix sums (4112), barriers (512)
+constexpr int kHeadBytes = 5120;                // prefix sums (4352), barriers (512)
+constexpr int kJoinBytes = 14336;               // joining the copies of rows, per tile 1024 of references and sums, 6144 of values
+__host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBytes : 0; }
 constexpr int kMaxStages = 12;
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
@@ -61,7 +63,8 @@ __device__ __forceinline__ int sequence_cost(const Args& a, const Seq& s) { retu
 __device__ __forceinline__ int range_start(int i, int n, int total) { return (int)((long long)i * total / n); }
 __device__ __forceinline__ int cta_count(const Args& a, int total) { return min(a.n_cta, total); }
 
-__device__ __forceinline__ int replicas_of(int rows) { return rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+// (with r_v > 64 a page takes the memory so long that one copy keeps up)
+__device__ __forceinline__ int replicas_of(int rows, int r_v) { return r_v > 64 ? 1 : rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
 
 struct Segment {
   int b, h, unit, slot;                         // unit: row block within the (sequence, KV head)
@@ -103,7 +106,7 @@ struct Walk {
       g.n = s.n;
       g.rows = min(s.n * a.L.G - g.unit * kUnitRows, kUnitRows);
       g.dual = g.rows <= kRows;
-      g.replicas = replicas_of(g.rows);
+      g.replicas = replicas_of(g.rows, a.L.r_v);
       g.valid = true;
       break;
     }
@@ -143,8 +146,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   int* pref = reinterpret_cast<int*>(smem);
   uint8_t* ctrl_ptr = smem + 4352;
   const uint32_t ctrl = smem_u32(ctrl_ptr);
-  const uint32_t q_smem = smem_u32(smem) + kHeadBytes, ring = q_smem + 2 * kQBytes;
-  uint8_t* ring_ptr = smem + kHeadBytes + 2 * kQBytes;
+  const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + 2 * kQBytes;
+  uint8_t* ring_ptr = smem + kHeadBytes + join_bytes(RV) + 2 * kQBytes;
   const int nst = a.nst;
   auto full_bar = [&](int s) { return ctrl + s * 8; };
   auto empty_bar = [&](int s) { return ctrl + (12 + s) * 8; };
@@ -262,6 +265,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 report(status, STIEF_ERR_BOUNDS);
                 pg = 0;
               }
+              if (q_due && first_q && j0 + jj == 4) send_queries(true);        // the first ones: a few pages are on their way
               if (use > 0) {
                 if (q_due) send_queries(!mbar_test_wait(empty_bar(st), (use - 1) & 1));        // no page to fetch: wait for the queries' place
                 mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
@@ -546,9 +550,55 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       mbar_wait(o_full(t), kt & 1, abort_flag, status);
       ++kt;
       tc_fence_after();
-      if (warp_live) {
-        const size_t slot = (size_t)g.slot * 2 + t;
-        float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * kRows + lane_row;
+      const size_t slot = (size_t)g.slot * 2 + t;
+      float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * kRows + row;
+      float2* pml = reinterpret_cast<float2*>(a.part_ml) + slot * kRows + row;
+      float weight = 1.0f, top = m_ref * c, total_l = l;
+      if (RV <= 64 && g.replicas > 1) {                         // a row's copies are joined here, 16 channels at a time
+        uint8_t* join = smem + kHeadBytes + t * (kJoinBytes / 2);
+        float2* copy_ml = reinterpret_cast<float2*>(join);      // [copy][row]
+        float4* copy_o = reinterpret_cast<float4*>(join + 1024);        // [copy - 1][four channels][row]
+        auto meet = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory"); };
+        copy_ml[lane_row] = make_float2(top, l);
+        meet();
+        for (int i = 0; i < g.replicas; ++i) top = fmaxf(top, copy_ml[i * wrap + row].x);
+        total_l = 0.f;
+        for (int i = 0; i < g.replicas; ++i) {
+          const float2 x = copy_ml[i * wrap + row];
+          total_l = fmaf(x.y, fast_exp2(x.x - top), total_l);
+        }
+        weight = fast_exp2(m_ref * c - top);
+#pragma unroll 1
+        for (int c0 = 0; c0 < RV; c0 += 16) {
+          uint32_t v[16];
+          tmem_ld16(t_o + c0, v);
+          tmem_ld_wait();
+          float* o = reinterpret_cast<float*>(v);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] *= weight;
+          if (replica > 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) copy_o[((replica - 1) * 4 + i) * wrap + row] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          }
+          meet();
+          if (replica == 0) {
+            for (int k = 0; k + 1 < g.replicas; ++k)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float4 x = copy_o[(k * 4 + i) * wrap + row];
+                o[4 * i] += x.x;
+                o[4 * i + 1] += x.y;
+                o[4 * i + 2] += x.z;
+                o[4 * i + 3] += x.w;
+              }
+            if (row_valid) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) po[(size_t)(c0 / 4 + i) * kRows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+          }
+          meet();
+        }
+      } else if (warp_live) {
 #pragma unroll 1
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16];
@@ -560,8 +610,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               po[(size_t)(c0 / 4 + i) * kRows] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
           }
         }
-        if (row_valid) reinterpret_cast<float2*>(a.part_ml)[slot * kRows + lane_row] = make_float2(m_ref * c, l);
       }
+      if (replica == 0 && row_valid) *pml = make_float2(top, total_l);
       tc_fence_before();                                        // ordered before this tile's next P by the arrival that publishes it
     }
   }
