@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   __shared__ int slot_of[kPartChunk];
   __shared__ float red[kJoinThreads / 32][kSmallRows];
   __shared__ float4 share[kSplit > 1 ? (kSplit - 1) * kItems : 1];
-  __shared__ int range_of[2];
+  __shared__ int start_of[kPartChunk], cost_of[2][kJoinThreads / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z, G = a.L.G, r0 = blockIdx.x * kSmallRows;
   const bool fold = a.L.U_v == nullptr;
@@ -104,29 +104,48 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) u[k][i] = *reinterpret_cast<const uint32_t*>(U + k * 16 + i * 8);
   }
+  // what the partition says, found again from the lengths while the kernel before still runs
   const Seq s = sequence(a, b);
   const int live = min(kSmallRows, s.n * G - r0);
-  grid_dependency_wait();
   if (live <= 0) return;
+  int before = 0, all = 0;                                      // running cost up to this sequence, and of all
+  for (int i = tid; i < a.Bt.B; i += kJoinThreads) {
+    const int cost = sequence_cost(a, sequence(a, i));
+    all += cost;
+    before += i < b ? cost : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) {
+    cost_of[0][warp] = before;
+    cost_of[1][warp] = all;
+  }
+  __syncthreads();
+  int total = 0;
+  before = 0;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 32; ++i) {
+    before += cost_of[0][i];
+    total += cost_of[1][i];
+  }
   const int unit = r0 / kUnitRows, rows = min(s.n * G - unit * kUnitRows, kUnitRows), in_unit = r0 - unit * kUnitRows;
   const bool dual = rows <= kRows;
   const int tile = dual ? 0 : in_unit / kRows, row0 = in_unit - tile * kRows;
-  const int total = a.prefix[a.Bt.B], n = cta_count(a, total);
-  const int first = a.prefix[b] + (h * s.units + unit) * (s.blocks + kPad) + kPad, end = first + s.blocks;     // real blocks
-  for (int i = tid; i < n; i += kJoinThreads) {                 // the CTAs that hold the unit's first and last block
-    const int lo_i = a.ranges[i], hi_i = a.ranges[i + 1];
-    if (lo_i <= first && first < hi_i) range_of[0] = i;
-    if (lo_i < end && end <= hi_i) range_of[1] = i;
-  }
+  const int n = cta_count(a, total);
+  const int first = before + (h * s.units + unit) * (s.blocks + kPad) + kPad, end = first + s.blocks;     // real blocks
+  // the CTA whose range holds position p is the last one that starts at or before it
+  auto owner = [&](int p) { return (int)((((long long)p + 1) * n - 1) / total); };
+  const int c0 = owner(first), c1 = owner(end - 1);
+  for (int i = tid; i <= c1 + 1 - c0 && i < kPartChunk; i += kJoinThreads) start_of[i] = range_start(c0 + i, n, total);
   __syncthreads();
   // Every CTA from the first to the last has a block of the unit, and so a part of tile 0 (or of the rows' own tile, when the
   // tiles hold different rows); tile 1 has one too where it had a block, else tile 0's part stands in with weight 0.
-  const int c0 = range_of[0], parts = (dual ? 2 : 1) * (range_of[1] - c0 + 1), slot0 = (c0 + (b * a.L.Hkv + h) * a.max_units + unit) * 2;
+  const int parts = (dual ? 2 : 1) * (c1 - c0 + 1), slot0 = (c0 + (b * a.L.Hkv + h) * a.max_units + unit) * 2;
   auto part_slot = [&](int p, bool& there) {
     there = true;
     if (!dual) return slot0 + 2 * p + tile;
-    const int cta = c0 + (p >> 1);
-    there = !(p & 1) || min(end, a.ranges[cta + 1]) - max(first, a.ranges[cta]) > 1;
+    const int i = p >> 1, lo = i + 1 < kPartChunk ? start_of[i] : range_start(c0 + i, n, total), hi = i + 1 < kPartChunk ? start_of[i + 1] : range_start(c0 + i + 1, n, total);
+    there = !(p & 1) || min(end, hi) - max(first, lo) > 1;
     return slot0 + p - (there ? 0 : 1);
   };
   const int r = tid % kSmallRows, grp = tid / kSmallRows, at = row0 + min(r, live - 1);
@@ -139,6 +158,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     for (int i = 1; i < kJoinThreads / 32; ++i) v = join(i > 1 ? v : red[0][r], red[i][r]);
     return v;
   };
+  grid_dependency_wait();
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at;
   float M = -INFINITY;
   for (int p = grp; p < parts; p += kGroups) {

@@ -206,11 +206,6 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  if (blockIdx.x == 0) {                        // for the combine kernel
-    const int total = pref[a.Bt.B], n = cta_count(a, total);
-    for (int b = tid; b <= a.Bt.B; b += kThreads) a.prefix[b] = pref[b];
-    for (int i = tid; i <= n && total > 0; i += kThreads) a.ranges[i] = range_start(i, n, total);
-  }
 
   Walk walk;
   walk.start(a, pref);
@@ -219,8 +214,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     if (warp == 8 || warp == 11) {
       // ---------------------------------------------------------------------------------------- cache pages, Q' tiles
       // One warp fetches the K halves of the pages, the other the V halves (a warp needs some 500 cycles per page for both,
-      // which is what a page of ranks 48/48 may take in all) and the queries, which it must not wait for before the ring
-      // is on its way: they come from a kernel that may still run, or their place is in use by the segment before.
+      // which is what a page of ranks 48/48 may take in all) and the queries.  The first of these come from the kernel before,
+      // which is over about when this one starts; later ones wait for their place, and pages go ahead of them meanwhile.
       const bool keys = warp == 8;
       if (lane == 0) {
         tma_prefetch_desc(keys ? &tmK : &tmV);
@@ -255,6 +250,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           }
         };
         int ids = lane < pages ? bt[lane] : 0;
+        if (lane == 0 && q_due && first_q) send_queries(true);
         for (int j0 = 0; j0 < pages; j0 += 32) {
           const int nxt = j0 + 32 + lane < pages ? bt[j0 + 32 + lane] : 0;     // a batch of page ids ahead
           const int cnt = min(32, pages - j0);
@@ -265,7 +261,6 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 report(status, STIEF_ERR_BOUNDS);
                 pg = 0;
               }
-              if (q_due && first_q && j0 + jj == 4) send_queries(true);        // the first ones: a few pages are on their way
               if (use > 0) {
                 if (q_due) send_queries(!mbar_test_wait(empty_bar(st), (use - 1) & 1));        // no page to fetch: wait for the queries' place
                 mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);

@@ -27,8 +27,6 @@ struct Args {
   int n_cta, max_units;                    // CTAs; units per (sequence, KV head) at most
   int nst;                                 // ring stages
   __nv_bfloat16* qp;                       // [B][Hkv][n_q G][r_k]  projected queries, rows (node, head of the group)
-  int* prefix;                             // [B + 1] running cost of the sequences
-  int* ranges;                             // [n_cta + 1] first position of every CTA
   float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][128 lanes] float4
   float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (base 2), sum
 };
@@ -45,13 +43,11 @@ inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_
     off += host::align_up(bytes, 128);
     return at;
   };
-  uint8_t *prefix = take((size_t)(B + 1) * 4), *ranges = take((size_t)(n_cta + 1) * 4), *qp = take((size_t)B * Hkv * rows * r_k * 2);
+  uint8_t* qp = take((size_t)B * Hkv * rows * r_k * 2);
   uint8_t *po = take(slots * 128 * r_v * 4), *ml = take(slots * 128 * 8);
   if (a) {
     a->n_cta = n_cta;
     a->max_units = max_units;
-    a->prefix = reinterpret_cast<int*>(prefix);
-    a->ranges = reinterpret_cast<int*>(ranges);
     a->qp = reinterpret_cast<__nv_bfloat16*>(qp);
     a->part_o = reinterpret_cast<float*>(po);
     a->part_ml = reinterpret_cast<float*>(ml);

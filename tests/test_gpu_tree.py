@@ -146,8 +146,8 @@ def test_tile_edges_of_large_trees(n, G):
     assert int(c.status) == 0
 
 
-@pytest.mark.parametrize("lens", [[5000], [20000], [3, 9000, 500, 0], [127, 128, 129, 191, 192, 193, 255, 256, 257, 383, 384, 385]])
-@pytest.mark.parametrize("n", [3, 17, 64])
+@pytest.mark.parametrize("lens", [[5000], [20000], [8000] * 4, [3, 9000, 500, 0], [127, 128, 129, 191, 192, 193, 255, 256, 257, 383, 384, 385]])
+@pytest.mark.parametrize("n", [3, 16, 17, 32, 64])
 def test_long_contexts_are_cut_and_joined(lens, n):
     c = TreeCase(sum(lens) + n, lens, n, Hq=32, Hkv=8)
     c.check(*c.run())
