@@ -237,8 +237,9 @@ class PageTable:
         cached = self.__dict__.get("_c")
         if cached is not None and cached[0] == key:
             return cached[1]
-        for t in (self.block_table, self.seq_lens, self.page_counts, self.ref_counts):
-            _int32(t, "page table")
+        at = _int32(self.block_table, "block_table")
+        for t in (self.seq_lens, self.page_counts, self.ref_counts):
+            _int32(t, "page table", None, at)
         B = self.block_table.shape[0]
         if self.block_table.dim() != 2 or self.seq_lens.shape != (B,) or self.page_counts.shape != (B,):
             raise ValueError("block_table [B, max_pages], seq_lens [B] and page_counts [B] disagree")
@@ -248,21 +249,30 @@ class PageTable:
         return st
 
 
-def _here(t: torch.Tensor, name: str) -> torch.Tensor:
-    """The kernels run on torch's current device and stream: a tensor of another device is refused."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str, device: Optional[int] = None) -> int:
+    """The kernels run on torch's current device and stream: a tensor of another device is refused.  Returns the device."""
+    at = t.get_device()
+    if at < 0 or at != (torch.cuda.current_device() if device is None else device):
         raise ValueError(f"{name} is on {t.device}, not on the current CUDA device")
-    return t
+    return at
 
 
-def _int32(t: torch.Tensor, name: str, shape=None) -> torch.Tensor:
-    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+def _int32(t: torch.Tensor, name: str, shape=None, device: Optional[int] = None) -> int:
+    if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be a contiguous int32 tensor" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    return _here(t, name)
+    return _here(t, name, device)
 
 
-def _status(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else _int32(t, "status").data_ptr()
+def _status(t: Optional[torch.Tensor], device: int) -> Optional[int]:
+    if t is None:
+        return None
+    _int32(t, "status", None, device)
+    return t.data_ptr()
+
+
+def _raw_stream(device: int) -> int:
+    """torch's current stream on the device, without making a Stream object for it (these calls take a few microseconds)."""
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 def _check(rc: int, where: str):
@@ -498,32 +508,36 @@ def stief_tree_attention(layer: Layer, batch: Batch, q: torch.Tensor, tree_mask:
     """A tree of drafted tokens over the cache: q [B, n_q, Hq, d_q] bf16 -> out [B, n_q, Hq, d_out] bf16 (strides over b and t
     free).  seq_lens is the context; node j is cached at position seq_lens[b] + j.  tree_mask [B, n_q, words] int32: bit j of
     row i = node i attends node j.  n_nodes [B] int32: real nodes per sequence (default n_q)."""
-    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.dim() != 4 or out.dim() != 4:
+    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or q.dim() != 4 or out.dim() != 4:
         raise ValueError("q and out must be bf16 [B, n_q, Hq, d]")
     B, n_q, Hq, d_q = q.shape
     d_out = D_HEAD if layer.U_v is not None else layer.r_v
-    if Hq != layer.Hq or d_q != (D_HEAD if layer.U_k is not None else layer.r_k) or tuple(out.shape) != (B, n_q, Hq, d_out) or B != batch.block_table.shape[0]:
+    if Hq != layer.Hq or d_q != (D_HEAD if layer.U_k is not None else layer.r_k) or out.shape != (B, n_q, Hq, d_out) or B != batch.block_table.shape[0]:
         raise ValueError("q, out, layer and batch disagree in shape")
-    if q.stride(3) != 1 or q.stride(2) != d_q or out.stride(3) != 1 or out.stride(2) != d_out:
+    qs, os_ = q.stride(), out.stride()
+    if qs[3] != 1 or (qs[2] != d_q and Hq > 1) or os_[3] != 1 or (os_[2] != d_out and Hq > 1):
         raise ValueError("heads and elements of q and out must be contiguous")
-    _int32(tree_mask, "tree_mask")
-    if tree_mask.dim() != 3 or tuple(tree_mask.shape[:2]) != (B, n_q):
+    at = _here(q, "q")
+    _int32(tree_mask, "tree_mask", None, at)
+    if tree_mask.dim() != 3 or tree_mask.shape[:2] != (B, n_q):
         raise ValueError("tree_mask must be [B, n_q, words]")
     if n_nodes is not None:
-        _int32(n_nodes, "n_nodes", (B,))
-    if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (B, n_q, Hq)):
-        raise ValueError("out_lse must be contiguous fp32 [B, n_q, Hq]")
-    for t, name in ((q, "q"), (out, "out"), (workspace, "workspace"), (layer.k_pool, "k_pool"), (batch.block_table, "block_table")):
-        _here(t, name)
-    _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), _ptr(q), _row_stride(q, 0), _row_stride(q, 1), n_q,
-                                      _ptr(n_nodes), _ptr(tree_mask), tree_mask.shape[2], _ptr(workspace),
-                                      workspace.numel() * workspace.element_size(), _ptr(out), _row_stride(out, 0), _row_stride(out, 1),
-                                      _ptr(out_lse), flags, _status(status), _stream()), "stief_tree_attention")
-
-
-def _row_stride(t: torch.Tensor, dim: int) -> int:
-    """Element stride of a leading dimension; one of extent 1 may carry any stride and gets the packed one."""
-    return t.stride(dim) if t.shape[dim] > 1 else max(t.stride(dim), t.stride(dim + 1) * t.shape[dim + 1])
+        _int32(n_nodes, "n_nodes", (B,), at)
+    if out_lse is not None:
+        if out_lse.dtype is not torch.float32 or not out_lse.is_contiguous() or out_lse.shape != (B, n_q, Hq):
+            raise ValueError("out_lse must be contiguous fp32 [B, n_q, Hq]")
+        _here(out_lse, "out_lse", at)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    for t, name in ((out, "out"), (workspace, "workspace"), (layer.k_pool, "k_pool"), (layer.v_pool, "v_pool"), (batch.block_table, "block_table"),
+                    (batch.seq_lens, "seq_lens")):
+        _here(t, name, at)
+    q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (max(qs[1], Hq * d_q), max(os_[1], Hq * d_out))       # an extent of 1 may carry any stride
+    q_b, o_b = (qs[0], os_[0]) if B > 1 else (max(qs[0], q_t), max(os_[0], o_t))
+    _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(n_nodes),
+                                      tree_mask.data_ptr(), tree_mask.shape[2], workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), out.data_ptr(), o_b, o_t, _ptr(out_lse), flags,
+                                      _status(status, at), _raw_stream(at)), "stief_tree_attention")
 
 
 def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Tensor, n_accepted: torch.Tensor,
@@ -531,45 +545,46 @@ def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Ten
     """Moves the cache rows of the accepted nodes to the end of the context, in all layers: node accepted[b, j] goes to
     position seq_lens[b] + j for j < n_accepted[b].  accepted [B, max_accept] int32, strictly increasing along j."""
     B = batch.block_table.shape[0]
-    _int32(n_accepted, "n_accepted", (B,))
-    _int32(accepted, "accepted")
+    at = _int32(n_accepted, "n_accepted", (B,))
+    _int32(accepted, "accepted", None, at)
     if accepted.dim() != 2 or accepted.shape[0] != B:
         raise ValueError("accepted must be [B, max_accept]")
-    _here(batch.block_table, "block_table")
-    arr = (_CLayer * max(len(layers), 1))(*[_here_layer(l).c() for l in layers])
-    _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), _ptr(accepted), accepted.shape[1], _ptr(n_accepted),
-                                   _status(status), _stream()), "stief_tree_accept")
-
-
-def _here_layer(layer):
-    for t in _page_tensors(layer):
-        _here(t, "pool")
-    return layer
+    _here(batch.block_table, "block_table", at)
+    _here(batch.seq_lens, "seq_lens", at)
+    arr = _descriptors(layers, at, "_accept", lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
+    _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), accepted.data_ptr(), accepted.shape[1], n_accepted.data_ptr(),
+                                   _status(status, at), _raw_stream(at)), "stief_tree_accept")
 
 
 def stief_advance_seq_lens_by(seq_lens: torch.Tensor, deltas: torch.Tensor):
-    _int32(deltas, "deltas", _int32(seq_lens, "seq_lens").shape)
-    _check(lib().stief_advance_seq_lens_by(_ptr(seq_lens), _ptr(deltas), seq_lens.numel(), _stream()), "stief_advance_seq_lens_by")
+    at = _int32(seq_lens, "seq_lens")
+    _int32(deltas, "deltas", seq_lens.shape, at)
+    _check(lib().stief_advance_seq_lens_by(seq_lens.data_ptr(), deltas.data_ptr(), seq_lens.numel(), _raw_stream(at)), "stief_advance_seq_lens_by")
 
 
 def stief_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
                            out_lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, flags: int = 0):
     """Causal attention over packed prompts: q [total, Hq, 128], k, v [total, Hkv, 128], out [total, Hq, 128] bf16 (strides
     over tokens free), cu_seqlens [B + 1] int32, out_lse [total, Hq] fp32."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k, v and out must be [total, heads, 128]")
     total, Hq, Hkv = q.shape[0], q.shape[1], k.shape[1]
+    at, args = _here(q, "q"), []
     for t, name, heads in ((q, "q", Hq), (k, "k", Hkv), (v, "v", Hkv), (out, "out", Hq)):
-        if t.dtype != torch.bfloat16 or tuple(t.shape) != (total, heads, D_HEAD) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != D_HEAD):
+        st = t.stride()
+        if t.dtype is not torch.bfloat16 or t.shape != (total, heads, D_HEAD) or st[2] != 1 or (st[1] != D_HEAD and heads > 1):
             raise ValueError(f"{name} must be bf16 [{total}, {heads}, {D_HEAD}] with contiguous heads and elements")
-        _here(t, name)
-    _int32(cu_seqlens, "cu_seqlens")
+        _here(t, name, at)
+        args += [t.data_ptr(), st[0] if total > 1 else max(st[0], heads * D_HEAD)]
+    _int32(cu_seqlens, "cu_seqlens", None, at)
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
         raise ValueError("cu_seqlens must be [B + 1]")
-    if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (total, Hq)):
-        raise ValueError("out_lse must be contiguous fp32 [total, Hq]")
-    row = lambda t: t.stride(0) if total > 1 else max(t.stride(0), t.shape[1] * D_HEAD)
-    _check(lib().stief_prompt_attention(Hq, Hkv, cu_seqlens.numel() - 1, total, _ptr(cu_seqlens), _ptr(q), row(q), _ptr(k), row(k), _ptr(v),
-                                        row(v), _ptr(out), row(out), _ptr(out_lse), flags, _status(status), _stream()),
-           "stief_prompt_attention")
+    if out_lse is not None:
+        if out_lse.dtype is not torch.float32 or not out_lse.is_contiguous() or out_lse.shape != (total, Hq):
+            raise ValueError("out_lse must be contiguous fp32 [total, Hq]")
+        _here(out_lse, "out_lse", at)
+    _check(lib().stief_prompt_attention(Hq, Hkv, cu_seqlens.numel() - 1, total, cu_seqlens.data_ptr(), *args, _ptr(out_lse), flags,
+                                        _status(status, at), _raw_stream(at)), "stief_prompt_attention")
 
 
 def _page_tensors(layer):
@@ -578,15 +593,36 @@ def _page_tensors(layer):
     return (layer.k_pool, layer.v_pool)
 
 
-def _page_pools(layers):
-    """C array of every pool of the layers (Layer or QLayer), checked to hold the same pages."""
+def _descriptors(layers, device: int, slot: str, make):
+    """The C array that ``make`` builds from the layers, kept with the first layer and built again when any layer holds other
+    tensors, or other sizes, than it was built from (marshalling 32 layers takes longer than moving their rows)."""
+    if not layers:
+        return make()
+    kept = layers[0].__dict__.get(slot)
+    if kept is not None and kept[0] == device and len(kept[1]) == len(layers) and all(type(l) is Layer for l in layers):
+        for l, (k, v, kp, vp, rk, rv, Hkv) in zip(layers, kept[1]):
+            if l.k_pool is not k or l.v_pool is not v or k.data_ptr() != kp or v.data_ptr() != vp or l.r_k != rk or l.r_v != rv or l.Hkv != Hkv:
+                break
+        else:
+            return kept[2]
     tensors = [t for l in layers for t in _page_tensors(l)]
     for t in tensors:
         if not t.is_contiguous() or t.shape[0] != tensors[0].shape[0]:
             raise ValueError("pools must be contiguous and have the same number of pages")
-        _here(t, "pool")
-    arr = (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
-    return arr, len(tensors), tensors[0].shape[0] if tensors else 0
+        _here(t, "pool", device)
+    arr = make()
+    if all(type(l) is Layer for l in layers):
+        layers[0].__dict__[slot] = (device, [(l.k_pool, l.v_pool, l.k_pool.data_ptr(), l.v_pool.data_ptr(), l.r_k, l.r_v, l.Hkv) for l in layers], arr)
+    return arr
+
+
+def _page_pools(layers, device: int):
+    """C array of every pool of the layers (Layer or QLayer), checked to hold the same pages; and their number of pages."""
+    def make():
+        tensors = [t for l in layers for t in _page_tensors(l)]
+        return (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
+    arr = _descriptors(layers, device, "_pools", make)
+    return arr, sum(2 if type(l) is Layer else 3 for l in layers), layers[0].num_pages if layers else 0
 
 
 def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:
@@ -595,31 +631,34 @@ def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:
 
 def stief_pages_reserve(table: PageTable, extra, status: Optional[torch.Tensor] = None):
     """Pages for ``extra`` more tokens behind every slot's sequence: an int for all, or an int32 tensor [B]."""
-    per_slot = isinstance(extra, torch.Tensor)
+    per_slot, at = isinstance(extra, torch.Tensor), _here(table.block_table, "block_table")
     if per_slot:
-        _int32(extra, "extra", (table.block_table.shape[0],))
-    _check(lib().stief_pages_reserve(ctypes.byref(table.c()), _ptr(extra) if per_slot else None, 0 if per_slot else int(extra),
-                                     _status(status), _stream()), "stief_pages_reserve")
+        _int32(extra, "extra", table.block_table.shape[:1], at)
+    _check(lib().stief_pages_reserve(ctypes.byref(table.c()), extra.data_ptr() if per_slot else None, 0 if per_slot else int(extra),
+                                     _status(status, at), _raw_stream(at)), "stief_pages_reserve")
 
 
 def stief_pages_fork(table: PageTable, layers, parent: torch.Tensor, workspace: torch.Tensor, status: Optional[torch.Tensor] = None):
     """Slot b becomes a copy of slot parent[b] (int32 [B]; b = unchanged, -1 = emptied).  ``layers``: every Layer / QLayer whose
     pools this table pages."""
-    _int32(parent, "parent", (table.block_table.shape[0],))
-    arr, n, num_pages = _page_pools(layers)
+    at = _here(table.block_table, "block_table")
+    _int32(parent, "parent", table.block_table.shape[:1], at)
+    arr, n, num_pages = _page_pools(layers, at)
     if n and num_pages < table.ref_counts.shape[0]:
         raise ValueError("the table counts more pages than the pools hold")
-    _here(workspace, "workspace")
-    _check(lib().stief_pages_fork(ctypes.byref(table.c()), arr, n, _ptr(parent), _ptr(workspace),
-                                  workspace.numel() * workspace.element_size(), _status(status), _stream()), "stief_pages_fork")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _here(workspace, "workspace", at)
+    _check(lib().stief_pages_fork(ctypes.byref(table.c()), arr, n, parent.data_ptr(), workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(), _status(status, at), _raw_stream(at)), "stief_pages_fork")
 
 
 def stief_pages_copy(layers, src: torch.Tensor, dst: torch.Tensor, status: Optional[torch.Tensor] = None):
     """Page src[i] -> page dst[i] (int32 [n]) in every pool of the layers."""
-    _int32(src, "src")
-    _int32(dst, "dst", src.shape)
-    arr, n, num_pages = _page_pools(layers)
-    _check(lib().stief_pages_copy(arr, n, num_pages, _ptr(src), _ptr(dst), src.numel(), _status(status), _stream()), "stief_pages_copy")
+    at = _int32(src, "src")
+    _int32(dst, "dst", src.shape, at)
+    arr, n, num_pages = _page_pools(layers, at)
+    _check(lib().stief_pages_copy(arr, n, num_pages, _ptr(src), _ptr(dst), src.numel(), _status(status, at), _raw_stream(at)), "stief_pages_copy")
 
 
 def stief_append_chunk(layer: Layer, batch: Batch, K: torch.Tensor, V: torch.Tensor, chunk_lens: Optional[torch.Tensor] = None,

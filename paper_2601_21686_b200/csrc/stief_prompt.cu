@@ -63,11 +63,6 @@ static_assert(kSmem <= 232448, "227 KiB of shared memory per CTA");
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
 
-// Length of prompt b, or -1 when its boundaries are not usable
-__device__ __forceinline__ int prompt_len(const Args& a, int b) {
-  const int lo = a.cu[b], hi = a.cu[b + 1];
-  return lo < 0 || hi < lo || hi > a.total ? -1 : hi - lo;
-}
 struct Prompts {                                // in shared memory, in order of falling length
   int lo[kMaxBatch], len[kMaxBatch];
 };
@@ -155,12 +150,19 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     return;
   }
 
+  if (tid == 0) {
+    tma_prefetch_desc(&tmQ);
+    tma_prefetch_desc(&tmK);
+    tma_prefetch_desc(&tmV);
+  }
   // prompts in order of falling length (ties by number): the rank of each is a count over all
-  int* lens = reinterpret_cast<int*>(tiles_ptr);
+  int *lens = reinterpret_cast<int*>(tiles_ptr), *los = lens + kMaxBatch;
   for (int b = tid; b < a.B; b += kThreads) {
-    const int len = prompt_len(a, b);
-    if (len < 0) report(status, STIEF_ERR_BOUNDS);
-    lens[b] = max(len, 0);
+    const int lo = a.cu[b], hi = a.cu[b + 1];
+    const bool ok = lo >= 0 && hi >= lo && hi <= a.total;      // else its boundaries are not usable
+    if (!ok) report(status, STIEF_ERR_BOUNDS);
+    lens[b] = ok ? hi - lo : 0;
+    los[b] = lo;
   }
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
@@ -187,7 +189,7 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     const int mine = lens[b];
     int rank = 0;
     for (int i = 0; i < a.B; ++i) rank += lens[i] > mine || (lens[i] == mine && i < b);
-    ps.lo[rank] = a.cu[b];
+    ps.lo[rank] = los[b];
     ps.len[rank] = mine;
   }
   fence_proxy_async_smem();                     // the scratch above becomes a target of TMA writes
@@ -201,11 +203,6 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");       // 512 x 128 registers at launch = 256 x 176 + 128 x 80 + 128 x 80
     if (warp == 12) {
       // ---------------------------------------------------------------------------------------- producer
-      if (lane == 0) {
-        tma_prefetch_desc(&tmQ);
-        tma_prefetch_desc(&tmK);
-        tma_prefetch_desc(&tmV);
-      }
       int st = 0, use = 0, nq[2] = {0, 0};
       auto put = [&](const CUtensorMap* tm, int tok, int head) {
         if (use > 0) mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);

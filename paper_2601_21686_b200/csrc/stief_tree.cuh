@@ -63,8 +63,10 @@ __device__ __forceinline__ int sequence_cost(const Args& a, const Seq& s) { retu
 __device__ __forceinline__ int range_start(int i, int n, int total) { return (int)((long long)i * total / n); }
 __device__ __forceinline__ int cta_count(const Args& a, int total) { return min(a.n_cta, total); }
 
-// (with r_v > 64 a page takes the memory so long that one copy keeps up)
-__device__ __forceinline__ int replicas_of(int rows, int r_v) { return r_v > 64 ? 1 : rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
+// Copies of the rows in a tile.  With r_v > 64 a page takes the memory so long that one copy keeps up; and a segment of
+// one block per tile gains less from them (0.6 us) than joining them costs (2.8 us; at five blocks it is the other way round).
+constexpr int kFewBlocks = 2;
+__device__ __forceinline__ int replicas_of(int rows, int r_v, int blocks) { return r_v > 64 || blocks <= kFewBlocks ? 1 : rows <= 32 ? 4 : rows <= 64 ? 2 : 1; }
 
 struct Segment {
   int b, h, unit, slot;                         // unit: row block within the (sequence, KV head)
@@ -106,7 +108,7 @@ struct Walk {
       g.n = s.n;
       g.rows = min(s.n * a.L.G - g.unit * kUnitRows, kUnitRows);
       g.dual = g.rows <= kRows;
-      g.replicas = replicas_of(g.rows, a.L.r_v);
+      g.replicas = replicas_of(g.rows, a.L.r_v, g.cnt);
       g.valid = true;
       break;
     }
