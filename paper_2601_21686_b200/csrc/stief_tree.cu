@@ -80,13 +80,13 @@ __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
 // weights of all parts are found first, then every thread sums four channels of a row over a share of the parts.  The back-projection runs on mma.sync with the joined rows as bf16 value + remainder (16
 // significant bits) and U_v fetched before the wait for the kernel that makes the parts.
 // ---------------------------------------------------------------------------------------------
-constexpr int kJoinThreads = 512;
 constexpr int kPartChunk = 256;                                 // parts whose weights are held at a time
 
-template <int RV>
+template <int RV, int kJoinThreads>
 __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
-  constexpr int kRow = RV + 8, kGroups = kJoinThreads / kSmallRows, kItems = kSmallRows * RV / 4, kSplit = kJoinThreads / kItems > 0 ? kJoinThreads / kItems : 1;
-  static_assert(kItems <= kJoinThreads, "an item per thread");
+  constexpr int kWarps = kJoinThreads / 32, kTiles = 16 / kWarps;          // 8 output channels per warp and step
+  constexpr int kRow = RV + 8, kGroups = kJoinThreads / kSmallRows, kItems = kSmallRows * RV / 4;
+  constexpr int kSplit = kJoinThreads / kItems > 0 ? kJoinThreads / kItems : 1, kPer = (kItems + kJoinThreads - 1) / kJoinThreads;
   __shared__ __align__(16) __nv_bfloat16 hi[kSmallRows * kRow], lo[kSmallRows * kRow];
   __shared__ float weight[kPartChunk][kSmallRows];
   __shared__ int slot_of[kPartChunk];
@@ -96,13 +96,15 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int h = blockIdx.y, b = blockIdx.z, G = a.L.G, r0 = blockIdx.x * kSmallRows;
   const bool fold = a.L.U_v == nullptr;
-  uint32_t u[RV / 16][2];                                       // B fragments of this warp's 8 output channels
+  uint32_t u[kTiles][RV / 16][2];                               // B fragments of this warp's output channels
   if (!fold) {
     const __nv_bfloat16* U = a.L.U_v + (size_t)h * a.L.uv_stride + (size_t)(warp * 8 + (lane >> 2)) * RV + (lane & 3) * 2;
 #pragma unroll
-    for (int k = 0; k < RV / 16; ++k)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) u[k][i] = *reinterpret_cast<const uint32_t*>(U + k * 16 + i * 8);
+      for (int k = 0; k < RV / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) u[t][k][i] = *reinterpret_cast<const uint32_t*>(U + t * kWarps * 8 * RV + k * 16 + i * 8);
   }
   // what the partition says, found again from the lengths while the kernel before still runs
   const Seq s = sequence(a, b);
@@ -167,8 +169,9 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   }
   M = over_groups(M, [](float x, float y) { return fmaxf(x, y); });
   float den = 0.f;
-  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int item = tid % kItems, share_i = tid / kItems, ir = item % kSmallRows, c4 = item / kSmallRows, iat = row0 + min(ir, live - 1);
+  float4 num[kPer] = {};
+  const int share_i = kSplit > 1 ? tid / kItems : 0;
+  auto item_of = [&](int i) { return kSplit > 1 ? tid % kItems : tid + i * kJoinThreads; };       // (four channels, row), the row fastest
   for (int p0 = 0; p0 < parts; p0 += kPartChunk) {
     if (p0) __syncthreads();                                    // the weights of the chunk before have been read
     const int cnt = min(parts - p0, kPartChunk);
@@ -183,19 +186,25 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     }
     __syncthreads();
     if (share_i < kSplit) {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int item = item_of(i), ir = item % kSmallRows, c4 = item / kSmallRows;
+        if (item >= kItems) continue;
+        const float4* po = reinterpret_cast<const float4*>(a.part_o) + (size_t)c4 * kRows + row0 + min(ir, live - 1);
 #pragma unroll 8
-      for (int p = share_i; p < cnt; p += kSplit) {             // neighbouring threads, neighbouring rows
-        const float w = weight[p][ir];
-        const float4 o = reinterpret_cast<const float4*>(a.part_o)[((size_t)slot_of[p] * (RV / 4) + c4) * kRows + iat];
-        num.x = fmaf(o.x, w, num.x);
-        num.y = fmaf(o.y, w, num.y);
-        num.z = fmaf(o.z, w, num.z);
-        num.w = fmaf(o.w, w, num.w);
+        for (int p = share_i; p < cnt; p += kSplit) {           // neighbouring threads, neighbouring rows
+          const float w = weight[p][ir];
+          const float4 o = po[(size_t)slot_of[p] * (RV / 4) * kRows];
+          num[i].x = fmaf(o.x, w, num[i].x);
+          num[i].y = fmaf(o.y, w, num[i].y);
+          num[i].z = fmaf(o.z, w, num[i].z);
+          num[i].w = fmaf(o.w, w, num[i].w);
+        }
       }
     }
   }
   den = over_groups(den, [](float x, float y) { return x + y; });
-  if (kSplit > 1 && share_i > 0 && share_i < kSplit) share[(share_i - 1) * kItems + item] = num;
+  if (kSplit > 1 && share_i > 0 && share_i < kSplit) share[(share_i - 1) * kItems + item_of(0)] = num[0];
   auto where = [&](int row, int& node, int& hq) {
     node = (r0 + row) / G;
     hq = h * G + r0 + row - node * G;
@@ -206,21 +215,26 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = den > 0.f ? kLn2 * (M + log2f(den)) : -INFINITY;
   }
   __syncthreads();
-  if (share_i == 0) {                                           // r == ir here: kItems is a multiple of 16
+  if (share_i == 0) {
+    const float inv = den > 0.f ? 1.0f / den : 0.f;             // (an item's row is r: items and threads are multiples of 16) no part of a row: zeros
 #pragma unroll
-    for (int i = 0; i + 1 < kSplit; ++i) {
-      const float4 o = share[i * kItems + item];
-      num.x += o.x;
-      num.y += o.y;
-      num.z += o.z;
-      num.w += o.w;
+    for (int i = 0; i < kPer; ++i) {
+      const int item = item_of(i), c4 = item / kSmallRows;
+      if (item >= kItems) continue;
+#pragma unroll
+      for (int k = 0; k + 1 < kSplit; ++k) {
+        const float4 o = share[k * kItems + item];
+        num[i].x += o.x;
+        num[i].y += o.y;
+        num[i].z += o.z;
+        num[i].w += o.w;
+      }
+      uint32_t v[2], x[2];
+      split_bf16(num[i].x * inv, num[i].y * inv, v[0], x[0]);
+      split_bf16(num[i].z * inv, num[i].w * inv, v[1], x[1]);
+      *reinterpret_cast<uint2*>(hi + r * kRow + c4 * 4) = make_uint2(v[0], v[1]);
+      *reinterpret_cast<uint2*>(lo + r * kRow + c4 * 4) = make_uint2(x[0], x[1]);
     }
-    const float inv = den > 0.f ? 1.0f / den : 0.f;             // a row that saw nothing: zeros
-    uint32_t v[2], x[2];
-    split_bf16(num.x * inv, num.y * inv, v[0], x[0]);
-    split_bf16(num.z * inv, num.w * inv, v[1], x[1]);
-    *reinterpret_cast<uint2*>(hi + ir * kRow + c4 * 4) = make_uint2(v[0], v[1]);
-    *reinterpret_cast<uint2*>(lo + ir * kRow + c4 * 4) = make_uint2(x[0], x[1]);
   }
   __syncthreads();
   if (fold) {
@@ -233,14 +247,17 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     }
     return;
   }
-  float acc[4] = {};
+  float acc[kTiles][4] = {};
 #pragma unroll
   for (int k = 0; k < RV / 16; ++k) {
     uint32_t A[4], B[4];
     ldsm_x4(smem_u32(hi + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), A[0], A[1], A[2], A[3]);
     ldsm_x4(smem_u32(lo + (lane & 15) * kRow + k * 16 + (lane >> 4) * 8), B[0], B[1], B[2], B[3]);
-    mma_bf16(acc, A, u[k][0], u[k][1]);
-    mma_bf16(acc, B, u[k][0], u[k][1]);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      mma_bf16(acc[t], A, u[t][k][0], u[t][k][1]);
+      mma_bf16(acc[t], B, u[t][k][0], u[t][k][1]);
+    }
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -249,7 +266,8 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     int node, hq;
     where(row, node, hq);
     __nv_bfloat16* o = a.out + (size_t)b * a.out_stride_b + (size_t)node * a.out_stride_t + (size_t)hq * kD + warp * 8 + (lane & 3) * 2;
-    *reinterpret_cast<uint32_t*>(o) = pack_bf16(acc[2 * i], acc[2 * i + 1]);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) *reinterpret_cast<uint32_t*>(o + t * kWarps * 8) = pack_bf16(acc[t][2 * i], acc[t][2 * i + 1]);
   }
 }
 
@@ -265,15 +283,24 @@ cudaError_t launch_project(const Args& a, dim3 grid, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_combine(const Args& a, dim3 grid, cudaStream_t st) {
+// A unit's parts are as many as the CTAs that share it.  Few units (one long sequence with few heads) mean many parts, which
+// 512 threads load faster (two tiles of up to 148 CTAs); many units mean many blocks, of which 128 threads let all run at once
+// (16 sequences, 8 heads, 26 nodes: 20 us with 512 threads).
+template <int RV>
+cudaError_t launch_combine_rv(const Args& a, dim3 grid, cudaStream_t st) {
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = after_previous(attr, grid, kJoinThreads, 0, st);
+  const bool many = (long long)a.Bt.B * a.L.Hkv * a.max_units * 8 < a.n_cta;
+  const cudaLaunchConfig_t cfg = after_previous(attr, grid, many ? 512 : 128, 0, st);
+  return many ? cudaLaunchKernelEx(&cfg, combine_kernel<RV, 512>, a) : cudaLaunchKernelEx(&cfg, combine_kernel<RV, 128>, a);
+}
+
+cudaError_t launch_combine(const Args& a, dim3 grid, cudaStream_t st) {
   switch (a.L.r_v) {
-    case 32: return cudaLaunchKernelEx(&cfg, combine_kernel<32>, a);
-    case 48: return cudaLaunchKernelEx(&cfg, combine_kernel<48>, a);
-    case 64: return cudaLaunchKernelEx(&cfg, combine_kernel<64>, a);
-    case 96: return cudaLaunchKernelEx(&cfg, combine_kernel<96>, a);
-    case 128: return cudaLaunchKernelEx(&cfg, combine_kernel<128>, a);
+    case 32: return launch_combine_rv<32>(a, grid, st);
+    case 48: return launch_combine_rv<48>(a, grid, st);
+    case 64: return launch_combine_rv<64>(a, grid, st);
+    case 96: return launch_combine_rv<96>(a, grid, st);
+    case 128: return launch_combine_rv<128>(a, grid, st);
     default: return cudaErrorInvalidValue;
   }
 }
@@ -307,7 +334,8 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
                            b.span == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : b.span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
   };
   const unsigned long long pool_rows = (unsigned long long)layer->num_pages * layer->Hkv * kPage;
-  if (!rows_map(&L.tmQ, a.qp, RK, (unsigned long long)batch->B * layer->Hkv * n_q * G, 32u, bk) ||
+  const unsigned long long q_rows = (unsigned long long)batch->B * layer->Hkv * n_q * G;
+  if (!rows_map(&L.tmQ, a.qp, RK, q_rows, tree::kRows, bk) || !rows_map(&L.tmQ32, a.qp, RK, q_rows, 32u, bk) ||
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
   const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + 2 * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;

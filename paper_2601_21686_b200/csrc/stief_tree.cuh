@@ -136,7 +136,7 @@ __device__ __forceinline__ uint32_t seen32(const uint32_t* m, int s, int n) {
 
 template <int RK, int RV>
 __global__ void __launch_bounds__(kThreads, 1)
-tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Args a) {
+tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmQ32, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Args a) {
   constexpr Blocks bk{(RK % 64 == 0) ? 64 : (RK % 32 == 0) ? 32 : 16, 0, 0, 0}, bv{(RV % 64 == 0) ? 64 : (RV % 32 == 0) ? 32 : 16, 0, 0, 0};
   constexpr int kSpanK = 2 * bk.bw, kSpanV = 2 * bv.bw, kNbK = RK / bk.bw, kNbV = RV / bv.bw;       // see Blocks in stief_tc.cuh
   constexpr int kLayK = kSpanK == 128 ? 2 : kSpanK == 64 ? 4 : 6, kLayV = kSpanV == 128 ? 2 : kSpanV == 64 ? 4 : 6;
@@ -174,7 +174,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     pref[0] = 0;
     for (int s = 0; s < kMaxStages; ++s) {
       mbar_init(full_bar(s), 2);                // the K half and the V half of a page
-      mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer, or from the only one that uses the page and the producer
+      mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(q_full(t), 1);
@@ -246,9 +246,12 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             q_due &= ~(1 << t);
             mbar_arrive_expect_tx(q_full(t), kQBytes);
 #pragma unroll
-            for (int i = 0; i < kNbK; ++i)
-              for (int r = 0; r < kRows; r += 32)
-                tma_load_2d(q_smem + t * kQBytes + (i * kRows + r) * kSpanK, &tmQ, i * bk.bw, row0 + (g.dual ? r % wrap : t * kRows + r), q_full(t));
+            for (int i = 0; i < kNbK; ++i) {
+              const uint32_t dst = q_smem + t * kQBytes + i * kRows * kSpanK;
+              if (g.replicas == 1) tma_load_2d(dst, &tmQ, i * bk.bw, row0 + (g.dual ? 0 : t * kRows), q_full(t));
+              else
+                for (int r = 0; r < kRows; r += 32) tma_load_2d(dst + r * kSpanK, &tmQ32, i * bk.bw, row0 + r % wrap, q_full(t));
+            }
           }
         };
         int ids = lane < pages ? bt[lane] : 0;
@@ -273,7 +276,6 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 mbar_arrive_expect_tx(full_bar(st), kPageK);
 #pragma unroll
                 for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
-                if (g.dual) mbar_arrive(empty_bar(st));
               } else {
                 mbar_arrive_expect_tx(full_bar(st), kStageBytes - kPageK);
 #pragma unroll
@@ -301,21 +303,31 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_pv = idesc_bf16_f32_bmn(kRows, RV);
       auto bar = [&](int i) { return ctrl_u + i * 8; };                        // as numbered above
       int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next page
-      auto step = [&](int pages) {
-        st += pages;
-        if (st >= nst) {
-          st -= nst;
-          ++use;
-        }
-      };
-      auto fetch = [&](int pages, int (&at)[2]) {                              // the next block's pages, once they have landed
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-          if (p < pages) {
-            mbar_wait_warp(bar(st), use & 1, abort_flag, status);
-            at[p] = st;
-            step(1);
+      // Both tiles see every page land, in order, the other tile's too, and both give it back: a barrier's parity tells a slot's
+      // page from the one before and the one behind it only to who keeps step with them.  `skip` pages of the other tile, then `want` of this one, whose slots are
+      // kept; without `block` only as far as they have landed, and whether that was all.
+      int skip = 0, want = 0, got = 0, cur[2], nxt[2];
+      auto observe = [&](bool block) {
+        while (skip > 0 || got < want) {
+          if (block) mbar_wait_warp(bar(st), use & 1, abort_flag, status);
+          else if (!__all_sync(0xffffffffu, mbar_test_wait(bar(st), use & 1))) return false;
+          if (skip > 0) {
+            --skip;
+            if (lane == 0) mbar_arrive(bar(12 + st));
+            __syncwarp();
+          } else if (got++ == 0) nxt[0] = st;
+          else nxt[1] = st;
+          if (++st == nst) {
+            st = 0;
+            ++use;
           }
+        }
+        return true;
+      };
+      auto expect = [&](int others, int own) {
+        skip = others;
+        want = own;
+        got = 0;
       };
       auto score = [&](int pages, const int (&at)[2], bool last) {             // S = Q' K^T, 64 columns per page
 #pragma unroll
@@ -334,39 +346,41 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       };
       for (Segment g = walk.next(a, pref); uniform((int)g.valid); g = walk.next(a, pref)) {
         const int cnt = uniform(g.cnt), j0 = uniform(g.j0), len = uniform(g.ctx + g.n);
-        const bool dual = uniform((int)g.dual) != 0, ahead = !dual || nst >= 6;
+        const bool dual = uniform((int)g.dual) != 0;
         const int pages = min(2 * cnt, (len + kPage - 1) / kPage - 2 * j0);    // pages of the segment
         const int steps = dual ? (cnt + 1 - t) >> 1 : cnt, stride = dual ? 2 : 1, at = dual ? t : 0;
         if (steps == 0) {
-          for (int i = 0; i < pages; ++i) step(1);                             // a lone block: the other tile's
+          expect(pages, 0);                                                    // a lone block: the other tile's
+          observe(true);
           continue;
         }
-        int here = min(2, pages - 2 * at), next = 0, cur[2], nxt[2];
-        if (at) step(2);
-        fetch(here, cur);
+        int here = min(2, pages - 2 * at);
+        expect(2 * at, here);
+        observe(true);
+        cur[0] = nxt[0];
+        cur[1] = nxt[1];
         mbar_wait_warp(bar(24 + t), kt & 1, abort_flag, status);
         tc_fence_after();
         score(here, cur, steps == 1);
         for (int s = 0; s < steps; ++s) {
-          // What the step needs besides P is waited for ahead of it, so that from P to the next scores only products are
-          // issued.  Two tiles on blocks of their own hold four pages and ask for two more: a shorter ring asks later.
-          auto fetch_next = [&]() {
-            if (s + 1 == steps) return;
-            if (dual) step(2);                                                 // the other tile's block between
-            next = min(2, pages - 2 * (at + (s + 1) * stride));
-            fetch(next, nxt);
-          };
+          // Where the next block's pages have landed already, all that its scores need is dealt with ahead of P, so that from P
+          // on only products are issued; where they have not, P is not kept waiting for them (nor the pages that its product
+          // gives back: with six pages in the ring that alone doubled the time).
+          bool early = false;
+          if (s + 1 < steps) {
+            expect(dual ? 2 : 0, min(2, pages - 2 * (at + (s + 1) * stride))); // the other tile's block lies between
+            early = observe(false);
+            if (early && kOwnP) {                                              // S is free once it has been read
+              mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
+              tc_fence_after();
+              score(want, nxt, s + 2 == steps);
+            }
+          }
           auto release = [&]() {
 #pragma unroll
             for (int p = 0; p < 2; ++p)
               if (p < here) umma_commit_warp(bar(12 + cur[p]));
           };
-          if (ahead) fetch_next();
-          if (kOwnP && ahead && s + 1 < steps) {                               // the next scores do not wait for P: S is free once it has been read
-            mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
-            tc_fence_after();
-            score(next, nxt, s + 2 == steps);
-          }
 #pragma unroll
           for (int p = 0; p < 2; ++p) {                                        // O += P V
             mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
@@ -379,22 +393,27 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             }
           }
           umma_commit_warp(bar(38 + t));
-          if (!ahead) {
+          if (s + 1 == steps) {
+            umma_commit_warp(bar(34 + t));
             release();
-            fetch_next();
-            if (kOwnP && s + 1 < steps) mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);     // S has been read long ago
+          } else if (!early) {
+            release();
+            observe(true);
+            if (kOwnP) mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status); // S has been read long ago
+            tc_fence_after();
+            score(want, nxt, s + 2 == steps);
+          } else {
+            if (!kOwnP) score(want, nxt, s + 2 == steps);
+            release();
           }
           ++n;
-          if (s + 1 == steps) umma_commit_warp(bar(34 + t));
-          else if (!kOwnP || !ahead) score(next, nxt, s + 2 == steps);
-          if (ahead) release();
-          here = next;
+          here = want;
           cur[0] = nxt[0];
           cur[1] = nxt[1];
         }
         if (dual) {                                                            // blocks behind this tile's last
-          const int done = 2 * (at + (steps - 1) * 2) + 2;
-          for (int i = done; i < pages; ++i) step(1);
+          expect(max(0, pages - 2 * (at + (steps - 1) * 2) - 2), 0);
+          observe(true);
         }
         ++kt;
       }
@@ -621,7 +640,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 
 struct Launch {
   Args a;
-  CUtensorMap tmQ, tmK, tmV;
+  CUtensorMap tmQ, tmQ32, tmK, tmV;         // tmQ32: boxes of 32 rows, for rows that a tile holds several times
   int grid, smem;
 };
 
