@@ -318,9 +318,9 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
           else if (cross) first_operands();
           if (own) {
             if (j == 0 && kt > 0) mbar_wait_warp(bar(28 + t), (kt - 1) & 1, abort_flag, status);   // the epilogue has read the item before
-            mbar_wait_warp(bar(22 + 2 * t), n & 1, abort_flag, status);
           }
           take_turn();
+          if (own) mbar_wait_warp(bar(22 + 2 * t), n & 1, abort_flag, status);
           tc_fence_after();
           if (own) {
             const uint32_t va = desc_lo(kRows * 128, v_addr);                  // O += P V; V MN-major, two halves of 64 channels
