@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
   const int dq = fold ? RK : kD;
   const int live = min(kSmallRows, n * G - r0);
   __nv_bfloat16* dst = a.qp + (((size_t)b * a.L.Hkv + h) * rows + r0) * RK;
+  __nv_bfloat16* rem = dst + (size_t)a.Bt.B * a.L.Hkv * rows * RK;
   auto src = [&](int r) {
     const int node = (r0 + r) / G, g = r0 + r - node * G;
     return reinterpret_cast<const uint4*>(a.q + (size_t)b * a.q_stride_b + (size_t)node * a.q_stride_t + (size_t)(h * G + g) * dq);
@@ -69,7 +70,12 @@ __global__ void __launch_bounds__(kSmallThreads) project_kernel(const Args a) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = (lane >> 2) + 8 * i;
-        if (r < live) *reinterpret_cast<uint32_t*>(dst + r * RK + p * 16 + t * 8 + (lane & 3) * 2) = pack_bf16(acc[t][2 * i], acc[t][2 * i + 1]);
+        uint32_t v, x;
+        split_bf16(acc[t][2 * i], acc[t][2 * i + 1], v, x);
+        if (r < live) {
+          *reinterpret_cast<uint32_t*>(dst + r * RK + p * 16 + t * 8 + (lane & 3) * 2) = v;
+          *reinterpret_cast<uint32_t*>(rem + r * RK + p * 16 + t * 8 + (lane & 3) * 2) = x;
+        }
       }
   }
 }
@@ -130,7 +136,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
     before += cost_of[0][i];
     total += cost_of[1][i];
   }
-  const int unit = r0 / kUnitRows, rows = min(s.n * G - unit * kUnitRows, kUnitRows), in_unit = r0 - unit * kUnitRows;
+  const int unit = r0 / a.unit_rows, rows = min(s.n * G - unit * a.unit_rows, a.unit_rows), in_unit = r0 - unit * a.unit_rows;
   const bool dual = rows <= kRows;
   const int tile = dual ? 0 : in_unit / kRows, row0 = in_unit - tile * kRows;
   const int n = cta_count(a, total);
@@ -334,11 +340,11 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
                            b.span == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : b.span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
   };
   const unsigned long long pool_rows = (unsigned long long)layer->num_pages * layer->Hkv * kPage;
-  const unsigned long long q_rows = (unsigned long long)batch->B * layer->Hkv * n_q * G;
+  const unsigned long long q_rows = 2ull * batch->B * layer->Hkv * n_q * G;      // values, then remainders
   if (!rows_map(&L.tmQ, a.qp, RK, q_rows, tree::kRows, bk) || !rows_map(&L.tmQ32, a.qp, RK, q_rows, 32u, bk) ||
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
-  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + 2 * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
+  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + tree::q_regions(RK) * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
   a.nst = (tree::kSmemLimit - fixed) / stage;
   if (a.nst > tree::kMaxStages) a.nst = tree::kMaxStages;
   L.smem = fixed + a.nst * stage;

@@ -3,8 +3,10 @@
 //   out_i = softmax(q_i' K_down[S_i]^T / sqrt(128)) V_down[S_i] U_v^T,   q_i' = q_i U_k.
 // A tree has few query rows (nodes x heads of the group) and a long cache, so the cache is what has to be streamed: every
 // row of it once per (sequence, KV head).  Three launches, each started while the one before it still runs:
-//   project_kernel   q' = q U_k in fp32, rounded once to bf16, rows packed per (sequence, KV head)
-//   tree_kernel      one persistent CTA per SM.  A unit is (sequence, KV head, up to 256 query rows); the units' blocks of 128
+//   project_kernel   q' = q U_k in fp32, kept as two bf16 terms (value and remainder, 16 significant bits: with the value alone
+//                    the scores' error was as large as all others together), rows packed per (sequence, KV head)
+//   tree_kernel      one persistent CTA per SM.  A unit is (sequence, KV head, up to 256 query rows,
+//                    128 at key ranks above 64, whose Q' fills the shared memory); the units' blocks of 128
 //                    positions lie end to end on one axis (each unit preceded by kPad blocks' worth of start-up cost) and
 //                    every CTA takes an equal range of it, so that ragged lengths and few units fill the GPU alike.  What a
 //                    CTA finds in one unit, a segment, leaves a partial result: unnormalised mix, reference, sum.
@@ -18,7 +20,7 @@
 // cost nothing here) and is joined with the others when the segment ends.
 //   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
 //   warps 8, 11     cache pages by TMA into a ring, a stage = K page | V page of one KV head; Q' tiles
-//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page), O += P V (N = r_v)
+//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page; Q' as value and remainder), O += P V (N = r_v)
 // TMEM (512 columns): per tile 128 for S and 128 for O; with r_v <= 64 half of O's are free and hold P, and the next scores are
 // made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
 #pragma once
@@ -40,6 +42,8 @@ constexpr int kHeadBytes = 5120;                // prefix sums (4352), barriers 
 constexpr int kJoinBytes = 14336;               // joining the copies of rows, per tile 1024 of references and sums, 6144 of values
 __host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBytes : 0; }
 constexpr int kMaxStages = 12;
+// Q' regions in shared memory: value and remainder of the rows, once where both tiles hold the same rows, for each tile else
+__host__ __device__ constexpr int q_regions(int RK) { return unit_rows_of(RK) > kRows ? 4 : 2; }
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
 
@@ -55,7 +59,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
   if (!fits && s.n > 0) report(a.status, STIEF_ERR_BOUNDS);
   if (!fits) s.n = 0;
   s.blocks = s.n > 0 ? (s.ctx + s.n + kBlock - 1) / kBlock : 0;
-  s.units = (s.n * a.L.G + kUnitRows - 1) / kUnitRows;
+  s.units = (s.n * a.L.G + a.unit_rows - 1) / a.unit_rows;
   return s;
 }
 __device__ __forceinline__ int sequence_cost(const Args& a, const Seq& s) { return a.L.Hkv * s.units * (s.blocks + kPad); }
@@ -106,7 +110,7 @@ struct Walk {
       g.slot = cta + (b * a.L.Hkv + g.h) * a.max_units + g.unit;
       g.ctx = s.ctx;
       g.n = s.n;
-      g.rows = min(s.n * a.L.G - g.unit * kUnitRows, kUnitRows);
+      g.rows = min(s.n * a.L.G - g.unit * a.unit_rows, a.unit_rows);
       g.dual = g.rows <= kRows;
       g.replicas = replicas_of(g.rows, a.L.r_v, g.cnt);
       g.valid = true;
@@ -148,13 +152,12 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   int* pref = reinterpret_cast<int*>(smem);
   uint8_t* ctrl_ptr = smem + 4352;
   const uint32_t ctrl = smem_u32(ctrl_ptr);
-  const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + 2 * kQBytes;
-  uint8_t* ring_ptr = smem + kHeadBytes + join_bytes(RV) + 2 * kQBytes;
+  const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + q_regions(RK) * kQBytes;
+  uint8_t* ring_ptr = smem + kHeadBytes + join_bytes(RV) + q_regions(RK) * kQBytes;
   const int nst = a.nst;
   auto full_bar = [&](int s) { return ctrl + s * 8; };
   auto empty_bar = [&](int s) { return ctrl + (12 + s) * 8; };
-  auto q_full = [&](int t) { return ctrl + (24 + t) * 8; };
-  auto q_empty = [&](int t) { return ctrl + (26 + t) * 8; };
+  const uint32_t q_full = ctrl + 24 * 8, q_empty = ctrl + 26 * 8;
   auto s_full = [&](int t) { return ctrl + (28 + t) * 8; };
   auto p_full = [&](int t, int half) { return ctrl + (30 + 2 * t + half) * 8; };
   auto o_full = [&](int t) { return ctrl + (34 + t) * 8; };
@@ -177,8 +180,6 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(q_full(t), 1);
-      mbar_init(q_empty(t), 1);
       mbar_init(s_full(t), 1);
       mbar_init(p_full(t, 0), 4);
       mbar_init(p_full(t, 1), 4);
@@ -186,6 +187,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       mbar_init(s_free(t), 4);
       mbar_init(p_free(t), 1);
     }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 2);                      // one arrival from each tile's issuer
     *abort_flag = 0;
     mbar_fence_init();
   }
@@ -223,36 +226,38 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tma_prefetch_desc(keys ? &tmK : &tmV);
         if (!keys) tma_prefetch_desc(&tmQ);
       }
-      int st = 0, use = 0, kt[2] = {0, 0};
+      int st = 0, use = 0, kt = 0;                              // ring position, segments so far
+      const int parts = a.L.U_k ? 2 : 1, q_rows = a.Bt.B * a.L.Hkv * (a.n_q * a.L.G);         // given queries have no remainder
       bool first_q = true;
       for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
         const int first = 2 * g.j0, pages = min(2 * g.cnt, (g.ctx + g.n + kPage - 1) / kPage - first);
         const int* bt = a.Bt.block_table + (size_t)g.b * a.Bt.max_pages + first;
-        int q_due = keys ? 0 : (tile_blocks(g, 0) > 0) | (tile_blocks(g, 1) > 0) << 1;         // tiles whose queries are still to be sent
+        bool q_due = !keys;                                     // the segment's queries are still to be sent
         auto send_queries = [&](bool wait) {                    // lane 0
           if (first_q) {
             grid_dependency_wait();                             // project_kernel has written them, with ordinary stores
             asm volatile("fence.proxy.async;" ::: "memory");
             first_q = false;
           }
-          const int row0 = (g.b * a.L.Hkv + g.h) * (a.n_q * a.L.G) + g.unit * kUnitRows, wrap = kRows / g.replicas;
-          for (int t = 0; t < 2; ++t) {
-            if (!(q_due >> t & 1)) continue;
-            if (kt[t] > 0) {
-              if (wait) mbar_wait(q_empty(t), (kt[t] - 1) & 1, abort_flag, status);
-              else if (!mbar_test_wait(q_empty(t), (kt[t] - 1) & 1)) continue;
-            }
-            ++kt[t];
-            q_due &= ~(1 << t);
-            mbar_arrive_expect_tx(q_full(t), kQBytes);
-#pragma unroll
-            for (int i = 0; i < kNbK; ++i) {
-              const uint32_t dst = q_smem + t * kQBytes + i * kRows * kSpanK;
-              if (g.replicas == 1) tma_load_2d(dst, &tmQ, i * bk.bw, row0 + (g.dual ? 0 : t * kRows), q_full(t));
-              else
-                for (int r = 0; r < kRows; r += 32) tma_load_2d(dst + r * kSpanK, &tmQ32, i * bk.bw, row0 + r % wrap, q_full(t));
-            }
+          if (kt > 0) {
+            if (wait) mbar_wait(q_empty, (kt - 1) & 1, abort_flag, status);
+            else if (!mbar_test_wait(q_empty, (kt - 1) & 1)) return;
           }
+          ++kt;
+          q_due = false;
+          const int row0 = (g.b * a.L.Hkv + g.h) * (a.n_q * a.L.G) + g.unit * a.unit_rows, wrap = kRows / g.replicas, tiles = g.dual ? 1 : 2;
+          mbar_arrive_expect_tx(q_full, tiles * parts * kQBytes);
+          for (int t = 0; t < tiles; ++t)
+            for (int x = 0; x < parts; ++x) {
+              const int row = row0 + t * kRows + x * q_rows;
+#pragma unroll
+              for (int i = 0; i < kNbK; ++i) {
+                const uint32_t dst = q_smem + (2 * t + x) * kQBytes + i * kRows * kSpanK;
+                if (g.replicas == 1) tma_load_2d(dst, &tmQ, i * bk.bw, row, q_full);
+                else
+                  for (int r = 0; r < kRows; r += 32) tma_load_2d(dst + r * kSpanK, &tmQ32, i * bk.bw, row + r % wrap, q_full);
+              }
+            }
         };
         int ids = lane < pages ? bt[lane] : 0;
         if (lane == 0 && q_due && first_q) send_queries(true);
@@ -297,7 +302,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       // ---------------------------------------------------------------------------------------- MMA issue, tile t
       const int t = uniform(warp) - 9;
       const uint32_t tmem_u = uniform(tmem_base) + t * 256, ring_u = uniform(ring), ctrl_u = uniform(ctrl);
-      const uint32_t qa = desc_lo(16, uniform(q_smem) + t * kQBytes);
+      const uint32_t q_u = uniform(q_smem);
+      const int parts = a.L.U_k ? 2 : 1;
+      uint32_t qa = 0;                                                         // this tile's Q' operand, its remainder one region on
       constexpr uint32_t kHiK = (uint32_t)((((uint64_t)(8 * kSpanK >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayK << 61)) >> 32);
       constexpr uint32_t kHiV = (uint32_t)((((uint64_t)(8 * kSpanV >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayV << 61)) >> 32);
       const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_pv = idesc_bf16_f32_bmn(kRows, RV);
@@ -335,31 +342,39 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           if (p < pages) {
             const uint32_t ka = desc_lo(16, ring_u + at[p] * kStageBytes);
 #pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
             for (int k = 0; k < RK / 16; ++k) {
+              if (x >= parts) continue;
               constexpr int kPer = bk.bw / 16;                                 // K steps per swizzled block
               const uint32_t qo = (uint32_t)((k / kPer) * kRows * kSpanK + (k % kPer) * 32) >> 4, ko = (uint32_t)((k / kPer) * kPage * kSpanK + (k % kPer) * 32) >> 4;
-              umma_ss(tmem_u + 64 * p, qa + qo, kHiK, ka + ko, kHiK, id_qk, k > 0 ? 1u : 0u);
+              umma_ss(tmem_u + 64 * p, qa + x * (kQBytes >> 4) + qo, kHiK, ka + ko, kHiK, id_qk, x > 0 || k > 0 ? 1u : 0u);
             }
           }
         umma_commit_warp(bar(28 + t));
-        if (last) umma_commit_warp(bar(26 + t));
+        if (last) umma_commit_warp(bar(26));
       };
       for (Segment g = walk.next(a, pref); uniform((int)g.valid); g = walk.next(a, pref)) {
         const int cnt = uniform(g.cnt), j0 = uniform(g.j0), len = uniform(g.ctx + g.n);
         const bool dual = uniform((int)g.dual) != 0;
         const int pages = min(2 * cnt, (len + kPage - 1) / kPage - 2 * j0);    // pages of the segment
         const int steps = dual ? (cnt + 1 - t) >> 1 : cnt, stride = dual ? 2 : 1, at = dual ? t : 0;
-        if (steps == 0) {
-          expect(pages, 0);                                                    // a lone block: the other tile's
+        if (steps == 0) {                                                      // a lone block: the other tile's
+          expect(pages, 0);
           observe(true);
+          mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
+          ++kt;
+          if (lane == 0) mbar_arrive(bar(26));
+          __syncwarp();
           continue;
         }
+        qa = desc_lo(16, q_u + (dual ? 0 : 2 * t) * kQBytes);
         int here = min(2, pages - 2 * at);
         expect(2 * at, here);
         observe(true);
         cur[0] = nxt[0];
         cur[1] = nxt[1];
-        mbar_wait_warp(bar(24 + t), kt & 1, abort_flag, status);
+        mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
         tc_fence_after();
         score(here, cur, steps == 1);
         for (int s = 0; s < steps; ++s) {
@@ -437,7 +452,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const int wrap = kRows / g.replicas, replica = lane_row / wrap, row = lane_row - replica * wrap;
       const int base_row = g.dual ? 0 : t * kRows, urow = base_row + row;
       const bool row_valid = urow < g.rows, warp_live = base_row + row - lane < g.rows;
-      const int node = min(g.unit * kUnitRows + urow, g.n * a.L.G - 1) / a.L.G;
+      const int node = min(g.unit * a.unit_rows + urow, g.n * a.L.G - 1) / a.L.G;
       const uint32_t* mask = a.mask + ((size_t)g.b * a.n_q + node) * a.mask_words;
       float m_ref = 0.f, l = 0.f;
       // One block, of whose 128 columns this thread takes kCols: all of them, or with the rows there twice or four times

@@ -7,7 +7,8 @@ namespace stief {
 namespace tree {
 
 constexpr int kMaxNodes = STIEF_TREE_MAX_NODES;
-constexpr int kUnitRows = 256;             // query rows of a work unit: two tiles of 128
+// query rows of a work unit: two tiles of 128, or one that both hold
+__host__ __device__ constexpr int unit_rows_of(int r_k) { return r_k <= 64 ? 256 : 128; }
 constexpr int kPad = 3;                    // start-up cost of a unit, in blocks of 128 positions
 
 struct Args {
@@ -24,9 +25,9 @@ struct Args {
   float* out_lse;                          // [B][n_q][Hq] or NULL
   int32_t* status;
   // planning and workspace (see carve)
-  int n_cta, max_units;                    // CTAs; units per (sequence, KV head) at most
+  int n_cta, max_units, unit_rows;         // CTAs; units per (sequence, KV head) at most; rows of a unit
   int nst;                                 // ring stages
-  __nv_bfloat16* qp;                       // [B][Hkv][n_q G][r_k]  projected queries, rows (node, head of the group)
+  __nv_bfloat16* qp;                       // [2][B][Hkv][n_q G][r_k]  projected queries and their remainders, rows (node, head of the group)
   float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][128 lanes] float4
   float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (base 2), sum
 };
@@ -34,7 +35,7 @@ struct Args {
 // Workspace: a segment is found by (CTA + unit), so there are at most n_cta + units of them
 inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_v, Args* a) {
   const int G = Hq / Hkv, rows = n_q * G, n_cta = host::sm_count();
-  const int max_units = (rows + kUnitRows - 1) / kUnitRows;
+  const int unit_rows = unit_rows_of(r_k), max_units = (rows + unit_rows - 1) / unit_rows;
   const size_t slots = 2 * ((size_t)n_cta + (size_t)B * Hkv * max_units);
   uint8_t* p = static_cast<uint8_t*>(base);
   size_t off = 0;
@@ -43,11 +44,12 @@ inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_
     off += host::align_up(bytes, 128);
     return at;
   };
-  uint8_t* qp = take((size_t)B * Hkv * rows * r_k * 2);
+  uint8_t* qp = take((size_t)B * Hkv * rows * r_k * 4);
   uint8_t *po = take(slots * 128 * r_v * 4), *ml = take(slots * 128 * 8);
   if (a) {
     a->n_cta = n_cta;
     a->max_units = max_units;
+    a->unit_rows = unit_rows;
     a->qp = reinterpret_cast<__nv_bfloat16*>(qp);
     a->part_o = reinterpret_cast<float*>(po);
     a->part_ml = reinterpret_cast<float*>(ml);
@@ -89,8 +91,8 @@ inline int check(const stief_layer* l, const stief_batch* batch, const uint16_t*
     return STIEF_ERR_INVALID_ARG;
   if ((long long)l->num_pages * l->Hkv * kPage >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;   // pool rows are counted in int
   // rows of the projected queries and positions of the work axis are counted in int
-  const long long rows = (long long)n_q * (l->Hq / l->Hkv), units = (long long)batch->B * l->Hkv * ((rows + kUnitRows - 1) / kUnitRows);
-  if ((long long)batch->B * l->Hkv * rows >= (1ll << 31) || units * (batch->max_pages_per_seq / 2 + 1 + kPad) >= (1ll << 31) ||
+  const long long rows = (long long)n_q * (l->Hq / l->Hkv), units = (long long)batch->B * l->Hkv * ((rows + 127) / 128);
+  if ((long long)batch->B * l->Hkv * rows >= (1ll << 30) || units * (batch->max_pages_per_seq / 2 + 1 + kPad) >= (1ll << 31) ||
       (units + host::sm_count()) * 256 >= (1ll << 31))
     return STIEF_ERR_INVALID_ARG;
   if (!workspace || !host::aligned(workspace, 128)) return STIEF_ERR_INVALID_ARG;
@@ -110,7 +112,7 @@ inline int check(const stief_layer* l, const stief_batch* batch, const uint16_t*
   a->out_stride_b = out_stride_b; a->out_stride_t = out_stride_t;
   a->out_lse = out_lse;
   a->status = status;
-  carve(workspace, batch->B, n_q, l->Hq, l->Hkv, 128, l->r_v, a);      // sized for the widest keys: r_k is no argument of the size
+  carve(workspace, batch->B, n_q, l->Hq, l->Hkv, l->r_k, l->r_v, a);   // (the size asked for is the widest keys': r_k is no argument there)
   return STIEF_OK;
 }
 
