@@ -344,7 +344,8 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
   if (!rows_map(&L.tmQ, a.qp, RK, q_rows, tree::kRows, bk) || !rows_map(&L.tmQ32, a.qp, RK, q_rows, 32u, bk) ||
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
-  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + tree::q_regions(RK) * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
+  a.q_regions = n_q * G > tree::kRows && a.unit_rows > tree::kRows ? 4 : 2;
+  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + a.q_regions * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
   a.nst = (tree::kSmemLimit - fixed) / stage;
   if (a.nst > tree::kMaxStages) a.nst = tree::kMaxStages;
   L.smem = fixed + a.nst * stage;

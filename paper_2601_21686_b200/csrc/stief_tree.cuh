@@ -19,7 +19,7 @@
 // them twice or four times, each copy takes its half or quarter of a block's columns (P is zero elsewhere, the wasted products
 // cost nothing here) and is joined with the others when the segment ends.
 //   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
-//   warps 8, 11     cache pages by TMA into a ring, a stage = K page | V page of one KV head; Q' tiles
+//   warps 8, 11     cache pages by TMA into a ring of K pages and V pages of one KV head; Q' tiles
 //   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page; Q' as value and remainder), O += P V (N = r_v)
 // TMEM (512 columns): per tile 128 for S and 128 for O; with r_v <= 64 half of O's are free and hold P, and the next scores are
 // made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
@@ -42,8 +42,6 @@ constexpr int kHeadBytes = 5120;                // prefix sums (4352), barriers 
 constexpr int kJoinBytes = 14336;               // joining the copies of rows, per tile 1024 of references and sums, 6144 of values
 __host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBytes : 0; }
 constexpr int kMaxStages = 12;
-// Q' regions in shared memory: value and remainder of the rows, once where both tiles hold the same rows, for each tile else
-__host__ __device__ constexpr int q_regions(int RK) { return unit_rows_of(RK) > kRows ? 4 : 2; }
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
 
@@ -146,15 +144,16 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   constexpr int kLayK = kSpanK == 128 ? 2 : kSpanK == 64 ? 4 : 6, kLayV = kSpanV == 128 ? 2 : kSpanV == 64 ? 4 : 6;
   constexpr bool kOwnP = RV <= 64;              // P has TMEM columns of its own: 192 .. 255 of the tile's
   constexpr int kColP = kOwnP ? 192 : 0;
-  constexpr int kPageK = kPage * RK * 2, kStageBytes = kPage * (RK + RV) * 2, kQBytes = kRows * RK * 2;
+  constexpr int kPageK = kPage * RK * 2, kPageV = kPage * RV * 2, kQBytes = kRows * RK * 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int* pref = reinterpret_cast<int*>(smem);
   uint8_t* ctrl_ptr = smem + 4352;
   const uint32_t ctrl = smem_u32(ctrl_ptr);
-  const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + q_regions(RK) * kQBytes;
-  uint8_t* ring_ptr = smem + kHeadBytes + join_bytes(RV) + q_regions(RK) * kQBytes;
+  const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + a.q_regions * kQBytes;
   const int nst = a.nst;
+  const uint32_t ring_v = ring + nst * kPageK;  // K pages side by side, then V pages: two neighbours are one operand of 128 rows
+  uint8_t* ring_v_ptr = smem + kHeadBytes + join_bytes(RV) + a.q_regions * kQBytes + nst * kPageK;
   auto full_bar = [&](int s) { return ctrl + s * 8; };
   auto empty_bar = [&](int s) { return ctrl + (12 + s) * 8; };
   const uint32_t q_full = ctrl + 24 * 8, q_empty = ctrl + 26 * 8;
@@ -276,15 +275,15 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
               }
               const int row = (pg * a.L.Hkv + g.h) * kPage;
-              const uint32_t dst = ring + st * kStageBytes;
+              const uint32_t dst = keys ? ring + st * kPageK : ring_v + st * kPageV;
               if (keys) {
                 mbar_arrive_expect_tx(full_bar(st), kPageK);
 #pragma unroll
                 for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
               } else {
-                mbar_arrive_expect_tx(full_bar(st), kStageBytes - kPageK);
+                mbar_arrive_expect_tx(full_bar(st), kPageV);
 #pragma unroll
-                for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + kPageK + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+                for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
               }
               if (++st == nst) {
                 st = 0;
@@ -301,13 +300,13 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     } else {
       // ---------------------------------------------------------------------------------------- MMA issue, tile t
       const int t = uniform(warp) - 9;
-      const uint32_t tmem_u = uniform(tmem_base) + t * 256, ring_u = uniform(ring), ctrl_u = uniform(ctrl);
+      const uint32_t tmem_u = uniform(tmem_base) + t * 256, ring_u = uniform(ring), ring_v_u = uniform(ring_v), ctrl_u = uniform(ctrl);
       const uint32_t q_u = uniform(q_smem);
       const int parts = a.L.U_k ? 2 : 1;
       uint32_t qa = 0;                                                         // this tile's Q' operand, its remainder one region on
       constexpr uint32_t kHiK = (uint32_t)((((uint64_t)(8 * kSpanK >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayK << 61)) >> 32);
       constexpr uint32_t kHiV = (uint32_t)((((uint64_t)(8 * kSpanV >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayV << 61)) >> 32);
-      const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_pv = idesc_bf16_f32_bmn(kRows, RV);
+      const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_qk2 = idesc_bf16_f32(kRows, kBlock), id_pv = idesc_bf16_f32_bmn(kRows, RV);
       auto bar = [&](int i) { return ctrl_u + i * 8; };                        // as numbered above
       int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next page
       // Both tiles see every page land, in order, the other tile's too, and both give it back: a barrier's parity tells a slot's
@@ -337,20 +336,26 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         got = 0;
       };
       auto score = [&](int pages, const int (&at)[2], bool last) {             // S = Q' K^T, 64 columns per page
+        auto product = [&](int slot, uint32_t d, uint32_t idesc) {
+          const uint32_t ka = desc_lo(16, ring_u + slot * kPageK);
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
-          if (p < pages) {
-            const uint32_t ka = desc_lo(16, ring_u + at[p] * kStageBytes);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
             for (int k = 0; k < RK / 16; ++k) {
               if (x >= parts) continue;
               constexpr int kPer = bk.bw / 16;                                 // K steps per swizzled block
               const uint32_t qo = (uint32_t)((k / kPer) * kRows * kSpanK + (k % kPer) * 32) >> 4, ko = (uint32_t)((k / kPer) * kPage * kSpanK + (k % kPer) * 32) >> 4;
-              umma_ss(tmem_u + 64 * p, qa + x * (kQBytes >> 4) + qo, kHiK, ka + ko, kHiK, id_qk, x > 0 || k > 0 ? 1u : 0u);
+              umma_ss(d, qa + x * (kQBytes >> 4) + qo, kHiK, ka + ko, kHiK, idesc, x > 0 || k > 0 ? 1u : 0u);
             }
-          }
+        };
+        // A key row in one swizzled block: pages in neighbouring slots are one operand (half as many products to issue)
+        if (kNbK == 1 && pages == 2 && at[1] == at[0] + 1) {
+          product(at[0], tmem_u, id_qk2);
+        } else {
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (p < pages) product(at[p], tmem_u + 64 * p, id_qk);
+        }
         umma_commit_warp(bar(28 + t));
         if (last) umma_commit_warp(bar(26));
       };
@@ -401,7 +406,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
             tc_fence_after();
             if (p < here) {
-              const uint32_t va = desc_lo(kPage * kSpanV, ring_u + cur[p] * kStageBytes + kPageK);
+              const uint32_t va = desc_lo(kPage * kSpanV, ring_v_u + cur[p] * kPageV);
 #pragma unroll
               for (int k = 0; k < kPage / 16; ++k)
                 umma_ts(tmem_u + 128, tmem_u + kColP + 32 * p + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || p > 0 || k > 0 ? 1u : 0u);
@@ -553,7 +558,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             const int dead = len - p0 - p * kPage;              // first dead row of the page
             const int idx = page0 + 2 * j + p, stg = idx % nst;
             mbar_wait(full_bar(stg), (idx / nst) & 1, abort_flag, status);
-            uint8_t* v = ring_ptr + stg * kStageBytes + kPageK;
+            uint8_t* v = ring_v_ptr + stg * kPageV;
             constexpr int kCpr = kSpanV / 16, kPerRow = RV / 8;
             for (int e = lane_row; e < (kPage - dead) * kPerRow; e += kRows) {
               const int r = dead + e / kPerRow, ch = e % kPerRow;

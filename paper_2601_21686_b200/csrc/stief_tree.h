@@ -27,6 +27,7 @@ struct Args {
   // planning and workspace (see carve)
   int n_cta, max_units, unit_rows;         // CTAs; units per (sequence, KV head) at most; rows of a unit
   int nst;                                 // ring stages
+  int q_regions;                           // Q' regions in shared memory: value and remainder, for each tile where a unit may have over 128 rows
   __nv_bfloat16* qp;                       // [2][B][Hkv][n_q G][r_k]  projected queries and their remainders, rows (node, head of the group)
   float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][128 lanes] float4
   float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (base 2), sum

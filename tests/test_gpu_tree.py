@@ -1,6 +1,6 @@
 """Attention of a tree of drafted tokens over the compressed cache, against the definition in fp64 on the cache rows the GPU
-holds.  Tolerances are error bounds: q' and the probabilities are rounded to bf16 once (half a step = 2^-8 of the value),
-the output once more; everything else is fp32 (and exponentials good to 1e-4)."""
+holds.  Tolerances are error bounds: the probabilities are rounded to bf16 once (half a step = 2^-8 of the value), the
+output once more, q' to two bf16 terms (2^-16); everything else is fp32 (and exponentials good to 1e-4)."""
 import math
 
 import pytest
@@ -104,8 +104,8 @@ class TreeCase:
                 lse = torch.logsumexp(s, -1)
                 p = torch.exp(s - lse.masked_fill(empty, 0.0)[..., None])
                 o, size = p @ V, p @ V.abs()
-                # scores are off by at most delta: one rounding of q' (none when it is handed over), and fp32 sums
-                rounding = (0.0 if Uk is None else HALF) + 256 * 2.0 ** -24
+                # scores are off by at most delta: q' in two terms (exact when it is handed over), and fp32 sums
+                rounding = (0.0 if Uk is None else HALF * HALF) + 256 * 2.0 ** -24
                 delta = (rounding * (qp.abs() @ K.abs().T) / math.sqrt(128)).masked_fill(~keep, 0.0).amax(-1) if K.shape[0] else torch.zeros_like(lse)
                 if Uv is not None:
                     o, size = o @ Uv.T, size @ Uv.abs().T
