@@ -401,8 +401,9 @@ int stief_mq_attention(const stief_layer* layer, const stief_batch* batch, const
  *   workspace  device, 128-byte aligned, stief_tree_workspace_bytes(...) bytes, contents irrelevant on entry; calls that share
  *              it must not overlap on the GPU
  *   out        device bf16 [B][n_q][Hq][d_out];  out_lse optional fp32 [B][n_q][Hq];  flags must be 0
- * Any number of query heads per KV head.  q' = q U_k and the probabilities pass through bf16, scores, sums and the mix keep
- * fp32 accuracy.  A sequence whose context and nodes do not fit its block table sets STIEF_ERR_BOUNDS and is skipped. */
+ * Any number of query heads per KV head.  The probabilities pass through bf16; q' = q U_k keeps 16 significant bits, scores,
+ * sums and the mix fp32 accuracy.  A sequence whose context and nodes do not fit its block table (or exceed 2^30 positions) sets
+ * STIEF_ERR_BOUNDS and is skipped.  A NaN or infinity in the cache row of a drafted node may reach rows that do not see it. */
 #define STIEF_TREE_MAX_NODES 1024
 size_t stief_tree_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t r_v);
 int stief_tree_attention(const stief_layer* layer, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b,
@@ -444,7 +445,7 @@ int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tok
  * can take and give back pages.  Slot b of the batch holds pages block_table[b][0 .. page_counts[b]); ref_counts[p] is the
  * number of slots that hold page p, and a page is free when that is 0.  The lowest-numbered free page is always taken first,
  * for the lowest slot first.  Only full pages are ever shared, so appending never writes a page of another slot.
- * Table entries at or behind page_counts[b] are left as they are. */
+ * Table entries at or behind page_counts[b] are left as they are.  Calls on one table must not overlap on the GPU. */
 typedef struct stief_page_table {
   int32_t B, max_pages_per_seq, num_pages;
   int32_t* block_table; /* [B][max_pages_per_seq] */

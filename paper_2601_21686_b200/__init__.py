@@ -532,6 +532,8 @@ def stief_tree_attention(layer: Layer, batch: Batch, q: torch.Tensor, tree_mask:
     for t, name in ((out, "out"), (workspace, "workspace"), (layer.k_pool, "k_pool"), (layer.v_pool, "v_pool"), (batch.block_table, "block_table"),
                     (batch.seq_lens, "seq_lens")):
         _here(t, name, at)
+    if batch.block_table.dtype is not torch.int32 or batch.seq_lens.dtype is not torch.int32:
+        raise ValueError("block_table and seq_lens must be int32")
     q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (max(qs[1], Hq * d_q), max(os_[1], Hq * d_out))       # an extent of 1 may carry any stride
     q_b, o_b = (qs[0], os_[0]) if B > 1 else (max(qs[0], q_t), max(os_[0], o_t))
     _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(n_nodes),
@@ -549,8 +551,8 @@ def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Ten
     _int32(accepted, "accepted", None, at)
     if accepted.dim() != 2 or accepted.shape[0] != B:
         raise ValueError("accepted must be [B, max_accept]")
-    _here(batch.block_table, "block_table", at)
-    _here(batch.seq_lens, "seq_lens", at)
+    _int32(batch.block_table, "block_table", None, at)
+    _int32(batch.seq_lens, "seq_lens", (B,), at)
     arr = _descriptors(layers, at, "_accept", lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
     _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), accepted.data_ptr(), accepted.shape[1], n_accepted.data_ptr(),
                                    _status(status, at), _raw_stream(at)), "stief_tree_accept")

@@ -456,6 +456,6 @@ const char* stief_status_string(int status) {
   }
 }
 
-int stief_version(void) { return 210; }
+int stief_version(void) { return 220; }
 
 }  // extern "C"

@@ -53,7 +53,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int b) {
   Seq s;
   s.ctx = a.Bt.seq_lens[b];
   s.n = a.n_nodes ? min(max(a.n_nodes[b], 0), a.n_q) : a.n_q;
-  const bool fits = s.ctx >= 0 && ((long long)s.ctx + s.n + kPage - 1) / kPage <= a.Bt.max_pages;
+  const bool fits = s.ctx >= 0 && s.ctx <= (1 << 30) && ((long long)s.ctx + s.n + kPage - 1) / kPage <= a.Bt.max_pages;      // positions are counted in int
   if (!fits && s.n > 0) report(a.status, STIEF_ERR_BOUNDS);
   if (!fits) s.n = 0;
   s.blocks = s.n > 0 ? (s.ctx + s.n + kBlock - 1) / kBlock : 0;

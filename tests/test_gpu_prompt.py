@@ -115,6 +115,12 @@ def test_rows_of_other_prompts_and_of_none_influence_nothing():
     assert torch.isnan(out[360:]).all() and torch.isnan(lse[360:]).all()
 
 
+def test_only_empty_prompts():
+    q, k, v, _ = _inputs(21, [64], 4, 2)
+    out, lse = _run(q, k, v, torch.zeros(4, dtype=torch.int32, device="cuda"))
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
+
+
 def test_later_tokens_do_not_change_earlier_rows():
     q, k, v, cu = _inputs(23, [400], 4, 2)
     a, _ = _run(q, k, v, cu)

@@ -170,6 +170,33 @@ def test_many_sequences():
     assert int(c.status) == 0
 
 
+def test_largest_batch():
+    lens = [(53 * i) % 200 for i in range(1024)]
+    c = TreeCase(6, lens, 3, [(i % 4) for i in range(1024)], Hq=2, Hkv=1, r_k=32, r_v=48)
+    c.check(*c.run())
+    assert int(c.status) == 0
+
+
+def test_two_captured_calls_share_a_workspace():
+    a, b = TreeCase(61, [3000, 500], 20, Hq=8, Hkv=2), TreeCase(62, [70, 9000, 10], 40, Hq=8, Hkv=2, r_k=96, r_v=128)
+    ws = torch.full((max(a.workspace.numel(), b.workspace.numel()),), 0xFF, dtype=torch.uint8, device="cuda")
+    want = [x.run()[0] for x in (a, b)]
+    outs, graphs = [], []
+    for x, w in zip((a, b), want):
+        out = torch.zeros_like(w)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            S.stief_tree_attention(x.layer, x.batch, x.q, x.mask, ws, out, n_nodes=x.n_nodes)
+        outs.append(out)
+        graphs.append(graph)
+    for i in (0, 1, 1, 0, 0, 1):
+        outs[i].zero_()
+        graphs[i].replay()
+        S.stief_tree_attention(b.layer, b.batch, b.q, b.mask, ws, torch.empty_like(want[1]), n_nodes=b.n_nodes)     # an eager one between
+        torch.cuda.synchronize()
+        assert torch.equal(torch.nan_to_num(outs[i]), torch.nan_to_num(want[i], nan=0.0))
+
+
 @pytest.mark.parametrize("fold_k,fold_v", [(True, True), (True, False), (False, True)])
 def test_folded_sides(fold_k, fold_v):
     c = TreeCase(17, [400, 90], 21, [21, 8], r_k=96, r_v=48, fold_k=fold_k, fold_v=fold_v)
@@ -304,7 +331,7 @@ def test_refusals():
     c = TreeCase(3, [100], 8)
     out = torch.empty(1, 8, 8, 128, dtype=torch.bfloat16, device="cuda")
     for bad in (dict(q=c.q.float()), dict(q=c.q[:, :, :4]), dict(out=out[..., :64]), dict(tree_mask=c.mask.long()), dict(tree_mask=c.mask[:, :4]),
-                dict(n_nodes=c.n_nodes.long()), dict(q=c.q.cpu()), dict(out_lse=torch.empty(1, 8, 4, device="cuda"))):
+                dict(n_nodes=c.n_nodes.long()), dict(batch=S.Batch(c.batch.block_table, c.batch.seq_lens.long())), dict(q=c.q.cpu()), dict(out_lse=torch.empty(1, 8, 4, device="cuda"))):
         args = dict(layer=c.layer, batch=c.batch, q=c.q, tree_mask=c.mask, workspace=c.workspace, out=out) | bad
         with pytest.raises(ValueError):
             S.stief_tree_attention(**args)
