@@ -13,8 +13,9 @@
 // 1300 from the last P to the next S).  Two tiles half a period apart overlap one's softmax with the other's products; there is
 // no TMEM for a third (512 columns: per tile 128 for S and 128 for O).  A quarter or an eighth of the exponentials as a
 // polynomial on the FMA pipe, starting them from the previous block's maximum, and two threads per row were measured: each
-// slower (polynomial 1/4: 596 against 535 us for four prompts of 4096; two threads per row: 557 against 469 us for one of 8192),
-// because the issue slots they cost are what the warps lack.
+// slower (polynomial 1/4: 596 against 535 us for four prompts of 4096; previous block's maximum: 571; two threads per row: 557
+// against 469 us for one of 8192): what they add to the instruction stream costs more than the unit that they relieve.  So does
+// publishing P at three quarters instead of the half (504 against 480 us).
 //
 // One persistent CTA per SM, 512 threads (128 registers each at launch, dealt out again by role):
 //   warps 0-3, 4-7  softmax of tile 0 / 1: thread = row = TMEM lane, the block's 128 scores in registers
@@ -30,8 +31,9 @@
 // The reference maximum of a row follows the true one only when that has grown by more than 2^8: the accumulator in TMEM is
 // rescaled a few times per row instead of at every block.
 //
-// Measured (32 query heads over 8, TFLOP/s of the causal half): one prompt of 16384 tokens 1174, four of 4096 1156; the
-// card's cuBLAS rates are 1709 in a burst and 1411 sustained.
+// Measured (32 query heads over 8, TFLOP/s of the causal half): one prompt of 16384 tokens 1.96 ms = 1121 back to back, four of
+// 4096 480 us = 1146; the card's cuBLAS rates are 1709 in a burst and 1411 sustained.  One of 8192 under the profiler: tensor pipe
+// 61 % and special-function units 62 % of their cycles, DRAM 130 MB (each input once), 38 % of the issue slots.
 #include <cstring>
 
 #include "stief_host_util.h"

@@ -23,6 +23,14 @@
 //   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page; Q' as value and remainder), O += P V (N = r_v)
 // TMEM (512 columns): per tile 128 for S and 128 for O; with r_v <= 64 half of O's are free and hold P, and the next scores are
 // made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
+//
+// What bounds it.  Up to 64 rows the memory: 4 sequences of 32768 tokens at ranks 64/64 are 269 MB, 42 us at the measured copy
+// rate; 8 / 16 nodes of 4 heads take 71 / 75 us, of which the stream takes 45, the first scores come 7 us after the start
+// (projection, launch, and the first pages behind those of all other SMs), CTAs end over 8 us, and joining takes 6.  From 65
+// rows on the softmax: its warps of a quarter share one scheduler, and 128 columns of 32 rows take about 1800 cycles there
+// (1024 of them the special-function units'), so 32 nodes take 87 us and 64 nodes, 256 rows, 136 us.  Tried there and
+// slower: a share of the exponentials as a polynomial (137 against 136 us, 80 against 76), turns of the two tiles at the
+// exponentials (145 to 151 against 134 to 141).
 #pragma once
 
 #include "stief_softmax.cuh"
