@@ -601,12 +601,14 @@ def _descriptors(layers, device: int, slot: str, make):
     if not layers:
         return make()
     kept = layers[0].__dict__.get(slot)
-    if kept is not None and kept[0] == device and len(kept[1]) == len(layers) and all(type(l) is Layer for l in layers):
-        for l, (k, v, kp, vp, rk, rv, Hkv) in zip(layers, kept[1]):
-            if l.k_pool is not k or l.v_pool is not v or k.data_ptr() != kp or v.data_ptr() != vp or l.r_k != rk or l.r_v != rv or l.Hkv != Hkv:
+    if kept is not None and kept[0] == device and len(kept[1]) == len(layers):
+        for l, (same, k, v, rk, rv, Hkv) in zip(layers, kept[1]):
+            d = l.__dict__
+            if l is not same or d["k_pool"] is not k or d["v_pool"] is not v or d["r_k"] != rk or d["r_v"] != rv or d["Hkv"] != Hkv:
                 break
         else:
-            return kept[2]
+            if list(map(torch.Tensor.data_ptr, kept[2])) == kept[3]:
+                return kept[4]
     tensors = [t for l in layers for t in _page_tensors(l)]
     for t in tensors:
         if not t.is_contiguous() or t.shape[0] != tensors[0].shape[0]:
@@ -614,7 +616,7 @@ def _descriptors(layers, device: int, slot: str, make):
         _here(t, "pool", device)
     arr = make()
     if all(type(l) is Layer for l in layers):
-        layers[0].__dict__[slot] = (device, [(l.k_pool, l.v_pool, l.k_pool.data_ptr(), l.v_pool.data_ptr(), l.r_k, l.r_v, l.Hkv) for l in layers], arr)
+        layers[0].__dict__[slot] = (device, [(l, l.k_pool, l.v_pool, l.r_k, l.r_v, l.Hkv) for l in layers], tensors, [t.data_ptr() for t in tensors], arr)
     return arr
 
 

@@ -41,6 +41,20 @@ inline int sm_count() {
   return cached[dev];
 }
 
+// Launch configuration of a kernel that may start while the one before it on the stream runs (it has to wait for it itself)
+inline cudaLaunchConfig_t after_previous(cudaLaunchAttribute* attr, dim3 grid, int threads, int smem, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
 inline int resolve_parts(int num_parts) { return num_parts > 0 ? num_parts : sm_count(); }
 inline int query_tiles(int Hq, int Hkv) { return (Hq / Hkv + kGroupTile - 1) / kGroupTile; }
 

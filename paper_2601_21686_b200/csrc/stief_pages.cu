@@ -213,6 +213,7 @@ __device__ __forceinline__ void fork_row(const TableDev& t, const ForkWork& f, c
 
 __global__ void __launch_bounds__(kRowThreads)
 fork_rows_kernel(const TableDev t, const int* parent, int* work, int32_t* status) {
+  launch_dependents();
   const ForkWork f = carve_fork(work, t.B, t.max_pages);
   fork_row(t, f, parent, status, blockIdx.x, threadIdx.x, kRowThreads, [](int x) { return __syncthreads_or(x); });
 }
@@ -223,7 +224,9 @@ __global__ void __launch_bounds__(kScanThreads)
 fork_pages_kernel(const TableDev t, const int* parent, int* work, int32_t* status) {
   __shared__ int warp_sums[32];
   __shared__ int got_page[kMaxBatch];
+  launch_dependents();
   const ForkWork f = carve_fork(work, t.B, t.max_pages);
+  if (!kRows) grid_dependency_wait();                                      // the rows are made by the launch before
   if (kRows) {
     for (int b = threadIdx.x >> 5; b < t.B; b += kScanThreads / 32)
       fork_row(t, f, parent, status, b, threadIdx.x & 31, 32, [](int x) { return __any_sync(0xffffffffu, x); });
@@ -291,6 +294,7 @@ __device__ __forceinline__ void copy_items(const Pools& pools, int n_pools, int 
 __global__ void __launch_bounds__(kCopyThreads)
 fork_copy_kernel(const TableDev t, const __grid_constant__ Pools pools, int n_pools, int chunks, int commit, const int* work) {
   const ForkWork f = carve_fork(const_cast<int*>(work), t.B, t.max_pages);
+  grid_dependency_wait();
   if (commit)
     for (int b = blockIdx.x; b < t.B; b += gridDim.x) {
       const int n = f.counts[b];
@@ -442,11 +446,13 @@ extern "C" int stief_pages_fork(const stief_page_table* table, const stief_page_
   if (workspace_bytes < stief_pages_workspace_bytes(t.B, t.max_pages)) return STIEF_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int* work = static_cast<int*>(workspace);
+  cudaLaunchAttribute attr[1];                                             // each launch starts while the one before it ends
   if ((long long)t.B * t.max_pages <= kFewEntries) {
     fork_pages_kernel<true><<<1, kScanThreads, 0, st>>>(t, parent, work, status);
   } else {
     fork_rows_kernel<<<t.B, kRowThreads, 0, st>>>(t, parent, work, status);
-    fork_pages_kernel<false><<<1, kScanThreads, 0, st>>>(t, parent, work, status);
+    const cudaLaunchConfig_t cfg = host::after_previous(attr, dim3(1), kScanThreads, 0, st);
+    if (cudaLaunchKernelEx(&cfg, fork_pages_kernel<false>, t, parent, work, status) != cudaSuccess) return STIEF_ERR_CUDA;
   }
   int first = 0;
   do {
@@ -455,7 +461,8 @@ extern "C" int stief_pages_fork(const stief_page_table* table, const stief_page_
     const int chunks = take_pools(pools_host, first, n, &p);
     long long items = (long long)t.B * n * chunks;
     if (items < t.B) items = t.B;
-    fork_copy_kernel<<<copy_grid(items), kCopyThreads, 0, st>>>(t, p, n, chunks, first == 0, work);
+    const cudaLaunchConfig_t cfg = host::after_previous(attr, dim3(copy_grid(items)), kCopyThreads, 0, st);
+    if (cudaLaunchKernelEx(&cfg, fork_copy_kernel, t, p, n, chunks, (int)(first == 0), (const int*)work) != cudaSuccess) return STIEF_ERR_CUDA;
     first += n;
   } while (first < n_pools);
   return cudaGetLastError() == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;

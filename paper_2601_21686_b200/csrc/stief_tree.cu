@@ -296,7 +296,7 @@ template <int RV>
 cudaError_t launch_combine_rv(const Args& a, dim3 grid, cudaStream_t st) {
   cudaLaunchAttribute attr[1];
   const bool many = (long long)a.Bt.B * a.L.Hkv * a.max_units * 8 < a.n_cta;
-  const cudaLaunchConfig_t cfg = after_previous(attr, grid, many ? 512 : 128, 0, st);
+  const cudaLaunchConfig_t cfg = host::after_previous(attr, grid, many ? 512 : 128, 0, st);
   return many ? cudaLaunchKernelEx(&cfg, combine_kernel<RV, 512>, a) : cudaLaunchKernelEx(&cfg, combine_kernel<RV, 128>, a);
 }
 

@@ -58,19 +58,6 @@ inline size_t carve(void* base, int B, int n_q, int Hq, int Hkv, int r_k, int r_
   return off;
 }
 
-// Launch configuration of a kernel that may start while the one before it on the stream runs
-inline cudaLaunchConfig_t after_previous(cudaLaunchAttribute* attr, dim3 grid, int threads, int smem, cudaStream_t st) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cfg;
-}
 
 inline int check(const stief_layer* l, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b, int64_t q_stride_t, int32_t n_q,
                  const int32_t* n_nodes, const uint32_t* mask, int32_t mask_words, void* workspace, size_t workspace_bytes, uint16_t* out,

@@ -20,7 +20,7 @@ static cudaError_t launch_one(const tree::Launch& l, cudaStream_t st) {
     configured[dev] = true;
   }
   cudaLaunchAttribute attr[1];
-  const cudaLaunchConfig_t cfg = tree::after_previous(attr, dim3(l.grid), tree::kThreads, l.smem, st);
+  const cudaLaunchConfig_t cfg = host::after_previous(attr, dim3(l.grid), tree::kThreads, l.smem, st);
   return cudaLaunchKernelEx(&cfg, kern, l.tmQ, l.tmQ32, l.tmK, l.tmV, l.a);
 }
 
