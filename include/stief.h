@@ -413,7 +413,7 @@ int stief_tree_attention(const stief_layer* layer, const stief_batch* batch, con
 
 /* Keeps the accepted nodes of every sequence's tree: row accepted[b][j] of the draft moves to position seq_lens[b] + j, for
  * j < n_accepted[b], in the key and value pools of all layers (layers_host: HOST array of descriptors with the same Hkv and
- * num_pages; bases are not used).  accepted: device int32 [B][max_accept], strictly increasing in j (a path from the root
+ * num_pages; bases are not used; no pool may be listed twice).  accepted: device int32 [B][max_accept], strictly increasing in j (a path from the root
  * is, when nodes are numbered parents first); n_accepted: device int32 [B].  A sequence whose list is not increasing or
  * leaves the block table sets STIEF_ERR_BOUNDS and keeps its rows.  The caller then advances its lengths
  * (stief_advance_seq_lens_by); rejected rows lie behind the new end and are overwritten by the next draft. */
@@ -445,7 +445,8 @@ int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tok
  * can take and give back pages.  Slot b of the batch holds pages block_table[b][0 .. page_counts[b]); ref_counts[p] is the
  * number of slots that hold page p, and a page is free when that is 0.  The lowest-numbered free page is always taken first,
  * for the lowest slot first.  Only full pages are ever shared, so appending never writes a page of another slot.
- * Table entries at or behind page_counts[b] are left as they are.  Calls on one table must not overlap on the GPU. */
+ * Table entries at or behind page_counts[b] are left as they are.  Calls on one table must not overlap on the GPU.
+ * num_pages and B * max_pages_per_seq <= 2^30. */
 typedef struct stief_page_table {
   int32_t B, max_pages_per_seq, num_pages;
   int32_t* block_table; /* [B][max_pages_per_seq] */

@@ -158,12 +158,13 @@ class Layer:
 
     def c(self) -> _CLayer:
         # the descriptor is rebuilt only when a tensor was replaced (marshalling is on the path of every step)
-        key = (_ptr(self.U_k), _ptr(self.U_v), _ptr(self.k_pool), _ptr(self.v_pool), self.Hq, self.Hkv, self.r_k, self.r_v)
+        uk_stride = 0 if self.U_k is None or self.U_k.size(0) == 1 else self.U_k.stride(0)
+        uv_stride = 0 if self.U_v is None or self.U_v.size(0) == 1 else self.U_v.stride(0)
+        key = (_ptr(self.U_k), _ptr(self.U_v), _ptr(self.k_pool), _ptr(self.v_pool), self.Hq, self.Hkv, self.r_k, self.r_v,
+               uk_stride, uv_stride, self.k_pool.size(0))
         cached = self.__dict__.get("_c")
         if cached is not None and cached[0] == key:
             return cached[1]
-        uk_stride = 0 if self.U_k is None or self.U_k.shape[0] == 1 else self.U_k.stride(0)
-        uv_stride = 0 if self.U_v is None or self.U_v.shape[0] == 1 else self.U_v.stride(0)
         st = _CLayer(self.Hq, self.Hkv, D_HEAD, self.r_k, self.r_v, self.num_pages, _ptr(self.U_k), uk_stride,
                      _ptr(self.U_v), uv_stride, _ptr(self.k_pool), _ptr(self.v_pool))
         self.__dict__["_c"] = (key, st)
@@ -498,6 +499,25 @@ def stief_mq_attention(layer: Layer, batch: Batch, q: torch.Tensor, out: torch.T
                                     out.stride(1), _ptr(out_lse), flags, _ptr(status), _stream()), "stief_mq_attention")
 
 
+def _cache_tensors(layer: Layer, device: int):
+    """Pools and bases of a layer: shapes, layout and device, looked at again when the layer holds other tensors."""
+    d = layer.__dict__
+    kept = d.get("_checked")
+    if kept is not None and kept[0] == device and kept[1] is layer.k_pool and kept[2] is layer.v_pool and kept[3] is layer.U_k and kept[4] is layer.U_v:
+        return
+    for pool, r, name in ((layer.k_pool, layer.r_k, "k_pool"), (layer.v_pool, layer.r_v, "v_pool")):
+        if pool.dtype is not torch.bfloat16 or not pool.is_contiguous() or pool.shape != (layer.num_pages, layer.Hkv, PAGE, r):
+            raise ValueError(f"{name} must be contiguous bf16 [num_pages, Hkv, {PAGE}, {r}]")
+        _here(pool, name, device)
+    for U, r, name in ((layer.U_k, layer.r_k, "U_k"), (layer.U_v, layer.r_v, "U_v")):
+        if U is None:
+            continue
+        if U.dtype is not torch.bfloat16 or U.shape[1:] != (D_HEAD, r) or U.shape[0] not in (1, layer.Hkv) or U.stride(1) != r or U.stride(2) != 1:
+            raise ValueError(f"{name} must be bf16 [Hkv or 1, {D_HEAD}, {r}] with contiguous rows")
+        _here(U, name, device)
+    d["_checked"] = (device, layer.k_pool, layer.v_pool, layer.U_k, layer.U_v)
+
+
 def stief_tree_workspace_bytes(B: int, n_q: int, Hq: int, Hkv: int, r_v: int) -> int:
     return lib().stief_tree_workspace_bytes(B, n_q, Hq, Hkv, r_v)
 
@@ -529,11 +549,11 @@ def stief_tree_attention(layer: Layer, batch: Batch, q: torch.Tensor, tree_mask:
         _here(out_lse, "out_lse", at)
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    for t, name in ((out, "out"), (workspace, "workspace"), (layer.k_pool, "k_pool"), (layer.v_pool, "v_pool"), (batch.block_table, "block_table"),
-                    (batch.seq_lens, "seq_lens")):
-        _here(t, name, at)
-    if batch.block_table.dtype is not torch.int32 or batch.seq_lens.dtype is not torch.int32:
-        raise ValueError("block_table and seq_lens must be int32")
+    _here(out, "out", at)
+    _here(workspace, "workspace", at)
+    _int32(batch.block_table, "block_table", None, at)
+    _int32(batch.seq_lens, "seq_lens", (B,), at)
+    _cache_tensors(layer, at)
     q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (max(qs[1], Hq * d_q), max(os_[1], Hq * d_out))       # an extent of 1 may carry any stride
     q_b, o_b = (qs[0], os_[0]) if B > 1 else (max(qs[0], q_t), max(os_[0], o_t))
     _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(n_nodes),
@@ -638,6 +658,8 @@ def stief_pages_reserve(table: PageTable, extra, status: Optional[torch.Tensor] 
     per_slot, at = isinstance(extra, torch.Tensor), _here(table.block_table, "block_table")
     if per_slot:
         _int32(extra, "extra", table.block_table.shape[:1], at)
+    elif int(extra) >= 1 << 31:
+        raise ValueError("extra must be a number of tokens that fits an int32")
     _check(lib().stief_pages_reserve(ctypes.byref(table.c()), extra.data_ptr() if per_slot else None, 0 if per_slot else int(extra),
                                      _status(status, at), _raw_stream(at)), "stief_pages_reserve")
 

@@ -6,6 +6,8 @@
 // zero, and the lowest free page is always taken first, so the result does not depend on the order in which threads
 // run (the only atomics add to integer reference counts).  A page that two sequences share is always full: rows are
 // only ever appended behind a sequence's last row, so a shared page is never written.
+#include <climits>
+
 #include "stief_host_util.h"
 
 namespace stief {
@@ -333,7 +335,7 @@ accept_kernel(const __grid_constant__ RowPools pools, const BatchDev Bt, int Hkv
   const int* bt = Bt.block_table + (size_t)b * Bt.max_pages;
   auto page_of = [&](long long pos) {
     const long long i = pos / kPage;
-    const int page = pos >= 0 && i < Bt.max_pages ? bt[i] : -1;
+    const int page = pos >= 0 && pos <= INT_MAX && i < Bt.max_pages ? bt[i] : -1;     // positions are ints below
     return page >= 0 && page < num_pages ? page : -1;
   };
   int bad = n < 0 || n > max_accept || len < 0;
@@ -379,6 +381,7 @@ __global__ void advance_by_kernel(int32_t* seq_lens, const int32_t* deltas, int 
 int check_table(const stief_page_table* t, TableDev* d) {
   if (!t || t->B <= 0 || t->B > kMaxBatch || t->max_pages_per_seq <= 0 || t->num_pages <= 0) return STIEF_ERR_INVALID_ARG;
   if (!t->block_table || !t->seq_lens || !t->page_counts || !t->ref_counts) return STIEF_ERR_INVALID_ARG;
+  if (t->num_pages > (1 << 30) || (long long)t->B * t->max_pages_per_seq > (1 << 30)) return STIEF_ERR_INVALID_ARG;   // sums of pages are ints
   d->B = t->B;
   d->max_pages = t->max_pages_per_seq;
   d->num_pages = t->num_pages;
@@ -410,6 +413,27 @@ int take_pools(const stief_page_pool* pools, int first, int n, Pools* out) {
 // Up to so many table entries one block finds the new rows as fast as a block per slot does, and a launch is saved (48 entries:
 // 8.1 -> 6.5 us for the whole call; 1088 entries: 26.7 -> 30.6 us)
 constexpr int kFewEntries = 256;
+
+// A pool that is listed twice (layers that share a cache) would have its rows moved twice.  An insertion into a table of
+// addresses while it is small (32 layers: 0.3 us), comparisons of all pairs beyond.
+bool pools_differ(const stief_layer* layers, int n) {
+  constexpr unsigned kSlots = 1024;
+  const void* seen[kSlots] = {};
+  auto pool = [&](int i) { return (const void*)(i & 1 ? layers[i >> 1].v_pool : layers[i >> 1].k_pool); };
+  if (n > (int)kSlots / 4) {
+    for (int i = 0; i < 2 * n; ++i)
+      for (int j = 0; j < i; ++j)
+        if (pool(i) == pool(j)) return false;
+    return true;
+  }
+  for (int i = 0; i < 2 * n; ++i) {
+    unsigned at = (unsigned)((reinterpret_cast<uintptr_t>(pool(i)) >> 7) * 0x9E3779B97F4A7C15ull >> 54);
+    for (; seen[at]; at = (at + 1) % kSlots)
+      if (seen[at] == pool(i)) return false;
+    seen[at] = pool(i);
+  }
+  return true;
+}
 
 int copy_grid(long long items) {
   const long long most = (long long)host::sm_count() * 8;                  // eight blocks of 256 threads fill an SM
@@ -498,6 +522,7 @@ extern "C" int stief_tree_accept(const stief_layer* layers_host, int32_t n_layer
     for (int r : {l.r_k, l.r_v})
       if (r != 32 && r != 48 && r != 64 && r != 96 && r != 128) return STIEF_ERR_UNSUPPORTED;
   }
+  if (!pools_differ(layers_host, n_layers)) return STIEF_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (int first = 0; first < n_layers; first += kPoolsPerLaunch / 2) {
     const int n = n_layers - first < kPoolsPerLaunch / 2 ? n_layers - first : kPoolsPerLaunch / 2;

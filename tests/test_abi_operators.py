@@ -40,13 +40,17 @@ def test_tree_attention_refuses(lib):
 
 def test_tree_accept_refuses(lib):
     batch = S._CBatch(2, 4, P, P)
-    two = (S._CLayer * 2)(_layer(), _layer(pages=11))
+    two = (S._CLayer * 2)(_layer(v=2 * P), _layer(pages=11))
 
     def call(layers=two, n=1, acc=P, most=4, cnt=P):
         return lib.stief_tree_accept(layers, n, ctypes.byref(batch), acc, most, cnt, None, None)
 
     assert call(layers=None) == call(n=0) == call(acc=None) == call(most=0) == call(cnt=None) == call(n=2) == BAD
     assert call(layers=(S._CLayer * 1)(_layer(r_k=33))) == UNSUP
+    assert call(layers=(S._CLayer * 1)(_layer())) == BAD                                     # one pool for keys and values
+    for n in (3, 300):                                                                       # the last layer's pool is the first's
+        ls = (S._CLayer * n)(*[_layer(k=P * (2 * i + 1), v=P * (2 * i + 2)) for i in range(n - 1)], _layer(k=P * (2 * n + 1), v=P))
+        assert call(layers=ls, n=n) == BAD
     assert lib.stief_advance_seq_lens_by(None, P, 4, None) == lib.stief_advance_seq_lens_by(P, P, 0, None) == BAD
 
 
@@ -70,7 +74,7 @@ def test_page_calls_refuse(lib):
         return lib.stief_pages_fork(ctypes.byref(t), pools, n, parent, ws, wb, None, None)
 
     for t in (S._CPageTable(0, 8, 100, P, P, P, P), S._CPageTable(1025, 8, 100, P, P, P, P), S._CPageTable(4, 0, 100, P, P, P, P),
-              S._CPageTable(4, 8, 0, P, P, P, P), S._CPageTable(4, 8, 100, None, P, P, P), S._CPageTable(4, 8, 100, P, P, P, None)):
+              S._CPageTable(4, 8, 0, P, P, P, P), S._CPageTable(4, 8, (1 << 30) + 1, P, P, P, P), S._CPageTable(1024, (1 << 20) + 1, 100, P, P, P, P), S._CPageTable(4, 8, 100, None, P, P, P), S._CPageTable(4, 8, 100, P, P, P, None)):
         assert fork(t=t) == lib.stief_pages_reserve(ctypes.byref(t), P, 0, None, None) == BAD
     assert fork(pools=None) == fork(n=-1) == fork(parent=None) == fork(ws=None) == fork(ws=P + 4) == BAD
     assert fork(wb=need - 4) == SMALL
@@ -89,3 +93,12 @@ def test_tensors_of_the_host_are_refused():
         S.stief_prompt_attention(t, t, t, torch.zeros(2, dtype=torch.int32), t)
     with pytest.raises(ValueError):
         S.stief_advance_seq_lens_by(torch.zeros(2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+
+
+def test_descriptors_follow_the_tensors():
+    """A view at the same address with another size or stride is another descriptor."""
+    U, pool = torch.zeros(2, 128, 64, dtype=torch.bfloat16), torch.zeros(10, 2, 64, 64, dtype=torch.bfloat16)
+    layer = S.Layer(8, 2, 64, 64, U, U, pool, pool.clone())
+    assert layer.c().num_pages == 10 and layer.c().uk_head_stride == 128 * 64
+    layer.k_pool, layer.U_k = pool[:5], U[:1]
+    assert layer.c().num_pages == 5 and layer.c().uk_head_stride == 0 and layer.c().uv_head_stride == 128 * 64

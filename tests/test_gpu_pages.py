@@ -225,6 +225,8 @@ def test_refusals():
     with pytest.raises(S.StiefError):
         S.stief_pages_reserve(s.table, -1)
     with pytest.raises(ValueError):
+        S.stief_pages_reserve(s.table, (1 << 32) + 1)
+    with pytest.raises(ValueError):
         S.stief_pages_fork(s.table, s.layers, i32([0, 1, 2]), s.work)
     with pytest.raises(ValueError):
         S.stief_pages_fork(s.table, bf16_layers(1, 5), i32([0, 1]), s.work)            # pools smaller than the table

@@ -335,6 +335,14 @@ def test_refusals():
         args = dict(layer=c.layer, batch=c.batch, q=c.q, tree_mask=c.mask, workspace=c.workspace, out=out) | bad
         with pytest.raises(ValueError):
             S.stief_tree_attention(**args)
+    l, bt = c.layer, c.batch.block_table
+    wide = torch.cat([l.k_pool, l.k_pool], 3)[..., :l.r_k]                                  # rows that do not lie end to end
+    for bad in (S.Layer(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k, l.U_v, wide, l.v_pool), S.Layer(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k, l.U_v, l.k_pool, l.v_pool[:-1]),
+                S.Layer(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k[..., :32], l.U_v, l.k_pool, l.v_pool), S.Layer(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k, l.U_v.cpu(), l.k_pool, l.v_pool)):
+        with pytest.raises(ValueError):
+            S.stief_tree_attention(bad, c.batch, c.q, c.mask, c.workspace, out)
+    with pytest.raises(ValueError):
+        S.stief_tree_attention(l, S.Batch(torch.cat([bt, bt], 1)[:, ::2], c.batch.seq_lens), c.q, c.mask, c.workspace, out)
     with pytest.raises(S.StiefError) as e:
         S.stief_tree_attention(c.layer, c.batch, c.q, c.mask, c.workspace[:64], out)
     assert e.value.code == S.STIEF_ERR_WORKSPACE
