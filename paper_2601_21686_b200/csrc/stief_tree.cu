@@ -345,7 +345,7 @@ extern "C" int stief_tree_attention(const stief_layer* layer, const stief_batch*
       !rows_map(&L.tmK, layer->k_pool, RK, pool_rows, kPage, bk) || !rows_map(&L.tmV, layer->v_pool, RV, pool_rows, kPage, bv))
     return STIEF_ERR_CUDA;
   a.q_regions = n_q * G > tree::kRows && a.unit_rows > tree::kRows ? 4 : 2;
-  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + a.q_regions * tree::kRows * RK * 2, stage = kPage * (RK + RV) * 2;
+  const int fixed = tree::kHeadBytes + tree::join_bytes(RV) + a.q_regions * tree::kRows * RK * 2, stage = tree::kBlock * (RK + RV) * 2;
   a.nst = (tree::kSmemLimit - fixed) / stage;
   if (a.nst > tree::kMaxStages) a.nst = tree::kMaxStages;
   L.smem = fixed + a.nst * stage;

@@ -152,7 +152,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   constexpr int kLayK = kSpanK == 128 ? 2 : kSpanK == 64 ? 4 : 6, kLayV = kSpanV == 128 ? 2 : kSpanV == 64 ? 4 : 6;
   constexpr bool kOwnP = RV <= 64;              // P has TMEM columns of its own: 192 .. 255 of the tile's
   constexpr int kColP = kOwnP ? 192 : 0;
-  constexpr int kPageK = kPage * RK * 2, kPageV = kPage * RV * 2, kQBytes = kRows * RK * 2;
+  constexpr int kBlockK = kBlock * RK * 2, kBlockV = kBlock * RV * 2, kQBytes = kRows * RK * 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int* pref = reinterpret_cast<int*>(smem);
@@ -160,8 +160,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   const uint32_t ctrl = smem_u32(ctrl_ptr);
   const uint32_t q_smem = smem_u32(smem) + kHeadBytes + join_bytes(RV), ring = q_smem + a.q_regions * kQBytes;
   const int nst = a.nst;
-  const uint32_t ring_v = ring + nst * kPageK;  // K pages side by side, then V pages: two neighbours are one operand of 128 rows
-  uint8_t* ring_v_ptr = smem + kHeadBytes + join_bytes(RV) + a.q_regions * kQBytes + nst * kPageK;
+  const uint32_t ring_v = ring + nst * kBlockK; // the blocks' keys, then their values, each one operand of 128 rows
+  uint8_t* ring_v_ptr = smem + kHeadBytes + join_bytes(RV) + a.q_regions * kQBytes + nst * kBlockK;
   auto full_bar = [&](int s) { return ctrl + s * 8; };
   auto empty_bar = [&](int s) { return ctrl + (12 + s) * 8; };
   const uint32_t q_full = ctrl + 24 * 8, q_empty = ctrl + 26 * 8;
@@ -183,7 +183,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   if (tid == 0) {
     pref[0] = 0;
     for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(full_bar(s), 2);                // the K half and the V half of a page
+      mbar_init(full_bar(s), 2);                // a block's keys and its values
       mbar_init(empty_bar(s), 2);               // one arrival from each tile's issuer
     }
     for (int t = 0; t < 2; ++t) {
@@ -271,27 +271,31 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         for (int j0 = 0; j0 < pages; j0 += 32) {
           const int nxt = j0 + 32 + lane < pages ? bt[j0 + 32 + lane] : 0;     // a batch of page ids ahead
           const int cnt = min(32, pages - j0);
-          for (int jj = 0; jj < cnt; ++jj) {
-            int pg = __shfl_sync(0xffffffffu, ids, jj);
+          for (int jj = 0; jj < cnt; jj += 2) {
+            const int here = min(2, cnt - jj);
+            int pg[2] = {__shfl_sync(0xffffffffu, ids, jj), __shfl_sync(0xffffffffu, ids, jj + 1)};
             if (lane == 0) {
-              if (pg < 0 || pg >= a.L.num_pages) {
-                report(status, STIEF_ERR_BOUNDS);
-                pg = 0;
-              }
               if (use > 0) {
-                if (q_due) send_queries(!mbar_test_wait(empty_bar(st), (use - 1) & 1));        // no page to fetch: wait for the queries' place
+                if (q_due) send_queries(!mbar_test_wait(empty_bar(st), (use - 1) & 1));        // no block to fetch: wait for the queries' place
                 mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
               }
-              const int row = (pg * a.L.Hkv + g.h) * kPage;
-              const uint32_t dst = keys ? ring + st * kPageK : ring_v + st * kPageV;
-              if (keys) {
-                mbar_arrive_expect_tx(full_bar(st), kPageK);
+              const uint32_t dst = keys ? ring + st * kBlockK : ring_v + st * kBlockV;
+              mbar_arrive_expect_tx(full_bar(st), (keys ? kBlockK : kBlockV) / 2 * here);
 #pragma unroll
-                for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + i * kPage * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
-              } else {
-                mbar_arrive_expect_tx(full_bar(st), kPageV);
+              for (int p = 0; p < 2; ++p) {
+                if (p >= here) continue;
+                if (pg[p] < 0 || pg[p] >= a.L.num_pages) {
+                  report(status, STIEF_ERR_BOUNDS);
+                  pg[p] = 0;
+                }
+                const int row = (pg[p] * a.L.Hkv + g.h) * kPage;
+                if (keys) {
 #pragma unroll
-                for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + i * kPage * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+                  for (int i = 0; i < kNbK; ++i) tma_load_2d(dst + (i * kBlock + p * kPage) * kSpanK, &tmK, i * bk.bw, row, full_bar(st));
+                } else {
+#pragma unroll
+                  for (int i = 0; i < kNbV; ++i) tma_load_2d(dst + (i * kBlock + p * kPage) * kSpanV, &tmV, i * bv.bw, row, full_bar(st));
+                }
               }
               if (++st == nst) {
                 st = 0;
@@ -316,54 +320,43 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       constexpr uint32_t kHiV = (uint32_t)((((uint64_t)(8 * kSpanV >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayV << 61)) >> 32);
       const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_qk2 = idesc_bf16_f32(kRows, kBlock), id_pv = idesc_bf16_f32_bmn(kRows, RV);
       auto bar = [&](int i) { return ctrl_u + i * 8; };                        // as numbered above
-      int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next page
-      // Both tiles see every page land, in order, the other tile's too, and both give it back: a barrier's parity tells a slot's
-      // page from the one before and the one behind it only to who keeps step with them.  `skip` pages of the other tile, then `want` of this one, whose slots are
-      // kept; without `block` only as far as they have landed, and whether that was all.
-      int skip = 0, want = 0, got = 0, cur[2], nxt[2];
-      auto observe = [&](bool block) {
-        while (skip > 0 || got < want) {
-          if (block) mbar_wait_warp(bar(st), use & 1, abort_flag, status);
-          else if (!__all_sync(0xffffffffu, mbar_test_wait(bar(st), use & 1))) return false;
-          if (skip > 0) {
-            --skip;
-            if (lane == 0) mbar_arrive(bar(12 + st));
-            __syncwarp();
-          } else if (got++ == 0) nxt[0] = st;
-          else nxt[1] = st;
-          if (++st == nst) {
-            st = 0;
-            ++use;
-          }
+      int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next block
+      // Both tiles see every block land, in order, the other tile's too, and both give it back: a barrier's parity tells a slot's
+      // block from the one before and the one behind it only to who keeps step with them.  `skip` blocks of the other tile, then
+      // this one's, whose slot is kept; without `wait` only as far as they have landed, and whether that was all.
+      int skip = 0, cur = 0, nxt = 0;
+      auto step = [&]() {
+        if (++st == nst) {
+          st = 0;
+          ++use;
         }
+      };
+      auto observe = [&](bool wait, bool own) {
+        for (; skip > 0; --skip) {
+          if (wait) mbar_wait_warp(bar(st), use & 1, abort_flag, status);
+          else if (!__all_sync(0xffffffffu, mbar_test_wait(bar(st), use & 1))) return false;
+          if (lane == 0) mbar_arrive(bar(12 + st));
+          __syncwarp();
+          step();
+        }
+        if (!own) return true;
+        if (wait) mbar_wait_warp(bar(st), use & 1, abort_flag, status);
+        else if (!__all_sync(0xffffffffu, mbar_test_wait(bar(st), use & 1))) return false;
+        nxt = st;
+        step();
         return true;
       };
-      auto expect = [&](int others, int own) {
-        skip = others;
-        want = own;
-        got = 0;
-      };
-      auto score = [&](int pages, const int (&at)[2], bool last) {             // S = Q' K^T, 64 columns per page
-        auto product = [&](int slot, uint32_t d, uint32_t idesc) {
-          const uint32_t ka = desc_lo(16, ring_u + slot * kPageK);
+      auto score = [&](int pages, int slot, bool last) {                       // S = Q' K^T, 64 columns per page
+        const uint32_t ka = desc_lo(16, ring_u + slot * kBlockK), idesc = pages == 2 ? id_qk2 : id_qk;
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int k = 0; k < RK / 16; ++k) {
-              if (x >= parts) continue;
-              constexpr int kPer = bk.bw / 16;                                 // K steps per swizzled block
-              const uint32_t qo = (uint32_t)((k / kPer) * kRows * kSpanK + (k % kPer) * 32) >> 4, ko = (uint32_t)((k / kPer) * kPage * kSpanK + (k % kPer) * 32) >> 4;
-              umma_ss(d, qa + x * (kQBytes >> 4) + qo, kHiK, ka + ko, kHiK, idesc, x > 0 || k > 0 ? 1u : 0u);
-            }
-        };
-        // A key row in one swizzled block: pages in neighbouring slots are one operand (half as many products to issue)
-        if (kNbK == 1 && pages == 2 && at[1] == at[0] + 1) {
-          product(at[0], tmem_u, id_qk2);
-        } else {
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            if (p < pages) product(at[p], tmem_u + 64 * p, id_qk);
-        }
+          for (int k = 0; k < RK / 16; ++k) {
+            if (x >= parts) continue;
+            constexpr int kPer = bk.bw / 16;                                   // K steps per swizzled block of columns
+            const uint32_t off = (uint32_t)((k / kPer) * kRows * kSpanK + (k % kPer) * 32) >> 4;           // kRows == kBlock
+            umma_ss(tmem_u, qa + x * (kQBytes >> 4) + off, kHiK, ka + off, kHiK, idesc, x > 0 || k > 0 ? 1u : 0u);
+          }
         umma_commit_warp(bar(28 + t));
         if (last) umma_commit_warp(bar(26));
       };
@@ -373,8 +366,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         const int pages = min(2 * cnt, (len + kPage - 1) / kPage - 2 * j0);    // pages of the segment
         const int steps = dual ? (cnt + 1 - t) >> 1 : cnt, stride = dual ? 2 : 1, at = dual ? t : 0;
         if (steps == 0) {                                                      // a lone block: the other tile's
-          expect(pages, 0);
-          observe(true);
+          skip = cnt;
+          observe(true, false);
           mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
           ++kt;
           if (lane == 0) mbar_arrive(bar(26));
@@ -383,65 +376,58 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         qa = desc_lo(16, q_u + (dual ? 0 : 2 * t) * kQBytes);
         int here = min(2, pages - 2 * at);
-        expect(2 * at, here);
-        observe(true);
-        cur[0] = nxt[0];
-        cur[1] = nxt[1];
+        skip = at;
+        observe(true, true);
+        cur = nxt;
         mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
         tc_fence_after();
         score(here, cur, steps == 1);
         for (int s = 0; s < steps; ++s) {
-          // Where the next block's pages have landed already, all that its scores need is dealt with ahead of P, so that from P
-          // on only products are issued; where they have not, P is not kept waiting for them (nor the pages that its product
-          // gives back: with six pages in the ring that alone doubled the time).
+          // Where the next block has landed already, all that its scores need is dealt with ahead of P, so that from P on only
+          // products are issued; where it has not, P is not kept waiting for it (nor the slot that its product gives back:
+          // with three blocks in the ring that alone doubled the time).
           bool early = false;
+          int want = 0;
           if (s + 1 < steps) {
-            expect(dual ? 2 : 0, min(2, pages - 2 * (at + (s + 1) * stride))); // the other tile's block lies between
-            early = observe(false);
+            want = min(2, pages - 2 * (at + (s + 1) * stride));
+            skip = dual ? 1 : 0;                                               // the other tile's block lies between
+            early = observe(false, true);
             if (early && kOwnP) {                                              // S is free once it has been read
               mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
               tc_fence_after();
               score(want, nxt, s + 2 == steps);
             }
           }
-          auto release = [&]() {
+          const uint32_t va = desc_lo(kBlock * kSpanV, ring_v_u + cur * kBlockV);
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-              if (p < here) umma_commit_warp(bar(12 + cur[p]));
-          };
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {                                        // O += P V
-            mbar_wait_warp(bar(30 + 2 * t + p), n & 1, abort_flag, status);
-            tc_fence_after();
-            if (p < here) {
-              const uint32_t va = desc_lo(kPage * kSpanV, ring_v_u + cur[p] * kPageV);
-#pragma unroll
-              for (int k = 0; k < kPage / 16; ++k)
-                umma_ts(tmem_u + 128, tmem_u + kColP + 32 * p + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || p > 0 || k > 0 ? 1u : 0u);
+          for (int k = 0; k < kBlock / 16; ++k) {                              // O += P V
+            if (kOwnP ? k == 0 : k % 4 == 0) {
+              mbar_wait_warp(bar(30 + 2 * t + (kOwnP || k > 0 ? 1 : 0)), n & 1, abort_flag, status);
+              tc_fence_after();
             }
+            if (k < 4 || here == 2) umma_ts(tmem_u + 128, tmem_u + kColP + 8 * k, va + (uint32_t)(k * 16 * kSpanV >> 4), kHiV, id_pv, s > 0 || k > 0 ? 1u : 0u);
           }
-          umma_commit_warp(bar(38 + t));
+          if (kOwnP) umma_commit_warp(bar(38 + t));
           if (s + 1 == steps) {
             umma_commit_warp(bar(34 + t));
-            release();
+            umma_commit_warp(bar(12 + cur));
           } else if (!early) {
-            release();
-            observe(true);
+            umma_commit_warp(bar(12 + cur));
+            observe(true, true);
             if (kOwnP) mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status); // S has been read long ago
             tc_fence_after();
             score(want, nxt, s + 2 == steps);
           } else {
             if (!kOwnP) score(want, nxt, s + 2 == steps);
-            release();
+            umma_commit_warp(bar(12 + cur));
           }
           ++n;
           here = want;
-          cur[0] = nxt[0];
-          cur[1] = nxt[1];
+          cur = nxt;
         }
         if (dual) {                                                            // blocks behind this tile's last
-          expect(max(0, pages - 2 * (at + (steps - 1) * 2) - 2), 0);
-          observe(true);
+          skip = cnt - 1 - (at + (steps - 1) * 2);
+          observe(true, false);
         }
         ++kt;
       }
@@ -452,14 +438,14 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const int t = warp >> 2, q4 = warp & 3, lane_row = 32 * q4 + lane;
     const uint32_t t_s = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256, t_o = t_s + 128, t_p = t_s + kColP;
     const float c = kLog2e * rsqrtf((float)kD);
-    int n = 0, kt = 0, ring_page = 0;                           // blocks and segments of this tile so far; pages of both
+    int n = 0, kt = 0, ring_block = 0;                          // blocks and segments of this tile so far; blocks of both
     auto arrive_warp = [&](uint32_t bar) {
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
     for (Segment g = walk.next(a, pref); g.valid; g = walk.next(a, pref)) {
-      const int len = g.ctx + g.n, page0 = ring_page;
-      ring_page += min(2 * g.cnt, (len + kPage - 1) / kPage - 2 * g.j0);
+      const int len = g.ctx + g.n, block0 = ring_block;
+      ring_block += g.cnt;
       const int steps = tile_blocks(g, t);
       if (steps == 0) continue;
       const int wrap = kRows / g.replicas, replica = lane_row / wrap, row = lane_row - replica * wrap;
@@ -541,7 +527,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             pk[i] = pack_bf16(e0, e1);
           }
           tmem_st16(t_p + col0 / 2 + 16 * q, pk);
-          if (kCols == 128 && q == 1) {                         // the first page's may be used already
+          if (kCols == 128 && q == 1 && !kOwnP) {               // the first page's may be used already
             tmem_st_wait();
             tc_fence_before();
             arrive_warp(p_full(t, 0));
@@ -549,7 +535,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         tmem_st_wait();
         tc_fence_before();
-        if (kCols < 128) arrive_warp(p_full(t, 0));
+        if (kCols < 128 && !kOwnP) arrive_warp(p_full(t, 0));
         arrive_warp(p_full(t, 1));
         float a0, a1;
         unpack2(add2(sum[0], sum[1]), a0, a1);
@@ -561,17 +547,14 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tc_fence_after();
         if (p0 + kBlock > len) {
           // Rows behind the sequence's end: whatever bits they have (NaN included) must not reach the accumulator through
-          // 0 * x.  Every tile that uses the page zeroes them.
-          for (int p = 0; p < 2 && p0 + p * kPage < len; ++p) {
-            const int dead = len - p0 - p * kPage;              // first dead row of the page
-            const int idx = page0 + 2 * j + p, stg = idx % nst;
-            mbar_wait(full_bar(stg), (idx / nst) & 1, abort_flag, status);
-            uint8_t* v = ring_v_ptr + stg * kPageV;
-            constexpr int kCpr = kSpanV / 16, kPerRow = RV / 8;
-            for (int e = lane_row; e < (kPage - dead) * kPerRow; e += kRows) {
-              const int r = dead + e / kPerRow, ch = e % kPerRow;
-              *reinterpret_cast<uint4*>(v + (ch / kCpr) * kPage * kSpanV + r * kSpanV + (ch % kCpr) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
+          // 0 * x.  Every tile that uses the block zeroes them, up to the end of its last page.
+          const int dead = len - p0, rows = (dead > kPage ? kBlock : kPage) - dead, idx = block0 + j, stg = idx % nst;
+          mbar_wait(full_bar(stg), (idx / nst) & 1, abort_flag, status);
+          uint8_t* v = ring_v_ptr + stg * kBlockV + dead * kSpanV;
+          constexpr int kCpr = kSpanV / 16, kPerRow = RV / 8;
+          for (int e = lane_row; e < rows * kPerRow; e += kRows) {
+            const int r = e / kPerRow, ch = e % kPerRow;
+            *reinterpret_cast<uint4*>(v + (ch / kCpr) * kBlock * kSpanV + r * kSpanV + (ch % kCpr) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           fence_proxy_async_smem();
         }
@@ -580,7 +563,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             arrive_warp(s_free(t));
             if (n > 0) mbar_wait(p_free(t), (n - 1) & 1, abort_flag, status);
           }
-          arrive_warp(p_full(t, 0));
+          if (!kOwnP) arrive_warp(p_full(t, 0));
           arrive_warp(p_full(t, 1));
         } else if (g.replicas == 1) {
           block(std::integral_constant<int, 128>{}, s_i, p0);
