@@ -52,6 +52,7 @@ __host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBy
 constexpr int kMaxStages = 12;
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
+constexpr int kPacePolls = 64, kPacedBlocks = 8;
 
 // Sequence b as every kernel sees it
 struct Seq {
@@ -320,7 +321,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       constexpr uint32_t kHiV = (uint32_t)((((uint64_t)(8 * kSpanV >> 4) << 32) | (1ull << 46) | ((uint64_t)kLayV << 61)) >> 32);
       const uint32_t id_qk = idesc_bf16_f32(kRows, kPage), id_qk2 = idesc_bf16_f32(kRows, kBlock), id_pv = idesc_bf16_f32_bmn(kRows, RV);
       auto bar = [&](int i) { return ctrl_u + i * 8; };                        // as numbered above
-      int st = 0, use = 0, kt = 0, n = 0;                                      // ring position of the next block
+      int st = 0, use = 0, kt = 0, n = 0, others = 0;                          // ring position of the next block; blocks of the other tile
       // Both tiles see every block land, in order, the other tile's too, and both give it back: a barrier's parity tells a slot's
       // block from the one before and the one behind it only to who keeps step with them.  `skip` blocks of the other tile, then
       // this one's, whose slot is kept; without `wait` only as far as they have landed, and whether that was all.
@@ -346,6 +347,13 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         step();
         return true;
       };
+      // The tiles' scores are issued in turn, each when the other's last have been read: the softmax of one then loads and looks for
+      // its maximum while the other's has the special-function units; side by side both wait for them.  Only pace, not
+      // order: the look has an end, and a wrong answer (a parity is one bit) costs nothing but the shift.
+      auto pace = [&](int phase) {
+        for (int i = 0; i < kPacePolls && !__all_sync(0xffffffffu, mbar_test_wait(bar(37 - t), phase & 1)); ++i) {
+        }
+      };
       auto score = [&](int pages, int slot, bool last) {                       // S = Q' K^T, 64 columns per page
         const uint32_t ka = desc_lo(16, ring_u + slot * kBlockK), idesc = pages == 2 ? id_qk2 : id_qk;
 #pragma unroll
@@ -370,6 +378,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           observe(true, false);
           mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
           ++kt;
+          others += cnt;
           if (lane == 0) mbar_arrive(bar(26));
           __syncwarp();
           continue;
@@ -381,6 +390,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         cur = nxt;
         mbar_wait_warp(bar(24), kt & 1, abort_flag, status);
         tc_fence_after();
+        const bool paced = kOwnP && !dual && cnt >= kPacedBlocks;
+        const int others_steps = dual ? (cnt + t) >> 1 : cnt;
+        if (paced && t == 1) pace(others);
         score(here, cur, steps == 1);
         for (int s = 0; s < steps; ++s) {
           // Where the next block has landed already, all that its scores need is dealt with ahead of P, so that from P on only
@@ -394,6 +406,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             early = observe(false, true);
             if (early && kOwnP) {                                              // S is free once it has been read
               mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
+              if (paced && s + t < others_steps) pace(others + s + t);
               tc_fence_after();
               score(want, nxt, s + 2 == steps);
             }
@@ -429,6 +442,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           skip = cnt - 1 - (at + (steps - 1) * 2);
           observe(true, false);
         }
+        others += others_steps;
         ++kt;
       }
     }
