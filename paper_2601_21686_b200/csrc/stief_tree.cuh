@@ -52,7 +52,7 @@ __host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBy
 constexpr int kMaxStages = 12;
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
-constexpr int kPacePolls = 64, kPacedBlocks = 8;
+constexpr int kPacePolls = 64, kPacedBlocks = 8, kLooks = 1 << 12;
 
 // Sequence b as every kernel sees it
 struct Seq {
@@ -403,7 +403,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           if (s + 1 < steps) {
             want = min(2, pages - 2 * (at + (s + 1) * stride));
             skip = dual ? 1 : 0;                                               // the other tile's block lies between
-            early = observe(false, true);
+            for (int i = 0; i < kLooks; ++i) {                                 // while P is not there yet, scores may be issued at any time
+              early = observe(false, true);
+              if (early || !kOwnP || __all_sync(0xffffffffu, mbar_test_wait(bar(31 + 2 * t), n & 1))) break;
+            }
             if (early && kOwnP) {                                              // S is free once it has been read
               mbar_wait_warp(bar(36 + t), n & 1, abort_flag, status);
               if (paced && s + t < others_steps) pace(others + s + t);
