@@ -15,7 +15,8 @@
 // polynomial on the FMA pipe, starting them from the previous block's maximum, and two threads per row were measured: each
 // slower (polynomial 1/4: 596 against 535 us for four prompts of 4096; previous block's maximum: 571; two threads per row: 557
 // against 469 us for one of 8192): what they add to the instruction stream costs more than the unit that they relieve.  So does
-// publishing P at three quarters instead of the half (504 against 480 us).
+// publishing P at three quarters instead of the half (504 against 480 us), and keeping half of the row, the other loaded again, so
+// that a polynomial share fits the registers (542 to 589 against 490 us).
 //
 // One persistent CTA per SM, 512 threads (128 registers each at launch, dealt out again by role):
 //   warps 0-3, 4-7  softmax of tile 0 / 1: thread = row = TMEM lane, the block's 128 scores in registers

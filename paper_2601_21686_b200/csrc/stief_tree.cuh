@@ -19,18 +19,23 @@
 // them twice or four times, each copy takes its half or quarter of a block's columns (P is zero elsewhere, the wasted products
 // cost nothing here) and is joined with the others when the segment ends.
 //   warps 0-3, 4-7  softmax of tile 0 / 1, thread = row = TMEM lane, 128 scores in registers; warps without rows skip
-//   warps 8, 11     cache pages by TMA into a ring of K pages and V pages of one KV head; Q' tiles
-//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 64 per page; Q' as value and remainder), O += P V (N = r_v)
+//   warps 8, 11     cache pages by TMA into a ring of blocks, two pages of keys and two of values of one KV head; Q' tiles
+//   warps 9, 10     MMA issue, a warp per tile:  S = Q' K^T (N = 128; Q' as value and remainder), O += P V (N = r_v)
 // TMEM (512 columns): per tile 128 for S and 128 for O; with r_v <= 64 half of O's are free and hold P, and the next scores are
 // made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
 //
 // What bounds it.  Up to 64 rows the memory: 4 sequences of 32768 tokens at ranks 64/64 are 269 MB, 42 us at the measured copy
-// rate; 8 / 16 nodes of 4 heads take 71 / 75 us, of which the stream takes 45, the first scores come 7 us after the start
+// rate; 8 / 16 nodes of 4 heads take 69 / 71 us, of which the stream takes 45, the first scores come 7 us after the start
 // (projection, launch, and the first pages behind those of all other SMs), CTAs end over 8 us, and joining takes 6.  From 65
-// rows on the softmax: its warps of a quarter share one scheduler, and 128 columns of 32 rows take about 1800 cycles there
-// (1024 of them the special-function units'), so 32 nodes take 87 us and 64 nodes, 256 rows, 136 us.  Tried there and
-// slower: a share of the exponentials as a polynomial (137 against 136 us, 80 against 76), turns of the two tiles at the
-// exponentials (145 to 151 against 134 to 141).
+// rows on the softmax, of which two warps share a scheduler: loading 32 rows of 128 scores, their maximum, exponentials and P
+// take 3250 cycles when the two are half a step apart (1024 each of the special-function units') and 4040 side by side; 32
+// nodes take 80 us, with three or four blocks in the ring instead of five 94 and 86, and 64 nodes, 256 rows, 116 us.
+//
+// An issuing warp runs beside two softmax warps and needs 100 to 180 cycles for a wait that is over already: with a barrier per
+// page and P in two halves it was the slowest part (64 nodes 136 us).  Tried and slower: a share of the exponentials as a
+// polynomial (64 nodes 136 and 149 against 118 us for an eighth and a quarter), turns of the softmax warps themselves (145 to
+// 151 against 134 to 141), pages brought to L2 one to four blocks ahead of the ring (32 nodes 86 to 88 against 80: a fetching
+// warp's time), waits tested ahead of the work before them (64 nodes 117 to 120 against 117).
 #pragma once
 
 #include "stief_softmax.cuh"
@@ -52,6 +57,9 @@ __host__ __device__ constexpr int join_bytes(int RV) { return RV <= 64 ? kJoinBy
 constexpr int kMaxStages = 12;
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
+// The looks at a barrier that nothing depends on: how many at most, and from how many blocks of a segment on the tiles are
+// paced.  Only tiles of their own rows are: with alternate blocks the ring's order already keeps them apart (paced, 32 nodes
+// 78 against 80 us, but 26 ragged 98 against 97 and 8 nodes 70 against 69).
 constexpr int kPacePolls = 64, kPacedBlocks = 8, kLooks = 1 << 12;
 
 // Sequence b as every kernel sees it
@@ -348,8 +356,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         return true;
       };
       // The tiles' scores are issued in turn, each when the other's last have been read: the softmax of one then loads and looks for
-      // its maximum while the other's has the special-function units; side by side both wait for them.  Only pace, not
-      // order: the look has an end, and a wrong answer (a parity is one bit) costs nothing but the shift.
+      // its maximum while the other's has the special-function units (64 nodes 133 -> 118 us).  Only pace, not order: the look
+      // has an end, and a wrong answer (a parity is one bit) costs nothing but the shift.
       auto pace = [&](int phase) {
         for (int i = 0; i < kPacePolls && !__all_sync(0xffffffffu, mbar_test_wait(bar(37 - t), phase & 1)); ++i) {
         }
