@@ -499,16 +499,23 @@ def stief_mq_attention(layer: Layer, batch: Batch, q: torch.Tensor, out: torch.T
                                     out.stride(1), _ptr(out_lse), flags, _ptr(status), _stream()), "stief_mq_attention")
 
 
+def _layer_pools(layer: Layer, device: int):
+    """The pools have to be what the layer says of them: the kernels compute every row's address from its ranks and heads."""
+    if not isinstance(layer, Layer):
+        raise ValueError("a Layer is expected (a quantised cache has no such call)")
+    for pool, r, name in ((layer.k_pool, layer.r_k, "k_pool"), (layer.v_pool, layer.r_v, "v_pool")):
+        if pool.dtype is not torch.bfloat16 or not pool.is_contiguous() or pool.shape != (layer.num_pages, layer.Hkv, PAGE, r):
+            raise ValueError(f"{name} must be contiguous bf16 [num_pages, Hkv, {PAGE}, {r}]")
+        _here(pool, name, device)
+
+
 def _cache_tensors(layer: Layer, device: int):
     """Pools and bases of a layer: shapes, layout and device, looked at again when the layer holds other tensors."""
     d = layer.__dict__
     kept = d.get("_checked")
     if kept is not None and kept[0] == device and kept[1] is layer.k_pool and kept[2] is layer.v_pool and kept[3] is layer.U_k and kept[4] is layer.U_v:
         return
-    for pool, r, name in ((layer.k_pool, layer.r_k, "k_pool"), (layer.v_pool, layer.r_v, "v_pool")):
-        if pool.dtype is not torch.bfloat16 or not pool.is_contiguous() or pool.shape != (layer.num_pages, layer.Hkv, PAGE, r):
-            raise ValueError(f"{name} must be contiguous bf16 [num_pages, Hkv, {PAGE}, {r}]")
-        _here(pool, name, device)
+    _layer_pools(layer, device)
     for U, r, name in ((layer.U_k, layer.r_k, "U_k"), (layer.U_v, layer.r_v, "U_v")):
         if U is None:
             continue
@@ -573,7 +580,12 @@ def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Ten
         raise ValueError("accepted must be [B, max_accept]")
     _int32(batch.block_table, "block_table", None, at)
     _int32(batch.seq_lens, "seq_lens", (B,), at)
-    arr = _descriptors(layers, at, "_accept", lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
+
+    def make():
+        for l in layers:
+            _layer_pools(l, at)
+        return (_CLayer * max(len(layers), 1))(*[l.c() for l in layers])
+    arr = _descriptors(layers, at, "_accept", make)
     _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), accepted.data_ptr(), accepted.shape[1], n_accepted.data_ptr(),
                                    _status(status, at), _raw_stream(at)), "stief_tree_accept")
 

@@ -1,0 +1,64 @@
+"""CPU-only checks of what the Python binding lets through to the tree, prompt and page calls: the library is replaced by a
+recorder, so a call that should have been refused is seen and never runs."""
+import pytest
+import torch
+
+import paper_2601_21686_b200 as S
+
+BF = torch.bfloat16
+
+
+class Recorder:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return S.STIEF_OK
+        return call
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Host tensors pass for the current device's; the list of calls that reached the library."""
+    rec = Recorder()
+    monkeypatch.setattr(S, "lib", lambda: rec)
+    monkeypatch.setattr(S, "_here", lambda t, name, device=None: 0)
+    monkeypatch.setattr(S, "_raw_stream", lambda device: 0)
+    return rec.calls
+
+
+def i32(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def layer(Hq=8, Hkv=2, r_k=64, r_v=64, pages=4, k=None, v=None):
+    pool = lambda r: torch.zeros(pages, Hkv, 64, r, dtype=BF)
+    basis = lambda r: torch.zeros(Hkv, 128, r, dtype=BF)
+    return S.Layer(Hq, Hkv, r_k, r_v, basis(r_k), basis(r_v), pool(r_k) if k is None else k, pool(r_v) if v is None else v)
+
+
+def accept(layers):
+    S.stief_tree_accept(layers, S.Batch(i32(2, 2), i32(2)), i32(2, 3), i32(2))
+
+
+def test_accept_refuses_pools_that_are_not_what_the_layer_says(calls):
+    good = layer()
+    accept([good])
+    assert len(calls) == 1
+    pool = lambda *shape, dtype=BF: torch.zeros(*shape, dtype=dtype)
+    for bad in (layer(r_k=128, k=pool(4, 2, 64, 64)), layer(r_v=32, v=pool(4, 2, 64, 64)),          # other ranks than the pools'
+                layer(r_k=32, r_v=64, k=pool(4, 2, 64, 64), v=pool(4, 2, 64, 32)),                    # swapped
+                layer(Hkv=8, k=pool(4, 2, 64, 64), v=pool(4, 2, 64, 64)),                             # other heads
+                layer(k=pool(4, 2, 32, 64)), layer(k=pool(4, 128, 64)), layer(v=pool(3, 2, 64, 64)),
+                layer(k=pool(4, 2, 64, 64, dtype=torch.float16)), layer(v=pool(4, 2, 64, 64, dtype=torch.float32)),
+                layer(k=pool(4, 2, 64, 128)[..., :64])):
+        for layers in ([bad], [good, bad]):
+            with pytest.raises(ValueError):
+                accept(layers)
+    codes = lambda *shape: torch.zeros(*shape, dtype=torch.uint8)
+    quantised = S.QLayer(8, 2, 64, 64, None, None, None, codes(4, 2, 64, 64), codes(4, 2, 64, 64), torch.zeros(4, 2, 64, 1, 2))
+    with pytest.raises(ValueError):
+        accept([good, quantised])
+    assert len(calls) == 1
