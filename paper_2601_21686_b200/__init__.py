@@ -510,11 +510,8 @@ def _layer_pools(layer: Layer, device: int):
 
 
 def _cache_tensors(layer: Layer, device: int):
-    """Pools and bases of a layer: shapes, layout and device, looked at again when the layer holds other tensors."""
-    d = layer.__dict__
-    kept = d.get("_checked")
-    if kept is not None and kept[0] == device and kept[1] is layer.k_pool and kept[2] is layer.v_pool and kept[3] is layer.U_k and kept[4] is layer.U_v:
-        return
+    """Pools and bases of a layer: shapes, layout and device.  Looked at in every call: ranks and tensors may have been replaced,
+    or changed in place, since the last."""
     _layer_pools(layer, device)
     for U, r, name in ((layer.U_k, layer.r_k, "U_k"), (layer.U_v, layer.r_v, "U_v")):
         if U is None:
@@ -522,7 +519,6 @@ def _cache_tensors(layer: Layer, device: int):
         if U.dtype is not torch.bfloat16 or U.shape[1:] != (D_HEAD, r) or U.shape[0] not in (1, layer.Hkv) or U.stride(1) != r or U.stride(2) != 1:
             raise ValueError(f"{name} must be bf16 [Hkv or 1, {D_HEAD}, {r}] with contiguous rows")
         _here(U, name, device)
-    d["_checked"] = (device, layer.k_pool, layer.v_pool, layer.U_k, layer.U_v)
 
 
 def stief_tree_workspace_bytes(B: int, n_q: int, Hq: int, Hkv: int, r_v: int) -> int:

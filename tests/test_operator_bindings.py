@@ -62,3 +62,36 @@ def test_accept_refuses_pools_that_are_not_what_the_layer_says(calls):
     with pytest.raises(ValueError):
         accept([good, quantised])
     assert len(calls) == 1
+
+
+def tree(l, n_q=4):
+    q, out = torch.zeros(2, n_q, l.Hq, 128, dtype=BF), torch.zeros(2, n_q, l.Hq, 128, dtype=BF)
+    S.stief_tree_attention(l, S.Batch(i32(2, 2), i32(2)), q, i32(2, n_q, 1), torch.zeros(1 << 10, dtype=torch.uint8), out)
+
+
+def _set(name, value):
+    return lambda l: setattr(l, name, value)
+
+
+CHANGES = {
+    "smaller key rank": _set("r_k", 32), "larger key rank": _set("r_k", 128), "smaller value rank": _set("r_v", 48), "larger value rank": _set("r_v", 96),
+    "more heads": _set("Hkv", 4), "fewer heads": _set("Hkv", 1),
+    "pool resized in place": lambda l: l.k_pool.resize_(4, 2, 32, 64),
+    "pool re-laid in place": lambda l: l.v_pool.transpose_(2, 3),
+    "pool pointed elsewhere in place": lambda l: l.v_pool.set_(torch.zeros(4, 2, 64, 32, dtype=BF)),
+    "pool of another type in place": lambda l: setattr(l.k_pool, "data", torch.zeros(4, 2, 64, 64)),
+    "basis resized in place": lambda l: l.U_k.resize_(2, 64, 64),
+    "basis pointed elsewhere in place": lambda l: l.U_v.set_(torch.zeros(2, 128, 32, dtype=BF)),
+}
+
+
+@pytest.mark.parametrize("change", CHANGES)
+def test_tree_attention_looks_at_the_layer_in_every_call(calls, change):
+    l = layer()
+    tree(l)
+    tree(l)
+    assert [name for name, _ in calls].count("stief_tree_attention") == 2
+    CHANGES[change](l)
+    with pytest.raises(ValueError):
+        tree(l)
+    assert [name for name, _ in calls].count("stief_tree_attention") == 2
