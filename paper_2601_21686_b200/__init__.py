@@ -233,21 +233,16 @@ class PageTable:
         return Batch(self.block_table, self.seq_lens)
 
     def c(self) -> _CPageTable:
-        key = (_ptr(self.block_table), _ptr(self.seq_lens), _ptr(self.page_counts), _ptr(self.ref_counts),
-               tuple(self.block_table.shape), self.ref_counts.shape[0])
-        cached = self.__dict__.get("_c")
-        if cached is not None and cached[0] == key:
-            return cached[1]
-        at = _int32(self.block_table, "block_table")
-        for t in (self.seq_lens, self.page_counts, self.ref_counts):
-            _int32(t, "page table", None, at)
+        # every tensor is looked at in every call: one may have been replaced by another of the same address
         B = self.block_table.shape[0]
-        if self.block_table.dim() != 2 or self.seq_lens.shape != (B,) or self.page_counts.shape != (B,):
-            raise ValueError("block_table [B, max_pages], seq_lens [B] and page_counts [B] disagree")
-        st = _CPageTable(B, self.block_table.shape[1], self.ref_counts.shape[0], _ptr(self.block_table), _ptr(self.seq_lens),
-                         _ptr(self.page_counts), _ptr(self.ref_counts))
-        self.__dict__["_c"] = (key, st)
-        return st
+        at = _int32(self.block_table, "block_table")
+        if self.block_table.dim() != 2 or self.ref_counts.dim() != 1:
+            raise ValueError("block_table [B, max_pages] and ref_counts [num_pages] are expected")
+        for t, name in ((self.seq_lens, "seq_lens"), (self.page_counts, "page_counts")):
+            _int32(t, name, (B,), at)
+        _int32(self.ref_counts, "ref_counts", None, at)
+        return _CPageTable(B, self.block_table.shape[1], self.ref_counts.shape[0], _ptr(self.block_table), _ptr(self.seq_lens),
+                           _ptr(self.page_counts), _ptr(self.ref_counts))
 
 
 def _here(t: torch.Tensor, name: str, device: Optional[int] = None) -> int:

@@ -95,3 +95,25 @@ def test_tree_attention_looks_at_the_layer_in_every_call(calls, change):
     with pytest.raises(ValueError):
         tree(l)
     assert [name for name, _ in calls].count("stief_tree_attention") == 2
+
+
+TABLE_CHANGES = {
+    "fewer lengths at the same address": lambda t: setattr(t, "seq_lens", t.seq_lens[:2]),
+    "fewer counts at the same address": lambda t: setattr(t, "page_counts", t.page_counts[:2]),
+    "lengths of another type": lambda t: setattr(t, "seq_lens", t.seq_lens.view(torch.float32)),
+    "a transposed table": lambda t: t.block_table.t_(), "counts in two dimensions": lambda t: t.page_counts.resize_(3, 1),
+    "fewer lengths in place": lambda t: t.seq_lens.resize_(2), "references in two dimensions": lambda t: t.ref_counts.resize_(4, 2),
+}
+
+
+@pytest.mark.parametrize("change", TABLE_CHANGES)
+def test_page_calls_look_at_the_table_in_every_call(calls, change):
+    table = S.PageTable(i32(3, 3), i32(3), i32(3), i32(8))
+    reserve = lambda: S.stief_pages_reserve(table, 5)
+    reserve()
+    reserve()
+    assert len(calls) == 2
+    TABLE_CHANGES[change](table)
+    with pytest.raises(ValueError):
+        reserve()
+    assert len(calls) == 2
