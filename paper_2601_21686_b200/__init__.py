@@ -234,15 +234,19 @@ class PageTable:
 
     def c(self) -> _CPageTable:
         # every tensor is looked at in every call: one may have been replaced by another of the same address
-        B = self.block_table.shape[0]
-        at = _int32(self.block_table, "block_table")
-        if self.block_table.dim() != 2 or self.ref_counts.dim() != 1:
+        bt, lens, counts, refs = self.block_table, self.seq_lens, self.page_counts, self.ref_counts
+        at, size = _int32(bt, "block_table"), bt.shape
+        if len(size) != 2 or refs.dim() != 1:
             raise ValueError("block_table [B, max_pages] and ref_counts [num_pages] are expected")
-        for t, name in ((self.seq_lens, "seq_lens"), (self.page_counts, "page_counts")):
-            _int32(t, name, (B,), at)
-        _int32(self.ref_counts, "ref_counts", None, at)
-        return _CPageTable(B, self.block_table.shape[1], self.ref_counts.shape[0], _ptr(self.block_table), _ptr(self.seq_lens),
-                           _ptr(self.page_counts), _ptr(self.ref_counts))
+        B, width = size
+        _int32(lens, "seq_lens", (B,), at)
+        _int32(counts, "page_counts", (B,), at)
+        _int32(refs, "ref_counts", None, at)
+        key = (B, width, refs.size(0), bt.data_ptr(), lens.data_ptr(), counts.data_ptr(), refs.data_ptr())
+        kept = self.__dict__.get("_c")                          # the same values in a C structure
+        if kept is None or kept[0] != key:
+            kept = self.__dict__["_c"] = (key, _CPageTable(*key))
+        return kept[1]
 
 
 def _here(t: torch.Tensor, name: str, device: Optional[int] = None) -> int:
@@ -498,10 +502,12 @@ def _layer_pools(layer: Layer, device: int):
     """The pools have to be what the layer says of them: the kernels compute every row's address from its ranks and heads."""
     if not isinstance(layer, Layer):
         raise ValueError("a Layer is expected (a quantised cache has no such call)")
+    pages, Hkv = layer.k_pool.size(0), layer.Hkv
     for pool, r, name in ((layer.k_pool, layer.r_k, "k_pool"), (layer.v_pool, layer.r_v, "v_pool")):
-        if pool.dtype is not torch.bfloat16 or not pool.is_contiguous() or pool.shape != (layer.num_pages, layer.Hkv, PAGE, r):
+        if pool.dtype is not torch.bfloat16 or not pool.is_contiguous() or pool.shape != (pages, Hkv, PAGE, r):
             raise ValueError(f"{name} must be contiguous bf16 [num_pages, Hkv, {PAGE}, {r}]")
-        _here(pool, name, device)
+        if pool.get_device() != device:
+            _here(pool, name, device)
 
 
 def _cache_tensors(layer: Layer, device: int):
@@ -511,9 +517,11 @@ def _cache_tensors(layer: Layer, device: int):
     for U, r, name in ((layer.U_k, layer.r_k, "U_k"), (layer.U_v, layer.r_v, "U_v")):
         if U is None:
             continue
-        if U.dtype is not torch.bfloat16 or U.shape[1:] != (D_HEAD, r) or U.shape[0] not in (1, layer.Hkv) or U.stride(1) != r or U.stride(2) != 1:
+        size, stride = U.shape, U.stride()
+        if U.dtype is not torch.bfloat16 or (size != (layer.Hkv, D_HEAD, r) and size != (1, D_HEAD, r)) or stride[1] != r or stride[2] != 1:
             raise ValueError(f"{name} must be bf16 [Hkv or 1, {D_HEAD}, {r}] with contiguous rows")
-        _here(U, name, device)
+        if U.get_device() != device:
+            _here(U, name, device)
 
 
 def stief_tree_workspace_bytes(B: int, n_q: int, Hq: int, Hkv: int, r_v: int) -> int:
