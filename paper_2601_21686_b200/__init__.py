@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import weakref
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -626,20 +627,34 @@ def _page_tensors(layer):
     return (layer.k_pool, layer.v_pool)
 
 
+def _unchanged(layers, kept) -> Optional[ctypes.Array]:
+    """The kept C array if the layers hold the tensors and sizes that it was built from.  Tensors are known by weak references
+    (the array must not keep a replaced cache allocated), and since one can be resized or pointed elsewhere in place, by
+    address and size as well."""
+    built_from, addresses, sizes, arr = kept
+    if len(built_from) != len(layers):
+        return None
+    tensors = []
+    for l, (k, v, rk, rv, Hkv) in zip(layers, built_from):
+        d = l.__dict__
+        kp, vp = d.get("k_pool"), d.get("v_pool")
+        if kp is None or kp is not k() or vp is not v() or d["r_k"] != rk or d["r_v"] != rv or d["Hkv"] != Hkv:
+            return None
+        tensors += (kp, vp)
+    same = list(map(torch.Tensor.data_ptr, tensors)) == addresses and list(map(torch.Tensor.numel, tensors)) == sizes
+    return arr if same else None
+
+
 def _descriptors(layers, device: int, slot: str, make):
     """The C array that ``make`` builds from the layers, kept with the first layer and built again when any layer holds other
     tensors, or other sizes, than it was built from (marshalling 32 layers takes longer than moving their rows)."""
     if not layers:
         return make()
     kept = layers[0].__dict__.get(slot)
-    if kept is not None and kept[0] == device and len(kept[1]) == len(layers):
-        for l, (same, k, v, rk, rv, Hkv) in zip(layers, kept[1]):
-            d = l.__dict__
-            if l is not same or d["k_pool"] is not k or d["v_pool"] is not v or d["r_k"] != rk or d["r_v"] != rv or d["Hkv"] != Hkv:
-                break
-        else:
-            if list(map(torch.Tensor.data_ptr, kept[2])) == kept[3]:
-                return kept[4]
+    if kept is not None and kept[0] == device:
+        arr = _unchanged(layers, kept[1])
+        if arr is not None:
+            return arr
     tensors = [t for l in layers for t in _page_tensors(l)]
     for t in tensors:
         if not t.is_contiguous() or t.shape[0] != tensors[0].shape[0]:
@@ -647,7 +662,8 @@ def _descriptors(layers, device: int, slot: str, make):
         _here(t, "pool", device)
     arr = make()
     if all(type(l) is Layer for l in layers):
-        layers[0].__dict__[slot] = (device, [(l, l.k_pool, l.v_pool, l.r_k, l.r_v, l.Hkv) for l in layers], tensors, [t.data_ptr() for t in tensors], arr)
+        layers[0].__dict__[slot] = (device, ([(weakref.ref(l.k_pool), weakref.ref(l.v_pool), l.r_k, l.r_v, l.Hkv) for l in layers],
+                                             [t.data_ptr() for t in tensors], [t.numel() for t in tensors], arr))
     return arr
 
 
@@ -657,7 +673,7 @@ def _page_pools(layers, device: int):
         tensors = [t for l in layers for t in _page_tensors(l)]
         return (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
     arr = _descriptors(layers, device, "_pools", make)
-    return arr, sum(2 if type(l) is Layer else 3 for l in layers), layers[0].num_pages if layers else 0
+    return arr, sum(3 if isinstance(l, QLayer) else 2 for l in layers), layers[0].num_pages if layers else 0
 
 
 def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:

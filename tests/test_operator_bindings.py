@@ -1,5 +1,8 @@
 """CPU-only checks of what the Python binding lets through to the tree, prompt and page calls: the library is replaced by a
 recorder, so a call that should have been refused is seen and never runs."""
+import gc
+import weakref
+
 import pytest
 import torch
 
@@ -117,3 +120,66 @@ def test_page_calls_look_at_the_table_in_every_call(calls, change):
     with pytest.raises(ValueError):
         reserve()
     assert len(calls) == 2
+
+
+def fork(layers, table):
+    S.stief_pages_fork(table, layers, i32(3), torch.zeros(1024, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("call", ["accept", "fork"])
+def test_kept_descriptors_own_no_cache_memory(calls, call):
+    """What is kept of a call must not hold the pools: a cache that is replaced is freed at once, without the collector."""
+    table = S.PageTable(i32(3, 3), i32(3), i32(3), i32(4))
+    run = (lambda ls: accept(ls)) if call == "accept" else (lambda ls: fork(ls, table))
+    gc.collect()
+    gc.disable()
+    try:
+        layers = [layer() for _ in range(3)]
+        run(layers)
+        tree(layers[1])
+        old = [weakref.ref(layers[1].k_pool), weakref.ref(layers[0].v_pool)]
+        layers[1].k_pool, layers[0].v_pool = torch.zeros(4, 2, 64, 64, dtype=BF), torch.zeros(4, 2, 64, 64, dtype=BF)
+        assert [r() for r in old] == [None, None]
+        run(layers)
+        every = [weakref.ref(x) for l in layers for x in (l, l.k_pool, l.v_pool, l.U_k)]
+        del layers
+        assert all(r() is None for r in every)
+    finally:
+        gc.enable()
+
+
+def pools_of(call, calls):
+    """Addresses that the last call was given."""
+    name, args = calls[-1]
+    if call == "accept":
+        return [p for l in args[0] for p in (l.k_pool, l.v_pool)]
+    return [p.base for p in args[1]]
+
+
+@pytest.mark.parametrize("call", ["accept", "fork"])
+def test_kept_descriptors_follow_every_change(calls, call):
+    table = S.PageTable(i32(3, 3), i32(3), i32(3), i32(4))
+    run = (lambda ls: accept(ls)) if call == "accept" else (lambda ls: fork(ls, table))
+    layers = [layer() for _ in range(3)]
+    now = lambda: [t.data_ptr() for l in layers for t in (l.k_pool, l.v_pool)]
+    for change in (lambda: None, lambda: setattr(layers[2], "k_pool", layers[2].k_pool.clone()), lambda: layers[1].v_pool.set_(layers[1].v_pool.clone()),
+                   lambda: layers.pop(), lambda: layers.reverse(), lambda: layers.append(layer()), lambda: layers.__setitem__(1, layer())):
+        change()
+        for _ in range(2):
+            run(layers)
+            assert pools_of(call, calls) == now()
+    seen = len(calls)
+    layers[1].k_pool.resize_(3, 2, 64, 64)                     # fewer pages at the same address
+    with pytest.raises(ValueError):
+        run(layers)
+    assert len(calls) == seen
+
+
+def test_pools_of_a_derived_layer_are_counted_once_each(calls):
+    class Named(S.Layer):
+        pass
+
+    l = layer()
+    layers = [l, Named(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k, l.U_v, l.k_pool.clone(), l.v_pool.clone())]
+    fork(layers, S.PageTable(i32(3, 3), i32(3), i32(3), i32(4)))
+    assert calls[-1][1][2] == 4 and len(calls[-1][1][1]) == 4
