@@ -115,7 +115,10 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   // what the partition says, found again from the lengths while the kernel before still runs
   const Seq s = sequence(a, b);
   const int live = min(kSmallRows, s.n * G - r0);
-  if (live <= 0) return;
+  if (live <= 0) {                                              // a grid none of whose blocks waited could end before the kernel
+    grid_dependency_wait();                                     // ahead of it, which reads lengths and counts: what follows on
+    return;                                                     // the stream may write them
+  }
   int before = 0, all = 0;                                      // running cost up to this sequence, and of all
   for (int i = tid; i < a.Bt.B; i += kJoinThreads) {
     const int cost = sequence_cost(a, sequence(a, i));

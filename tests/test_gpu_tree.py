@@ -163,6 +163,28 @@ def test_many_blocks_per_segment_at_every_rank_pair(r_k, r_v, n):
     assert int(c.status) == 0
 
 
+def test_a_call_without_any_node_and_the_next_on_its_stream():
+    """Such a call ends in stream order like any other: the counts that the next call reads may be written behind it."""
+    c = TreeCase(67, [9000, 300, 40, 0], 16, [16, 3, 0, 1], Hq=32, Hkv=8)
+    counts, none = c.n_nodes.clone(), torch.zeros_like(c.n_nodes)
+    want, want_lse = c.run()
+    c.check(want, want_lse)
+    for _ in range(20):
+        c.n_nodes.copy_(none)
+        out, lse = c.run()
+        c.n_nodes.copy_(counts)
+        again, again_lse = c.run()
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
+        assert torch.equal(again.view(torch.int16), want.view(torch.int16)) and torch.equal(again_lse.view(torch.int32), want_lse.view(torch.int32))
+    lens = c.batch.seq_lens.clone()
+    c.batch.seq_lens.fill_(-1)                                 # nothing to do because everything is refused
+    out, _ = c.run()
+    c.batch.seq_lens.copy_(lens)
+    again, _ = c.run()
+    assert torch.isnan(out).all() and torch.equal(again.view(torch.int16), want.view(torch.int16))
+    assert int(c.status) == S.STIEF_ERR_BOUNDS
+
+
 def test_many_sequences():
     lens = [(37 * i) % 450 for i in range(200)]
     c = TreeCase(5, lens, 6, [(i % 7) for i in range(200)], Hq=8, Hkv=2)
