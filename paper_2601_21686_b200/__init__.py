@@ -261,7 +261,7 @@ def _here(t: torch.Tensor, name: str, device: Optional[int] = None) -> int:
 def _int32(t: torch.Tensor, name: str, shape=None, device: Optional[int] = None) -> int:
     if t.dtype is not torch.int32 or not t.is_contiguous() or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must be a contiguous int32 tensor" + (f" of shape {tuple(shape)}" if shape is not None else ""))
-    return _here(t, name, device)
+    return device if t.get_device() == device else _here(t, name, device)
 
 
 def _status(t: Optional[torch.Tensor], device: int) -> Optional[int]:
@@ -673,7 +673,7 @@ def _page_pools(layers, device: int):
         tensors = [t for l in layers for t in _page_tensors(l)]
         return (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
     arr = _descriptors(layers, device, "_pools", make)
-    return arr, sum(3 if isinstance(l, QLayer) else 2 for l in layers), layers[0].num_pages if layers else 0
+    return arr, len(arr) if layers else 0, layers[0].num_pages if layers else 0
 
 
 def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:
