@@ -561,8 +561,8 @@ def stief_tree_attention(layer: Layer, batch: Batch, q: torch.Tensor, tree_mask:
     _int32(batch.block_table, "block_table", None, at)
     _int32(batch.seq_lens, "seq_lens", (B,), at)
     _cache_tensors(layer, at)
-    q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (max(qs[1], Hq * d_q), max(os_[1], Hq * d_out))       # an extent of 1 may carry any stride
-    q_b, o_b = (qs[0], os_[0]) if B > 1 else (max(qs[0], q_t), max(os_[0], o_t))
+    q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (Hq * d_q, Hq * d_out)        # an extent of 1 may carry any stride: the call gets one that fits
+    q_b, o_b = (qs[0], os_[0]) if B > 1 else (q_t, o_t)
     _check(lib().stief_tree_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(n_nodes),
                                       tree_mask.data_ptr(), tree_mask.shape[2], workspace.data_ptr(),
                                       workspace.numel() * workspace.element_size(), out.data_ptr(), o_b, o_t, _ptr(out_lse), flags,
@@ -609,7 +609,7 @@ def stief_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu
         if t.dtype is not torch.bfloat16 or t.shape != (total, heads, D_HEAD) or st[2] != 1 or (st[1] != D_HEAD and heads > 1):
             raise ValueError(f"{name} must be bf16 [{total}, {heads}, {D_HEAD}] with contiguous heads and elements")
         _here(t, name, at)
-        args += [t.data_ptr(), st[0] if total > 1 else max(st[0], heads * D_HEAD)]
+        args += [t.data_ptr(), st[0] if total > 1 else heads * D_HEAD]       # an extent of 1 may carry any stride
     _int32(cu_seqlens, "cu_seqlens", None, at)
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
         raise ValueError("cu_seqlens must be [B + 1]")

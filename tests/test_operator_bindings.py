@@ -183,3 +183,22 @@ def test_pools_of_a_derived_layer_are_counted_once_each(calls):
     layers = [l, Named(l.Hq, l.Hkv, l.r_k, l.r_v, l.U_k, l.U_v, l.k_pool.clone(), l.v_pool.clone())]
     fork(layers, S.PageTable(i32(3, 3), i32(3), i32(3), i32(4)))
     assert calls[-1][1][2] == 4 and len(calls[-1][1][1]) == 4
+
+
+@pytest.mark.parametrize("stride", [1, 1029, 1 << 40])
+def test_an_extent_of_one_may_carry_any_stride(calls, stride):
+    l, row = layer(), 8 * 128
+    storage = torch.zeros(2 * 4 * row + 64, dtype=BF)
+    ws, batch = torch.zeros(16, dtype=torch.uint8), S.Batch(i32(2, 2), i32(2))
+    q = storage.as_strided((2, 1, 8, 128), (row, stride, 128, 1))
+    S.stief_tree_attention(l, batch, q, i32(2, 1, 1), ws, q)
+    args = calls[-1][1]
+    assert args[3:5] == (row, row) and args[12:14] == (row, row)
+    q = storage.as_strided((1, 3, 8, 128), (stride, row, 128, 1))
+    S.stief_tree_attention(l, S.Batch(i32(1, 2), i32(1)), q, i32(1, 3, 1), ws, q)
+    args = calls[-1][1]
+    assert args[3:5] == (row, row) and args[12:14] == (row, row)
+    q = storage.as_strided((1, 8, 128), (stride, 128, 1))
+    S.stief_prompt_attention(q, q, q, i32(2), q)
+    args = calls[-1][1]
+    assert [args[i] for i in (6, 8, 10, 12)] == [row] * 4
