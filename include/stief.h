@@ -392,7 +392,8 @@ int stief_mq_attention(const stief_layer* layer, const stief_batch* batch, const
  * itself, for a tree; any set of nodes is allowed).  seq_lens counts the context only; node j's compressed row sits at
  * position seq_lens[b] + j (stief_append_chunk with ends_at_len = 0 puts it there, and the pages must be assigned).  A row
  * that sees nothing (empty context and empty mask row) gives zeros and lse = -inf.
- *   q          device bf16 [B][n_q][Hq][d_q], strides as in stief_mq_attention
+ *   q          device bf16 [B][n_q][Hq][d_q], strides as in stief_mq_attention, here in either order (a batch stride below the token
+ *              stride: token-major tensors)
  *   n_q        nodes per sequence in q, the mask and out (1 .. STIEF_TREE_MAX_NODES)
  *   n_nodes    device int32 [B] or NULL: how many of them are real (clamped to 0 .. n_q); rows behind are neither read,
  *              computed nor written, and nobody attends them.  NULL = n_q everywhere

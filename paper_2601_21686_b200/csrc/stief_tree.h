@@ -70,8 +70,8 @@ inline int check(const stief_layer* l, const stief_batch* batch, const uint16_t*
   auto rank_ok = [](int r) { return r == 32 || r == 48 || r == 64 || r == 96 || r == 128; };
   if (l->d != kD || !rank_ok(l->r_k) || !rank_ok(l->r_v) || n_q > kMaxNodes) return STIEF_ERR_UNSUPPORTED;
   const long long q_row = (long long)l->Hq * (l->U_k ? kD : l->r_k), o_row = (long long)l->Hq * (l->U_v ? kD : l->r_v);
-  if (q_stride_t < q_row || q_stride_b < q_stride_t || q_stride_t % 8 || q_stride_b % 8 || out_stride_t < o_row ||
-      out_stride_b < out_stride_t || out_stride_t % 8 || out_stride_b % 8)
+  if (q_stride_t < q_row || q_stride_b < q_row || q_stride_t % 8 || q_stride_b % 8 || out_stride_t < o_row || out_stride_b < o_row ||
+      out_stride_t % 8 || out_stride_b % 8)                     // sequences or tokens outermost
     return STIEF_ERR_INVALID_ARG;
   if (!host::aligned(q, 16) || !host::aligned(out, 16) || !host::aligned(l->k_pool, 128) || !host::aligned(l->v_pool, 128) ||
       (l->U_k && !host::aligned(l->U_k, 16)) || (l->U_v && !host::aligned(l->U_v, 16)) || l->uk_head_stride % 8 ||

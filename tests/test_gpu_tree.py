@@ -163,6 +163,19 @@ def test_many_blocks_per_segment_at_every_rank_pair(r_k, r_v, n):
     assert int(c.status) == 0
 
 
+def test_token_major_queries_and_outputs():
+    c = TreeCase(71, [400, 90, 1000], 21, [21, 8, 1])
+    want, _ = c.run()
+    B, n, Hq, d = c.q.shape
+    out = torch.full((n, B, Hq, 128), NAN, dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    c.run(q=c.q.transpose(0, 1).contiguous().transpose(0, 1), out=out)
+    c.check(out)
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(want))
+    c = TreeCase(72, [400, 90, 1000], 1)                       # one node each: [1, B, ...] seen as [B, 1, ...]
+    c.check(*c.run(q=c.q.transpose(0, 1).contiguous().transpose(0, 1)))
+    assert int(c.status) == 0
+
+
 def test_a_call_without_any_node_and_the_next_on_its_stream():
     """Such a call ends in stream order like any other: the counts that the next call reads may be written behind it."""
     c = TreeCase(67, [9000, 300, 40, 0], 16, [16, 3, 0, 1], Hq=32, Hkv=8)
