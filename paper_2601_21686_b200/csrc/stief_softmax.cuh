@@ -48,6 +48,22 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// Exponents are (s - m) c for scores s and a row's reference m, as one fma(s, c, -(m c)).  That rounds m c: by up to 2^-15 where
+// it is at most kFarLog2, but by more than an exponent holds from about 2^32 on, where rows came out as NaN.  Rows with larger
+// references take s - m first, which is exact next to the maximum, and nothing is left for the fma to add.
+constexpr float kFarLog2 = 1024.f;
+// For a warp of which some rows lie beyond: their scores less the reference, in place; returns what the fma adds
+template <int N>
+__device__ __forceinline__ float near_scores(float* s, float m, float c) {
+  const bool far = fabsf(m * c) > kFarLog2;
+  const float shift = far ? m : 0.f;                            // a row's bits do not depend on its neighbours: they subtract 0
+  if (__any_sync(0xffffffffu, far)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] -= shift;
+  }
+  return far ? 0.f : -m * c;
+}
+
 // 16 fp32 values of a row -> 8 packed bf16 words
 __device__ __forceinline__ void pack16(const uint32_t (&v)[16], float scale, uint32_t (&w)[8]) {
 #pragma unroll
