@@ -408,13 +408,17 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
       if (lane == 0) mbar_arrive(bar);
     };
     walk.start(a, ps);
-    for (Item w = walk.next(a, ps); w.np[0] > 0; w = walk.next(a, ps)) {       // every item has a tile 0
+    Item w = walk.next(a, ps);
+    while (w.valid) {
+      const Item nx = walk.next(a, ps);
       const int item0 = item;
       item += 2 * max(w.np[0], w.np[1]);
-      const int np = t ? w.np[1] : w.np[0], tok0 = (np - 1) * kRows, len = w.len;
+      const int np = t ? w.np[1] : w.np[0], tok0 = t ? w.tok0[1] : w.tok0[0], len = w.len;
+      w = nx;
       if (np == 0) continue;
       const bool warp_live = tok0 + 32 * q4 < len;
       float m_ref = 0.f, l = 0.f;
+      float c_row = c;                                          // of the row's exponents
       for (int j = 0; j < np; ++j, ++n) {
         const int p0 = j * kRows;
         const bool diag = j == np - 1;
@@ -458,27 +462,23 @@ prompt_attention_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_co
         if (j == 0) {
           m_ref = fmaxf(mx, -FLT_MAX);
           l = 0.f;
-        }
-        const bool grown = (mx - m_ref) * c > kRescaleLog2;     // (never in the first block)
-        float neg = -m_ref * c;
-        if (__any_sync(0xffffffffu, grown || fabsf(neg) > kFarLog2)) {
-          if (__any_sync(0xffffffffu, grown)) {
-            const float f = grown ? fast_exp2((m_ref - mx) * c) : 1.0f;     // a row's bits do not depend on its neighbours
-            if (grown) m_ref = mx;
-            l *= f;
+          c_row = exponent_scale(m_ref, c);
+        } else if (const bool grown = (mx - m_ref) * c > kRescaleLog2; __any_sync(0xffffffffu, grown)) {
+          const float f = grown ? reference_weight(m_ref, mx, c) : 1.0f;    // a row's bits do not depend on its neighbours
+          if (grown) m_ref = mx;
+          c_row = exponent_scale(m_ref, c);
+          l *= f;
 #pragma unroll 1
-            for (int c0 = 0; c0 < kD; c0 += 16) {
-              uint32_t v[16];
-              tmem_ld16(t_o + c0, v);
-              tmem_ld_wait();
+          for (int c0 = 0; c0 < kD; c0 += 16) {
+            uint32_t v[16];
+            tmem_ld16(t_o + c0, v);
+            tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-              tmem_st16(t_o + c0, v);
-            }
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_st16(t_o + c0, v);
           }
-          neg = near_scores<128>(s, m_ref, c);
         }
-        const uint64_t c2 = pack2(c, c), neg2 = pack2(neg, neg);
+        const uint64_t c2 = pack2(c_row, c_row), neg2 = pack2(-m_ref * c_row, -m_ref * c_row);
         uint64_t sum[2] = {0ull, 0ull};                         // pairs of +0
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                           // 64 columns: probabilities as bf16 pairs over the scores

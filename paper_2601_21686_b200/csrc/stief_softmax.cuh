@@ -48,20 +48,17 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
-// Exponents are (s - m) c for scores s and a row's reference m, as one fma(s, c, -(m c)).  That rounds m c: by up to 2^-15 where
-// it is at most kFarLog2, but by more than an exponent holds from about 2^32 on, where rows came out as NaN.  Rows with larger
-// references take s - m first, which is exact next to the maximum, and nothing is left for the fma to add.
-constexpr float kFarLog2 = 1024.f;
-// For a warp of which some rows lie beyond: their scores less the reference, in place; returns what the fma adds
-template <int N>
-__device__ __forceinline__ float near_scores(float* s, float m, float c) {
-  const bool far = fabsf(m * c) > kFarLog2;
-  const float shift = far ? m : 0.f;                            // a row's bits do not depend on its neighbours: they subtract 0
-  if (__any_sync(0xffffffffu, far)) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) s[i] -= shift;
-  }
-  return far ? 0.f : -m * c;
+// Exponents are (s - m) c for scores s and a row's reference m, as one fma(s, c, -(m c)).  That rounds m c, which does no harm as
+// long as it is the rounded product that counts as the reference (below, and in the row's log-sum-exp): up to kFarScore it
+// moves the exponents of a row by at most 16, all alike.  Much beyond, it would be more than an exponent holds.  But there
+// neighbouring scores lie at least 256 apart, so that all but the largest weigh nothing: any factor near c will do, and with a
+// power of two m c is exact.
+constexpr float kFarScore = 4294967296.f;                       // 2^32
+__device__ __forceinline__ float exponent_scale(float m, float c) { return fabsf(m) > kFarScore ? 0.125f : c; }
+// 2^((m - M) c): what a sum with reference m counts for next to one with a larger reference, M
+__device__ __forceinline__ float reference_weight(float m, float M, float c) {
+  const float cM = exponent_scale(M, c);
+  return fast_exp2(__fsub_rn(__fmul_rn(m, cM), __fmul_rn(M, cM)));
 }
 
 // 16 fp32 values of a row -> 8 packed bf16 words
