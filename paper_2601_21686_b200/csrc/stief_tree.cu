@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   };
   grid_dependency_wait();
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + at;
+  const float c = kLog2e * rsqrtf((float)kD);
   float M = -INFINITY;
   for (int p = grp; p < parts; p += kGroups) {
     bool there;
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
       bool there;
       const int slot = part_slot(p0 + p, there);
       const float2 x = ml[(size_t)slot * kRows];
-      const float w = there ? fast_exp2(x.x - M) : 0.f;
+      const float w = there ? reference_weight(x.x, M, c) : 0.f;
       if (r == 0) slot_of[p] = slot;
       den = fmaf(x.y, w, den);
       weight[p][r] = w;
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kJoinThreads) combine_kernel(const Args a) {
   if (a.out_lse && grp == 0 && r < live) {
     int node, hq;
     where(r, node, hq);
-    a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = den > 0.f ? kLn2 * (M + log2f(den)) : -INFINITY;
+    a.out_lse[((size_t)b * a.n_q + node) * a.L.Hq + hq] = den > 0.f ? kLn2 * (__fmul_rn(M, c) + log2f(den)) : -INFINITY;
   }
   __syncthreads();
   if (share_i == 0) {

@@ -38,6 +38,8 @@
 // warp's time), waits tested ahead of the work before them (64 nodes 117 to 120 against 117).
 #pragma once
 
+#include <cfloat>
+
 #include "stief_softmax.cuh"
 #include "stief_tree.h"
 #include "stief_umma.cuh"
@@ -516,10 +518,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           tc_fence_after();
         }
         if (s_i == 0) {
-          m_ref = fmaxf(mx, -1e30f);                            // a row that sees nothing here keeps p = 0 and l = 0
+          m_ref = fmaxf(mx, -FLT_MAX);                          // a row that sees nothing here keeps p = 0 and l = 0
           l = 0.f;
         } else if (const bool grown = (mx - m_ref) * c > kRescaleLog2; __any_sync(0xffffffffu, grown)) {
-          const float f = grown ? fast_exp2((m_ref - mx) * c) : 1.0f;       // a row's bits do not depend on its neighbours
+          const float f = grown ? reference_weight(m_ref, mx, c) : 1.0f;    // a row's bits do not depend on its neighbours
           if (grown) m_ref = mx;
           l *= f;
 #pragma unroll 1
@@ -538,7 +540,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           for (int w = 0; w < 64; w += 16)
             if (w / kWords != replica) tmem_st16(t_p + w, zero);
         }
-        const uint64_t c2 = pack2(c, c), neg2 = pack2(-m_ref * c, -m_ref * c);
+        const float c_row = exponent_scale(m_ref, c);
+        const uint64_t c2 = pack2(c_row, c_row), neg2 = pack2(-m_ref * c_row, -m_ref * c_row);
         uint64_t sum[2] = {0ull, 0ull};                         // pairs of +0
 #pragma unroll
         for (int q = 0; q < kCols / 32; ++q) {                  // probabilities as bf16 pairs
@@ -605,7 +608,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const size_t slot = (size_t)g.slot * 2 + t;
       float4* po = reinterpret_cast<float4*>(a.part_o) + slot * (RV / 4) * kRows + row;
       float2* pml = reinterpret_cast<float2*>(a.part_ml) + slot * kRows + row;
-      float weight = 1.0f, top = m_ref * c, total_l = l;
+      float weight = 1.0f, top = m_ref, total_l = l;
       if (RV <= 64 && g.replicas > 1) {                         // a row's copies are joined here, 16 channels at a time
         uint8_t* join = smem + kHeadBytes + t * (kJoinBytes / 2);
         float2* copy_ml = reinterpret_cast<float2*>(join);      // [copy][row]
@@ -617,9 +620,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         total_l = 0.f;
         for (int i = 0; i < g.replicas; ++i) {
           const float2 x = copy_ml[i * wrap + row];
-          total_l = fmaf(x.y, fast_exp2(x.x - top), total_l);
+          total_l = fmaf(x.y, reference_weight(x.x, top, c), total_l);
         }
-        weight = fast_exp2(m_ref * c - top);
+        weight = reference_weight(m_ref, top, c);
 #pragma unroll 1
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16];

@@ -30,7 +30,7 @@ struct Args {
   int q_regions;                           // Q' regions in shared memory: value and remainder, for each tile where a unit may have over 128 rows
   __nv_bfloat16* qp;                       // [2][B][Hkv][n_q G][r_k]  projected queries and their remainders, rows (node, head of the group)
   float* part_o;                           // [(n_cta + units)][2 tiles][r_v / 4][128 lanes] float4
-  float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (base 2), sum
+  float* part_ml;                          // [(n_cta + units)][2 tiles][128] float2: reference (a score), sum
 };
 
 // Workspace: a segment is found by (CTA + unit), so there are at most n_cta + units of them

@@ -295,6 +295,41 @@ def test_growing_scores_rescale():
     assert int(c.status) == 0
 
 
+@pytest.mark.parametrize("exponent", [-9, -2, 4, 8, 13, 16, 19, 24, 28, 30, 31, 60, 100, 120])
+@pytest.mark.parametrize("r_v,n,lens", [(64, 3, [9000, 0, 5]), (64, 12, [700, 1]), (128, 8, [3000, 90]), (48, 64, [2000, 0])])
+def test_scores_far_from_zero(exponent, r_v, n, lens):
+    """Scores that are exact in fp32 (19 bits), of sizes up to 2^125 and either sign: nothing but the rounding of probabilities and
+    output remains.  In large ones the largest score's ties share the row."""
+    c = TreeCase(83 + exponent, lens, n, r_v=r_v, fold_k=True, fold_v=True)
+    keys = [torch.zeros_like(K) for K in c.K]
+    for b, K in enumerate(keys):
+        for i in range(2):
+            K[..., i] = (1 + torch.randint(0, 64, K.shape[:2], generator=torch.Generator().manual_seed(b + n + 7 * i)).cuda() / 64).to(torch.bfloat16)
+        for i in range((len(K) + 63) // 64):
+            part = K[64 * i:64 * i + 64].transpose(0, 1)
+            c.layer.k_pool[c.batch.block_table[b, i], :, :part.shape[1]] = part
+    c.q.zero_()
+    sign = torch.tensor([1.0, -1.0], device="cuda").repeat(c.layer.Hq // 2)
+    c.q[..., 0] = (sign * 2.0 ** exponent * 4).to(torch.bfloat16)          # odd heads: all scores far below zero
+    c.q[..., 1] = c.q[..., 0] * 2.0 ** -12                     # and scores close to one another
+    out, lse = c.run()
+    assert int(c.status) == 0
+    G = c.layer.Hq // c.layer.Hkv
+    for b, (ctx, m) in enumerate(zip(c.lens, c.counts)):
+        for g in range(c.layer.Hq):
+            s = c.q[b, :m, g].double() @ keys[b][:, g // G].double().T / math.sqrt(128)
+            s[:, ctx:].masked_fill_(~c.seen[b, :m, :m], -math.inf)
+            V = c.V[b][:, g // G].double()
+            want_lse = torch.logsumexp(s, -1)
+            p = torch.softmax(s, -1)                           # (the lse of far scores has lost the number of ties)
+            o, size = p @ V, p @ V.abs()
+            # what the rounding of a reference does to its row's exponents, it does to all alike
+            bound = (HALF + 3e-4) * size + HALF * o.abs() + 1e-6
+            err = (out[b, :m, g].double() - o).abs()
+            assert torch.isfinite(err).all() and (err <= bound).all(), f"sequence {b}, head {g}: {(err / bound).max().item():.2f} of the bound"
+            assert ((lse[b, :m, g].double() - want_lse).abs() <= 2e-4 + 1e-6 * want_lse.abs()).all()
+
+
 def test_offsets_beyond_32_bits():
     c = TreeCase(43, [150], 8, Hq=8, Hkv=8, r_k=128, r_v=128)
     num_pages = 33000                                          # 2^31 elements are 32768 pages of 8 heads x 64 x 128
