@@ -485,6 +485,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       // its copy's half or quarter, P being zero elsewhere.
       auto block = [&](auto cols_tag, int s_i, int p0) {
         constexpr int kCols = decltype(cols_tag)::value, kWords = kCols / 2;
+        static_assert(kCols == 128 || kOwnP, "copies have P's own columns");
         const int col0 = kCols == 128 ? 0 : replica * kCols;
         uint32_t sv[kCols];
         float* s = reinterpret_cast<float*>(sv);
@@ -534,7 +535,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             tmem_st16(t_o + c0, v);
           }
         }
-        if (kCols < 128 && (!kOwnP || s_i == 0)) {              // the other copies' columns: once, or wherever S has been
+        if (kCols < 128 && s_i == 0) {                          // the other copies' columns, in P's own: once
           const uint32_t zero[16] = {};
 #pragma unroll 1
           for (int w = 0; w < 64; w += 16)
@@ -555,7 +556,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             pk[i] = pack_bf16(e0, e1);
           }
           tmem_st16(t_p + col0 / 2 + 16 * q, pk);
-          if (kCols == 128 && q == 1 && !kOwnP) {               // the first page's may be used already
+          if (!kOwnP && q == 1) {                               // the first page's may be used already
             tmem_st_wait();
             tc_fence_before();
             arrive_warp(p_full(t, 0));
@@ -563,7 +564,6 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         tmem_st_wait();
         tc_fence_before();
-        if (kCols < 128 && !kOwnP) arrive_warp(p_full(t, 0));
         arrive_warp(p_full(t, 1));
         float a0, a1;
         unpack2(add2(sum[0], sum[1]), a0, a1);
@@ -593,12 +593,11 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           }
           if (!kOwnP) arrive_warp(p_full(t, 0));
           arrive_warp(p_full(t, 1));
-        } else if (g.replicas == 1) {
+        } else if (!kOwnP || g.replicas == 1) {                 // copies only where r_v <= 64 (replicas_of)
           block(std::integral_constant<int, 128>{}, s_i, p0);
-        } else if (g.replicas == 2) {
-          block(std::integral_constant<int, 64>{}, s_i, p0);
-        } else {
-          block(std::integral_constant<int, 32>{}, s_i, p0);
+        } else if constexpr (kOwnP) {
+          if (g.replicas == 2) block(std::integral_constant<int, 64>{}, s_i, p0);
+          else block(std::integral_constant<int, 32>{}, s_i, p0);
         }
       }
       // ---- the segment's partial result, [slot][RV / 4][128 lanes] float4: a warp writes 512 contiguous bytes
