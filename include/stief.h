@@ -402,8 +402,9 @@ int stief_mq_attention(const stief_layer* layer, const stief_batch* batch, const
  *   workspace  device, 128-byte aligned, stief_tree_workspace_bytes(...) bytes, contents irrelevant on entry; calls that share
  *              it must not overlap on the GPU
  *   out        device bf16 [B][n_q][Hq][d_out];  out_lse optional fp32 [B][n_q][Hq];  flags must be 0
- * Any number of query heads per KV head.  The probabilities pass through bf16; q' = q U_k keeps 16 significant bits, scores,
- * sums and the mix fp32 accuracy.  A sequence whose context and nodes do not fit its block table (or exceed 2^30 positions) sets
+ * Any number of query heads per KV head.  The probabilities pass through bf16; q' = q U_k and the normalised mix that goes
+ * into U_v keep 16 significant bits, scores, sums and the accumulated mix fp32 accuracy.  Scores (q k, unscaled) have to stay
+ * within fp32's range.  A sequence whose context and nodes do not fit its block table (or exceed 2^30 positions) sets
  * STIEF_ERR_BOUNDS and is skipped.  A NaN or infinity in the cache row of a drafted node may reach rows that do not see it. */
 #define STIEF_TREE_MAX_NODES 1024
 size_t stief_tree_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t r_v);
@@ -433,7 +434,7 @@ int stief_advance_seq_lens_by(int32_t* seq_lens, const int32_t* deltas, int32_t 
  *   out        device bf16 [total_tokens][Hq][128]; rows of tokens that belong to no prompt are left as they are, and
  *              whatever such rows of q, k, v hold (NaN included) influences nothing
  *   out_lse    optional device fp32 [total_tokens][Hq]: natural-log sum-exp of each row's scaled scores
- * The probabilities pass through bf16; scores, sums and the mix are fp32.  A prompt with a negative length or outside
+ * The probabilities pass through bf16; scores (q k, unscaled, within fp32's range), sums and the mix are fp32.  A prompt with a negative length or outside
  * 0 .. total_tokens sets STIEF_ERR_BOUNDS and is skipped.  B <= 1024; flags must be 0.  A NaN or infinity in a value row
  * reaches every row of its prompt that attends it, and may reach up to 127 rows before it. */
 int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tokens, const int32_t* cu_seqlens,
@@ -445,7 +446,9 @@ int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tok
  * The other entry points only read block_table and seq_lens; these calls write them, on the device, so that a captured step
  * can take and give back pages.  Slot b of the batch holds pages block_table[b][0 .. page_counts[b]); ref_counts[p] is the
  * number of slots that hold page p, and a page is free when that is 0.  The lowest-numbered free page is always taken first,
- * for the lowest slot first.  Only full pages are ever shared, so appending never writes a page of another slot.
+ * for the lowest slot first.  Only full pages are ever shared, so appending never writes a page of another slot, as long as
+ * nobody lowers seq_lens of a slot below the end of a page that it shares (ref_counts > 1): the rows appended there would be
+ * the other slots' too.
  * Table entries at or behind page_counts[b] are left as they are.  Calls on one table must not overlap on the GPU.
  * num_pages and B * max_pages_per_seq <= 2^30. */
 typedef struct stief_page_table {

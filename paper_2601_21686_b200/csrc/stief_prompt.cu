@@ -32,9 +32,11 @@
 // The reference maximum of a row follows the true one only when that has grown by more than 2^8: the accumulator in TMEM is
 // rescaled a few times per row instead of at every block.
 //
-// Measured (32 query heads over 8, TFLOP/s of the causal half): one prompt of 16384 tokens 1.96 ms = 1121 back to back, four of
-// 4096 480 us = 1146; the card's cuBLAS rates are 1709 in a burst and 1411 sustained.  One of 8192 under the profiler: tensor pipe
-// 61 % and special-function units 62 % of their cycles, DRAM 130 MB (each input once), 38 % of the issue slots.
+// Measured (32 query heads over 8, TFLOP/s of the causal half): one prompt of 16384 tokens 1.95 to 2.00 ms = 1128 to 1100 call
+// after call, at 1616 MHz under the power limit, and 1.76 ms = 1252 in bursts of five with pauses; four of 4096 546 us = 1007 and
+// 490 us = 1122; the card's cuBLAS rates are 1709 in a burst and 1411 sustained.  One of 8192 under the profiler: tensor pipe
+// 61 % and special-function units 61 % of their cycles, DRAM 130 MB (each input once), 38 % of the issue slots.  The factor per
+// row that far scores need (stief_softmax.cuh) costs 1 to 2 %.
 #include <cfloat>
 #include <cstring>
 

@@ -26,8 +26,9 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 }
 // 2^x for a pair of x in [-125, 16] on the FMA pipe: x = n + f with n = rint(x) (the 1.5 * 2^23 trick leaves n in the low
 // mantissa bits of t), 2^f by a cubic fitted to [-0.5, 0.5] (relative error 7.5e-5, far below the bf16 rounding of
-// the probabilities), 2^n by adding n to the exponent field.  The special-function pipe does 16 ex2 per clock and SM,
-// which at 64 of them per score row and page is this kernel's tightest unit; a quarter of the exponentials go here.
+// the probabilities), 2^n by adding n to the exponent field.  For the multi-query kernel (stief_mq.cuh): the special-function pipe
+// does 16 ex2 per clock and SM, which at 64 of them per score row and page is its tightest unit, and a quarter of them go here.
+// The prompt and tree kernels use no share of it: they were slower with one.
 __device__ __forceinline__ void exp2_pair_fma(uint64_t x2, float& e0, float& e1) {
   const uint64_t magic = pack2(12582912.f, 12582912.f), neg_magic = pack2(-12582912.f, -12582912.f);
   const uint64_t t = add2(x2, magic);

@@ -25,14 +25,18 @@
 // made while the softmax still works; with more P lies over S.  Everything else follows the prompt kernel (stief_prompt.cu).
 //
 // What bounds it.  Up to 64 rows the memory: 4 sequences of 32768 tokens at ranks 64/64 are 269 MB, 42 us at the measured copy
-// rate; 8 / 16 nodes of 4 heads take 69 / 71 us, of which the stream takes 45, the first scores come 7 us after the start
+// rate; 8 / 16 nodes of 4 heads take 71 / 75 us, of which the stream takes 45, the first scores come 7 us after the start
 // (projection, launch, and the first pages behind those of all other SMs), CTAs end over 8 us, and joining takes 6.  From 65
 // rows on the softmax, of which two warps share a scheduler: loading 32 rows of 128 scores, their maximum, exponentials and P
 // take 3250 cycles when the two are half a step apart (1024 each of the special-function units') and 4040 side by side; 32
-// nodes take 80 us, with three or four blocks in the ring instead of five 94 and 86, and 64 nodes, 256 rows, 116 us.
+// nodes take 87 us and 64 nodes, 256 rows, 127 us.  At ranks 128/128, 537 MB and a ring of two blocks, 16 / 64 nodes take 138 / 260 us.
+// These are bursts of five calls replayed from a graph, at 1965 MHz; without pauses the power limit brings the clock down, and
+// 8 / 16 / 32 / 64 nodes called one by one take 74 / 76 / 86 / 132 us at 1890 / 1852 / 1875 / 1777 MHz.
 //
-// An issuing warp runs beside two softmax warps and needs 100 to 180 cycles for a wait that is over already: with a barrier per
-// page and P in two halves it was the slowest part (64 nodes 136 us).  Tried and slower: a share of the exponentials as a
+// The steps to this form were timed in such bursts, before far scores (stief_softmax.cuh, 1 to 2 %), on a card where 32 / 64 nodes
+// took 80 / 117 us: with a ring of three or four blocks instead of five 32 nodes took 94 and 86.  An issuing warp runs beside two
+// softmax warps and needs 100 to 180 cycles for a wait that is over already: with a barrier per page and P in two halves it was
+// the slowest part (64 nodes 136 us).  Tried and slower: a share of the exponentials as a
 // polynomial (64 nodes 136 and 149 against 118 us for an eighth and a quarter), turns of the softmax warps themselves (145 to
 // 151 against 134 to 141), pages brought to L2 one to four blocks ahead of the ring (32 nodes 86 to 88 against 80: a fetching
 // warp's time), waits tested ahead of the work before them (64 nodes 117 to 120 against 117).
@@ -60,8 +64,8 @@ constexpr int kMaxStages = 12;
 constexpr int kTmemCols = 512;
 constexpr float kRescaleLog2 = 8.0f;
 // The looks at a barrier that nothing depends on: how many at most, and from how many blocks of a segment on the tiles are
-// paced.  Only tiles of their own rows are: with alternate blocks the ring's order already keeps them apart (paced, 32 nodes
-// 78 against 80 us, but 26 ragged 98 against 97 and 8 nodes 70 against 69).
+// paced.  Only tiles of their own rows are: with alternate blocks the ring's order already keeps them apart (paced, on the same
+// card, 32 nodes 78 against 80 us, but 26 ragged 98 against 97 and 8 nodes 70 against 69).
 constexpr int kPacePolls = 64, kPacedBlocks = 8, kLooks = 1 << 12;
 
 // Sequence b as every kernel sees it
