@@ -580,12 +580,7 @@ def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Ten
         raise ValueError("accepted must be [B, max_accept]")
     _int32(batch.block_table, "block_table", None, at)
     _int32(batch.seq_lens, "seq_lens", (B,), at)
-
-    def make():
-        for l in layers:
-            _layer_pools(l, at)
-        return (_CLayer * max(len(layers), 1))(*[l.c() for l in layers])
-    arr = _descriptors(layers, at, "_accept", make)
+    arr = _descriptors(layers, at, "_accept", _layer_pools, lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
     _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), accepted.data_ptr(), accepted.shape[1], n_accepted.data_ptr(),
                                    _status(status, at), _raw_stream(at)), "stief_tree_accept")
 
@@ -645,7 +640,15 @@ def _unchanged(layers, kept) -> Optional[ctypes.Array]:
     return arr if same else None
 
 
-def _descriptors(layers, device: int, slot: str, make):
+def _contiguous_pools(layer, device: int):
+    for t in _page_tensors(layer):
+        if not t.is_contiguous():
+            raise ValueError("pools must be contiguous")
+        if t.get_device() != device:
+            _here(t, "pool", device)
+
+
+def _descriptors(layers, device: int, slot: str, check, make):
     """The C array that ``make`` builds from the layers, kept with the first layer and built again when any layer holds other
     tensors, or other sizes, than it was built from (marshalling 32 layers takes longer than moving their rows)."""
     if not layers:
@@ -655,11 +658,11 @@ def _descriptors(layers, device: int, slot: str, make):
         arr = _unchanged(layers, kept[1])
         if arr is not None:
             return arr
+    for l in layers:
+        check(l, device)
     tensors = [t for l in layers for t in _page_tensors(l)]
-    for t in tensors:
-        if not t.is_contiguous() or t.shape[0] != tensors[0].shape[0]:
-            raise ValueError("pools must be contiguous and have the same number of pages")
-        _here(t, "pool", device)
+    if len({t.size(0) for t in tensors}) > 1:
+        raise ValueError("pools must have the same number of pages")
     arr = make()
     if all(type(l) is Layer for l in layers):
         layers[0].__dict__[slot] = (device, ([(weakref.ref(l.k_pool), weakref.ref(l.v_pool), l.r_k, l.r_v, l.Hkv) for l in layers],
@@ -672,7 +675,7 @@ def _page_pools(layers, device: int):
     def make():
         tensors = [t for l in layers for t in _page_tensors(l)]
         return (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
-    arr = _descriptors(layers, device, "_pools", make)
+    arr = _descriptors(layers, device, "_pools", _contiguous_pools, make)
     return arr, len(arr) if layers else 0, layers[0].num_pages if layers else 0
 
 
