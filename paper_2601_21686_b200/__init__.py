@@ -580,7 +580,7 @@ def stief_tree_accept(layers: Sequence[Layer], batch: Batch, accepted: torch.Ten
         raise ValueError("accepted must be [B, max_accept]")
     _int32(batch.block_table, "block_table", None, at)
     _int32(batch.seq_lens, "seq_lens", (B,), at)
-    arr = _descriptors(layers, at, "_accept", _layer_pools, lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
+    arr, _ = _descriptors(layers, at, "_accept", _layer_pools, lambda: (_CLayer * max(len(layers), 1))(*[l.c() for l in layers]))
     _check(lib().stief_tree_accept(arr, len(layers), ctypes.byref(batch.c()), accepted.data_ptr(), accepted.shape[1], n_accepted.data_ptr(),
                                    _status(status, at), _raw_stream(at)), "stief_tree_accept")
 
@@ -622,11 +622,11 @@ def _page_tensors(layer):
     return (layer.k_pool, layer.v_pool)
 
 
-def _unchanged(layers, kept) -> Optional[ctypes.Array]:
-    """The kept C array if the layers hold the tensors and sizes that it was built from.  Tensors are known by weak references
+def _unchanged(layers, kept) -> Optional[tuple]:
+    """The kept C array and number of pages if the layers hold the tensors and sizes that it was built from.  Tensors are known by weak references
     (the array must not keep a replaced cache allocated), and since one can be resized or pointed elsewhere in place, by
     address and size as well."""
-    built_from, addresses, sizes, arr = kept
+    built_from, addresses, sizes, result = kept
     if len(built_from) != len(layers):
         return None
     tensors = []
@@ -637,7 +637,7 @@ def _unchanged(layers, kept) -> Optional[ctypes.Array]:
             return None
         tensors += (kp, vp)
     same = list(map(torch.Tensor.data_ptr, tensors)) == addresses and list(map(torch.Tensor.numel, tensors)) == sizes
-    return arr if same else None
+    return result if same else None
 
 
 def _contiguous_pools(layer, device: int):
@@ -648,26 +648,28 @@ def _contiguous_pools(layer, device: int):
             _here(t, "pool", device)
 
 
-def _descriptors(layers, device: int, slot: str, check, make):
-    """The C array that ``make`` builds from the layers, kept with the first layer and built again when any layer holds other
-    tensors, or other sizes, than it was built from (marshalling 32 layers takes longer than moving their rows)."""
+def _descriptors(layers, device: int, slot: str, check, make) -> tuple:
+    """The C array that ``make`` builds from the layers, and the pages of each pool in it; kept with the first layer and built again
+    when any layer holds other tensors, or other sizes, than it was built from (marshalling 32 layers takes longer than moving
+    their rows)."""
     if not layers:
-        return make()
+        return make(), 0
     kept = layers[0].__dict__.get(slot)
     if kept is not None and kept[0] == device:
-        arr = _unchanged(layers, kept[1])
-        if arr is not None:
-            return arr
+        result = _unchanged(layers, kept[1])
+        if result is not None:
+            return result
     for l in layers:
         check(l, device)
     tensors = [t for l in layers for t in _page_tensors(l)]
-    if len({t.size(0) for t in tensors}) > 1:
+    pages = {t.size(0) for t in tensors}
+    if len(pages) > 1:
         raise ValueError("pools must have the same number of pages")
-    arr = make()
+    result = make(), pages.pop()
     if all(type(l) is Layer for l in layers):
         layers[0].__dict__[slot] = (device, ([(weakref.ref(l.k_pool), weakref.ref(l.v_pool), l.r_k, l.r_v, l.Hkv) for l in layers],
-                                             [t.data_ptr() for t in tensors], [t.numel() for t in tensors], arr))
-    return arr
+                                             [t.data_ptr() for t in tensors], [t.numel() for t in tensors], result))
+    return result
 
 
 def _page_pools(layers, device: int):
@@ -675,8 +677,8 @@ def _page_pools(layers, device: int):
     def make():
         tensors = [t for l in layers for t in _page_tensors(l)]
         return (_CPagePool * max(len(tensors), 1))(*[_CPagePool(t.data_ptr(), t.stride(0) * t.element_size()) for t in tensors])
-    arr = _descriptors(layers, device, "_pools", _contiguous_pools, make)
-    return arr, len(arr) if layers else 0, layers[0].num_pages if layers else 0
+    arr, pages = _descriptors(layers, device, "_pools", _contiguous_pools, make)
+    return arr, len(arr) if layers else 0, pages
 
 
 def stief_pages_workspace_bytes(B: int, max_pages_per_seq: int) -> int:

@@ -202,3 +202,15 @@ def test_an_extent_of_one_may_carry_any_stride(calls, stride):
     S.stief_prompt_attention(q, q, q, i32(2), q)
     args = calls[-1][1]
     assert [args[i] for i in (6, 8, 10, 12)] == [row] * 4
+
+
+def test_pages_are_counted_as_the_descriptors_were_built(calls):
+    """A pool reshaped in place to more, smaller pages: ids go by the pages that the kept descriptors know."""
+    layers, table = [layer(), layer()], S.PageTable(i32(3, 3), i32(3), i32(3), i32(4))
+    fork(layers, table)
+    layers[0].k_pool.resize_(8, 2, 32, 64)
+    table.ref_counts = i32(8)
+    with pytest.raises(ValueError):
+        fork(layers, table)
+    S.stief_pages_copy(layers, i32(2), i32(2))
+    assert calls[-1][1][2] == 4 and len(calls) == 2
