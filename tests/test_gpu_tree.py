@@ -397,6 +397,20 @@ def test_repeats_streams_and_graphs_give_the_same_bits():
     c.check(out)
 
 
+def test_two_streams_at_once():
+    cases = [TreeCase(91, [6000, 100, 900], 20, Hq=32, Hkv=8), TreeCase(92, [70, 4000], 60, Hq=8, Hkv=2, r_k=96, r_v=128)]
+    want = [c.run()[0] for c in cases]
+    outs, streams = [torch.full_like(w, NAN) for w in want], [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, o, s in zip(cases, outs, streams):
+            with torch.cuda.stream(s):
+                c.run(out=o, lse=False)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o.view(torch.int16), w.view(torch.int16)) for o, w in zip(outs, want))
+    assert all(int(c.status) == 0 for c in cases)
+
+
 def test_refusals():
     c = TreeCase(3, [100], 8)
     out = torch.empty(1, 8, 8, 128, dtype=torch.bfloat16, device="cuda")
