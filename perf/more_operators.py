@@ -179,9 +179,10 @@ def _handles(s):
     if s["op"] == "decode":
         s["workspace"] = torch.zeros(st.stief_decode_workspace_bytes(B, Hq, s["Hkv"], s["r_v"]), dtype=torch.uint8, device="cuda")
         st.stief_decode_workspace_init(s["workspace"])
+        s["q_row"], s["out_row"] = s["q"][:, 0], s["out"][:, 0]
     else:
-        s["splits"] = st.stief_mq_num_splits(B, n, Hq, s["Hkv"], s["table"].shape[1])
-        s["workspace"] = torch.zeros(max(128, st.stief_mq_workspace_bytes(B, n, Hq, s["r_v"], s["splits"])), dtype=torch.uint8, device="cuda")
+        s["splits"] = st.stief_f8_mq_num_splits(B, n, Hq, s["Hkv"], s["table"].shape[1])
+        s["workspace"] = torch.zeros(max(128, st.stief_f8_mq_workspace_bytes(B, n, Hq, s["r_v"], s["splits"])), dtype=torch.uint8, device="cuda")
 
 
 # ------------------------------------------------------------------------------------------------- one pass
@@ -198,7 +199,7 @@ def _run_own(s):
         call(s["layer"], s["batch"], s["k"], s["v"], s["cu"], rotation=s["turn"], q=s["q"], q_out=s["q_out"], positions=s["positions"])
         return _appended(s)
     if s["op"] == "decode":
-        st.stief_f8_decode_attention(s["layer"], s["batch"], s["q"], s["workspace"], s["out"])
+        st.stief_f8_decode_attention(s["layer"], s["batch"], s["q_row"], s["workspace"], s["out_row"])
     else:
         st.stief_f8_mq_attention(s["layer"], s["batch"], s["q"], s["out"], q_lens=s["counts"], workspace=s["workspace"], num_splits=s["splits"])
     return s["out"]
