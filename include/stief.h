@@ -27,7 +27,7 @@
  *  - The softmax scale is always 1/sqrt(d_h) = 1/sqrt(128), never 1/sqrt(r_k): attention is defined
  *    on tensors of the original dimension (Eq. 7, Eq. 18).
  *  - RoPE (or any other positional map) is the caller's business: k, q arrive as the attention block
- *    sees them.
+ *    sees them.  stief_rope_append and stief_f8_append alone can rotate them on the way in.
  */
 #ifndef STIEF_H_
 #define STIEF_H_
@@ -442,6 +442,86 @@ int stief_prompt_attention(int32_t Hq, int32_t Hkv, int32_t B, int32_t total_tok
                            int64_t v_stride_t, uint16_t* out, int64_t out_stride_t, float* out_lse, uint32_t flags,
                            int32_t* status, void* stream);
 
+/* ---- the position rotation on the way into the cache -------------------------------------------------------------
+ * New tokens of B sequences, packed behind one another (tokens cu_seqlens[b] .. cu_seqlens[b+1] - 1 belong to sequence b,
+ * device int32 [B + 1], non-decreasing; a sequence may have none): queries and keys are rotated by the angles of their
+ * positions, keys and values projected (Eq. 1) and stored in the paged cache, in one launch.  One token per sequence, chunks
+ * and whole prompts go through the same call.
+ *   rotation    HOST pointer, or NULL: nothing is rotated.  Channels [0, rot_dim) of every query and key head are turned in
+ *               pairs, (a, b) -> (a cos - b sin, b cos + a sin) in fp32, the others stay.  interleaved = 0: channel i pairs
+ *               with i + rot_dim / 2; 1: channel 2 i with 2 i + 1.  table (device fp32 [max_pos][rot_dim], 16-byte aligned)
+ *               holds, for each position, the rot_dim / 2 cosines and then the sines.  rot_dim: a multiple of 16, 16 .. 128
+ *   q, q_out    bf16 [total_tokens][Hq][128], or both NULL: no queries (they need a rotation).  q_out may be q itself (the same
+ *               strides), else they must not overlap
+ *   k, v        bf16 [total_tokens][Hkv][128] (r elements per head on a side without basis, whose rows are stored as they
+ *               are; a rotated key side without basis has r_k = 128).  Heads and elements contiguous, element strides between
+ *               tokens free (multiples of 8, rows 16-byte aligned)
+ *   positions   device int32 [total_tokens] or NULL: the position that a token is rotated by (a drafted node's depth), which
+ *               leaves the place where it is stored alone; NULL: the two are the same
+ *   ends_at_len 0: token i of sequence b is stored at position seq_lens[b] + i; 1: seq_lens already counts the new tokens,
+ *               the last of which is stored at seq_lens[b] - 1
+ * Rows of q_out and pages that no token belongs to are left as they are.  A rotated key is not rounded before it is
+ * projected (two bf16 terms; three for the 8-bit cache).  STIEF_ERR_BOUNDS, and nothing of the token is written: a
+ * position outside the table; nothing of the page: a page outside the pool or a place behind the block table (or 2^30);
+ * nothing of the sequence: its range is not within 0 .. total_tokens, or would begin before position 0.  Pages must not be
+ * shared by sequences that append to them.  B <= 1024. */
+typedef struct stief_rotation {
+  const float* table;
+  int32_t max_pos, rot_dim, interleaved;
+} stief_rotation;
+
+int stief_rope_append(const stief_layer* layer, const stief_batch* batch, const stief_rotation* rotation, const uint16_t* q,
+                      int64_t q_stride_t, const uint16_t* k, int64_t k_stride_t, const uint16_t* v, int64_t v_stride_t,
+                      int32_t total_tokens, const int32_t* cu_seqlens, const int32_t* positions, int32_t ends_at_len,
+                      uint16_t* q_out, int64_t q_out_stride_t, int32_t* status, void* stream);
+
+/* ---- compressed cache in 8-bit floating point, one scale for each page and KV head -------------------------------
+ * k_codes [num_pages][Hkv][64][r_k] and v_codes [num_pages][Hkv][64][r_v] hold e4m3 values, indexed like the bf16 pools;
+ * scales [num_pages][Hkv][4] fp32 holds for each page and KV head (key scale, value scale, unused, unused); a code c stands for
+ * c * scale.  Scales are powers of two, 2^e with e in -100 .. 119: the least that brings the block's largest magnitude to
+ * at most 448.  An element then keeps 4 significant bits whatever its channel's share of the block (down to 2^-13 of the
+ * block's largest magnitude), and a page whose scale has to grow when a larger row joins it has its older rows moved to
+ * the new scale by their exponents alone (only values below 2^-6 of the new scale are rounded again).  NaN and infinities
+ * are stored as NaN and leave the scale alone.
+ * A side without basis (NULL) is taken as in stief_layer.  Alignment: code pools and bases 128 bytes, scales 16. */
+typedef struct stief_f8layer {
+  int32_t Hq, Hkv, d;
+  int32_t r_k, r_v;
+  int32_t num_pages;
+  const uint16_t* U_k;
+  int64_t uk_head_stride;
+  const uint16_t* U_v;
+  int64_t uv_head_stride;
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* scales;
+} stief_f8layer;
+
+/* stief_rope_append into the 8-bit cache (rotation NULL: a plain append).  The rows are quantised from fp32, not rounded to
+ * bf16 first.  A page whose row 0 is written starts a new scale; otherwise rows 0 .. up to the first new one are the page's
+ * older rows. */
+int stief_f8_append(const stief_f8layer* layer, const stief_batch* batch, const stief_rotation* rotation, const uint16_t* q,
+                    int64_t q_stride_t, const uint16_t* k, int64_t k_stride_t, const uint16_t* v, int64_t v_stride_t,
+                    int32_t total_tokens, const int32_t* cu_seqlens, const int32_t* positions, int32_t ends_at_len,
+                    uint16_t* q_out, int64_t q_out_stride_t, int32_t* status, void* stream);
+
+/* Decode attention over the 8-bit cache, one query token per sequence: arguments, workspace (stief_decode_workspace_bytes
+ * with the same r_v), flags and empty sequences as in stief_decode_attention; out must not be NULL.  With U_k NULL q has r_k
+ * elements per head, with U_v NULL out has r_v. */
+int stief_f8_decode_attention(const stief_f8layer* layer, const stief_batch* batch, const uint16_t* q, int32_t len_add,
+                              void* workspace, size_t workspace_bytes, int32_t num_parts, uint16_t* out, float* out_lse,
+                              uint32_t flags, int32_t* status, void* stream);
+
+/* Several causal query rows per head over the 8-bit cache: arguments as stief_mq_attention, for any number of query heads per
+ * KV head up to 128, and strides in either order (a batch stride below the token stride).  num_splits: 1 .. 32, from
+ * stief_f8_mq_num_splits.  q' = q U_k and the probabilities pass through f16, each row scaled by a power of two of its own. */
+int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t max_pages_per_seq);
+size_t stief_f8_mq_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t r_v, int32_t num_splits);
+int stief_f8_mq_attention(const stief_f8layer* layer, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b,
+                          int64_t q_stride_t, int32_t n_q, const int32_t* q_lens, void* workspace, size_t workspace_bytes,
+                          int32_t num_splits, uint16_t* out, int64_t out_stride_b, int64_t out_stride_t, float* out_lse,
+                          uint32_t flags, int32_t* status, void* stream);
+
 /* ---- pages of the cache: taking, forking, reordering, copying, freeing ---------------------------------------------
  * The other entry points only read block_table and seq_lens; these calls write them, on the device, so that a captured step
  * can take and give back pages.  Slot b of the batch holds pages block_table[b][0 .. page_counts[b]); ref_counts[p] is the
@@ -460,7 +540,8 @@ typedef struct stief_page_table {
 } stief_page_table;
 
 /* One pool whose pages lie page_bytes apart (a multiple of 16), page 0 at base (16-byte aligned): a key or value pool of any
- * layer, the code pools and v_params of a quantised layer.  k_params have no pages. */
+ * layer, the code pools and v_params of a quantised layer, the code pools and scales of a layer in 8-bit floating point.
+ * k_params have no pages. */
 typedef struct stief_page_pool {
   void* base;
   int64_t page_bytes;

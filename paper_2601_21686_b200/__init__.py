@@ -51,6 +51,18 @@ class _CQLayer(ctypes.Structure):
                 ("v_params", ctypes.c_void_p)]
 
 
+class _CF8Layer(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("r_k", ctypes.c_int32), ("r_v", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("U_k", ctypes.c_void_p), ("uk_head_stride", ctypes.c_int64),
+                ("U_v", ctypes.c_void_p), ("uv_head_stride", ctypes.c_int64),
+                ("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class _CRotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("max_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 class _CBatch(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
                 ("block_table", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p)]
@@ -82,7 +94,8 @@ def lib() -> ctypes.CDLL:
         L = ctypes.CDLL(LIB_PATH)
         P, I32, I64, SZ, U32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_uint32
         LP, BP, QP = ctypes.POINTER(_CLayer), ctypes.POINTER(_CBatch), ctypes.POINTER(_CQLayer)
-        TP = ctypes.POINTER(_CPageTable)
+        TP, FP, RP = ctypes.POINTER(_CPageTable), ctypes.POINTER(_CF8Layer), ctypes.POINTER(_CRotation)
+        appended = [RP, P, I64, P, I64, P, I64, I32, P, P, I32, P, I64, P, P]
         sig = {
             "stief_prefill_compress": (ctypes.c_int, [LP, BP, P, P, I64, I64, I64, I64, I32, U32, P, P]),
             "stief_append": (ctypes.c_int, [LP, BP, P, P, P, P]),
@@ -118,6 +131,12 @@ def lib() -> ctypes.CDLL:
             "stief_pages_reserve": (ctypes.c_int, [TP, P, I32, P, P]),
             "stief_pages_fork": (ctypes.c_int, [TP, P, I32, P, P, SZ, P, P]),
             "stief_pages_copy": (ctypes.c_int, [P, I32, I32, P, P, I32, P, P]),
+            "stief_rope_append": (ctypes.c_int, [LP, BP, *appended]),
+            "stief_f8_append": (ctypes.c_int, [FP, BP, *appended]),
+            "stief_f8_decode_attention": (ctypes.c_int, [FP, BP, P, I32, P, SZ, I32, P, P, U32, P, P]),
+            "stief_f8_mq_attention": (ctypes.c_int, [FP, BP, P, I64, I64, I32, P, P, SZ, I32, P, I64, I64, P, U32, P, P]),
+            "stief_f8_mq_num_splits": (I32, [I32, I32, I32, I32, I32]),
+            "stief_f8_mq_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
             "stief_select_ranks": (ctypes.c_int, [I32, I32, P, I32, P, I32, ctypes.c_double, P, _SURFACE_FN, P, P, P, P, P]),
             "stief_selftest_wait_limit": (ctypes.c_int, [P, P, I32, P]),
             "stief_trace_next_decode_kernel": (ctypes.c_int, [P, SZ]),
@@ -201,6 +220,55 @@ class QLayer:
         return _CQLayer(self.Hq, self.Hkv, D_HEAD, self.r_k, self.r_v, self.num_pages, _ptr(self.U_k), uk_stride,
                         _ptr(self.U_v), uv_stride, _ptr(self.k_params), _ptr(self.k_codes), _ptr(self.v_codes),
                         _ptr(self.v_params))
+
+
+@dataclass
+class F8Layer:
+    """One decoder layer's compressed cache in 8-bit floating point (device tensors): U_k [Hkv or 1, 128, r_k], U_v [Hkv or 1,
+    128, r_v] bf16 (None = that side is not projected); k_codes [num_pages, Hkv, 64, r_k], v_codes [num_pages, Hkv, 64, r_v] e4m3
+    (uint8 or float8_e4m3fn); scales [num_pages, Hkv, 4] fp32: (key scale, value scale, unused, unused), powers of two."""
+    Hq: int
+    Hkv: int
+    r_k: int
+    r_v: int
+    U_k: Optional[torch.Tensor]
+    U_v: Optional[torch.Tensor]
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    scales: torch.Tensor
+
+    @property
+    def num_pages(self) -> int:
+        return self.k_codes.shape[0]
+
+    def c(self) -> _CF8Layer:
+        uk_stride = 0 if self.U_k is None or self.U_k.size(0) == 1 else self.U_k.stride(0)
+        uv_stride = 0 if self.U_v is None or self.U_v.size(0) == 1 else self.U_v.stride(0)
+        key = (self.Hq, self.Hkv, D_HEAD, self.r_k, self.r_v, self.k_codes.size(0), _ptr(self.U_k), uk_stride, _ptr(self.U_v), uv_stride,
+               self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.scales.data_ptr())
+        kept = self.__dict__.get("_c")                          # the same values in a C structure
+        if kept is None or kept[0] != key:
+            kept = self.__dict__["_c"] = (key, _CF8Layer(*key))
+        return kept[1]
+
+
+@dataclass
+class Rotation:
+    """Angles of the position rotation: table [max_pos, rot_dim] fp32 on the device, for each position the rot_dim / 2 cosines and
+    then the sines.  Channel i is paired with i + rot_dim / 2, or 2 i with 2 i + 1 when ``interleaved``."""
+    table: torch.Tensor
+    interleaved: bool = False
+
+    def c(self, device: int) -> _CRotation:
+        t = self.table
+        if t.dtype is not torch.float32 or t.dim() != 2 or not t.is_contiguous():
+            raise ValueError("the rotation's table must be contiguous fp32 [max_pos, rot_dim]")
+        _here(t, "table", device)
+        key = (t.data_ptr(), t.size(0), t.size(1), 1 if self.interleaved else 0)
+        kept = self.__dict__.get("_c")
+        if kept is None or kept[0] != key:
+            kept = self.__dict__["_c"] = (key, _CRotation(*key))
+        return kept[1]
 
 
 @dataclass
@@ -515,6 +583,10 @@ def _cache_tensors(layer: Layer, device: int):
     """Pools and bases of a layer: shapes, layout and device.  Looked at in every call: ranks and tensors may have been replaced,
     or changed in place, since the last."""
     _layer_pools(layer, device)
+    _bases(layer, device)
+
+
+def _bases(layer, device: int):
     for U, r, name in ((layer.U_k, layer.r_k, "U_k"), (layer.U_v, layer.r_v, "U_v")):
         if U is None:
             continue
@@ -616,7 +688,149 @@ def stief_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu
                                         _status(status, at), _raw_stream(at)), "stief_prompt_attention")
 
 
+def _f8_tensors(layer: F8Layer, device: int):
+    """Codes, scales and bases of an 8-bit layer, in every call: the kernels compute addresses from its ranks and heads."""
+    if not isinstance(layer, F8Layer):
+        raise ValueError("an F8Layer is expected")
+    pages, Hkv = layer.k_codes.size(0), layer.Hkv
+    for pool, r, name in ((layer.k_codes, layer.r_k, "k_codes"), (layer.v_codes, layer.r_v, "v_codes")):
+        if (pool.dtype is not torch.uint8 and pool.dtype is not torch.float8_e4m3fn) or not pool.is_contiguous() or pool.shape != (pages, Hkv, PAGE, r):
+            raise ValueError(f"{name} must be contiguous uint8 or float8_e4m3fn [num_pages, Hkv, {PAGE}, {r}]")
+        if pool.get_device() != device:
+            _here(pool, name, device)
+    scales = layer.scales
+    if scales.dtype is not torch.float32 or not scales.is_contiguous() or scales.shape != (pages, Hkv, 4):
+        raise ValueError("scales must be contiguous fp32 [num_pages, Hkv, 4]")
+    if scales.get_device() != device:
+        _here(scales, "scales", device)
+    _bases(layer, device)
+
+
+def _token_rows(t: torch.Tensor, name: str, total: int, heads: int, width: int, device: int):
+    """Address and token stride of a packed tensor [total, heads, width]."""
+    st = t.stride()
+    if t.dtype is not torch.bfloat16 or t.shape != (total, heads, width) or st[2] != 1 or (st[1] != width and heads > 1):
+        raise ValueError(f"{name} must be bf16 [{total}, {heads}, {width}] with contiguous heads and elements")
+    if t.get_device() != device:
+        _here(t, name, device)
+    return t.data_ptr(), st[0] if total > 1 else heads * width                 # an extent of 1 may carry any stride
+
+
+def _append_rows(call: str, check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status):
+    at = _here(k, "k")
+    check(layer, at)
+    total, Hkv = k.shape[0], layer.Hkv
+    kv = (*_token_rows(k, "k", total, Hkv, D_HEAD if layer.U_k is not None else layer.r_k, at),
+          *_token_rows(v, "v", total, Hkv, D_HEAD if layer.U_v is not None else layer.r_v, at))
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    qp = qs = op = os_ = None
+    if q is not None:
+        qp, qs = _token_rows(q, "q", total, layer.Hq, D_HEAD, at)
+        op, os_ = _token_rows(q_out, "q_out", total, layer.Hq, D_HEAD, at)
+    B = batch.block_table.shape[0]
+    _int32(batch.block_table, "block_table", None, at)
+    _int32(batch.seq_lens, "seq_lens", (B,), at)
+    _int32(cu_seqlens, "cu_seqlens", (B + 1,), at)
+    if positions is not None:
+        _int32(positions, "positions", (total,), at)
+    _check(getattr(lib(), call)(ctypes.byref(layer.c()), ctypes.byref(batch.c()), None if rotation is None else ctypes.byref(rotation.c(at)),
+                                qp, qs or 0, *kv, total, cu_seqlens.data_ptr(), _ptr(positions), 1 if ends_at_len else 0, op, os_ or 0,
+                                _status(status, at), _raw_stream(at)), call)
+
+
+def stief_rope_append(layer: Layer, batch: Batch, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                      rotation: Optional[Rotation] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                      positions: Optional[torch.Tensor] = None, ends_at_len: bool = False, status: Optional[torch.Tensor] = None):
+    """Packed new tokens into the bf16 cache, rotated on the way: k, v [total, Hkv, 128 (r on a side without basis)], q, q_out
+    [total, Hq, 128] bf16 (strides over tokens free), cu_seqlens [B + 1] int32; positions [total] int32 where tokens are rotated
+    by other positions than they are stored at.  q_out may be q."""
+    _append_rows("stief_rope_append", _cache_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
+
+
+def stief_f8_append(layer: F8Layer, batch: Batch, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
+                    rotation: Optional[Rotation] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, ends_at_len: bool = False, status: Optional[torch.Tensor] = None):
+    """stief_rope_append into the 8-bit cache."""
+    _append_rows("stief_f8_append", _f8_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
+
+
+def stief_f8_decode_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor, num_parts: int = 0,
+                              out_lse: Optional[torch.Tensor] = None, len_add: int = 0, status: Optional[torch.Tensor] = None, flags: int = 0):
+    """One query token per sequence over the 8-bit cache: q [B, Hq, 128 (r_k without key basis)] -> out [B, Hq, 128 (r_v without
+    value basis)] bf16, contiguous; workspace as for stief_decode_attention."""
+    at = _here(q, "q")
+    _f8_tensors(layer, at)
+    B, Hq = batch.block_table.shape[0], layer.Hq
+    d_q, d_out = D_HEAD if layer.U_k is not None else layer.r_k, D_HEAD if layer.U_v is not None else layer.r_v
+    for t, name, width in ((q, "q", d_q), (out, "out", d_out)):
+        if t.dtype is not torch.bfloat16 or t.shape != (B, Hq, width) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous bf16 [{B}, {Hq}, {width}]")
+    _here(out, "out", at)
+    if out_lse is not None:
+        if out_lse.dtype is not torch.float32 or not out_lse.is_contiguous() or out_lse.shape != (B, Hq):
+            raise ValueError("out_lse must be contiguous fp32 [B, Hq]")
+        _here(out_lse, "out_lse", at)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _here(workspace, "workspace", at)
+    _int32(batch.block_table, "block_table", None, at)
+    _int32(batch.seq_lens, "seq_lens", (B,), at)
+    _check(lib().stief_f8_decode_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), len_add, workspace.data_ptr(),
+                                           workspace.numel() * workspace.element_size(), num_parts, out.data_ptr(), _ptr(out_lse), flags,
+                                           _status(status, at), _raw_stream(at)), "stief_f8_decode_attention")
+
+
+def stief_f8_mq_num_splits(B: int, n_q: int, Hq: int, Hkv: int, max_pages_per_seq: int) -> int:
+    return lib().stief_f8_mq_num_splits(B, n_q, Hq, Hkv, max_pages_per_seq)
+
+
+def stief_f8_mq_workspace_bytes(B: int, n_q: int, Hq: int, r_v: int, num_splits: int) -> int:
+    return lib().stief_f8_mq_workspace_bytes(B, n_q, Hq, r_v, num_splits)
+
+
+def stief_f8_mq_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, out: torch.Tensor, q_lens: Optional[torch.Tensor] = None,
+                          out_lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, flags: int = 0,
+                          workspace: Optional[torch.Tensor] = None, num_splits: int = 1):
+    """Several causal query rows per head over the 8-bit cache: q [B, n_q, Hq, d_q] -> out [B, n_q, Hq, d_out] bf16 (strides over b
+    and t free), the queries being the last q_lens[b] (default n_q) tokens of each cached sequence.  num_splits > 1 needs a
+    workspace tensor of stief_f8_mq_workspace_bytes(...) bytes."""
+    if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or q.dim() != 4 or out.dim() != 4:
+        raise ValueError("q and out must be bf16 [B, n_q, Hq, d]")
+    at = _here(q, "q")
+    _f8_tensors(layer, at)
+    B, n_q, Hq, d_q = q.shape
+    d_out = D_HEAD if layer.U_v is not None else layer.r_v
+    if Hq != layer.Hq or d_q != (D_HEAD if layer.U_k is not None else layer.r_k) or out.shape != (B, n_q, Hq, d_out) or B != batch.block_table.shape[0]:
+        raise ValueError("q, out, layer and batch disagree in shape")
+    qs, os_ = q.stride(), out.stride()
+    if qs[3] != 1 or (qs[2] != d_q and Hq > 1) or os_[3] != 1 or (os_[2] != d_out and Hq > 1):
+        raise ValueError("heads and elements of q and out must be contiguous")
+    _here(out, "out", at)
+    if q_lens is not None:
+        _int32(q_lens, "q_lens", (B,), at)
+    if out_lse is not None:
+        if out_lse.dtype is not torch.float32 or not out_lse.is_contiguous() or out_lse.shape != (B, n_q, Hq):
+            raise ValueError("out_lse must be contiguous fp32 [B, n_q, Hq]")
+        _here(out_lse, "out_lse", at)
+    ws_bytes = 0
+    if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        _here(workspace, "workspace", at)
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _int32(batch.block_table, "block_table", None, at)
+    _int32(batch.seq_lens, "seq_lens", (B,), at)
+    q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (Hq * d_q, Hq * d_out)        # an extent of 1 may carry any stride: the call gets one that fits
+    q_b, o_b = (qs[0], os_[0]) if B > 1 else (q_t, o_t)
+    _check(lib().stief_f8_mq_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(q_lens),
+                                       _ptr(workspace), ws_bytes, num_splits, out.data_ptr(), o_b, o_t, _ptr(out_lse), flags,
+                                       _status(status, at), _raw_stream(at)), "stief_f8_mq_attention")
+
+
 def _page_tensors(layer):
+    if isinstance(layer, F8Layer):
+        return (layer.k_codes, layer.v_codes, layer.scales)
     if isinstance(layer, QLayer):
         return (layer.k_codes, layer.v_codes, layer.v_params)
     return (layer.k_pool, layer.v_pool)

@@ -1,0 +1,62 @@
+// The compressed cache in 8-bit floating point (e4m3, one power-of-two scale for each page, KV head and side): what its
+// kernels share.
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "stief_common.cuh"
+
+namespace stief {
+namespace f8 {
+
+constexpr float kTop = 448.f;                    // the largest e4m3 value
+constexpr int kLowest = -100, kHighest = 119;    // exponents of a scale: codes times scales stay within fp32's and bf16's range
+constexpr int kScalesPerTile = 4;                // floats of a (page, head): key scale, value scale, two unused (16 bytes, one bulk copy)
+
+// The layer as the attention kernels see it: LayerDev's pool pointers are unused.
+struct Pools {
+  uint8_t* k_codes;      // [pages][Hkv][64][r_k]
+  uint8_t* v_codes;      // [pages][Hkv][64][r_v]
+  float* scales;         // [pages][Hkv][kScalesPerTile]
+};
+
+__host__ __device__ __forceinline__ float pow2(int e) {        // 2^e, e in -126 .. 127
+  const uint32_t u = (uint32_t)(e + 127) << 23;
+#ifdef __CUDA_ARCH__
+  return __uint_as_float(u);
+#else
+  union { uint32_t i; float f; } x;
+  x.i = u;
+  return x.f;
+#endif
+}
+
+// The least power of two s with top <= 448 s (448 = 1.75 * 2^8), within the range that scales have.  top is finite and >= 0.
+__device__ __forceinline__ float scale_for(float top) {
+  const uint32_t u = __float_as_uint(top);
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);      // a mantissa above 1.75 takes the next one
+  return pow2(min(max(e, kLowest), kHighest));                 // subnormal tops end at the lowest too
+}
+
+// Four values as e4m3, rounded to nearest even; NaN and infinities become NaN, values beyond the range its largest value.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  auto nan_if_inf = [](float x) { return fabsf(x) <= 3.402823466e38f ? x : __uint_as_float(0x7fc00000u); };
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(nan_if_inf(a), nan_if_inf(b)), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(nan_if_inf(c), nan_if_inf(d)), __NV_SATFINITE, __NV_E4M3);
+  return lo | (hi << 16);
+}
+
+// Two e4m3 codes (bits [0, 16) of w) as two f16: exact, NaN stays NaN
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 p;\n\tcvt.u16.u32 p, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, p;\n\t}" : "=r"(r) : "r"(w));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t w) {
+  const uint32_t r = e4m3x2_to_f16x2(w);
+  return __half22float2(*reinterpret_cast<const __half2*>(&r));
+}
+
+}  // namespace f8
+}  // namespace stief
