@@ -1,6 +1,6 @@
 // Attention over the compressed cache in 8-bit floating point: argument checks and launches of stief_f8_decode_attention and
 // stief_f8_mq_attention.
-#include "stief_f8.cuh"
+#include "stief_f8_decode.cuh"
 #include "stief_host_util.h"
 
 namespace stief {
@@ -136,24 +136,37 @@ extern "C" int stief_f8_decode_attention(const stief_f8layer* layer, const stief
   if (rc) return rc;
   if (!q || !aligned(q, 16) || !workspace || !aligned(workspace, 128) || !out || !aligned(out, 16)) return STIEF_ERR_INVALID_ARG;
   if (len_add < 0 || len_add > 1 || num_parts < 0 || num_parts > 65535) return STIEF_ERR_INVALID_ARG;
-  const int n_cta = resolve_parts(num_parts);
+  const int n_cta = resolve_parts(num_parts), QT = query_tiles(layer->Hq, layer->Hkv);
+  if ((long long)batch->B * (batch->max_pages_per_seq + f8::seg_pad(layer->r_k, layer->r_v)) * layer->Hkv * QT >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;
   const Workspace w = carve(workspace, batch->B, layer->Hq, layer->Hkv, layer->r_v, n_cta, workspace_bytes);
   if (w.bytes > workspace_bytes) return STIEF_ERR_WORKSPACE;
-  f8::SimpleArgs a;
+  F8DecodeArgs a;
   a.L = f8layer_to_dev(layer);
   a.P = f8::Pools{layer->k_codes, layer->v_codes, layer->scales};
   a.Bt = to_dev(batch);
   a.q = reinterpret_cast<const __nv_bfloat16*>(q);
-  a.q_b = a.q_t = (long long)layer->Hq * (layer->U_k ? kD : layer->r_k);
-  a.n_q = 1;
-  a.len_add = len_add;
-  a.q_lens = nullptr;
+  const bool ov = (flags & STIEF_DECODE_OVERLAP_PREVIOUS) != 0 && n_cta >= sm_count();   // full grids only (see run_decode)
+  const WorkspaceTurn turn = take_workspace_turn(workspace);
+  a.partial_o = w.partial_o[turn.section]; a.partial_lse = w.partial_lse[turn.section]; a.counters = w.counters[turn.section];
+  a.finished = w.control + turn.section;
+  a.units_done = w.control + kWorkspaceSections + turn.section;
+  a.epoch = turn.epoch;
+  a.prev_epoch = ov ? turn.prev_epoch : 0u;
   a.out = reinterpret_cast<__nv_bfloat16*>(out);
-  a.o_b = a.o_t = (long long)layer->Hq * (layer->U_v ? kD : layer->r_v);
   a.out_lse = out_lse;
+  a.len_add = len_add;
+  a.QT = QT;
   a.status = status;
-  f8::f8_rows_kernel<<<dim3(1, layer->Hq, batch->B), 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaErrorInvalidValue;
+  switch (layer->r_k) {
+    case 32: e = launch_f8_decode_rk32(a, n_cta, ov, st); break;
+    case 48: e = launch_f8_decode_rk48(a, n_cta, ov, st); break;
+    case 64: e = launch_f8_decode_rk64(a, n_cta, ov, st); break;
+    case 96: e = launch_f8_decode_rk96(a, n_cta, ov, st); break;
+    case 128: e = launch_f8_decode_rk128(a, n_cta, ov, st); break;
+  }
+  return e == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
 }
 
 extern "C" int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t max_pages_per_seq) {
