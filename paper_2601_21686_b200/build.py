@@ -43,6 +43,8 @@ def _units():
                       [f"-DSTIEF_RK={rk}"]))
         units.append((os.path.join(CSRC, "stief_f8_decode_inst.cu"), os.path.join(OBJ, f"stief_f8_decode_rk{rk}.o"),
                       [f"-DSTIEF_RK={rk}"]))
+        units.append((os.path.join(CSRC, "stief_f8_mq_inst.cu"), os.path.join(OBJ, f"stief_f8_mq_rk{rk}.o"),
+                      [f"-DSTIEF_RK={rk}"]))
         for bits in (8, 4):
             units.append((os.path.join(CSRC, "stief_decode_q_inst.cu"), os.path.join(OBJ, f"stief_decode_q_rk{rk}_b{bits}.o"),
                           [f"-DSTIEF_RK={rk}", f"-DSTIEF_QBITS={bits}"]))

@@ -1,97 +1,10 @@
 // Attention over the compressed cache in 8-bit floating point: argument checks and launches of stief_f8_decode_attention and
 // stief_f8_mq_attention.
 #include "stief_f8_decode.cuh"
+#include "stief_f8_mq.cuh"
 #include "stief_host_util.h"
 
 namespace stief {
-namespace f8 {
-
-struct SimpleArgs {
-  LayerDev L;
-  Pools P;
-  BatchDev Bt;
-  const __nv_bfloat16* q;
-  long long q_b, q_t;
-  int n_q, len_add;
-  const int32_t* q_lens;
-  __nv_bfloat16* out;
-  long long o_b, o_t;
-  float* out_lse;
-  int32_t* status;
-};
-
-// One block per (token, query head, sequence): a pass over the pages with the running maximum and sum of the softmax.
-__global__ void __launch_bounds__(128)
-f8_rows_kernel(const SimpleArgs a) {
-  __shared__ float qp[kD], p[kPage], od[kD], red[4];
-  const int i = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
-  const int h = hq / a.L.G, RK = a.L.r_k, RV = a.L.r_v;
-  int ql = a.q_lens ? a.q_lens[b] : a.n_q;
-  ql = min(max(ql, 0), a.n_q);
-  if (i >= ql) return;
-  const int len = a.Bt.seq_lens[b] + a.len_add;
-  const bool fold_k = a.L.U_k == nullptr, fold_v = a.L.U_v == nullptr;
-  if ((a.q_lens || a.n_q > 1) && len < ql || (len + kPage - 1) / kPage > a.Bt.max_pages) {
-    if (tid == 0) report(a.status, STIEF_ERR_BOUNDS);
-    return;
-  }
-  const int n = max(0, len - ql + i + 1);
-  const __nv_bfloat16* qr = a.q + b * a.q_b + i * a.q_t + (long long)hq * (fold_k ? RK : kD);
-  if (tid < RK) {
-    float x = 0.f;
-    if (fold_k) x = __bfloat162float(qr[tid]);
-    else
-      for (int d = 0; d < kD; ++d) x = fmaf(__bfloat162float(qr[d]), __bfloat162float(a.L.U_k[(size_t)h * a.L.uk_stride + d * RK + tid]), x);
-    qp[tid] = x * 0.08838834764831845f;
-  }
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int pg = 0; pg * kPage < n; ++pg) {
-    int page = a.Bt.block_table[(size_t)b * a.Bt.max_pages + pg];
-    if (page < 0 || page >= a.L.num_pages) {
-      if (tid == 0) report(a.status, STIEF_ERR_BOUNDS);
-      page = 0;
-    }
-    const size_t tile = (size_t)page * a.L.Hkv + h;
-    const int cnt = min(kPage, n - pg * kPage);
-    if (tid < kPage) {
-      float s = 0.f;
-      const uint8_t* k = a.P.k_codes + (tile * kPage + tid) * RK;
-      for (int c = 0; c < RK; c += 2) {
-        const float2 x = e4m3x2_to_float2(*reinterpret_cast<const uint16_t*>(k + c));
-        s = fmaf(qp[c + 1], x.y, fmaf(qp[c], x.x, s));
-      }
-      p[tid] = tid < cnt ? s * a.P.scales[tile * kScalesPerTile] : -INFINITY;
-    }
-    __syncthreads();
-    float top = m;
-    for (int t = 0; t < cnt; ++t) top = fmaxf(top, p[t]);
-    const float f = __expf(m - top), vs = a.P.scales[tile * kScalesPerTile + 1];
-    m = top;
-    l *= f;
-    o *= f;
-    for (int t = 0; t < cnt; ++t) {
-      const float w = __expf(p[t] - m);
-      l += w;
-      if (tid < RV) o = fmaf(w * vs, e4m3x2_to_float2(a.P.v_codes[(tile * kPage + t) * RV + tid]).x, o);
-    }
-    __syncthreads();
-  }
-  if (tid < RV) od[tid] = l > 0.f ? o / l : 0.f;
-  __syncthreads();
-  const int d_out = fold_v ? RV : kD;
-  if (tid < d_out) {
-    float x = 0.f;
-    if (fold_v) x = od[tid];
-    else
-      for (int c = 0; c < RV; ++c) x = fmaf(od[c], __bfloat162float(a.L.U_v[(size_t)h * a.L.uv_stride + tid * RV + c]), x);
-    a.out[b * a.o_b + i * a.o_t + (long long)hq * d_out + tid] = __float2bfloat16_rn(x);
-  }
-  if (tid == 0 && a.out_lse) a.out_lse[((size_t)b * a.n_q + i) * a.L.Hq + hq] = l > 0.f ? m + logf(l) : -INFINITY;
-}
-
-}  // namespace f8
-
 namespace {
 
 using namespace host;
@@ -205,21 +118,66 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
   if (q_stride_t < q_row || q_stride_b < q_row || q_stride_t % 8 || q_stride_b % 8 || out_stride_t < o_row || out_stride_b < o_row ||
       out_stride_t % 8 || out_stride_b % 8 || !aligned(q, 16) || !aligned(out, 16))
     return STIEF_ERR_INVALID_ARG;
-  f8::SimpleArgs a;
+  const int RK = layer->r_k, RV = layer->r_v, TT = kMqRows / G;
+  const bool fold_k = !layer->U_k, fold_v = !layer->U_v;
+  const long long n_units = ((long long)n_q + 2 * TT - 1) / (2 * TT) * batch->B * layer->Hkv * num_splits;
+  if (n_q > (1 << 30) || n_units >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;
+  f8mq::Launch L = {};
+  const tc::Blocks bk = tc::blocks_of(RK), bv = tc::blocks_of(RV);
+  const unsigned long long nq = n_q, Hq = layer->Hq, B = batch->B;
+  if (!fold_k) {
+    const unsigned long long dims[4] = {(unsigned long long)kD, Hq, nq, B};
+    const unsigned long long strides[3] = {kD * 2, (unsigned long long)q_stride_t * 2, (unsigned long long)q_stride_b * 2};
+    const unsigned box[4] = {64u, (unsigned)G, (unsigned)TT, 1u};
+    if (!encode_bf16_map(&L.tmQ, q, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B)) return STIEF_ERR_CUDA;
+  }
+  auto basis_map = [&](CUtensorMap* tm, const void* U, long long head_stride, int R, const tc::Blocks& b) {
+    const unsigned long long nh = head_stride ? (unsigned long long)layer->Hkv : 1ull;
+    const unsigned long long dims[3] = {(unsigned long long)R, (unsigned long long)kD, nh};
+    const unsigned long long strides[2] = {(unsigned long long)R * 2, (unsigned long long)(head_stride ? head_stride : (long long)kD * R) * 2};
+    const unsigned box[3] = {(unsigned)b.bw, (unsigned)kD, 1u};
+    return encode_bf16_map(tm, U, 3, dims, strides, box, b.span == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : b.span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
+  };
+  if (!fold_k && !basis_map(&L.tmUk, layer->U_k, layer->uk_head_stride, RK, bk)) return STIEF_ERR_CUDA;
+  if (!fold_v && !basis_map(&L.tmUv, layer->U_v, layer->uv_head_stride, RV, bv)) return STIEF_ERR_CUDA;
+  mq::Args& a = L.a.m;
   a.L = f8layer_to_dev(layer);
-  a.P = f8::Pools{layer->k_codes, layer->v_codes, layer->scales};
   a.Bt = to_dev(batch);
-  a.q = reinterpret_cast<const __nv_bfloat16*>(q);
-  a.q_b = q_stride_b;
-  a.q_t = q_stride_t;
-  a.n_q = n_q;
-  a.len_add = 0;
   a.q_lens = q_lens;
+  a.n_q = n_q;
   a.out = reinterpret_cast<__nv_bfloat16*>(out);
-  a.o_b = out_stride_b;
-  a.o_t = out_stride_t;
+  a.out_stride_b = out_stride_b;
+  a.out_stride_t = out_stride_t;
   a.out_lse = out_lse;
   a.status = status;
-  f8::f8_rows_kernel<<<dim3(n_q, layer->Hq, batch->B), 128, 0, static_cast<cudaStream_t>(stream)>>>(a);
-  return cudaGetLastError() == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
+  a.n_split = num_splits;
+  a.dual = (num_splits > 1 && n_q <= TT) ? 1 : 0;                // the second tile would have no rows of its own
+  a.n_parts = num_splits * (1 + a.dual);
+  a.part_o = num_splits > 1 ? static_cast<float*>(workspace) : nullptr;
+  a.part_ml = a.part_o ? a.part_o + (size_t)batch->B * n_q * layer->Hq * a.n_parts * RV : nullptr;
+  a.qp_bytes = f8mq::kRows * 2 * (fold_v ? RK : (RK > RV ? RK : RV));
+  L.a.P = f8::Pools{layer->k_codes, layer->v_codes, layer->scales};
+  L.a.q = reinterpret_cast<const __nv_bfloat16*>(q);
+  L.a.q_stride_b = q_stride_b;
+  L.a.q_stride_t = q_stride_t;
+  // Shared memory: four operand stages where at least four pages of codes fit beside them, else three (two query tiles and U_k are
+  // in the ring together); the rest holds codes, which is what keeps the memory busy.
+  const int code = f8mq::code_stage_bytes(RK, RV), room = mq::kSmemLimit - 1024 - 2 * a.qp_bytes - f8mq::kCtrlBytes;
+  a.nst = room - 4 * f8mq::kStageBytes >= 4 * code ? 4 : 3;
+  L.a.n_code = (room - a.nst * f8mq::kStageBytes) / code;
+  if (L.a.n_code > f8mq::kMaxCodeStages) L.a.n_code = f8mq::kMaxCodeStages;
+  if (L.a.n_code < 2) return STIEF_ERR_UNSUPPORTED;
+  L.smem = 1024 + 2 * a.qp_bytes + f8mq::kCtrlBytes + a.nst * f8mq::kStageBytes + L.a.n_code * code;
+  L.grid = (int)(n_units < sm_count() ? n_units : sm_count());
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaErrorInvalidValue;
+  switch (RK) {
+    case 32: e = launch_f8_mq_rk32(L, st); break;
+    case 48: e = launch_f8_mq_rk48(L, st); break;
+    case 64: e = launch_f8_mq_rk64(L, st); break;
+    case 96: e = launch_f8_mq_rk96(L, st); break;
+    case 128: e = launch_f8_mq_rk128(L, st); break;
+  }
+  if (e == cudaSuccess && num_splits > 1) e = launch_mq_combine(a, st);
+  return e == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
 }

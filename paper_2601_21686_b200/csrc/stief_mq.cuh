@@ -120,7 +120,7 @@ __device__ __forceinline__ Unit decode_unit(const Args& a, int u, int TT) {
   w.tok0[0] = t2 * 2 * TT;
   w.tok0[1] = a.dual ? w.tok0[0] : w.tok0[0] + TT;
   if (w.tok0[0] >= ql) return w;
-  if (w.q_start < 0 || (sl + kPage - 1) / kPage > a.Bt.max_pages) {   // fewer cached tokens than query rows, or a table too short
+  if (w.q_start < 0 || (sl - 1) / kPage + 1 > a.Bt.max_pages) {   // fewer cached tokens than query rows, or a table too short
     report(a.status, STIEF_ERR_BOUNDS);
     return w;
   }
@@ -681,7 +681,7 @@ mq_combine_kernel(const Args a) {
   int ql = a.q_lens ? a.q_lens[b] : a.n_q;
   ql = min(max(ql, 0), a.n_q);
   const int sl = a.Bt.seq_lens[b], q_start = sl - ql;
-  if (tok >= ql || q_start < 0 || (sl + kPage - 1) / kPage > a.Bt.max_pages) return;
+  if (tok >= ql || q_start < 0 || (sl - 1) / kPage + 1 > a.Bt.max_pages) return;
   // pages of the row's tile and of the unit (both tiles), as decode_unit derives them
   const int t2 = tok / (2 * TT), first = t2 * 2 * TT;
   int full[2] = {0, 0};
