@@ -160,14 +160,15 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
   L.a.q = reinterpret_cast<const __nv_bfloat16*>(q);
   L.a.q_stride_b = q_stride_b;
   L.a.q_stride_t = q_stride_t;
-  // Shared memory: four operand stages where at least four pages of codes fit beside them, else three (two query tiles and U_k are
-  // in the ring together); the rest holds codes, which is what keeps the memory busy.
-  const int code = f8mq::code_stage_bytes(RK, RV), room = mq::kSmemLimit - 1024 - 2 * a.qp_bytes - f8mq::kCtrlBytes;
-  a.nst = room - 4 * f8mq::kStageBytes >= 4 * code ? 4 : 3;
-  L.a.n_code = (room - a.nst * f8mq::kStageBytes) / code;
-  if (L.a.n_code > f8mq::kMaxCodeStages) L.a.n_code = f8mq::kMaxCodeStages;
-  if (L.a.n_code < 2) return STIEF_ERR_UNSUPPORTED;
-  L.smem = 1024 + 2 * a.qp_bytes + f8mq::kCtrlBytes + a.nst * f8mq::kStageBytes + L.a.n_code * code;
+  // Shared memory: as many operand stages as fit beside four slots of codes (at 128/128 four: two blocks), the rest holds codes,
+  // which is what keeps the memory busy.
+  const int stage = f8mq::stage_bytes(RK, RV), slot = f8mq::slot_bytes(RK, RV), room = mq::kSmemLimit - 1024 - 2 * a.qp_bytes - f8mq::kCtrlBytes;
+  a.nst = (room - f8mq::kMinCodeSlots * slot) / stage;
+  if (a.nst > f8mq::kMaxStages) a.nst = f8mq::kMaxStages;
+  L.a.n_code = (room - a.nst * stage) / slot;
+  if (L.a.n_code > f8mq::kMaxCodeSlots) L.a.n_code = f8mq::kMaxCodeSlots;
+  if (a.nst < f8mq::kMinStages || L.a.n_code < f8mq::kMinCodeSlots) return STIEF_ERR_UNSUPPORTED;
+  L.smem = 1024 + 2 * a.qp_bytes + f8mq::kCtrlBytes + a.nst * stage + L.a.n_code * slot;
   L.grid = (int)(n_units < sm_count() ? n_units : sm_count());
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
@@ -178,6 +179,10 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
     case 96: e = launch_f8_mq_rk96(L, st); break;
     case 128: e = launch_f8_mq_rk128(L, st); break;
   }
-  if (e == cudaSuccess && num_splits > 1) e = launch_mq_combine(a, st);
+  if (e == cudaSuccess && num_splits > 1) {
+    cudaLaunchAttribute attr[1];
+    const cudaLaunchConfig_t cfg = after_previous(attr, dim3(n_q, layer->Hkv, batch->B), f8mq::kCombineThreads, 0, st);
+    e = cudaLaunchKernelEx(&cfg, f8mq::f8_mq_combine_kernel<0>, a);
+  }
   return e == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
 }

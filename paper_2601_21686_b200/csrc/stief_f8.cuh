@@ -58,5 +58,14 @@ __device__ __forceinline__ float2 e4m3x2_to_float2(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&r));
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// four codes -> two f16 pairs
+__device__ __forceinline__ void expand4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 p, q;\n\tmov.b32 {p, q}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, p;\n\tcvt.rn.f16x2.e4m3x2 %1, q;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+
 }  // namespace f8
 }  // namespace stief

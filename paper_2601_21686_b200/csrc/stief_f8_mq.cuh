@@ -1,7 +1,7 @@
 // Attention of several causal query rows per head over the 8-bit floating-point cache (chunked prefill, speculative decode):
 //     out_i = softmax(q_i' (c_k S_k)[0..p_i]^T / sqrt(128)) (c_v S_v)[0..p_i] U_v^T,   q_i' = q_i U_k,
 // on the 5th-generation tensor cores, in the form of stief_mq.cuh: the same work units (sequence, KV head, 256 query rows in two
-// tiles of 128), the same split of a long page range into parts, the same merge.  What the codes change:
+// tiles of 128), the same split of a long page range into parts.  What the codes change:
 //   operands   kind::f16 products want both operands in one 16-bit type, so every page is expanded once per CTA, for both
 //              tiles, from codes to f16 (exact, one conversion per two codes), by warps of their own: they read the page's codes
 //              from a ring that 1-D bulk copies fill and write the K and V blocks, swizzled as tcgen05.mma reads them, into the
@@ -14,11 +14,15 @@
 //              whose scales lie far apart keep their precision; the row sum takes w 2^-e.
 //   weights    f16 (11 bits, where bf16 would leave 8), at most 2^15: the reference is moved when a row's largest has grown by
 //              more than 2^8, and w = 2^7 at the reference.
+// A step is a block of two pages, 128 positions: waits, TMEM round trips and reductions are paid once per 128 scores of a row.
 // 512 threads, registers split by role (setmaxnreg):
-//   warp 0        fetches the codes of the pages
-//   warps 1, 2    MMA issue, one per tile (control flow and descriptors in uniform registers, stief_umma.cuh)
+//   warp 0        fetches the codes of the pages, keys and values of a page apart
+//   warps 1, 2    MMA issue, one per tile (control flow and descriptors in uniform registers, stief_umma.cuh).  Up to r_v = 64 the
+//                 weights have TMEM columns of their own and the next block's scores are issued ahead of P V; above, P lies
+//                 over the scores and the next scores follow P V
 //   warps 4-11    softmax and epilogue, four per tile; thread = row = TMEM lane
 //   warps 12-15   fill the ring of operands: expand the pages; raw queries, U_k and U_v come straight into it by TMA
+// TMEM, per tile 256 columns: scores 0-127 (also Q' at the start of a unit and OUT at its end), P 128-191 and O 192-255, or O 128-255.
 // Every wait is bounded (see mbar_wait): on a timeout the status word says so, later waits return at once, every role walks
 // to the end of its loops and TMEM is released.
 #pragma once
@@ -34,26 +38,48 @@ using namespace tc;
 
 constexpr int kThreads = 512;
 constexpr int kRows = mq::kRows;
-constexpr int kStageBytes = 32768;               // one stage of the operand ring: a page's K and V, a raw query tile, or a basis
+constexpr int kBlock = 2 * kPage;                // positions per step
 constexpr int kCtrlBytes = 1024;
-constexpr int kMaxStages = 4, kMaxCodeStages = 8;
+constexpr int kMinStages = 4, kMaxStages = 8, kMinCodeSlots = 4, kMaxCodeSlots = 16;
+constexpr int kScaleSlots = 8;                   // blocks whose scales are kept: more than the operand ring holds
+constexpr int kPacePolls = 64, kPacedBlocks = 8;
 constexpr float kRescaleLog2 = 8.0f;             // move a row's reference when its largest exponent grew by more
+constexpr float kFarReference = 1024.f;
 constexpr float kHeadroomLog2 = 7.0f;            // weights are 2^7 at the reference: at most 2^15 in f16
-constexpr int kPolyEvery = 4;                    // every fourth pair of exponentials as a polynomial (small ranks, see mq_attention_kernel)
 
 struct Args {
   mq::Args m;                    // layer, batch, rows, outputs, parts; m.nst and m.qp_bytes as there, the pools in m.L are unused
   f8::Pools P;
   const __nv_bfloat16* q;        // read directly where the key side has no basis
   long long q_stride_b, q_stride_t;
-  int n_code;                    // stages of the ring of codes
+  int n_code;                    // slots of the ring of codes
 };
 
-__host__ __device__ constexpr int code_stage_bytes(int rk, int rv) { return (kPage * (rk + rv) + f8::kScalesPerTile * 4 + 127) / 128 * 128; }
+// One stage of the operand ring: K or V of a block, half a raw query tile, or a basis; one slot of codes: one side of a page, and scales
+__host__ __device__ constexpr int stage_bytes(int rk, int rv) { return 256 * (rk > rv ? (rk > 64 ? rk : 64) : (rv > 64 ? rv : 64)); }
+__host__ __device__ constexpr int slot_bytes(int rk, int rv) { return kPage * (rk > rv ? rk : rv) + 128; }
 
 // instruction descriptors of kind::f16 with f16 operands (format 0) and fp32 accumulators; B K-major, or MN-major (bit 16)
 __device__ __forceinline__ uint32_t idesc_f16_f32(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
 __device__ __forceinline__ uint32_t idesc_f16_f32_bmn(int M, int N) { return idesc_f16_f32(M, N) | (1u << 16); }
+
+// A unit as every role derives it: pages and blocks.  With two streams over the same rows (dual) the tiles take alternate blocks.
+struct Unit : mq::Unit {
+  int blocks;                    // of the unit, in the ring
+  int nb[2];                     // of each tile
+  int last[2];                   // first position behind the pages that the tile's rows may attend in this unit
+};
+__device__ __forceinline__ Unit block_unit(const mq::Args& a, int u, int TT) {
+  Unit w;
+  static_cast<mq::Unit&>(w) = mq::decode_unit(a, u, TT);
+  w.blocks = (w.cnt + 1) >> 1;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    w.nb[t] = a.dual ? (w.blocks + 1 - t) >> 1 : (w.np[t] + 1) >> 1;
+    w.last[t] = (w.p_lo + (a.dual ? w.cnt : w.np[t])) * kPage;
+  }
+  return w;
+}
 
 template <int RK, int RV>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -65,28 +91,20 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - smem_u32(smem_raw));
   const int nst = a.nst, n_code = args.n_code;
-  constexpr int kCode = code_stage_bytes(RK, RV);
+  constexpr int kStage = stage_bytes(RK, RV), kSlot = slot_bytes(RK, RV);
+  constexpr bool kOwnP = RV <= 64;               // P has TMEM columns of its own
+  constexpr int kP = kOwnP ? 128 : 0, kO = kOwnP ? 192 : 128;
   const uint32_t ring = base;
-  const uint32_t qp = ring + nst * kStageBytes;                 // Q' / O_down operands, one region per tile
+  const uint32_t qp = ring + nst * kStage;                      // Q' / O_down operands, one region per tile
   const uint32_t codes = qp + 2 * a.qp_bytes;
-  const uint32_t ctrl = codes + n_code * kCode;
+  const uint32_t ctrl = codes + n_code * kSlot;
   uint8_t *qp_ptr = base_ptr + (qp - base), *codes_ptr = base_ptr + (codes - base), *ctrl_ptr = base_ptr + (ctrl - base);
-  auto full_bar = [&](int s) { return ctrl + s * 8; };
-  auto empty_bar = [&](int s) { return ctrl + (4 + s) * 8; };
-  auto s_full = [&](int t, int i) { return ctrl + (8 + t * 2 + i) * 8; };
-  auto p_full = [&](int t, int i) { return ctrl + (12 + t * 2 + i) * 8; };
-  auto p_free = [&](int t, int i) { return ctrl + (16 + t * 2 + i) * 8; };
-  auto qacc_full = [&](int t) { return ctrl + (20 + t) * 8; };
-  auto qp_ready = [&](int t) { return ctrl + (22 + t) * 8; };
-  auto o_full = [&](int t) { return ctrl + (24 + t) * 8; };
-  auto od_ready = [&](int t) { return ctrl + (26 + t) * 8; };
-  auto out_full = [&](int t) { return ctrl + (28 + t) * 8; };
-  auto unit_done = [&](int t) { return ctrl + (30 + t) * 8; };
-  auto code_full = [&](int s) { return ctrl + (32 + s) * 8; };
-  auto code_empty = [&](int s) { return ctrl + (40 + s) * 8; };
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + 48 * 8);
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 48 * 8 + 4);
-  volatile float2* page_scales = reinterpret_cast<volatile float2*>(ctrl_ptr + 50 * 8);     // [nst]: of the page in each operand stage
+  enum Bar { kFull = 0, kEmpty = 8, kCodeFull = 16, kCodeEmpty = 32, kSFull = 48, kSFree = 50, kPFull = 52, kPvDone = 56, kQacc = 58, kQReady = 60,
+             kOFull = 62, kOdReady = 64, kOutFull = 66, kUnitDone = 68, kBars = 70 };
+  auto bar_at = [&](int i) { return ctrl + i * 8; };
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + kBars * 8);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + kBars * 8 + 4);
+  float4* block_scales = reinterpret_cast<float4*>(ctrl_ptr + (kBars + 2) * 8);     // [kScaleSlots]: (key, value) of both pages
 
   const int G = a.L.G, Hkv = a.L.Hkv;
   const bool fold_k = a.L.U_k == nullptr, fold_v = a.L.U_v == nullptr;
@@ -96,32 +114,32 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   const bool backproj = !fold_v && a.n_split == 1;               // else the compressed (partial) result leaves the kernel
   int32_t* status = a.status;
 
+  launch_dependents();
   if (tid == 0) {
     for (int s = 0; s < kMaxStages; ++s) {
-      mbar_init(full_bar(s), 4);         // one arrival from each filling warp
-      mbar_init(empty_bar(s), 2);        // one arrival from each tile's issuer
+      mbar_init(bar_at(kFull + s), 4);            // one arrival from each filling warp
+      mbar_init(bar_at(kEmpty + s), 2);           // one arrival from each tile's issuer
     }
-    for (int s = 0; s < kMaxCodeStages; ++s) {
-      mbar_init(code_full(s), 1);
-      mbar_init(code_empty(s), 4);       // one arrival from each expanding warp
+    for (int s = 0; s < kMaxCodeSlots; ++s) {
+      mbar_init(bar_at(kCodeFull + s), 1);
+      mbar_init(bar_at(kCodeEmpty + s), 4);       // one arrival from each filling warp
     }
     for (int t = 0; t < 2; ++t) {
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(s_full(t, i), 1);
-        mbar_init(p_full(t, i), 4);       // one arrival per softmax warp of the tile
-        mbar_init(p_free(t, i), 1);
-      }
-      mbar_init(qacc_full(t), 1);
-      mbar_init(qp_ready(t), 4);
-      mbar_init(o_full(t), 1);
-      mbar_init(od_ready(t), 4);
-      mbar_init(out_full(t), 1);
-      mbar_init(unit_done(t), 4);
+      mbar_init(bar_at(kSFull + t), 1);
+      mbar_init(bar_at(kSFree + t), 4);           // one arrival per softmax warp of the tile
+      mbar_init(bar_at(kPFull + 2 * t), 4);
+      mbar_init(bar_at(kPFull + 2 * t + 1), 4);
+      mbar_init(bar_at(kPvDone + t), 1);
+      mbar_init(bar_at(kQacc + t), 1);
+      mbar_init(bar_at(kQReady + t), 4);
+      mbar_init(bar_at(kOFull + t), 1);
+      mbar_init(bar_at(kOdReady + t), 4);
+      mbar_init(bar_at(kOutFull + t), 1);
+      mbar_init(bar_at(kUnitDone + t), 4);
     }
     *abort_flag = 0;
     mbar_fence_init();
   }
-  launch_dependents();
   if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), mq::kTmemCols);
   tc_fence_before();
   __syncthreads();
@@ -129,41 +147,44 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   const uint32_t tmem_base = *tmem_slot;
   grid_dependency_wait();                                       // the setup above ran beside the kernel before; everything below reads its results
 
-  // ring items of a unit ahead of its pages, and in all
-  auto lead_of = [&](const mq::Unit& w) { return fold_k ? 0 : (w.np[0] > 0) + (w.np[1] > 0) + 1; };
-
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");       // 512 x 128 registers at launch = 256 x 168 + 128 x 88 + 128 x 88
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");       // 512 x 128 registers at launch = 256 x 176 + 128 x 80 + 128 x 80
     if (warp == 0) {
       // ---------------------------------------------------------------------------------------- codes of the pages
-      int cs = 0, use = 0;                                      // stage of the next page's codes, times it has been used
+      int cs = 0, use = 0;                                      // slot of the next codes, times it has been used
+      auto fetch = [&](const uint8_t* src, uint32_t bytes, const float* scales) {
+        if (use > 0) mbar_wait(bar_at(kCodeEmpty + cs), (use - 1) & 1, abort_flag, status);
+        const uint32_t dst = codes + cs * kSlot, bar = bar_at(kCodeFull + cs);
+        mbar_arrive_expect_tx(bar, bytes + (scales ? f8::kScalesPerTile * 4 : 0));
+        bulk_load_1d(dst, src, bytes, bar);
+        if (scales) bulk_load_1d(dst + kSlot - 128, scales, f8::kScalesPerTile * 4, bar);
+        if (++cs == n_code) {
+          cs = 0;
+          ++use;
+        }
+      };
       for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-        const mq::Unit w = mq::decode_unit(a, u, TT);
+        const Unit w = block_unit(a, u, TT);
         if (!w.valid) continue;
-        const int npmax = w.cnt;
         const int* bt = a.Bt.block_table + (size_t)w.b * a.Bt.max_pages;
-        int ids = lane < npmax ? bt[w.p_lo + lane] : 0;
-        for (int j0 = 0; j0 < npmax; j0 += 32) {
-          const int nxt = j0 + 32 + lane < npmax ? bt[w.p_lo + j0 + 32 + lane] : 0;    // the next batch, a batch ahead
-          const int cnt = min(32, npmax - j0);
-          for (int jj = 0; jj < cnt; ++jj) {
-            int pg = __shfl_sync(0xffffffffu, ids, jj);
+        int ids = lane < w.cnt ? bt[w.p_lo + lane] : 0;
+        for (int j0 = 0; j0 < w.cnt; j0 += 32) {
+          const int nxt = j0 + 32 + lane < w.cnt ? bt[w.p_lo + j0 + 32 + lane] : 0;    // the next batch, a batch ahead
+          const int cnt = min(32, w.cnt - j0);
+          for (int jj = 0; jj < cnt; jj += 2) {
+            int pg[2] = {__shfl_sync(0xffffffffu, ids, jj), __shfl_sync(0xffffffffu, ids, (jj + 1) & 31)};
             if (lane == 0) {
-              if (pg < 0 || pg >= a.L.num_pages) {
-                report(status, STIEF_ERR_BOUNDS);
-                pg = 0;
+              const int both = jj + 1 < cnt ? 2 : 1;
+              size_t tile[2];
+              for (int i = 0; i < both; ++i) {
+                if (pg[i] < 0 || pg[i] >= a.L.num_pages) {
+                  report(status, STIEF_ERR_BOUNDS);
+                  pg[i] = 0;
+                }
+                tile[i] = (size_t)pg[i] * Hkv + w.h;
               }
-              if (use > 0) mbar_wait(code_empty(cs), (use - 1) & 1, abort_flag, status);
-              const size_t tile = (size_t)pg * Hkv + w.h;
-              const uint32_t dst = codes + cs * kCode;
-              mbar_arrive_expect_tx(code_full(cs), kPage * (RK + RV) + f8::kScalesPerTile * 4);
-              bulk_load_1d(dst, args.P.k_codes + tile * (kPage * RK), kPage * RK, code_full(cs));
-              bulk_load_1d(dst + kPage * RK, args.P.v_codes + tile * (kPage * RV), kPage * RV, code_full(cs));
-              bulk_load_1d(dst + kPage * (RK + RV), args.P.scales + tile * f8::kScalesPerTile, f8::kScalesPerTile * 4, code_full(cs));
-              if (++cs == n_code) {
-                cs = 0;
-                ++use;
-              }
+              for (int i = 0; i < both; ++i) fetch(args.P.k_codes + tile[i] * (kPage * RK), kPage * RK, args.P.scales + tile[i] * f8::kScalesPerTile);
+              for (int i = 0; i < both; ++i) fetch(args.P.v_codes + tile[i] * (kPage * RV), kPage * RV, nullptr);
             }
           }
           ids = nxt;
@@ -174,142 +195,179 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       // Both issuers walk ALL ring items in order; an item one has no use for is released with a plain arrive once it has
       // landed, so each stage always collects two arrivals.
       const int mt = uniform(warp) - 1;
-      const uint32_t t_s = uniform(tmem_base) + mt * 256, t_o = t_s + 128;       // score buffers; Q' / O accumulator
+      const uint32_t t_s = uniform(tmem_base) + mt * 256, t_p = t_s + kP, t_o = t_s + kO;
       const uint32_t ring_u = uniform(ring), ctrl_u = uniform(ctrl), qp_u = uniform(qp) + mt * uniform(a.qp_bytes);
-      auto bar = [&](int i) { return ctrl_u + i * 8; };                          // as numbered above
-      const uint32_t id_qk = idesc_f16_f32(kRows, kPage), id_pv = idesc_f16_f32_bmn(kRows, RV);
+      auto bar = [&](int i) { return ctrl_u + i * 8; };
+      const uint32_t id_qk = idesc_f16_f32(kRows, kBlock), id_pv = idesc_f16_f32_bmn(kRows, RV);
       const uint32_t id_pj = idesc_bf16_f32_bmn(kRows, RK), id_bp = idesc_bf16_f32(kRows, kD);
       const uint32_t hi_k = desc_hi(desc_template(bk.layout, 16, 8 * bk.span)), hi_v = desc_hi(desc_template(bv.layout, 16, 8 * bv.span));
       const uint32_t hi_q = desc_hi(desc_template(2, 16, 1024));
       constexpr int nk = RK / 16, nv = RV / 16;
-      // descriptor offset (in 16-byte units) of K step k of a K-major operand: inside a block 2 units per step, then the next block
+      // descriptor offset (in 16-byte units) of K step k of a K-major operand of 128 rows: inside a block 2 units per step, then the
+      // next block
       const int lgk = bk.bw == 64 ? 2 : bk.bw == 32 ? 1 : 0, lgv = bv.bw == 64 ? 2 : bv.bw == 32 ? 1 : 0;
       auto koff = [](int k, int lg, uint32_t blk) { return (uint32_t)(k >> lg) * blk + (uint32_t)(k & ((1 << lg) - 1)) * 2u; };
-      const uint32_t qblk = (uint32_t)(kRows * bk.span) >> 4, kblk = (uint32_t)(kPage * bk.span) >> 4, oblk = (uint32_t)(kRows * bv.span) >> 4;
-      const uint32_t pv_b = (uint32_t)(16 * bv.span) >> 4;                       // V page: 16 rows per K step
+      const uint32_t kblk = (uint32_t)(kRows * bk.span) >> 4, vblk = (uint32_t)(kRows * bv.span) >> 4;
+      const uint32_t pv_b = (uint32_t)(16 * bv.span) >> 4;                       // V block: 16 rows per K step
       const uint32_t dq = desc_lo(16, qp_u);                                     // this tile's Q' operand, and its O_down operand
-      int st = 0, use = 0, kt = 0, pn = 0;
       const int nst_u = uniform(nst);
+      const bool dual = uniform(a.dual) != 0, fold_k_u = uniform((int)fold_k) != 0, backproj_u = uniform((int)backproj) != 0;
+      int st = 0, use = 0, kt = 0, n = 0, others = 0;                            // n: blocks of this tile so far; of the other tile
       auto consume = [&](uint32_t& addr, int& stage) {                           // next item of the ring, once it has landed
-        mbar_wait_warp(bar(st), use & 1, abort_flag, status);
-        addr = ring_u + st * kStageBytes;
+        mbar_wait_warp(bar(kFull + st), use & 1, abort_flag, status);
+        addr = ring_u + st * kStage;
         stage = st;
         if (++st == nst_u) {
           st = 0;
           ++use;
         }
       };
-      auto drop = [&](int stage) {                                               // an item this tile has no use for
-        if (lane == 0) mbar_arrive(bar(4 + stage));
-        __syncwarp();
-      };
-      const bool dual = uniform(a.dual) != 0, fold_k_u = uniform((int)fold_k) != 0, backproj_u = uniform((int)backproj) != 0;
-      for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-        const mq::Unit w = mq::decode_unit(a, u, TT);
-        if (uniform((int)w.valid) == 0) continue;
-        const int wnp0 = uniform(w.np[0]), wnp1 = uniform(w.np[1]), npmax = uniform(w.cnt);
-        const int np = mt ? wnp1 : wnp0;
-        const bool active = np > 0;
-        if (!fold_k_u) {
-          uint32_t qa = 0, ua, tmp;
-          int qs = 0, us, ts;
-          if (wnp0 > 0) {                                                        // tile 0's raw queries
-            if (mt == 0) consume(qa, qs);
-            else { consume(tmp, ts); drop(ts); }
-          }
-          if (wnp1 > 0) {                                                        // tile 1's
-            if (mt == 1) consume(qa, qs);
-            else { consume(tmp, ts); drop(ts); }
-          }
-          consume(ua, us);
-          if (active) {
-            if (kt > 0) mbar_wait_warp(bar(30 + mt), (kt - 1) & 1, abort_flag, status);   // the tile's accumulator columns are free
-            tc_fence_after();
-            const uint32_t da = desc_lo(16, qa), db = desc_lo(kD * bk.span, ua);
-#pragma unroll
-            for (int k = 0; k < kD / 16; ++k)
-              umma_ss(t_o, da + (uint32_t)(((k >> 2) * (kStageBytes / 2) + (k & 3) * 32) >> 4), hi_q, db + (uint32_t)(k * bk.span), hi_k, id_pj, k > 0 ? 1u : 0u);
-            umma_commit_warp(bar(20 + mt));
-            umma_commit_warp(bar(4 + qs));
-            umma_commit_warp(bar(4 + us));
-          } else {
-            drop(us);
-          }
-        }
-        if (active) mbar_wait_warp(bar(22 + mt), kt & 1, abort_flag, status);
-        tc_fence_after();
-
-        // jo counts this tile's own pages within the unit (every page it shares with the other tile, or every second page of
-        // the range when the tiles run as two streams over the same rows)
-        auto issue_pv = [&](int jo, uint32_t vaddr, int stage) {
-          const int n = pn + jo;
-          mbar_wait_warp(bar(12 + 2 * mt + (n & 1)), (n >> 1) & 1, abort_flag, status);
-          tc_fence_after();
-          const uint32_t pa = t_s + (n & 1) * 64;                                // P_n: f16 pairs in the score buffer's first 32 columns
-          const uint32_t db = desc_lo(kPage * bv.span, vaddr);
-#pragma unroll
-          for (int k = 0; k < kPage / 16; ++k) umma_ts(t_o, pa + 8 * k, db + (uint32_t)k * pv_b, hi_v, id_pv, (jo > 0 || k > 0) ? 1u : 0u);
-          umma_commit_warp(bar(16 + 2 * mt + (n & 1)));
-          umma_commit_warp(bar(4 + stage));                                      // K and V of this page are no longer needed by this tile
-        };
-        uint32_t prev_v = 0;
-        int prev_stage = 0, jo = 0;                                              // the page whose P V is still to be issued; own pages so far
-        for (int j = 0; j < npmax; ++j) {
-          uint32_t kaddr;
+      auto drop = [&](int items) {                                               // items this tile has no use for
+        for (int i = 0; i < items; ++i) {
+          uint32_t addr;
           int stage;
-          consume(kaddr, stage);
-          const bool mine = dual ? (j & 1) == mt : j < np;
-          if (!mine) {
-            drop(stage);
-            continue;
-          }
-          const int n = pn + jo;
-          if (n >= 2) mbar_wait_warp(bar(16 + 2 * mt + (n & 1)), ((n >> 1) - 1) & 1, abort_flag, status);   // P_(n-2), which sat in this buffer, has been consumed
-          tc_fence_after();
-          const uint32_t d_tmem = t_s + (n & 1) * 64, db = desc_lo(16, kaddr);
-#pragma unroll
-          for (int k = 0; k < nk; ++k) umma_ss(d_tmem, dq + koff(k, lgk, qblk), hi_k, db + koff(k, lgk, kblk), hi_k, id_qk, k > 0 ? 1u : 0u);
-          umma_commit_warp(bar(8 + 2 * mt + (n & 1)));
-          if (jo > 0) issue_pv(jo - 1, prev_v, prev_stage);
-          prev_v = kaddr + kPage * RK * 2;
-          prev_stage = stage;
-          ++jo;
+          consume(addr, stage);
+          if (lane == 0) mbar_arrive(bar(kEmpty + stage));
+          __syncwarp();
         }
-        if (jo > 0) issue_pv(jo - 1, prev_v, prev_stage);
-        if (active) umma_commit_warp(bar(24 + mt));
+      };
+      for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
+        const Unit w = block_unit(a, u, TT);
+        if (uniform((int)w.valid) == 0) continue;
+        const int nb0 = uniform(w.nb[0]), nb1 = uniform(w.nb[1]), blocks = uniform(w.blocks);
+        const int nb = mt ? nb1 : nb0;
+        const bool active = nb > 0;
+        if (!fold_k_u) {                                                         // each tile has U_k and its two halves of raw queries in the ring
+          if (mt == 1 && nb0 > 0) drop(3);
+          if (active) {
+            uint32_t ua, qa;
+            int us, qs;
+            consume(ua, us);
+            if (kt > 0) mbar_wait_warp(bar(kUnitDone + mt), (kt - 1) & 1, abort_flag, status);   // the tile's TMEM columns are free
+            const uint32_t db = desc_lo(kD * bk.span, ua);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              consume(qa, qs);
+              tc_fence_after();
+              const uint32_t da = desc_lo(16, qa);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                umma_ss(t_s, da + 2u * k, hi_q, db + (uint32_t)((4 * half + k) * bk.span), hi_k, id_pj, half + k > 0 ? 1u : 0u);
+              umma_commit_warp(bar(kEmpty + qs));
+            }
+            umma_commit_warp(bar(kQacc + mt));
+            umma_commit_warp(bar(kEmpty + us));
+          }
+          if (mt == 0 && nb1 > 0) drop(3);
+        }
+        if (active) {
+          mbar_wait_warp(bar(kQReady + mt), kt & 1, abort_flag, status);
+          tc_fence_after();
+        }
+        int jb = 0;                                                              // next block in the ring
+        auto to_own = [&]() {                                                    // past the blocks of the other tile; is there one of this tile's?
+          while (jb < blocks && !(dual ? (jb & 1) == mt : jb < nb)) {
+            drop(2);
+            ++jb;
+          }
+          return jb < blocks;
+        };
+        auto score = [&]() {                                                     // S = Q' K^T of block jb
+          uint32_t ka;
+          int ks;
+          consume(ka, ks);
+          tc_fence_after();
+          const uint32_t db = desc_lo(16, ka);
+#pragma unroll
+          for (int k = 0; k < nk; ++k) umma_ss(t_s, dq + koff(k, lgk, kblk), hi_k, db + koff(k, lgk, kblk), hi_k, id_qk, k > 0 ? 1u : 0u);
+          umma_commit_warp(bar(kSFull + mt));
+          umma_commit_warp(bar(kEmpty + ks));
+        };
+        // Tiles of their own rows have their scores issued in turn, each when the other's last have been read: the softmax of one then
+        // loads and looks for its maximum while the other's has the special-function units.  Only pace, not order: the look has an
+        // end, and a wrong answer (a parity is one bit) costs nothing but the shift.
+        const int theirs = mt ? nb0 : nb1;
+        const bool paced = kOwnP && !dual && nb0 >= kPacedBlocks && nb1 >= kPacedBlocks;
+        auto pace = [&](int block) {
+          if (!paced || block >= theirs) return;
+          for (int i = 0; i < kPacePolls && !__all_sync(0xffffffffu, mbar_test_wait(bar(kSFree + 1 - mt), (others + block) & 1)); ++i) {
+          }
+        };
+        bool have = to_own(), first = true;
+        int own = 0;                                                             // blocks of this tile in the unit so far
+        if (have) {
+          if (mt == 1) pace(0);
+          score();
+        }
+        while (have) {
+          uint32_t va;
+          int vs;
+          consume(va, vs);
+          ++jb;
+          bool more = false;
+          if constexpr (kOwnP) {
+            more = to_own();
+            if (more) {
+              mbar_wait_warp(bar(kSFree + mt), n & 1, abort_flag, status);       // the scores of block n are in registers
+              pace(own + mt);
+              tc_fence_after();
+              score();
+            }
+          }
+          const uint32_t db = desc_lo(kBlock * bv.span, va);
+#pragma unroll
+          for (int k = 0; k < kBlock / 16; ++k) {
+            if (k == 0 || k == 4) {
+              mbar_wait_warp(bar(kPFull + 2 * mt + (k >> 2)), n & 1, abort_flag, status);
+              tc_fence_after();
+            }
+            umma_ts(t_o, t_p + 8 * k, db + (uint32_t)k * pv_b, hi_v, id_pv, (!first || k > 0) ? 1u : 0u);
+          }
+          umma_commit_warp(bar(kPvDone + mt));
+          umma_commit_warp(bar(kEmpty + vs));
+          first = false;
+          ++n;
+          ++own;
+          if constexpr (!kOwnP) {
+            more = to_own();
+            if (more) score();
+          }
+          have = more;
+        }
+        if (active) umma_commit_warp(bar(kOFull + mt));
         if (backproj_u) {
           // OUT = O_down U_v^T with O_down handed over as two bf16 terms (value, then residual): two accumulating passes into the
           // tile's score columns, which are idle by now
-          uint32_t ua;
-          int us;
-          consume(ua, us);
           if (active) {
+            uint32_t ua;
+            int us;
+            consume(ua, us);
             const uint32_t db = desc_lo(16, ua);
             for (int pass = 0; pass < 2; ++pass) {
-              mbar_wait_warp(bar(26 + mt), pass, abort_flag, status);
+              mbar_wait_warp(bar(kOdReady + mt), pass, abort_flag, status);
               tc_fence_after();
 #pragma unroll
-              for (int k = 0; k < nv; ++k) umma_ss(t_s, dq + koff(k, lgv, oblk), hi_v, db + koff(k, lgv, oblk), hi_v, id_bp, (pass > 0 || k > 0) ? 1u : 0u);
-              umma_commit_warp(bar(28 + mt));
+              for (int k = 0; k < nv; ++k) umma_ss(t_s, dq + koff(k, lgv, vblk), hi_v, db + koff(k, lgv, vblk), hi_v, id_bp, (pass > 0 || k > 0) ? 1u : 0u);
+              umma_commit_warp(bar(kOutFull + mt));
             }
-            umma_commit_warp(bar(4 + us));
+            umma_commit_warp(bar(kEmpty + us));
           } else {
-            drop(us);
+            drop(1);
           }
         }
-        pn += np;
         kt += active;
+        others += theirs;
       }
     }
   } else if (warp >= 12) {
-    // ------------------------------------------------------------------------------------------ expansion of the pages
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    // ------------------------------------------------------------------------------------------ the ring of operands
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     const int et = tid - 12 * 32;                               // 0 .. 127
-    int st = 0, use = 0, cs = 0, cuse = 0;
-    // All items of the operand ring are filled from here, in order (whoever waits for a stage has seen every earlier phase of its
-    // barrier): raw queries and bases are TMA loads that one thread issues.
+    int st = 0, use = 0, cs = 0, cuse = 0, blk = 0;
+    // All items are filled from here, in order (whoever waits for a stage has seen every earlier phase of its barrier): raw queries
+    // and bases are TMA loads that one thread issues.
     auto acquire = [&]() {
-      if (use > 0) mbar_wait(empty_bar(st), (use - 1) & 1, abort_flag, status);
+      if (use > 0) mbar_wait(bar_at(kEmpty + st), (use - 1) & 1, abort_flag, status);
     };
     auto advance = [&]() {
       if (++st == nst) {
@@ -322,14 +380,72 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       __syncwarp();
       if (lane == 0) {
         if (warp == 12) {
-          mbar_arrive_expect_tx(full_bar(st), bytes);
-          issue(ring + st * kStageBytes, full_bar(st));
+          mbar_arrive_expect_tx(bar_at(kFull + st), bytes);
+          issue(ring + st * kStage, bar_at(kFull + st));
         } else {
-          mbar_arrive(full_bar(st));
+          mbar_arrive(bar_at(kFull + st));
         }
       }
       advance();
     };
+    auto named_barrier = [&]() { asm volatile("bar.sync 1, 128;" ::: "memory"); };      // of the four warps
+    auto publish = [&]() {                                      // the stage is written
+      fence_proxy_async_smem();                                 // generic writes -> visible to the tensor core's reads
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_at(kFull + st));
+      advance();
+    };
+    // One side of a block: codes of the next one or two slots -> the current stage.  A thread has the same pieces of 16 codes of every
+    // page, 64 R / 16 of them over 128 threads: `off` is where a piece's first 8 values go in the block, the other 8 go to the
+    // neighbouring 16 bytes, the second page 64 rows on.  Rows from `live` on are written as zeros (also those of a second page
+    // that is not there: its weights are zeros).
+    auto expand = [&](auto rank_tag, const auto& off, uint32_t page_bytes, int pages, int live, float2* scales) {
+      constexpr int R = decltype(rank_tag)::value, NP = (R * 4 + 127) / 128;
+      acquire();
+      uint8_t* dst = base_ptr + st * kStage;
+#pragma unroll 1
+      for (int pg = 0; pg < pages; ++pg) {
+        const uint8_t* src = codes_ptr + cs * kSlot;
+        mbar_wait(bar_at(kCodeFull + cs), cuse & 1, abort_flag, status);
+        uint4 w[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+          if (R % 32 == 0 || et + 128 * i < R * 4) w[i] = reinterpret_cast<const uint4*>(src)[et + 128 * i];
+        if (scales) scales[pg] = *reinterpret_cast<const float2*>(src + kSlot - 128);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          if (R % 32 == 0 || et + 128 * i < R * 4) {
+            uint4 lo, hi;
+            f8::expand4(w[i].x, lo.x, lo.y);
+            f8::expand4(w[i].y, lo.z, lo.w);
+            f8::expand4(w[i].z, hi.x, hi.y);
+            f8::expand4(w[i].w, hi.z, hi.w);
+            *reinterpret_cast<uint4*>(dst + off[i]) = lo;
+            *reinterpret_cast<uint4*>(dst + (off[i] ^ 16u)) = hi;
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_at(kCodeEmpty + cs));
+        if (++cs == n_code) {
+          cs = 0;
+          ++cuse;
+        }
+        dst += page_bytes;
+      }
+      if (live < kBlock) {
+        const Blocks bl = blocks_of(R);
+        dst = base_ptr + st * kStage;
+        named_barrier();                                        // other threads' values are in place before they are overwritten
+#pragma unroll 1
+        for (int e = et; e < (kBlock - live) * (R / 8); e += 128)
+          *reinterpret_cast<uint4*>(dst + block_offset(bl, kBlock, live + e / (R / 8), e % (R / 8) * 8)) = make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    uint32_t k_off[(RK * 4 + 127) / 128], v_off[(RV * 4 + 127) / 128];
+#pragma unroll
+    for (int i = 0; i < (RK * 4 + 127) / 128; ++i) k_off[i] = block_offset(bk, kBlock, (et + 128 * i) / (RK / 16), (et + 128 * i) % (RK / 16) * 16);
+#pragma unroll
+    for (int i = 0; i < (RV * 4 + 127) / 128; ++i) v_off[i] = block_offset(bv, kBlock, (et + 128 * i) / (RV / 16), (et + 128 * i) % (RV / 16) * 16);
     if (et == 0) {
       if (!fold_k) {
         tma_prefetch_desc(&tmQ);
@@ -338,78 +454,28 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       if (backproj) tma_prefetch_desc(&tmUv);
     }
     for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-      const mq::Unit w = mq::decode_unit(a, u, TT);
+      const Unit w = block_unit(a, u, TT);
       if (!w.valid) continue;
       if (!fold_k) {
         for (int t = 0; t < 2; ++t) {
-          if (w.np[t] == 0) continue;
-          load((uint32_t)(TT * G) * kD * 2, [&](uint32_t dst, uint32_t bar) {
-            tma_load_4d(dst, &tmQ, 0, w.h * G, w.tok0[t], w.b, bar);
-            tma_load_4d(dst + kStageBytes / 2, &tmQ, 64, w.h * G, w.tok0[t], w.b, bar);
+          if (w.nb[t] == 0) continue;
+          load(kD * RK * 2, [&](uint32_t dst, uint32_t bar) {
+            for (int i = 0; i < bk.nb; ++i) tma_load_3d(dst + i * kD * bk.span, &tmUk, i * bk.bw, 0, a.L.uk_stride ? w.h : 0, bar);
           });
+          for (int half = 0; half < 2; ++half)
+            load((uint32_t)(TT * G) * kD, [&](uint32_t dst, uint32_t bar) { tma_load_4d(dst, &tmQ, 64 * half, w.h * G, w.tok0[t], w.b, bar); });
         }
-        load(kD * RK * 2, [&](uint32_t dst, uint32_t bar) {
-          for (int i = 0; i < bk.nb; ++i) tma_load_3d(dst + i * kD * bk.span, &tmUk, i * bk.bw, 0, a.L.uk_stride ? w.h : 0, bar);
-        });
       }
-      for (int j = 0; j < w.cnt; ++j) {
-        const int live = w.seq_len - (w.p_lo + j) * kPage;      // rows of the page that belong to the sequence (64 or more: all)
-        mbar_wait(code_full(cs), cuse & 1, abort_flag, status);
-        const uint8_t* src = codes_ptr + cs * kCode;
-        constexpr int NK = (RK * 4 + 127) / 128, NV = (RV * 4 + 127) / 128;
-        static_assert(NK <= 4 && NV <= 4, "pieces per thread");
-        uint4 kq[NK], vq[NV];
-#pragma unroll
-        for (int i = 0; i < NK; ++i)
-          if (RK % 32 == 0 || et + 128 * i < RK * 4) kq[i] = reinterpret_cast<const uint4*>(src)[et + 128 * i];
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (RV % 32 == 0 || et + 128 * i < RV * 4) vq[i] = reinterpret_cast<const uint4*>(src + kPage * RK)[et + 128 * i];
-        float2 sc = make_float2(0.f, 0.f);
-        if (et == 0) sc = *reinterpret_cast<const float2*>(src + kPage * (RK + RV));
-        acquire();
-        uint8_t* dst = base_ptr + st * kStageBytes;
-        auto expand = [&](const uint4& q, uint4& lo, uint4& hi) {
-          lo = make_uint4(f8::e4m3x2_to_f16x2(q.x & 0xffffu), f8::e4m3x2_to_f16x2(q.x >> 16), f8::e4m3x2_to_f16x2(q.y & 0xffffu), f8::e4m3x2_to_f16x2(q.y >> 16));
-          hi = make_uint4(f8::e4m3x2_to_f16x2(q.z & 0xffffu), f8::e4m3x2_to_f16x2(q.z >> 16), f8::e4m3x2_to_f16x2(q.w & 0xffffu), f8::e4m3x2_to_f16x2(q.w >> 16));
-        };
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-          const int piece = et + 128 * i, row = piece / (RK / 16), c = piece % (RK / 16) * 16;
-          if (RK % 32 == 0 || piece < RK * 4) {
-            uint4 lo, hi;
-            expand(kq[i], lo, hi);
-            *reinterpret_cast<uint4*>(dst + block_offset(bk, kPage, row, c)) = lo;
-            *reinterpret_cast<uint4*>(dst + block_offset(bk, kPage, row, c + 8)) = hi;
-          }
-        }
-        dst += kPage * RK * 2;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          const int piece = et + 128 * i, row = piece / (RV / 16), c = piece % (RV / 16) * 16;
-          if (RV % 32 == 0 || piece < RV * 4) {
-            uint4 lo, hi;
-            expand(vq[i], lo, hi);
-            if (row >= live) lo = hi = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4*>(dst + block_offset(bv, kPage, row, c)) = lo;
-            *reinterpret_cast<uint4*>(dst + block_offset(bv, kPage, row, c + 8)) = hi;
-          }
-        }
-        if (et == 0) {
-          page_scales[st].x = sc.x;
-          page_scales[st].y = sc.y;
-        }
-        fence_proxy_async_smem();                               // generic writes -> visible to the tensor core's reads
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(full_bar(st));
-          mbar_arrive(code_empty(cs));
-        }
-        advance();
-        if (++cs == n_code) {
-          cs = 0;
-          ++cuse;
-        }
+      for (int jb = 0; jb < w.blocks; ++jb, ++blk) {
+        const bool both = 2 * jb + 1 < w.cnt;
+        const int live = w.seq_len - (w.p_lo + 2 * jb) * kPage;             // rows of the block that belong to the sequence
+        const int pages = both ? 2 : 1;
+        float2 sc[2] = {make_float2(1.f, 1.f), make_float2(1.f, 1.f)};
+        expand(std::integral_constant<int, RK>{}, k_off, kPage * bk.span, pages, kBlock, sc);      // keys: positions that nobody attends are masked
+        if (et == 0) block_scales[blk % kScaleSlots] = make_float4(sc[0].x, sc[0].y, sc[1].x, sc[1].y);
+        publish();
+        expand(std::integral_constant<int, RV>{}, v_off, kPage * bv.span, pages, min(live, pages * kPage), nullptr);
+        publish();
       }
       if (backproj)
         load(kD * RV * 2, [&](uint32_t dst, uint32_t bar) {
@@ -418,32 +484,30 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
     }
   } else {
     // ------------------------------------------------------------------------------------------ softmax / epilogue
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     const int t = (warp - 4) >> 2;                              // the tile this warp works for
     const int q4 = warp & 3;                                    // TMEM lane quarter this warp may access
     const int row = 32 * q4 + lane;                             // row of the tile = TMEM lane
-    const uint32_t t_lane = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256;
-    const uint32_t t_out = t_lane + 128;                        // Q' / O columns
+    const uint32_t t_s = tmem_base + ((uint32_t)(32 * q4) << 16) + t * 256, t_p = t_s + kP, t_o = t_s + kO;
     uint8_t* my_qp = qp_ptr + t * a.qp_bytes;
     const float c = kLog2e * rsqrtf((float)kD);                 // scores are scaled by 1/sqrt(d_h); exponent in base 2
     const int d_out = fold_v ? RV : kD;
-    int kt = 0, pn = 0;
-    int item = 0;                                               // ring items issued before the current unit
+    int kt = 0, n = 0, blk = 0;                                 // units and blocks of this tile so far; blocks of the ring before the unit
     auto arrive_warp = [&](uint32_t bar) {                      // after every lane's shared/TMEM accesses are ordered
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
     for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-      const mq::Unit w = mq::decode_unit(a, u, TT);
+      const Unit w = block_unit(a, u, TT);
       if (!w.valid) continue;
-      const int lead = lead_of(w);
-      const int item0 = item + lead;
-      item += lead + w.cnt + (backproj ? 1 : 0);
-      if (w.np[t] == 0) continue;
-      const int np = w.np[t];
+      const int blk0 = blk;
+      blk += w.blocks;
+      if (w.nb[t] == 0) continue;
+      const int nb = w.nb[t];
       const int tok = w.tok0[t] + row / G, g = row - (row / G) * G;
       const bool row_valid = tok < w.q_len && row < TT * G;
-      const int q_pos = w.q_start + min(tok, w.q_len - 1);      // rows past the end behave like the last valid token
+      // first position that the row does not attend; rows past the end behave like the last valid token
+      const int end = min(w.q_start + min(tok, w.q_len - 1) + 1, w.last[t]);
 
       // ---- Q' as f16 into the A operand of the score products, each row scaled by a power of two of its own
       float c_row;
@@ -464,12 +528,12 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
               x[2 * i + 1] = bf16_hi(v[i]);
             }
           } else {
-            tmem_ld16(t_out + c0, *reinterpret_cast<uint32_t(*)[16]>(&x));
+            tmem_ld16(t_s + c0, *reinterpret_cast<uint32_t(*)[16]>(&x));
             tmem_ld_wait();
           }
         };
         if (!fold_k) {
-          mbar_wait(qacc_full(t), kt & 1, abort_flag, status);
+          mbar_wait(bar_at(kQacc + t), kt & 1, abort_flag, status);
           tc_fence_after();
         }
         for (int c0 = 0; c0 < RK; c0 += 16) {
@@ -486,109 +550,119 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           piece(c0, x);
           uint32_t pk[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const __half2 v = __floats2half2_rn(x[2 * i] * norm, x[2 * i + 1] * norm);
-            pk[i] = *reinterpret_cast<const uint32_t*>(&v);
-          }
+          for (int i = 0; i < 8; ++i) pk[i] = f8::pack_f16(x[2 * i] * norm, x[2 * i + 1] * norm);
           *reinterpret_cast<uint4*>(my_qp + block_offset(bk, kRows, row, c0)) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
           *reinterpret_cast<uint4*>(my_qp + block_offset(bk, kRows, row, c0 + 8)) = make_uint4(pk[4], pk[5], pk[6], pk[7]);
         }
         fence_proxy_async_smem();
         tc_fence_before();
-        arrive_warp(qp_ready(t));
+        arrive_warp(bar_at(kQReady + t));
       }
 
       float m_ref = -INFINITY, l = 0.f;                         // the largest exponent when the reference was last set; row sum
-      int stg = (item0 + (a.dual ? t : 0)) % nst;               // operand stage of the next page
-      for (int jo = 0; jo < np; ++jo) {
-        const int j = a.dual ? 2 * jo + t : jo;                 // the page within the unit's range
-        const int n = pn + jo, sb = n & 1;
-        mbar_wait(s_full(t, sb), (n >> 1) & 1, abort_flag, status);
+      for (int jo = 0; jo < nb; ++jo, ++n) {
+        const int j = a.dual ? 2 * jo + t : jo;                 // the block within the unit's range
+        mbar_wait(bar_at(kSFull + t), n & 1, abort_flag, status);
         tc_fence_after();
-        uint32_t sv[64];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld16(t_lane + sb * 64 + i * 16, *reinterpret_cast<uint32_t(*)[16]>(&sv[16 * i]));
-        // written before the arrival that these scores' product waited for; the stage is not refilled before P is handed over
-        const float ks = page_scales[stg].x, vs = page_scales[stg].y;
-        stg += a.dual ? 2 : 1;
-        while (stg >= nst) stg -= nst;
-        tmem_ld_wait();
+        uint32_t sv[kBlock];
         float* s = reinterpret_cast<float*>(sv);
-        const int p0 = (w.p_lo + j) * kPage;
-        const bool edge = p0 + kPage - 1 > q_pos;
-        if (edge) {                                             // a boundary page: positions after the row's own are masked
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (p0 + i > q_pos) s[i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32 * i, sv + 32 * i);
+        // written before the arrival that these scores' product waited for; overwritten eight blocks on
+        const float4 sc = block_scales[(blk0 + j) % kScaleSlots];
+        tmem_ld_wait();
+        if constexpr (kOwnP) {
+          tc_fence_before();
+          arrive_warp(bar_at(kSFree + t));
         }
-        float mx0 = max3(s[0], s[1], s[2]), mx1 = max3(s[3], s[4], s[5]);     // two chains of three-input maxima
+        const int p0 = (w.p_lo + 2 * j) * kPage;
+        const bool edge = p0 + kBlock > end;
+        if (edge) {                                             // positions after the row's own, and pages that are not in the unit
 #pragma unroll
-        for (int i = 6; i < 62; i += 4) {
-          mx0 = max3(mx0, s[i], s[i + 1]);
-          mx1 = max3(mx1, s[i + 2], s[i + 3]);
+          for (int i = 0; i < kBlock; ++i)
+            if (p0 + i >= end) s[i] = -INFINITY;
         }
-        const float f = fmaxf(c_row * ks, 1e-37f);              // above zero: masked scores stay -inf
-        const int ev = min(max((int)((__float_as_uint(vs) >> 23) & 255u) - 127, -126), 126);
-        const float mx = fmaf(fmaxf(max3(mx0, s[62], s[63]), mx1), f, (float)ev);     // the rounded exponents are what the reference goes by
+        // exponents x = s f + e of the two pages; f is above zero, so that masked scores stay -inf
+        const float f0 = fmaxf(c_row * sc.x, 1e-37f), f1 = fmaxf(c_row * sc.z, 1e-37f);
+        const int e0 = min(max((int)((__float_as_uint(sc.y) >> 23) & 255u) - 127, -126), 126), e1 = min(max((int)((__float_as_uint(sc.w) >> 23) & 255u) - 127, -126), 126);
+        float mx;
+        {
+          float m[4] = {s[0], s[1], s[64], s[65]};
+#pragma unroll
+          for (int i = 2; i < 62; i += 4)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              m[2 * h] = max3(m[2 * h], s[64 * h + i], s[64 * h + i + 1]);
+              m[2 * h + 1] = max3(m[2 * h + 1], s[64 * h + i + 2], s[64 * h + i + 3]);
+            }
+          mx = fmaxf(fmaf(fmaxf(max3(m[0], s[62], s[63]), m[1]), f0, (float)e0), fmaf(fmaxf(max3(m[2], s[126], s[127]), m[3]), f1, (float)e1));
+        }
+        // P and the accumulator are idle once the block before is mixed (with P over the scores, these scores came after that)
+        auto mixed = [&]() {
+          if constexpr (kOwnP) {
+            if (n > 0) {
+              mbar_wait(bar_at(kPvDone + t), (n - 1) & 1, abort_flag, status);
+              tc_fence_after();
+            }
+          }
+        };
         if (jo == 0) {
           m_ref = mx;                                           // -inf when a part of a split range begins behind the row's position
         } else if (__any_sync(0xffffffffu, mx - m_ref > kRescaleLog2)) {
-          mbar_wait(p_free(t, (n - 1) & 1), ((n - 1) >> 1) & 1, abort_flag, status);   // every earlier update of O is complete
-          tc_fence_after();
+          mixed();
           const bool grown = mx - m_ref > kRescaleLog2;         // a row's bits do not depend on its neighbours
           const float r = grown ? fast_exp2(m_ref - mx) : 1.f;
           l *= r;
           if (grown) m_ref = mx;
           for (int c0 = 0; c0 < RV; c0 += 16) {
             uint32_t v[16];
-            tmem_ld16(t_out + c0, v);
+            tmem_ld16(t_o + c0, v);
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * r);
-            tmem_st16(t_out + c0, v);
+            tmem_st16(t_o + c0, v);
           }
           tmem_st_wait();
         }
         const float ref = m_ref > -INFINITY ? m_ref - kHeadroomLog2 : 0.f;
-        const uint64_t f2 = pack2(f, f), ev2 = pack2((float)ev, (float)ev), ref2 = pack2(-ref, -ref);
-        uint64_t sum2 = pack2(0.f, 0.f);
-        uint32_t pk[32];
-        // Part of the pairs go to the FMA pipe as a polynomial where the exponentials set the pace (small ranks); it cannot
-        // return an exact zero, so a page on which some row of the warp has masked positions takes the special-function unit.
-        auto exponentials = [&](auto poly_tag) {
-          constexpr bool kPoly = decltype(poly_tag)::value;
+        // Exponents x - ref as one fma with e - ref where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
+        // rounded x is what counts, less the reference.  A page at a time: its weights are mixed while the next one's are made.
+        auto weights = [&](auto far_tag) {
+          constexpr bool kFar = decltype(far_tag)::value;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float x0, x1, e0, e1;
-            unpack2(add2(fma2(pack2(s[2 * i], s[2 * i + 1]), f2, ev2), ref2), x0, x1);
-            if (kPoly && (i % kPolyEvery) == 0) {
-              exp2_pair_fma(pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f)), e0, e1);
-            } else {
-              e0 = fast_exp2(x0);
-              e1 = fast_exp2(x1);
+          for (int h = 0; h < 2; ++h) {
+            const float f = h ? f1 : f0, e = (float)(h ? e1 : e0), shift = kFar ? e : e - ref;
+            const uint64_t f2 = pack2(f, f), e2 = pack2(shift, shift), ref2 = pack2(-ref, -ref);
+            uint64_t sum2 = pack2(0.f, 0.f);
+            uint32_t pk[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              uint64_t x2 = fma2(pack2(s[64 * h + 2 * i], s[64 * h + 2 * i + 1]), f2, e2);
+              if constexpr (kFar) x2 = add2(x2, ref2);
+              float x0, x1;
+              unpack2(x2, x0, x1);
+              x0 = fast_exp2(x0);
+              x1 = fast_exp2(x1);
+              sum2 = add2(sum2, pack2(x0, x1));
+              pk[i] = f8::pack_f16(x0, x1);
             }
-            sum2 = add2(sum2, pack2(e0, e1));
-            const __half2 v = __floats2half2_rn(e0, e1);
-            pk[i] = *reinterpret_cast<const uint32_t*>(&v);
+            if (h == 0) mixed();
+            tmem_st16(t_p + 32 * h, *reinterpret_cast<uint32_t(*)[16]>(&pk[0]));
+            tmem_st16(t_p + 32 * h + 16, *reinterpret_cast<uint32_t(*)[16]>(&pk[16]));
+            float a0, a1;
+            unpack2(sum2, a0, a1);
+            l = fmaf(a0 + a1, f8::pow2(h ? -e1 : -e0), l);
+            tmem_st_wait();
+            tc_fence_before();
+            arrive_warp(bar_at(kPFull + 2 * t + h));
           }
         };
-        if ((RK + RV <= 160) && !__any_sync(0xffffffffu, edge)) exponentials(std::true_type{});
-        else exponentials(std::false_type{});
-        {
-          float a0, a1;
-          unpack2(sum2, a0, a1);
-          l = fmaf(a0 + a1, f8::pow2(-ev), l);
-        }
-        // P_n replaces the scores in TMEM: f16 pairs in the first 32 columns of the buffer, where the P V product reads its A operand
-        tmem_st16(t_lane + sb * 64, *reinterpret_cast<uint32_t(*)[16]>(&pk[0]));
-        tmem_st16(t_lane + sb * 64 + 16, *reinterpret_cast<uint32_t(*)[16]>(&pk[16]));
-        tmem_st_wait();
-        tc_fence_before();
-        arrive_warp(p_full(t, sb));
+        if (__any_sync(0xffffffffu, fabsf(ref) > kFarReference)) weights(std::true_type{});
+        else weights(std::false_type{});
       }
 
       // ---- epilogue of the unit
-      mbar_wait(o_full(t), kt & 1, abort_flag, status);
+      mbar_wait(bar_at(kOFull + t), kt & 1, abort_flag, status);
       tc_fence_after();
       const float ref = m_ref - kHeadroomLog2;
       const float inv = 1.0f / l;
@@ -598,7 +672,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         const size_t prow = (((size_t)w.b * a.n_q + tok) * a.L.Hq + w.h * G + g) * a.n_parts + (a.dual ? 2 * w.split + t : w.split);
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16];
-          tmem_ld16(t_out + c0, v);
+          tmem_ld16(t_o + c0, v);
           tmem_ld_wait();
           if (row_valid) {
             float4* dst = reinterpret_cast<float4*>(a.part_o + prow * RV + c0);
@@ -611,7 +685,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       } else if (fold_v) {
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16], pk[8];
-          tmem_ld16(t_out + c0, v);
+          tmem_ld16(t_o + c0, v);
           tmem_ld_wait();
           pack16(v, inv, pk);
           if (row_valid) {
@@ -625,7 +699,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         for (int pass = 0; pass < 2; ++pass) {
           for (int c0 = 0; c0 < RV; c0 += 16) {
             uint32_t v[16], pk[8];
-            tmem_ld16(t_out + c0, v);
+            tmem_ld16(t_o + c0, v);
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -639,13 +713,13 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           }
           fence_proxy_async_smem();
           tc_fence_before();
-          arrive_warp(od_ready(t));
-          mbar_wait(out_full(t), pass, abort_flag, status);     // the pass has read the operand (after the second: OUT is complete)
+          arrive_warp(bar_at(kOdReady + t));
+          mbar_wait(bar_at(kOutFull + t), pass, abort_flag, status);     // the pass has read the operand (after the second: OUT is complete)
           tc_fence_after();
         }
         for (int c0 = 0; c0 < kD; c0 += 16) {
           uint32_t v[16], pk[8];
-          tmem_ld16(t_lane + c0, v);
+          tmem_ld16(t_s + c0, v);
           tmem_ld_wait();
           pack16(v, 1.0f, pk);
           if (row_valid) {
@@ -657,8 +731,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       if (row_valid && a.out_lse && a.n_split == 1)
         a.out_lse[((size_t)w.b * a.n_q + tok) * a.L.Hq + w.h * G + g] = kLn2 * (ref + log2f(l));
       tc_fence_before();
-      arrive_warp(unit_done(t));                                // the tile's TMEM columns and operand region are free
-      pn += np;
+      arrive_warp(bar_at(kUnitDone + t));                       // the tile's TMEM columns and operand region are free
       ++kt;
     }
   }
@@ -666,6 +739,119 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tmem_dealloc(tmem_base, mq::kTmemCols);
+}
+
+// Merges the parts of a split page range (by their references), normalises, back-projects and writes the rows.  One block per
+// (token, KV head, sequence): its G query rows share U_v, eight at a time.  A part that had no block for the row's tile was
+// never written and is left out by redoing the range arithmetic of decode_unit.
+constexpr int kCombineThreads = 128, kCombineRows = 8, kMaxParts = 64;
+template <int kInstance>                                        // a template only so that the header can be included by several units
+__global__ void __launch_bounds__(kCombineThreads)
+f8_mq_combine_kernel(const mq::Args a) {
+  __shared__ float od[kCombineRows][kD], weight[kCombineRows][kMaxParts], total[kCombineRows];
+  launch_dependents();
+  grid_dependency_wait();
+  const int tok = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.L.G, RV = a.L.r_v, TT = kRows / G, NP = a.n_parts;
+  int ql = a.q_lens ? a.q_lens[b] : a.n_q;
+  ql = min(max(ql, 0), a.n_q);
+  const int sl = a.Bt.seq_lens[b], q_start = sl - ql;
+  if (tok >= ql || q_start < 0 || (sl - 1) / kPage + 1 > a.Bt.max_pages) return;
+  // pages of the row's tile and of the unit (both tiles), as decode_unit derives them
+  const int t2 = tok / (2 * TT), first = t2 * 2 * TT;
+  int full[2] = {0, 0};
+  for (int t = 0; t < 2; ++t)
+    if (first + t * TT < ql) full[t] = (q_start + min(first + (t + 1) * TT, ql) - 1) / kPage + 1;
+  const int all = max(full[0], full[1]), mine = full[(tok - first) / TT];
+  auto exists = [&](int i) {
+    const int sp = a.dual ? i >> 1 : i;
+    const int lo = (int)((long long)sp * all / a.n_split), hi = min((int)((long long)(sp + 1) * all / a.n_split), mine);
+    return a.dual ? (i & 1) < (hi - lo + 1) >> 1 : hi > lo;
+  };
+  const bool fold_v = a.L.U_v == nullptr;
+  const int d_out = fold_v ? RV : kD;
+  const __nv_bfloat16* Uv = fold_v ? nullptr : a.L.U_v + (size_t)h * a.L.uv_stride;
+  for (int g0 = 0; g0 < G; g0 += kCombineRows) {
+    const int ng = min(kCombineRows, G - g0);
+    const size_t row0 = ((size_t)b * a.n_q + tok) * a.L.Hq + h * G + g0;
+    __syncthreads();
+    for (int g = warp; g < ng; g += kCombineThreads / 32) {      // weights of the row's parts, two to a lane
+      const size_t prow = (row0 + g) * NP;
+      float m[2], l[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = lane + 32 * i;
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+        if (p < NP && exists(p)) {
+          const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (prow + p) * 2);
+          m[i] = ml.x;
+          l[i] = ml.y;
+        }
+      }
+      float M = fmaxf(m[0], m[1]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      float den = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float wgt = l[i] > 0.f || l[i] != l[i] ? fast_exp2(m[i] - M) : 0.f;        // a part that the row attends nothing of has l = 0
+        den += l[i] > 0.f || l[i] != l[i] ? l[i] * wgt : 0.f;
+        if (lane + 32 * i < NP) weight[g][lane + 32 * i] = wgt;
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+      if (lane == 0) {
+        total[g] = den;
+        if (a.out_lse) a.out_lse[row0 + g] = kLn2 * (M + log2f(den));
+      }
+    }
+    __syncthreads();
+    for (int e = tid; e < ng * RV / 4; e += kCombineThreads) {
+      const int g = e / (RV / 4), c = e % (RV / 4);
+      const float4* src = reinterpret_cast<const float4*>(a.part_o + (row0 + g) * NP * RV) + c;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int i = 0; i < NP; ++i) {
+        const float wgt = weight[g][i];
+        if (wgt != 0.f) {
+          const float4 v = src[(size_t)i * (RV / 4)];
+          x.x = fmaf(v.x, wgt, x.x);
+          x.y = fmaf(v.y, wgt, x.y);
+          x.z = fmaf(v.z, wgt, x.z);
+          x.w = fmaf(v.w, wgt, x.w);
+        }
+      }
+      const float inv = 1.f / total[g];
+      *reinterpret_cast<float4*>(&od[g][4 * c]) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    }
+    __syncthreads();
+    __nv_bfloat16* orow = a.out + (size_t)b * a.out_stride_b + (size_t)tok * a.out_stride_t + (size_t)(h * G + g0) * d_out;
+    if (fold_v) {
+      for (int e = tid; e < ng * RV; e += kCombineThreads) orow[e] = __float2bfloat16_rn(od[e / RV][e % RV]);
+    } else {                                                    // one output element per thread and row: row `tid` of U_v
+      const uint4* urow = reinterpret_cast<const uint4*>(Uv + (size_t)tid * RV);
+      float acc[kCombineRows] = {};
+#pragma unroll 4
+      for (int c8 = 0; c8 < RV / 8; ++c8) {
+        const uint4 u = urow[c8];
+        const uint32_t wv[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int g = 0; g < kCombineRows; ++g) {
+          if (g < ng) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[g] = fmaf(od[g][c8 * 8 + 2 * i], bf16_lo(wv[i]), acc[g]);
+              acc[g] = fmaf(od[g][c8 * 8 + 2 * i + 1], bf16_hi(wv[i]), acc[g]);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < kCombineRows; ++g)
+        if (g < ng) orow[(size_t)g * kD + tid] = __float2bfloat16_rn(acc[g]);
+    }
+  }
 }
 
 // What the host hands to a launcher: the argument block, the tensor maps, the launch shape.
