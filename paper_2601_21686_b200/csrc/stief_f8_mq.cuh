@@ -100,7 +100,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   const uint32_t ctrl = codes + n_code * kSlot;
   uint8_t *qp_ptr = base_ptr + (qp - base), *codes_ptr = base_ptr + (codes - base), *ctrl_ptr = base_ptr + (ctrl - base);
   enum Bar { kFull = 0, kEmpty = 8, kCodeFull = 16, kCodeEmpty = 32, kSFull = 48, kSFree = 50, kPFull = 52, kPvDone = 56, kQacc = 58, kQReady = 60,
-             kOFull = 62, kOdReady = 64, kOutFull = 66, kUnitDone = 68, kBars = 70 };
+             kOFull = 62, kOdReady = 64, kOutFull = 66, kUnitDone = 68, kTurn = 70, kBars = 72 };
   auto bar_at = [&](int i) { return ctrl + i * 8; };
   volatile int* abort_flag = reinterpret_cast<volatile int*>(ctrl_ptr + kBars * 8);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + kBars * 8 + 4);
@@ -136,6 +136,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       mbar_init(bar_at(kOdReady + t), 4);
       mbar_init(bar_at(kOutFull + t), 1);
       mbar_init(bar_at(kUnitDone + t), 4);
+      mbar_init(bar_at(kTurn + t), 1);
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -283,20 +284,21 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           umma_commit_warp(bar(kSFull + mt));
           umma_commit_warp(bar(kEmpty + ks));
         };
-        // Tiles of their own rows have their scores issued in turn, each when the other's last have been read: the softmax of one then
-        // loads and looks for its maximum while the other's has the special-function units.  Only pace, not order: the look has an
+        // Tiles of their own rows take turns: left alone they fall into step, want the special-function units at the same time and
+        // leave them idle at the same time.  With P in columns of its own a tile's scores are issued when the other's last have been
+        // read; with P over the scores, P V and the next scores of the two tiles alternate.  Only pace, not order: the look has an
         // end, and a wrong answer (a parity is one bit) costs nothing but the shift.
         const int theirs = mt ? nb0 : nb1;
-        const bool paced = kOwnP && !dual && nb0 >= kPacedBlocks && nb1 >= kPacedBlocks;
+        const bool paced = !dual && nb0 >= kPacedBlocks && nb1 >= kPacedBlocks;
         auto pace = [&](int block) {
-          if (!paced || block >= theirs) return;
-          for (int i = 0; i < kPacePolls && !__all_sync(0xffffffffu, mbar_test_wait(bar(kSFree + 1 - mt), (others + block) & 1)); ++i) {
+          if (!paced || block < 0 || block >= theirs) return;
+          for (int i = 0; i < kPacePolls && !__all_sync(0xffffffffu, mbar_test_wait(bar((kOwnP ? kSFree : kTurn) + 1 - mt), (others + block) & 1)); ++i) {
           }
         };
         bool have = to_own(), first = true;
         int own = 0;                                                             // blocks of this tile in the unit so far
         if (have) {
-          if (mt == 1) pace(0);
+          if (kOwnP && mt == 1) pace(0);
           score();
         }
         while (have) {
@@ -314,6 +316,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
               score();
             }
           }
+          if constexpr (!kOwnP) pace(own - 1 + mt);
           const uint32_t db = desc_lo(kBlock * bv.span, va);
 #pragma unroll
           for (int k = 0; k < kBlock / 16; ++k) {
@@ -331,6 +334,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           if constexpr (!kOwnP) {
             more = to_own();
             if (more) score();
+            if (lane == 0) mbar_arrive(bar(kTurn + mt));
+            __syncwarp();
           }
           have = more;
         }
