@@ -8,16 +8,17 @@
 //
 // One launch, two kinds of CTAs of 128 threads, all resident at once:
 //   rows of the cache  a CTA belongs to one (head, side) and keeps its basis as B fragments in registers (warp w: the 8-column
-//                      tiles w, w + 4, ...).  It walks the pages that the call touches: up to 64 rows of one page are loaded,
-//                      rotated in fp32 and left in shared memory as bf16 terms (value and residuals: 2 terms keep 16 significant
-//                      bits, far below the rounding to bf16; 3 keep fp32's 24, so that an e4m3 code is the one fp32 arithmetic
-//                      gives; values and unrotated keys are bf16 already), multiplied, and leave through shared memory as one
-//                      contiguous piece of the page.
+//                      tiles w, w + 4, ...).  It walks tiles of 64 row slots: up to 64 rows of one page, or fewer rows of several
+//                      pages (a decode batch has one row in each).  Rows arrive by cp.async a tile ahead, are rotated in fp32 and
+//                      left in shared memory as bf16 terms (value and residuals: 2 terms keep 16 significant bits, far below
+//                      the rounding to bf16; 3 keep fp32's 24, so that an e4m3 code is the one fp32 arithmetic gives;
+//                      values and unrotated keys are bf16 already), multiplied, and leave through shared memory as
+//                      contiguous pieces of the pages.
 //   queries            16 tokens x 8 heads at a time; a thread owns one eighth of a token's channels, so its cosines and sines
 //                      serve all 8 heads.
 //
-// The 8-bit cache: a CTA sees all rows that a page receives, so the block's scale is settled in one exchange between its
-// warps: the larger of the scale that the page's older rows have and the least power of two that holds the new rows.  When it
+// The 8-bit cache: a tile holds all rows that a page receives, so the block's scale is settled in one exchange between the
+// CTA's warps: the larger of the scale that the page's older rows have and the least power of two that holds the new rows.  When it
 // grows, the same CTA moves the older rows' codes.
 #include "stief_f8.cuh"
 #include "stief_host_util.h"
@@ -29,7 +30,12 @@ constexpr int kThreads = 128;
 constexpr int kRowBytes = kD * 2;                 // a row in shared memory: 16 chunks of 16 bytes, chunk c at place c ^ (row & 7)
 constexpr int kTermBytes = kPage * kRowBytes;
 constexpr int kTokQ = 16, kHeadsQ = 8;            // tokens and heads of a query unit
+constexpr double kKeyShare = 0.35, kValueShare = 0.25;
 constexpr int kMaxPlace = 1 << 30;                // places in the cache end here
+
+// raw rows and up to three terms (8-bit cache), or two
+template <bool F8>
+constexpr int tile_bytes() { return (F8 ? 4 : 3) * kTermBytes; }
 
 struct Args {
   LayerDev L;                    // bf16 pools: k_pool, v_pool
@@ -43,13 +49,14 @@ struct Args {
   int total, ends_at_len;
   const float* table;            // [max_pos][rot]; rot = 0: no rotation
   int max_pos, rot, interleaved;
-  int n_kv, per_slot;            // CTAs for the cache's rows: per_slot for each (head, side); the others are for the queries
+  int per_key, per_value;        // CTAs for the cache's rows: per_key for each head's keys, per_value for its values; the others are
+                                 // for the queries
   int32_t* status;
 };
 
 // The sequences of a call, in shared memory: first packed token, tokens, place of the first token, prefix sums of touched pages.
 struct Sequences {
-  int *cu, *n, *start, *pref;
+  int *cu, *n, *start, *pref, *most;             // most: the largest number of tokens
 };
 __device__ __forceinline__ Sequences sequences_at(uint8_t* p, int B) {
   Sequences s;
@@ -57,9 +64,10 @@ __device__ __forceinline__ Sequences sequences_at(uint8_t* p, int B) {
   s.n = s.cu + B;
   s.start = s.n + B;
   s.pref = s.start + B;
+  s.most = s.pref + B + 1;
   return s;
 }
-constexpr int sequences_bytes(int B) { return (4 * B + 1) * 4; }
+constexpr int sequences_bytes(int B) { return (4 * B + 2) * 4; }
 
 // Called by all threads; ends with a barrier.
 __device__ __forceinline__ void load_sequences(const Sequences& s, const Args& a) {
@@ -80,10 +88,11 @@ __device__ __forceinline__ void load_sequences(const Sequences& s, const Args& a
   __syncthreads();
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
-    int carry = 0;
+    int carry = 0, most = 0;
     for (int base = 0; base < B; base += 32) {
       const int b = base + lane;
       const int v = b < B && s.n[b] > 0 ? (s.start[b] % kPage + s.n[b] + kPage - 1) / kPage : 0;
+      if (b < B) most = max(most, s.n[b]);
       int x = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -93,7 +102,11 @@ __device__ __forceinline__ void load_sequences(const Sequences& s, const Args& a
       if (b < B) s.pref[b + 1] = carry + x;
       carry += __shfl_sync(0xffffffffu, x, 31);
     }
-    if (lane == 0) s.pref[0] = 0;
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+      s.pref[0] = 0;
+      *s.most = most;
+    }
   }
   __syncthreads();
 }
@@ -216,12 +229,31 @@ __device__ __forceinline__ void turn_queries(const Args& a, const Sequences& s, 
 // ---------------------------------------------------------------------------------------------
 // rows of the cache
 // ---------------------------------------------------------------------------------------------
+// What a tile knows of each of its pages (a "touch": the rows that one page receives)
+struct Touch {
+  int tok0, m;                   // first packed token, rows (0: nothing to do)
+  int place0;                    // place of the first row in the sequence
+  int page;
+};
+struct TileState {
+  Touch touch[3][kPage];         // of this tile, of the next, and of the one before, whose rows may still be on their way out
+  int row_ok[kPage];
+  float tops[4][kPage];          // largest magnitude of each row, by warp
+  float scale[kPage], half_top[2];
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t row_chunk(int row, int chunk) { return row * kRowBytes + ((chunk ^ (row & 7)) << 4); }
+
 // NT: 8-column tiles of a warp at most (rank 32: 1, 48 and 64: 2, 96: 3, 128: 4)
 template <int NT, bool F8>
-__device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, uint8_t* smem, int* row_ok, float* tops) {
+__device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, uint8_t* smem, TileState& ts) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tid4 = lane & 3;
-  const int slot = blockIdx.x / a.per_slot, part = blockIdx.x - slot * a.per_slot;
-  const int h = slot >> 1, side = slot & 1;
+  const int n_key = a.per_key * a.L.Hkv;
+  const int side = (int)blockIdx.x >= n_key, at = side ? blockIdx.x - n_key : blockIdx.x, per_slot = side ? a.per_value : a.per_key;
+  const int h = at / per_slot, part = at - h * per_slot;
   const int R = side ? a.L.r_v : a.L.r_k;
   const __nv_bfloat16* Ub = side ? a.L.U_v : a.L.U_k;
   const __nv_bfloat16* U = Ub ? Ub + (size_t)h * (side ? a.L.uv_stride : a.L.uk_stride) : nullptr;
@@ -231,122 +263,153 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
   const int n_terms = rot == 0 || (!F8 && !U) ? 1 : F8 ? 3 : 2;
   const __nv_bfloat16* X = side ? a.v : a.k;
   const long long stride = side ? a.v_stride : a.k_stride;
-  const uint32_t tile = smem_u32(smem);
-  const int pages = s.pref[a.Bt.B];
-  if (part >= pages) return;
+  uint8_t* pool = F8 ? (side ? a.P.v_codes : a.P.k_codes) : reinterpret_cast<uint8_t*>(side ? a.L.v_pool : a.L.k_pool);
+
+  // Row slots of a page: all 64, unless that makes more tiles than there are CTAs; then as few as the pages' rows leave room for
+  const int touches = s.pref[a.Bt.B];
+  int cap = kPage;
+  while (cap > 1 && cap >= 2 * min(*s.most, kPage) && (long long)touches * cap > (long long)kPage * per_slot) cap >>= 1;
+  const int lg = 31 - __clz(cap), group = kPage >> lg, tiles = (touches + group - 1) / group;
+  if (part >= tiles) return;
+
+  auto find_touches = [&](int tile, int buf) {                             // threads 0 .. group - 1
+    if (tid >= group) return;
+    Touch t = {0, 0, 0, -1};
+    const int it = tile * group + tid;
+    if (it < touches) {
+      const int b = last_at_most(s.pref, a.Bt.B, it);                      // empty sequences repeat a prefix: the last one is meant
+      const int start = s.start[b], n = s.n[b];
+      const int pi = start / kPage + it - s.pref[b];
+      t.place0 = max(start, pi * kPage);
+      t.m = min(start + n, pi * kPage + kPage) - t.place0;
+      t.tok0 = s.cu[b] + t.place0 - start;
+      if (pi < a.Bt.max_pages) t.page = a.Bt.block_table[(size_t)b * a.Bt.max_pages + pi];
+      if (t.page < 0 || t.page >= a.L.num_pages) {
+        report(a.status, STIEF_ERR_BOUNDS);
+        t.m = 0;
+      }
+    }
+    ts.touch[buf][tid] = t;
+  };
+  // Shared memory: the raw rows, then the terms.  With one term the rows are multiplied as they arrive: two tiles take turns.
+  const uint32_t base = smem_u32(smem);
+  auto raw_at = [&](int n) { return n_terms == 1 ? (n & 1) * kTermBytes : 0; };
+  const int term0 = kTermBytes;                                            // n_terms > 1: where the terms lie
+  auto fetch = [&](int buf, int raw) {
+    const int row_chunks = d_in / 8;
+#pragma unroll
+    for (int i = 0; i < kPage * 16 / kThreads; ++i) {
+      const int u = tid + i * kThreads, slot = u >> 4, chunk = u & 15;
+      const Touch& t = ts.touch[buf][slot >> lg];
+      const int row = slot & (cap - 1);
+      if (row < t.m && chunk < row_chunks)
+        cp_async16(base + raw + row_chunk(slot, chunk), X + (size_t)(t.tok0 + row) * stride + (size_t)h * d_in + chunk * 8);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
 
   // ---- the basis as B fragments: tile t = warp + 4 i, k-step ks: rows 16 ks + 2 tid4, + 1 (and + 8, + 9) of column 8 t + gid
   uint32_t uf[NT][8][2];
+  find_touches(part, 0);
   if (U) {
     const int rowb = R * 2;
-    for (int i = tid; i < kD * R / 8; i += kThreads) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(U) + i);
-      reinterpret_cast<uint4*>(smem)[i] = w;
-    }
+    for (int i = tid; i < kD * R / 8; i += kThreads) reinterpret_cast<uint4*>(smem)[i] = __ldg(reinterpret_cast<const uint4*>(U) + i);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
       const int t = min(warp + 4 * i, R / 8 - 1);                          // a warp without a tile repeats the last (its results are not used)
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
-        ldsm_x4_t(tile + (32 * kk + lane) * rowb + t * 16, uf[i][2 * kk][0], uf[i][2 * kk][1], uf[i][2 * kk + 1][0], uf[i][2 * kk + 1][1]);
+        ldsm_x4_t(base + (32 * kk + lane) * rowb + t * 16, uf[i][2 * kk][0], uf[i][2 * kk][1], uf[i][2 * kk + 1][0], uf[i][2 * kk + 1][1]);
     }
-    __syncthreads();
   }
+  __syncthreads();
+  fetch(0, raw_at(0));
 
-  for (int it = part; it < pages; it += a.per_slot) {
-    const int b = last_at_most(s.pref, a.Bt.B, it);                        // empty sequences repeat a prefix: the last one is meant
-    const int start = s.start[b], n = s.n[b];
-    const int pi = start / kPage + it - s.pref[b];
-    const int place0 = max(start, pi * kPage), m = min(start + n, pi * kPage + kPage) - place0;
-    const int slot0 = place0 & (kPage - 1), tok0 = s.cu[b] + place0 - start;
-    int page = -1;
-    if (pi < a.Bt.max_pages) page = a.Bt.block_table[(size_t)b * a.Bt.max_pages + pi];
-    if (page < 0 || page >= a.L.num_pages) {                               // the same for every thread
-      if (tid == 0) report(a.status, STIEF_ERR_BOUNDS);
-      continue;
-    }
-    const size_t tile_id = (size_t)page * a.L.Hkv + h;
-    float s_old = 0.f;
-    if (F8 && slot0 > 0) s_old = a.P.scales[tile_id * f8::kScalesPerTile + side];
+  int n = 0, buf = 0;
+  for (int tile = part; tile < tiles; tile += per_slot, ++n) {
+    const Touch* touch = ts.touch[buf];
+    const int next = buf == 2 ? 0 : buf + 1;
+    find_touches(tile + per_slot, next);                                   // past the last tile: touches without rows
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    const int raw = raw_at(n);
+    const int operand = n_terms > 1 ? term0 : raw;
 
-    // ---- rows into shared memory, rotated, as bf16 terms
-    bool any = false;
+    // ---- which rows are real, and their rotation: raw rows -> terms
 #pragma unroll
     for (int i = 0; i < kPage * 8 / kThreads; ++i) {
-      const int u = tid + i * kThreads, row = u >> 3, j = u & 7;
-      if (row >= m) continue;
-      const int tok = tok0 + row;
-      const Eighth e = eighth_of(j, rot, a.interleaved);
-      const uint4* src = reinterpret_cast<const uint4*>(X + (size_t)tok * stride + (size_t)h * d_in);
-      uint4 w0 = make_uint4(0u, 0u, 0u, 0u), w1 = w0;
-      if (e.c0 * 8 < d_in) w0 = __ldg(src + e.c0);
-      if (e.c1 * 8 < d_in) w1 = __ldg(src + e.c1);
-      bool ok = true;
-      if (a.rot) {                                                         // values too: a token outside the table is not stored at all
-        const int pos = a.positions ? a.positions[tok] : place0 + row;
+      const int u = tid + i * kThreads, slot = u >> 3, j = u & 7;
+      const Touch& t = touch[slot >> lg];
+      const int row = slot & (cap - 1);
+      bool ok = row < t.m;
+      if (ok && a.rot) {                                                   // values too: a token outside the table is not stored at all
+        const int pos = a.positions ? a.positions[t.tok0 + row] : t.place0 + row;
         ok = pos >= 0 && pos < a.max_pos;
-        if (ok && e.turned) {
-          float cs[8], sn[8], x[8], y[8];
-          load_angles(a, pos, j, cs, sn);
+        if (!ok && j == 0) report(a.status, STIEF_ERR_BOUNDS);
+        if (ok && n_terms > 1) {
+          const Eighth e = eighth_of(j, rot, a.interleaved);
+          float x[8], y[8];
+          const uint4 w0 = *reinterpret_cast<const uint4*>(smem + raw + row_chunk(slot, e.c0)), w1 = *reinterpret_cast<const uint4*>(smem + raw + row_chunk(slot, e.c1));
           unpack8(w0, x);
           unpack8(w1, y);
-          turn_eighth(x, y, cs, sn, a.interleaved);
-          w0 = pack8(x);
-          w1 = pack8(y);
-          if (n_terms > 1) {
-            uint4 r0 = w0, r1 = w1;
-            for (int term = 1; term < n_terms; ++term) {
-              float p[8];
-              unpack8(r0, p);
-#pragma unroll
-              for (int c = 0; c < 8; ++c) x[c] -= p[c];
-              unpack8(r1, p);
-#pragma unroll
-              for (int c = 0; c < 8; ++c) y[c] -= p[c];
-              r0 = pack8(x);
-              r1 = pack8(y);
-              uint8_t* dst = smem + term * kTermBytes + row * kRowBytes;
-              *reinterpret_cast<uint4*>(dst + ((e.c0 ^ (row & 7)) << 4)) = r0;
-              *reinterpret_cast<uint4*>(dst + ((e.c1 ^ (row & 7)) << 4)) = r1;
-            }
+          if (e.turned) {
+            float cs[8], sn[8];
+            load_angles(a, pos, j, cs, sn);
+            turn_eighth(x, y, cs, sn, a.interleaved);
           }
-        } else if (n_terms > 1) {
-          for (int term = 1; term < n_terms; ++term) {
-            uint8_t* dst = smem + term * kTermBytes + row * kRowBytes;
-            *reinterpret_cast<uint4*>(dst + ((e.c0 ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
-            *reinterpret_cast<uint4*>(dst + ((e.c1 ^ (row & 7)) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+          for (int term = 0; term < (F8 ? 3 : 2); ++term) {
+            const uint4 r0 = pack8(x), r1 = pack8(y);
+            uint8_t* dst = smem + term0 + term * kTermBytes;
+            *reinterpret_cast<uint4*>(dst + row_chunk(slot, e.c0)) = r0;
+            *reinterpret_cast<uint4*>(dst + row_chunk(slot, e.c1)) = r1;
+            float p[8];
+            unpack8(r0, p);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[c] -= p[c];
+            unpack8(r1, p);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c] -= p[c];
+          }
+        } else if (ok && rot) {                                            // rotated, one term, no basis: in place
+          const Eighth e = eighth_of(j, rot, a.interleaved);
+          if (e.turned) {
+            float cs[8], sn[8], x[8], y[8];
+            load_angles(a, pos, j, cs, sn);
+            uint4 *p0 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c0)), *p1 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c1));
+            unpack8(*p0, x);
+            unpack8(*p1, y);
+            turn_eighth(x, y, cs, sn, a.interleaved);
+            *p0 = pack8(x);
+            *p1 = pack8(y);
           }
         }
       }
-      *reinterpret_cast<uint4*>(smem + row * kRowBytes + ((e.c0 ^ (row & 7)) << 4)) = w0;
-      *reinterpret_cast<uint4*>(smem + row * kRowBytes + ((e.c1 ^ (row & 7)) << 4)) = w1;
-      if (j == 0) {
-        row_ok[row] = ok;
-        if (!ok) report(a.status, STIEF_ERR_BOUNDS);
-      }
-      any |= ok;
+      if (j == 0) ts.row_ok[slot] = ok;
     }
-    if (!__syncthreads_or(any)) continue;
+    __syncthreads();
+    fetch(next, raw_at(n + 1));
 
     // ---- products, the smallest term first
     float acc[kPage / 16][NT][4];
+    const int rows = cap == kPage ? touch[0].m : kPage;                    // slots behind hold nothing
 #pragma unroll
     for (int mt = 0; mt < kPage / 16; ++mt) {
 #pragma unroll
       for (int i = 0; i < NT; ++i) acc[mt][i][0] = acc[mt][i][1] = acc[mt][i][2] = acc[mt][i][3] = 0.f;
-      if (mt * 16 < m && U) {
+      if (mt * 16 < rows && U) {
         const int row = 16 * mt + (lane & 15);
         for (int term = n_terms - 1; term >= 0; --term) {
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks) {
             uint32_t af[4];
-            ldsm_x4(tile + term * kTermBytes + row * kRowBytes + (((2 * ks + (lane >> 4)) ^ (row & 7)) << 4), af[0], af[1], af[2], af[3]);
+            ldsm_x4(base + operand + term * kTermBytes + row_chunk(row, 2 * ks + (lane >> 4)), af[0], af[1], af[2], af[3]);
 #pragma unroll
             for (int i = 0; i < NT; ++i) mma_bf16(acc[mt][i], af, uf[i][ks][0], uf[i][ks][1]);
           }
         }
-      } else if (mt * 16 < m) {                                            // no basis: the rows themselves
+      } else if (mt * 16 < rows) {                                         // no basis: the rows themselves
         for (int term = n_terms - 1; term >= 0; --term) {
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
@@ -354,8 +417,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
             if (t >= R / 8) continue;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const int row = 16 * mt + gid + 8 * e;
-              const uint32_t w = *reinterpret_cast<const uint32_t*>(smem + term * kTermBytes + row * kRowBytes + ((t ^ (row & 7)) << 4) + 4 * tid4);
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(smem + operand + term * kTermBytes + row_chunk(16 * mt + gid + 8 * e, t) + 4 * tid4);
               acc[mt][i][2 * e] += bf16_lo(w);
               acc[mt][i][2 * e + 1] += bf16_hi(w);
             }
@@ -364,126 +426,152 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       }
     }
 
-    // ---- the block's scale
-    float scale = 1.f, inv = 1.f;
+    // ---- scales of the pages
     if constexpr (F8) {
-      float top = 0.f;
 #pragma unroll
       for (int mt = 0; mt < kPage / 16; ++mt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int row = 16 * mt + gid + 8 * e;
-          if (row < m && row_ok[row]) {
+          float top = 0.f;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-              if (warp + 4 * i < R / 8) {
-                const float x = fabsf(acc[mt][i][2 * e]), y = fabsf(acc[mt][i][2 * e + 1]);
-                top = fmaxf(top, fmaxf(x <= 3.402823466e38f ? x : 0.f, y <= 3.402823466e38f ? y : 0.f));   // NaN and infinities leave the scale alone
-              }
+          for (int i = 0; i < NT; ++i) {
+            if (warp + 4 * i < R / 8) {
+              const float x = fabsf(acc[mt][i][2 * e]), y = fabsf(acc[mt][i][2 * e + 1]);
+              top = fmaxf(top, fmaxf(x <= 3.402823466e38f ? x : 0.f, y <= 3.402823466e38f ? y : 0.f));     // NaN and infinities leave the scale alone
             }
           }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          if (tid4 == 0) ts.tops[warp][16 * mt + gid + 8 * e] = top;
         }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (lane == 0) tops[warp] = top;
       __syncthreads();                                                     // also: every warp has read its operands
-      top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-      scale = fmaxf(f8::scale_for(top), s_old);
-      inv = 1.f / scale;                                                   // exact for a power of two
-      if (slot0 > 0 && scale != s_old) {                                   // the page's older rows move to the larger scale
-        const float ratio = s_old * inv;
-        uint4* old = reinterpret_cast<uint4*>((side ? a.P.v_codes : a.P.k_codes) + tile_id * kPage * R);
-        for (int i = tid; i < slot0 * R / 16; i += kThreads) {
-          uint4 w = old[i];
-          uint32_t* p = reinterpret_cast<uint32_t*>(&w);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const float2 x = f8::e4m3x2_to_float2(p[c] & 0xffffu), y = f8::e4m3x2_to_float2(p[c] >> 16);
-            p[c] = f8::pack_e4m3(x.x * ratio, x.y * ratio, y.x * ratio, y.y * ratio);
-          }
-          old[i] = w;
+      if (tid < kPage) {                                                   // thread = row slot; a page without a real row ends below zero
+        float top = ts.row_ok[tid] ? fmaxf(fmaxf(ts.tops[0][tid], ts.tops[1][tid]), fmaxf(ts.tops[2][tid], ts.tops[3][tid])) : -1.f;
+        for (int o = 1; o < cap && o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (cap == kPage) {
+          if (lane == 0) ts.half_top[warp] = top;
+        } else if ((tid & (cap - 1)) == 0) {
+          ts.scale[tid >> lg] = top < 0.f ? 0.f : f8::scale_for(top);
         }
       }
-      if (tid == 0) a.P.scales[tile_id * f8::kScalesPerTile + side] = scale;
-    } else {
       __syncthreads();
+      // the larger of the new rows' scale and the one of the page's older rows, which move to it when it grows: a warp per page
+      for (int g = warp; g < group; g += kThreads / 32) {
+        const Touch& t = touch[g];
+        const float top = cap == kPage ? fmaxf(ts.half_top[0], ts.half_top[1]) : 0.f;
+        const float need = cap == kPage ? (top < 0.f ? 0.f : f8::scale_for(top)) : ts.scale[g];
+        if (t.m == 0 || need == 0.f) continue;
+        float* where = a.P.scales + ((size_t)t.page * a.L.Hkv + h) * f8::kScalesPerTile + side;
+        const int held = t.place0 & (kPage - 1);
+        const float old = held > 0 ? *where : 0.f;
+        const float scale = fmaxf(need, old);
+        __syncwarp();
+        if (held > 0 && scale != old) {
+          const float ratio = old / scale;
+          uint4* codes = reinterpret_cast<uint4*>(pool + ((size_t)t.page * a.L.Hkv + h) * kPage * R);
+          for (int i = lane; i < held * R / 16; i += 32) {
+            uint4 w = codes[i];
+            uint32_t* p = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const float2 x = f8::e4m3x2_to_float2(p[c] & 0xffffu), y = f8::e4m3x2_to_float2(p[c] >> 16);
+              p[c] = f8::pack_e4m3(x.x * ratio, x.y * ratio, y.x * ratio, y.y * ratio);
+            }
+            codes[i] = w;
+          }
+        }
+        if (lane == 0) {
+          *where = scale;
+          ts.scale[g] = scale;
+        }
+      }
     }
+    __syncthreads();
 
-    // ---- results through shared memory: rows back to back, as they lie in the page
+    // ---- results through shared memory: rows back to back, as they lie in their page
     constexpr int kElt = F8 ? 1 : 2;
+    uint8_t* stage = smem + operand;
 #pragma unroll
     for (int mt = 0; mt < kPage / 16; ++mt) {
-      if (mt * 16 >= m) break;
+      if (mt * 16 >= rows) break;
 #pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        const int t = warp + 4 * i;
-        if (t < R / 8) {
+      for (int e = 0; e < 2; ++e) {
+        const int row = 16 * mt + gid + 8 * e;
+        float inv = 1.f;
+        if constexpr (F8) inv = 1.f / ts.scale[row >> lg];                 // exact for a power of two (pages without rows: not used)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int row = 16 * mt + gid + 8 * e, col = 8 * t + 2 * tid4;
+        for (int i = 0; i < NT; ++i) {
+          const int t = warp + 4 * i, col = 8 * t + 2 * tid4;
+          if (t < R / 8) {
             if constexpr (F8)
-              *reinterpret_cast<uint16_t*>(smem + row * R + col) = (uint16_t)f8::pack_e4m3(acc[mt][i][2 * e] * inv, acc[mt][i][2 * e + 1] * inv, 0.f, 0.f);
+              *reinterpret_cast<uint16_t*>(stage + row * R + col) = (uint16_t)f8::pack_e4m3(acc[mt][i][2 * e] * inv, acc[mt][i][2 * e + 1] * inv, 0.f, 0.f);
             else
-              *reinterpret_cast<uint32_t*>(smem + (row * R + col) * 2) = pack_bf16(acc[mt][i][2 * e], acc[mt][i][2 * e + 1]);
+              *reinterpret_cast<uint32_t*>(stage + (row * R + col) * 2) = pack_bf16(acc[mt][i][2 * e], acc[mt][i][2 * e + 1]);
           }
         }
       }
     }
     __syncthreads();
-    {
-      const int per_row = R * kElt / 16;
-      uint8_t* pool = F8 ? (side ? a.P.v_codes : a.P.k_codes) : reinterpret_cast<uint8_t*>(side ? a.L.v_pool : a.L.k_pool);
-      uint4* dst = reinterpret_cast<uint4*>(pool + (tile_id * kPage + slot0) * R * kElt);
-      for (int i = tid; i < m * per_row; i += kThreads)
-        if (row_ok[i / per_row]) dst[i] = reinterpret_cast<const uint4*>(smem)[i];
+    const int per_row = R * kElt / 16;
+    for (int i = tid; i < rows * per_row; i += kThreads) {
+      const int slot = i / per_row;
+      if (!ts.row_ok[slot]) continue;
+      const Touch& t = touch[slot >> lg];
+      uint4* dst = reinterpret_cast<uint4*>(pool + (((size_t)t.page * a.L.Hkv + h) * kPage + ((t.place0 + (slot & (cap - 1))) & (kPage - 1))) * R * kElt);
+      dst[i - slot * per_row] = reinterpret_cast<const uint4*>(stage)[i];
     }
-    __syncthreads();                                                       // the tile and row_ok are free
+    buf = next;
   }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 template <int NT, bool F8>
-__global__ void __launch_bounds__(kThreads, NT > 2 ? 3 : 4)
+__global__ void __launch_bounds__(kThreads, NT > 2 || F8 ? 3 : 4)
 append_rotated_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int row_ok[kPage];
-  __shared__ float tops[4];
-  const int tile_bytes = F8 ? 3 * kTermBytes : 2 * kTermBytes;
-  const Sequences s = sequences_at(smem + tile_bytes, a.Bt.B);
+  __shared__ TileState ts;
+  launch_dependents();
+  grid_dependency_wait();
+  const Sequences s = sequences_at(smem + tile_bytes<F8>(), a.Bt.B);
   load_sequences(s, a);
-  if ((int)blockIdx.x >= a.n_kv) {
-    turn_queries(a, s, blockIdx.x - a.n_kv, gridDim.x - a.n_kv);
-    return;
-  }
-  append_rows<NT, F8>(a, s, smem, row_ok, tops);
+  const int n_kv = (a.per_key + a.per_value) * a.L.Hkv;
+  if ((int)blockIdx.x >= n_kv) turn_queries(a, s, blockIdx.x - n_kv, gridDim.x - n_kv);
+  else append_rows<NT, F8>(a, s, smem, ts);
 }
 
 template <int NT, bool F8>
 cudaError_t launch(Args a, cudaStream_t st) {
   auto kern = append_rotated_kernel<NT, F8>;
-  const int smem = (F8 ? 3 : 2) * kTermBytes + sequences_bytes(a.Bt.B);
+  const int smem = tile_bytes<F8>() + sequences_bytes(a.Bt.B);
   static bool configured[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!configured[dev]) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (F8 ? 3 : 2) * kTermBytes + sequences_bytes(kMaxBatch));
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_bytes<F8>() + sequences_bytes(kMaxBatch));
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  const int resident = host::sm_count() * (NT > 2 ? 3 : 4), slots = 2 * a.L.Hkv;
+  // CTAs that are resident together, in shares by the time that rows of keys, values and queries take; no more than there are
+  // pages to touch
+  const int resident = host::sm_count() * (NT > 2 || F8 ? 3 : 4), Hkv = a.L.Hkv;
   const long long few = a.total < a.Bt.B ? a.total : a.Bt.B;
-  const long long pages = a.total / kPage + 2 * few < a.total ? a.total / kPage + 2 * few : a.total;      // pages touched, at most
-  long long per_slot = (resident * 9 / 20) / slots;
-  per_slot = per_slot < 1 ? 1 : per_slot > pages ? pages : per_slot;
-  a.per_slot = (int)per_slot;
-  a.n_kv = slots * a.per_slot;
+  const long long pages = a.total / kPage + 2 * few < a.total ? a.total / kPage + 2 * few : a.total;
+  auto share = [&](double part) {
+    long long n = (long long)(resident * part) / Hkv;
+    return (int)(n < 1 ? 1 : n > pages ? pages : n);
+  };
+  a.per_key = share(kKeyShare);
+  a.per_value = share(kValueShare);
+  const int n_kv = (a.per_key + a.per_value) * Hkv;
   long long n_q = 0;
   if (a.q) {
     n_q = (long long)((a.total + kTokQ - 1) / kTokQ) * ((a.L.Hq + kHeadsQ - 1) / kHeadsQ);
-    const long long left = resident - a.n_kv > resident / 4 ? resident - a.n_kv : resident / 4;
+    const long long left = resident - n_kv > resident / 4 ? resident - n_kv : resident / 4;
     if (n_q > left) n_q = left;
   }
-  kern<<<(unsigned)(a.n_kv + n_q), kThreads, smem, st>>>(a);
-  return cudaGetLastError();
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = host::after_previous(attr, dim3((unsigned)(n_kv + n_q)), kThreads, smem, st);
+  return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
 template <bool F8>
