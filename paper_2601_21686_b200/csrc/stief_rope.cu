@@ -20,6 +20,8 @@
 // The 8-bit cache: a tile holds all rows that a page receives, so the block's scale is settled in one exchange between the
 // CTA's warps: the larger of the scale that the page's older rows have and the least power of two that holds the new rows.  When it
 // grows, the same CTA moves the older rows' codes.
+#include <type_traits>
+
 #include "stief_f8.cuh"
 #include "stief_host_util.h"
 
@@ -265,11 +267,13 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
   const long long stride = side ? a.v_stride : a.k_stride;
   uint8_t* pool = F8 ? (side ? a.P.v_codes : a.P.k_codes) : reinterpret_cast<uint8_t*>(side ? a.L.v_pool : a.L.k_pool);
 
-  // Row slots of a page: all 64, unless that makes more tiles than there are CTAs; then as few as the pages' rows leave room for
+  // A page has as many row slots as the longest sequence needs (a power of two), and a tile takes so many pages that there are no
+  // more tiles than CTAs, as far as its slots go
   const int touches = s.pref[a.Bt.B];
-  int cap = kPage;
-  while (cap > 1 && cap >= 2 * min(*s.most, kPage) && (long long)touches * cap > (long long)kPage * per_slot) cap >>= 1;
-  const int lg = 31 - __clz(cap), group = kPage >> lg, tiles = (touches + group - 1) / group;
+  int lg = 0;
+  while ((1 << lg) < min(*s.most, kPage)) ++lg;
+  const int cap = 1 << lg, group = min(kPage >> lg, max(1, (touches + per_slot - 1) / per_slot)), tiles = (touches + group - 1) / group;
+  const int slots = group << lg;
   if (part >= tiles) return;
 
   auto find_touches = [&](int tile, int buf) {                             // threads 0 .. group - 1
@@ -302,7 +306,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       const int u = tid + i * kThreads, slot = u >> 4, chunk = u & 15;
       const Touch& t = ts.touch[buf][slot >> lg];
       const int row = slot & (cap - 1);
-      if (row < t.m && chunk < row_chunks)
+      if (slot < slots && row < t.m && chunk < row_chunks)
         cp_async16(base + raw + row_chunk(slot, chunk), X + (size_t)(t.tok0 + row) * stride + (size_t)h * d_in + chunk * 8);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -342,7 +346,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       const int u = tid + i * kThreads, slot = u >> 3, j = u & 7;
       const Touch& t = touch[slot >> lg];
       const int row = slot & (cap - 1);
-      bool ok = row < t.m;
+      bool ok = slot < slots && row < t.m;
       if (ok && a.rot) {                                                   // values too: a token outside the table is not stored at all
         const int pos = a.positions ? a.positions[t.tok0 + row] : t.place0 + row;
         ok = pos >= 0 && pos < a.max_pos;
@@ -393,28 +397,38 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
 
     // ---- products, the smallest term first
     float acc[kPage / 16][NT][4];
-    const int rows = cap == kPage ? touch[0].m : kPage;                    // slots behind hold nothing
+    const int rows = group == 1 ? touch[0].m : slots;                      // slots behind hold nothing
 #pragma unroll
-    for (int mt = 0; mt < kPage / 16; ++mt) {
+    for (int mt = 0; mt < kPage / 16; ++mt)
 #pragma unroll
       for (int i = 0; i < NT; ++i) acc[mt][i][0] = acc[mt][i][1] = acc[mt][i][2] = acc[mt][i][3] = 0.f;
-      if (mt * 16 < rows && U) {
-        const int row = 16 * mt + (lane & 15);
-        for (int term = n_terms - 1; term >= 0; --term) {
+    // row tiles side by side, so that their chains overlap: all four, or the first alone (a decode batch)
+    auto products = [&](auto tiles_tag, uint32_t from) {
+      constexpr int MT = decltype(tiles_tag)::value;
 #pragma unroll
-          for (int ks = 0; ks < 8; ++ks) {
-            uint32_t af[4];
-            ldsm_x4(base + operand + term * kTermBytes + row_chunk(row, 2 * ks + (lane >> 4)), af[0], af[1], af[2], af[3]);
+      for (int ks = 0; ks < 8; ++ks) {
+        uint32_t af[MT][4];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) mma_bf16(acc[mt][i], af, uf[i][ks][0], uf[i][ks][1]);
-          }
-        }
-      } else if (mt * 16 < rows) {                                         // no basis: the rows themselves
-        for (int term = n_terms - 1; term >= 0; --term) {
+        for (int mt = 0; mt < MT; ++mt) ldsm_x4(from + row_chunk(16 * mt + (lane & 15), 2 * ks + (lane >> 4)), af[mt][0], af[mt][1], af[mt][2], af[mt][3]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int i = 0; i < NT; ++i) mma_bf16(acc[mt][i], af[mt], uf[i][ks][0], uf[i][ks][1]);
+      }
+    };
+#pragma unroll 1
+    for (int term = n_terms - 1; term >= 0; --term) {
+      if (U) {
+        const uint32_t from = base + operand + term * kTermBytes;
+        if (rows > 16) products(std::integral_constant<int, kPage / 16>{}, from);
+        else products(std::integral_constant<int, 1>{}, from);
+      } else {                                                             // no basis: the rows themselves
+#pragma unroll
+        for (int mt = 0; mt < kPage / 16; ++mt)
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
             const int t = warp + 4 * i;
-            if (t >= R / 8) continue;
+            if (mt * 16 >= rows || t >= R / 8) continue;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const uint32_t w = *reinterpret_cast<const uint32_t*>(smem + operand + term * kTermBytes + row_chunk(16 * mt + gid + 8 * e, t) + 4 * tid4);
@@ -422,7 +436,6 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
               acc[mt][i][2 * e + 1] += bf16_hi(w);
             }
           }
-        }
       }
     }
 
