@@ -6,15 +6,15 @@
 // bound by memory, so the products run on mma.sync from registers (a tcgen05 tile would want the rotated rows in shared
 // memory all the same, and its rate is not needed).
 //
-// One launch, two kinds of CTAs of 128 threads, all resident at once:
+// One launch, two kinds of CTAs of 256 threads, all resident at once:
 //   rows of the cache  a CTA belongs to one (head, side) and keeps its basis as B fragments in registers (warp w: the 8-column
-//                      tiles w, w + 4, ...).  It walks tiles of 64 row slots: up to 64 rows of one page, or fewer rows of several
+//                      tiles w and w + 8).  It walks tiles of 64 row slots: up to 64 rows of one page, or fewer rows of several
 //                      pages (a decode batch has one row in each).  Rows arrive by cp.async a tile ahead, are rotated in fp32 and
 //                      left in shared memory as bf16 terms (value and residuals: 2 terms keep 16 significant bits, far below
 //                      the rounding to bf16; 3 keep fp32's 24, so that an e4m3 code is the one fp32 arithmetic gives;
 //                      values and unrotated keys are bf16 already), multiplied, and leave through shared memory as
 //                      contiguous pieces of the pages.
-//   queries            16 tokens x 8 heads at a time; a thread owns one eighth of a token's channels, so its cosines and sines
+//   queries            32 tokens x 8 heads at a time; a thread owns one eighth of a token's channels, so its cosines and sines
 //                      serve all 8 heads.
 //
 // The 8-bit cache: a tile holds all rows that a page receives, so the block's scale is settled in one exchange between the
@@ -28,11 +28,12 @@
 namespace stief {
 namespace rope {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kRowBytes = kD * 2;                 // a row in shared memory: 16 chunks of 16 bytes, chunk c at place c ^ (row & 7)
 constexpr int kTermBytes = kPage * kRowBytes;
-constexpr int kTokQ = 16, kHeadsQ = 8;            // tokens and heads of a query unit
-constexpr double kKeyShare = 0.35, kValueShare = 0.25;
+constexpr int kTokQ = kThreads / 8, kHeadsQ = 8;            // tokens and heads of a query unit
+constexpr int kRotateUnroll = 2;
+constexpr double kKeyShare = 0.45, kValueShare = 0.3, kValueShareLow = 0.25;      // of the CTAs; measured on 16000 prompt tokens
 constexpr int kMaxPlace = 1 << 30;                // places in the cache end here
 
 // raw rows and up to three terms (8-bit cache), or two
@@ -240,8 +241,8 @@ struct Touch {
 struct TileState {
   Touch touch[3][kPage];         // of this tile, of the next, and of the one before, whose rows may still be on their way out
   int row_ok[kPage];
-  float tops[4][kPage];          // largest magnitude of each row, by warp
-  float scale[kPage], half_top[2];
+  float tops[kWarps][kPage];          // largest magnitude of each row, by warp
+  float scale[kPage], inverse[kPage], half_top[2];
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -249,7 +250,7 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
 }
 __device__ __forceinline__ uint32_t row_chunk(int row, int chunk) { return row * kRowBytes + ((chunk ^ (row & 7)) << 4); }
 
-// NT: 8-column tiles of a warp at most (rank 32: 1, 48 and 64: 2, 96: 3, 128: 4)
+// NT: 8-column tiles of a warp at most (ranks up to 64: 1, above: 2)
 template <int NT, bool F8>
 __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, uint8_t* smem, TileState& ts) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, gid = lane >> 2, tid4 = lane & 3;
@@ -299,15 +300,27 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
   const uint32_t base = smem_u32(smem);
   auto raw_at = [&](int n) { return n_terms == 1 ? (n & 1) * kTermBytes : 0; };
   const int term0 = kTermBytes;                                            // n_terms > 1: where the terms lie
+  // Results on their way out: rows back to back, the 16-byte pieces of a row exchanged so that the eight rows that a store
+  // instruction writes lie in different banks
+  const int row_bytes = R * (F8 ? 1 : 2);
+  const int swz_shift = row_bytes % 128 == 0 ? 0 : row_bytes % 64 == 0 ? 1 : 2, swz_mask = row_bytes % 128 == 0 ? 7 : row_bytes % 64 == 0 ? 3 : row_bytes == 48 ? 0 : 1;
+  auto staged = [&](int row, int byte) { return row * row_bytes + (byte ^ (((row >> swz_shift) & swz_mask) << 4)); };
+  const bool single = group == 1;                                          // one page per tile: its rows lie behind one another, here and there
   auto fetch = [&](int buf, int raw) {
-    const int row_chunks = d_in / 8;
-#pragma unroll
-    for (int i = 0; i < kPage * 16 / kThreads; ++i) {
-      const int u = tid + i * kThreads, slot = u >> 4, chunk = u & 15;
-      const Touch& t = ts.touch[buf][slot >> lg];
-      const int row = slot & (cap - 1);
-      if (slot < slots && row < t.m && chunk < row_chunks)
-        cp_async16(base + raw + row_chunk(slot, chunk), X + (size_t)(t.tok0 + row) * stride + (size_t)h * d_in + chunk * 8);
+    const int row0 = tid >> 4, chunk = tid & 15;
+    if (chunk < d_in / 8) {
+      if (single) {
+        const Touch& t = ts.touch[buf][0];
+        const __nv_bfloat16* src = X + (size_t)(t.tok0 + row0) * stride + (size_t)h * d_in + chunk * 8;
+        uint32_t dst = base + raw + row_chunk(row0, chunk);                // a multiple of eight rows on: the same place in its group of eight
+        for (int row = row0; row < t.m; row += kThreads / 16, src += (kThreads / 16) * stride, dst += (kThreads / 16) * kRowBytes) cp_async16(dst, src);
+      } else {
+        for (int slot = row0; slot < slots; slot += kThreads / 16) {
+          const Touch& t = ts.touch[buf][slot >> lg];
+          const int row = slot & (cap - 1);
+          if (row < t.m) cp_async16(base + raw + row_chunk(slot, chunk), X + (size_t)(t.tok0 + row) * stride + (size_t)h * d_in + chunk * 8);
+        }
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -321,7 +334,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      const int t = min(warp + 4 * i, R / 8 - 1);                          // a warp without a tile repeats the last (its results are not used)
+      const int t = min(warp + kWarps * i, R / 8 - 1);                          // a warp without a tile repeats the last (its results are not used)
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
         ldsm_x4_t(base + (32 * kk + lane) * rowb + t * 16, uf[i][2 * kk][0], uf[i][2 * kk][1], uf[i][2 * kk + 1][0], uf[i][2 * kk + 1][1]);
@@ -340,59 +353,65 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
     const int raw = raw_at(n);
     const int operand = n_terms > 1 ? term0 : raw;
 
-    // ---- which rows are real, and their rotation: raw rows -> terms
-#pragma unroll
-    for (int i = 0; i < kPage * 8 / kThreads; ++i) {
-      const int u = tid + i * kThreads, slot = u >> 3, j = u & 7;
+    // ---- which rows are real (values too: a token outside the table is not stored at all)
+    auto position = [&](int slot, bool& ok) {                              // of the token in a slot
       const Touch& t = touch[slot >> lg];
       const int row = slot & (cap - 1);
-      bool ok = slot < slots && row < t.m;
-      if (ok && a.rot) {                                                   // values too: a token outside the table is not stored at all
-        const int pos = a.positions ? a.positions[t.tok0 + row] : t.place0 + row;
-        ok = pos >= 0 && pos < a.max_pos;
-        if (!ok && j == 0) report(a.status, STIEF_ERR_BOUNDS);
-        if (ok && n_terms > 1) {
-          const Eighth e = eighth_of(j, rot, a.interleaved);
+      ok = slot < slots && row < t.m;
+      if (!ok || !a.rot) return 0;
+      const int pos = a.positions ? a.positions[t.tok0 + row] : t.place0 + row;
+      ok = pos >= 0 && pos < a.max_pos;
+      return pos;
+    };
+    bool missing = false;                                                  // a row of a page that is not to be stored
+    if (tid < kPage) {
+      bool ok;
+      position(tid, ok);
+      ts.row_ok[tid] = ok;
+      missing = !ok && tid < slots && (tid & (cap - 1)) < touch[tid >> lg].m;
+      if (missing) report(a.status, STIEF_ERR_BOUNDS);
+    }
+    // ---- rotation: raw rows -> terms; an eighth of a row at a time
+    if (rot) {
+      const int j = tid & 7;
+      const Eighth e = eighth_of(j, rot, a.interleaved);
+#pragma unroll kRotateUnroll
+      for (int i = 0; i < kPage * 8 / kThreads; ++i) {
+        const int slot = (tid >> 3) + i * (kThreads / 8);
+        bool ok;
+        const int pos = position(slot, ok);
+        if (ok) {
+          float cs[8], sn[8];
+          if (e.turned) load_angles(a, pos, j, cs, sn);
           float x[8], y[8];
-          const uint4 w0 = *reinterpret_cast<const uint4*>(smem + raw + row_chunk(slot, e.c0)), w1 = *reinterpret_cast<const uint4*>(smem + raw + row_chunk(slot, e.c1));
-          unpack8(w0, x);
-          unpack8(w1, y);
-          if (e.turned) {
-            float cs[8], sn[8];
-            load_angles(a, pos, j, cs, sn);
-            turn_eighth(x, y, cs, sn, a.interleaved);
-          }
-#pragma unroll
-          for (int term = 0; term < (F8 ? 3 : 2); ++term) {
-            const uint4 r0 = pack8(x), r1 = pack8(y);
-            uint8_t* dst = smem + term0 + term * kTermBytes;
-            *reinterpret_cast<uint4*>(dst + row_chunk(slot, e.c0)) = r0;
-            *reinterpret_cast<uint4*>(dst + row_chunk(slot, e.c1)) = r1;
-            float p[8];
-            unpack8(r0, p);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[c] -= p[c];
-            unpack8(r1, p);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) y[c] -= p[c];
-          }
-        } else if (ok && rot) {                                            // rotated, one term, no basis: in place
-          const Eighth e = eighth_of(j, rot, a.interleaved);
-          if (e.turned) {
-            float cs[8], sn[8], x[8], y[8];
-            load_angles(a, pos, j, cs, sn);
-            uint4 *p0 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c0)), *p1 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c1));
-            unpack8(*p0, x);
-            unpack8(*p1, y);
-            turn_eighth(x, y, cs, sn, a.interleaved);
+          uint4 *p0 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c0)), *p1 = reinterpret_cast<uint4*>(smem + raw + row_chunk(slot, e.c1));
+          unpack8(*p0, x);
+          unpack8(*p1, y);
+          if (e.turned) turn_eighth(x, y, cs, sn, a.interleaved);
+          if (n_terms == 1) {                                              // no basis: in place
             *p0 = pack8(x);
             *p1 = pack8(y);
+          } else {
+            uint8_t *d0 = smem + term0 + row_chunk(slot, e.c0), *d1 = smem + term0 + row_chunk(slot, e.c1);
+#pragma unroll
+            for (int term = 0; term < (F8 ? 3 : 2); ++term) {
+              const uint4 r0 = pack8(x), r1 = pack8(y);
+              *reinterpret_cast<uint4*>(d0 + term * kTermBytes) = r0;
+              *reinterpret_cast<uint4*>(d1 + term * kTermBytes) = r1;
+              float p[8];
+              unpack8(r0, p);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) x[c] -= p[c];
+              unpack8(r1, p);
+#pragma unroll
+              for (int c = 0; c < 8; ++c) y[c] -= p[c];
+            }
           }
         }
       }
-      if (j == 0) ts.row_ok[slot] = ok;
     }
-    __syncthreads();
+    const bool whole = single && !__syncthreads_or(missing);               // one page, all of its rows: the common case of prompts
+    if (!single) __syncthreads();
     fetch(next, raw_at(n + 1));
 
     // ---- products, the smallest term first
@@ -427,7 +446,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
         for (int mt = 0; mt < kPage / 16; ++mt)
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
-            const int t = warp + 4 * i;
+            const int t = warp + kWarps * i;
             if (mt * 16 >= rows || t >= R / 8) continue;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -440,39 +459,77 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
     }
 
     // ---- scales of the pages
+    bool odd = false;                                                      // NaN or infinities among this thread's values
     if constexpr (F8) {
+      float row_top[kPage / 16][2], most = 0.f;
+      const int last = single ? touch[0].m : kPage;
 #pragma unroll
       for (int mt = 0; mt < kPage / 16; ++mt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float top = 0.f;
+          float top = 0.f, sum = 0.f;
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
-            if (warp + 4 * i < R / 8) {
-              const float x = fabsf(acc[mt][i][2 * e]), y = fabsf(acc[mt][i][2 * e + 1]);
-              top = fmaxf(top, fmaxf(x <= 3.402823466e38f ? x : 0.f, y <= 3.402823466e38f ? y : 0.f));     // NaN and infinities leave the scale alone
+            if (warp + kWarps * i < R / 8) {
+              const float x = acc[mt][i][2 * e], y = acc[mt][i][2 * e + 1];
+              top = fmaxf(top, fmaxf(fabsf(x), fabsf(y)));
+              sum += (x - x) + (y - y);                                    // NaN if one of them is not finite
             }
           }
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          if (tid4 == 0) ts.tops[warp][16 * mt + gid + 8 * e] = top;
+          if (sum != 0.f) {
+            odd = true;
+            top = 0.f;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+              if (warp + kWarps * i < R / 8) {                                  // they leave the scale alone
+                const float x = fabsf(acc[mt][i][2 * e]), y = fabsf(acc[mt][i][2 * e + 1]);
+                top = fmaxf(top, fmaxf(x <= 3.402823466e38f ? x : 0.f, y <= 3.402823466e38f ? y : 0.f));
+              }
+          }
+          row_top[mt][e] = top;
+          if (16 * mt + gid + 8 * e < last) most = fmaxf(most, top);
         }
-      __syncthreads();                                                     // also: every warp has read its operands
-      if (tid < kPage) {                                                   // thread = row slot; a page without a real row ends below zero
-        float top = ts.row_ok[tid] ? fmaxf(fmaxf(ts.tops[0][tid], ts.tops[1][tid]), fmaxf(ts.tops[2][tid], ts.tops[3][tid])) : -1.f;
-        for (int o = 1; o < cap && o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (cap == kPage) {
-          if (lane == 0) ts.half_top[warp] = top;
-        } else if ((tid & (cap - 1)) == 0) {
-          ts.scale[tid >> lg] = top < 0.f ? 0.f : f8::scale_for(top);
+      if (whole) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        if (lane == 0) ts.tops[0][warp] = most;
+        __syncthreads();                                                   // also: every warp has read its operands
+        if (tid == 0) {
+          for (int w = 1; w < kWarps; ++w) most = fmaxf(most, ts.tops[0][w]);
+          ts.scale[0] = f8::scale_for(most);
+        }
+      } else {
+#pragma unroll
+        for (int mt = 0; mt < kPage / 16; ++mt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = row_top[mt][e];
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            if (tid4 == 0) ts.tops[warp][16 * mt + gid + 8 * e] = top;
+          }
+        __syncthreads();                                                   // also: every warp has read its operands
+        if (tid < kPage) {                                                 // thread = row slot; a page without a real row ends below zero
+          float top = ts.row_ok[tid] ? 0.f : -1.f;
+          for (int w = 0; w < kWarps; ++w) top = ts.row_ok[tid] ? fmaxf(top, ts.tops[w][tid]) : top;
+          for (int o = 1; o < cap && o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          if (cap == kPage) {
+            if (lane == 0) ts.half_top[warp] = top;
+          } else if ((tid & (cap - 1)) == 0) {
+            ts.scale[tid >> lg] = top < 0.f ? 0.f : f8::scale_for(top);
+          }
+        }
+        __syncthreads();
+        if (cap == kPage && tid == 0) {
+          const float top = fmaxf(ts.half_top[0], ts.half_top[1]);
+          ts.scale[0] = top < 0.f ? 0.f : f8::scale_for(top);
         }
       }
-      __syncthreads();
+      __syncwarp();
       // the larger of the new rows' scale and the one of the page's older rows, which move to it when it grows: a warp per page
-      for (int g = warp; g < group; g += kThreads / 32) {
+      for (int g = warp; g < group; g += kWarps) {
         const Touch& t = touch[g];
-        const float top = cap == kPage ? fmaxf(ts.half_top[0], ts.half_top[1]) : 0.f;
-        const float need = cap == kPage ? (top < 0.f ? 0.f : f8::scale_for(top)) : ts.scale[g];
+        const float need = ts.scale[g];
         if (t.m == 0 || need == 0.f) continue;
         float* where = a.P.scales + ((size_t)t.page * a.L.Hkv + h) * f8::kScalesPerTile + side;
         const int held = t.place0 & (kPage - 1);
@@ -495,15 +552,15 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
         }
         if (lane == 0) {
           *where = scale;
-          ts.scale[g] = scale;
+          ts.inverse[g] = 1.f / scale;                                     // exact for a power of two
         }
       }
     }
     __syncthreads();
 
     // ---- results through shared memory: rows back to back, as they lie in their page
-    constexpr int kElt = F8 ? 1 : 2;
     uint8_t* stage = smem + operand;
+    const bool plain = !__any_sync(0xffffffffu, odd);
 #pragma unroll
     for (int mt = 0; mt < kPage / 16; ++mt) {
       if (mt * 16 >= rows) break;
@@ -511,27 +568,35 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       for (int e = 0; e < 2; ++e) {
         const int row = 16 * mt + gid + 8 * e;
         float inv = 1.f;
-        if constexpr (F8) inv = 1.f / ts.scale[row >> lg];                 // exact for a power of two (pages without rows: not used)
+        if constexpr (F8) inv = ts.inverse[row >> lg];                     // (of pages without rows: not used)
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          const int t = warp + 4 * i, col = 8 * t + 2 * tid4;
-          if (t < R / 8) {
-            if constexpr (F8)
-              *reinterpret_cast<uint16_t*>(stage + row * R + col) = (uint16_t)f8::pack_e4m3(acc[mt][i][2 * e] * inv, acc[mt][i][2 * e + 1] * inv, 0.f, 0.f);
-            else
-              *reinterpret_cast<uint32_t*>(stage + (row * R + col) * 2) = pack_bf16(acc[mt][i][2 * e], acc[mt][i][2 * e + 1]);
+          if (warp + kWarps * i < R / 8) {
+            const float x = acc[mt][i][2 * e] * inv, y = acc[mt][i][2 * e + 1] * inv;
+            if constexpr (F8) {
+              const uint32_t w = plain ? (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3) : f8::pack_e4m3(x, y, 0.f, 0.f);
+              *reinterpret_cast<uint16_t*>(stage + staged(row, 8 * (warp + kWarps * i) + 2 * tid4)) = (uint16_t)w;
+            } else {
+              *reinterpret_cast<uint32_t*>(stage + staged(row, 16 * (warp + kWarps * i) + 4 * tid4)) = pack_bf16(x, y);
+            }
           }
         }
       }
     }
     __syncthreads();
-    const int per_row = R * kElt / 16;
+    const int per_row = row_bytes / 16;
+    const uint32_t recip = 65536u / per_row + 1;                           // i / per_row of i < 1024
+    uint4* whole_dst = reinterpret_cast<uint4*>(pool + (((size_t)touch[0].page * a.L.Hkv + h) * kPage + (touch[0].place0 & (kPage - 1))) * row_bytes);
     for (int i = tid; i < rows * per_row; i += kThreads) {
-      const int slot = i / per_row;
-      if (!ts.row_ok[slot]) continue;
-      const Touch& t = touch[slot >> lg];
-      uint4* dst = reinterpret_cast<uint4*>(pool + (((size_t)t.page * a.L.Hkv + h) * kPage + ((t.place0 + (slot & (cap - 1))) & (kPage - 1))) * R * kElt);
-      dst[i - slot * per_row] = reinterpret_cast<const uint4*>(stage)[i];
+      const int slot = (i * recip) >> 16, piece = i - slot * per_row;
+      const uint4 w = *reinterpret_cast<const uint4*>(stage + staged(slot, piece * 16));
+      if (whole) {
+        whole_dst[i] = w;
+      } else if (ts.row_ok[slot]) {
+        const Touch& t = touch[slot >> lg];
+        uint4* dst = reinterpret_cast<uint4*>(pool + (((size_t)t.page * a.L.Hkv + h) * kPage + ((t.place0 + (slot & (cap - 1))) & (kPage - 1))) * row_bytes);
+        dst[piece] = w;
+      }
     }
     buf = next;
   }
@@ -539,7 +604,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
 }
 
 template <int NT, bool F8>
-__global__ void __launch_bounds__(kThreads, NT > 2 || F8 ? 3 : 4)
+__global__ void __launch_bounds__(kThreads, NT > 1 || F8 ? 2 : 3)
 append_rotated_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TileState ts;
@@ -566,7 +631,7 @@ cudaError_t launch(Args a, cudaStream_t st) {
   }
   // CTAs that are resident together, in shares by the time that rows of keys, values and queries take; no more than there are
   // pages to touch
-  const int resident = host::sm_count() * (NT > 2 || F8 ? 3 : 4), Hkv = a.L.Hkv;
+  const int resident = host::sm_count() * (NT > 1 || F8 ? 2 : 3), Hkv = a.L.Hkv;
   const long long few = a.total < a.Bt.B ? a.total : a.Bt.B;
   const long long pages = a.total / kPage + 2 * few < a.total ? a.total / kPage + 2 * few : a.total;
   auto share = [&](double part) {
@@ -574,7 +639,7 @@ cudaError_t launch(Args a, cudaStream_t st) {
     return (int)(n < 1 ? 1 : n > pages ? pages : n);
   };
   a.per_key = share(kKeyShare);
-  a.per_value = share(kValueShare);
+  a.per_value = share(NT > 1 ? kValueShare : kValueShareLow);
   const int n_kv = (a.per_key + a.per_value) * Hkv;
   long long n_q = 0;
   if (a.q) {
@@ -590,7 +655,7 @@ cudaError_t launch(Args a, cudaStream_t st) {
 template <bool F8>
 cudaError_t launch_rank(const Args& a, cudaStream_t st) {
   const int r = a.L.r_k > a.L.r_v ? a.L.r_k : a.L.r_v;
-  return r <= 32 ? launch<1, F8>(a, st) : r <= 64 ? launch<2, F8>(a, st) : r <= 96 ? launch<3, F8>(a, st) : launch<4, F8>(a, st);
+  return r <= 64 ? launch<1, F8>(a, st) : launch<2, F8>(a, st);
 }
 
 bool rank_ok(int r) { return r == 32 || r == 48 || r == 64 || r == 96 || r == 128; }
