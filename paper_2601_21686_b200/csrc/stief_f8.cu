@@ -2,6 +2,7 @@
 // stief_f8_mq_attention.
 #include "stief_f8_decode.cuh"
 #include "stief_f8_mq.cuh"
+#include "stief_f8_rows.cuh"
 #include "stief_host_util.h"
 
 namespace stief {
@@ -89,6 +90,7 @@ extern "C" int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, in
   const int TT = kMqRows / G;
   const long long base = ((long long)n_q + 2 * TT - 1) / (2 * TT) * B * Hkv;            // units without splitting
   long long s = sm_count() / base;                                                      // parts so that the units about fill the GPU
+  if (s < 2 && (long long)n_q * G <= f8rows::kMaxRows) s = 2;                           // few rows have a kernel of their own for split ranges
   if (s > 32) s = 32;
   if (s > max_pages_per_seq / 4) s = max_pages_per_seq / 4;                             // at least a few pages per part
   return (int32_t)(s < 1 ? 1 : s);
@@ -151,7 +153,8 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
   a.out_lse = out_lse;
   a.status = status;
   a.n_split = num_splits;
-  a.dual = (num_splits > 1 && n_q <= TT) ? 1 : 0;                // the second tile would have no rows of its own
+  const bool few = num_splits > 1 && (long long)n_q * G <= f8rows::kMaxRows;       // a tensor-core tile would be mostly empty
+  a.dual = (!few && num_splits > 1 && n_q <= TT) ? 1 : 0;        // the second tile would have no rows of its own
   a.n_parts = num_splits * (1 + a.dual);
   a.part_o = num_splits > 1 ? static_cast<float*>(workspace) : nullptr;
   a.part_ml = a.part_o ? a.part_o + (size_t)batch->B * n_q * layer->Hq * a.n_parts * RV : nullptr;
@@ -173,11 +176,11 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
   switch (RK) {
-    case 32: e = launch_f8_mq_rk32(L, st); break;
-    case 48: e = launch_f8_mq_rk48(L, st); break;
-    case 64: e = launch_f8_mq_rk64(L, st); break;
-    case 96: e = launch_f8_mq_rk96(L, st); break;
-    case 128: e = launch_f8_mq_rk128(L, st); break;
+    case 32: e = few ? launch_f8_rows_rk32(L.a, st) : launch_f8_mq_rk32(L, st); break;
+    case 48: e = few ? launch_f8_rows_rk48(L.a, st) : launch_f8_mq_rk48(L, st); break;
+    case 64: e = few ? launch_f8_rows_rk64(L.a, st) : launch_f8_mq_rk64(L, st); break;
+    case 96: e = few ? launch_f8_rows_rk96(L.a, st) : launch_f8_mq_rk96(L, st); break;
+    case 128: e = few ? launch_f8_rows_rk128(L.a, st) : launch_f8_mq_rk128(L, st); break;
   }
   if (e == cudaSuccess && num_splits > 1) {
     cudaLaunchAttribute attr[1];
