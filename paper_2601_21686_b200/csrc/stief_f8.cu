@@ -70,15 +70,16 @@ extern "C" int stief_f8_decode_attention(const stief_f8layer* layer, const stief
   a.out_lse = out_lse;
   a.len_add = len_add;
   a.QT = QT;
+  a.wait_first = !ov;
   a.status = status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaErrorInvalidValue;
   switch (layer->r_k) {
-    case 32: e = launch_f8_decode_rk32(a, n_cta, ov, st); break;
-    case 48: e = launch_f8_decode_rk48(a, n_cta, ov, st); break;
-    case 64: e = launch_f8_decode_rk64(a, n_cta, ov, st); break;
-    case 96: e = launch_f8_decode_rk96(a, n_cta, ov, st); break;
-    case 128: e = launch_f8_decode_rk128(a, n_cta, ov, st); break;
+    case 32: e = launch_f8_decode_rk32(a, n_cta, st); break;
+    case 48: e = launch_f8_decode_rk48(a, n_cta, st); break;
+    case 64: e = launch_f8_decode_rk64(a, n_cta, st); break;
+    case 96: e = launch_f8_decode_rk96(a, n_cta, st); break;
+    case 128: e = launch_f8_decode_rk128(a, n_cta, st); break;
   }
   return e == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
 }

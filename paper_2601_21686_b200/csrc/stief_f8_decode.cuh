@@ -41,6 +41,7 @@ struct F8DecodeArgs {
   float* out_lse;
   int len_add;
   int QT;
+  int wait_first;                // 1: no input may be read before the kernel that precedes this one has completed
   int32_t* status;
 };
 
@@ -92,8 +93,9 @@ struct DecodeCfg8 {
 };
 
 // D += A(16x16, row) * B(16x8, col), f16 inputs, fp32 accumulate
+// (not volatile: the compiler may move it past the loads around it)
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -142,6 +144,8 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     *last_flag = 0;
     mbar_fence_init();
   }
+  // Without the overlap flag everything from here on waits for the kernel before; the launch itself and the setup above did not.
+  if (a.wait_first) grid_dependency_wait();
   const int pad = seg_pad(RK, RV);
   build_page_prefix(pref, a.Bt, a.len_add, pad, c == 0 ? a.status : nullptr);   // ends with __syncthreads
 
@@ -460,20 +464,22 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     int first, last;
     unit_cta_span(pref, upb, pad, P, b, seg.j, &first, &last);
     const int nseg = last - first + 1;
-    __threadfence();
-    bar1(NT);
+    bar1(NT);                                              // the CTA's partial is written; a fence of one thread behind it covers all of it
     if (tid == 0) {
       int is_last = 1;
       if (nseg > 1) {
+        __threadfence();
         const int prev = atomicAdd(a.counters + u, 1);
         is_last = (prev == nseg - 1);
-        if (is_last) a.counters[u] = 0;                    // leave the counter clean for the next call
+        if (is_last) {
+          a.counters[u] = 0;                               // leave the counter clean for the next call
+          __threadfence();
+        }
       }
       *last_flag = is_last;
     }
     bar1(NT);
     if (*last_flag) {
-      __threadfence();
       combine_unit<RV>(a.L, b, h, qt, first + u, nseg, a.partial_o, a.partial_lse, a.out, a.out_lse, un, tid, NT);
       ++n_final;
     }
@@ -514,10 +520,10 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 }  // namespace f8
 
 // One launcher per key rank (each its own translation unit); cudaErrorInvalidValue for a value rank that is not compiled in.
-cudaError_t launch_f8_decode_rk32(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st);
-cudaError_t launch_f8_decode_rk48(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st);
-cudaError_t launch_f8_decode_rk64(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st);
-cudaError_t launch_f8_decode_rk96(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st);
-cudaError_t launch_f8_decode_rk128(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st);
+cudaError_t launch_f8_decode_rk32(const F8DecodeArgs& a, int n_cta, cudaStream_t st);
+cudaError_t launch_f8_decode_rk48(const F8DecodeArgs& a, int n_cta, cudaStream_t st);
+cudaError_t launch_f8_decode_rk64(const F8DecodeArgs& a, int n_cta, cudaStream_t st);
+cudaError_t launch_f8_decode_rk96(const F8DecodeArgs& a, int n_cta, cudaStream_t st);
+cudaError_t launch_f8_decode_rk128(const F8DecodeArgs& a, int n_cta, cudaStream_t st);
 
 }  // namespace stief

@@ -20,7 +20,7 @@ static bool lines_map(CUtensorMap* tm, const void* pool, unsigned long long tile
 }
 
 template <int RK, int RV>
-static cudaError_t launch_one(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st) {
+static cudaError_t launch_one(const F8DecodeArgs& a, int n_cta, cudaStream_t st) {
   using C = f8::DecodeCfg8<RK, RV>;
   auto kern = f8::decode_f8_kernel<RK, RV>;
   static bool configured[64] = {};
@@ -39,16 +39,8 @@ static cudaError_t launch_one(const F8DecodeArgs& a, int n_cta, bool overlap_pre
   CUtensorMap tmK = {}, tmV = {};
   if (!f8::PageTile<RK>::BULK && !lines_map<RK>(&tmK, a.P.k_codes, tiles)) return cudaErrorInvalidValue;
   if (!f8::PageTile<RV>::BULK && !lines_map<RV>(&tmV, a.P.v_codes, tiles)) return cudaErrorInvalidValue;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_cta);
-  cfg.blockDim = dim3(C::THREADS);
-  cfg.dynamicSmemBytes = C::SMEM_BYTES;
-  cfg.stream = st;
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = overlap_previous ? 1 : 0;
+  const cudaLaunchConfig_t cfg = host::after_previous(attr, dim3(n_cta), C::THREADS, C::SMEM_BYTES, st);
   return cudaLaunchKernelEx(&cfg, kern, tmK, tmV, a);
 }
 
@@ -76,13 +68,13 @@ static cudaError_t launch_rows(const f8mq::Args& a, cudaStream_t st) {
 #define STIEF_CAT_(a, b) a##b
 #define STIEF_CAT(a, b) STIEF_CAT_(a, b)
 
-cudaError_t STIEF_CAT(launch_f8_decode_rk, STIEF_RK)(const F8DecodeArgs& a, int n_cta, bool overlap_previous, cudaStream_t st) {
+cudaError_t STIEF_CAT(launch_f8_decode_rk, STIEF_RK)(const F8DecodeArgs& a, int n_cta, cudaStream_t st) {
   switch (a.L.r_v) {
-    case 32: return launch_one<STIEF_RK, 32>(a, n_cta, overlap_previous, st);
-    case 48: return launch_one<STIEF_RK, 48>(a, n_cta, overlap_previous, st);
-    case 64: return launch_one<STIEF_RK, 64>(a, n_cta, overlap_previous, st);
-    case 96: return launch_one<STIEF_RK, 96>(a, n_cta, overlap_previous, st);
-    case 128: return launch_one<STIEF_RK, 128>(a, n_cta, overlap_previous, st);
+    case 32: return launch_one<STIEF_RK, 32>(a, n_cta, st);
+    case 48: return launch_one<STIEF_RK, 48>(a, n_cta, st);
+    case 64: return launch_one<STIEF_RK, 64>(a, n_cta, st);
+    case 96: return launch_one<STIEF_RK, 96>(a, n_cta, st);
+    case 128: return launch_one<STIEF_RK, 128>(a, n_cta, st);
     default: return cudaErrorInvalidValue;
   }
 }
