@@ -716,27 +716,55 @@ def _token_rows(t: torch.Tensor, name: str, total: int, heads: int, width: int, 
     return t.data_ptr(), st[0] if total > 1 else heads * width                 # an extent of 1 may carry any stride
 
 
-def _append_rows(call: str, check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status):
-    at = _here(k, "k")
+_address, _strides, _device_of = torch.Tensor.data_ptr, torch.Tensor.stride, torch.Tensor.get_device
+
+
+def _signature(tensors, values) -> tuple:
+    """All that the checks of a call and its arguments go by: address, strides, device, shape and type of every tensor (which may
+    have been replaced, resized or pointed elsewhere since the last call), and the other values.  Where it equals that of an
+    earlier call, so would the outcome of the checks and the arguments."""
+    here = [t for t in tensors if t is not None]
+    return (values, [t is None for t in tensors], *map(_address, here), *map(_strides, here), *map(_device_of, here),
+            *[t.shape for t in here], *[t.dtype for t in here])
+
+
+def _append_rows(call: str, kind, check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status):
+    if not isinstance(layer, kind):
+        raise ValueError(f"{call} takes a {kind.__name__}")
+    at, d, table = _here(k, "k"), layer.__dict__, None if rotation is None else rotation.table
+    tensors = (k, v, q, q_out, cu_seqlens, positions, batch.block_table, batch.seq_lens, table, layer.U_k, layer.U_v, *_page_tensors(layer))
+    sig = _signature(tensors, (at, layer.Hq, layer.Hkv, layer.r_k, layer.r_v, ends_at_len, rotation is not None and rotation.interleaved))
+    kept = d.get("_append")
+    if kept is None or kept[0] != sig:
+        kept = d["_append"] = (sig, _append_args(check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, at))
+    _check(getattr(lib(), call)(*kept[1], _status(status, at), _raw_stream(at)), call)
+
+
+def _append_args(check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, at: int) -> tuple:
     check(layer, at)
+    if k.dim() != 3:
+        raise ValueError("k and v must be [total, Hkv, 128 (r on a side without basis)]")
     total, Hkv = k.shape[0], layer.Hkv
     kv = (*_token_rows(k, "k", total, Hkv, D_HEAD if layer.U_k is not None else layer.r_k, at),
           *_token_rows(v, "v", total, Hkv, D_HEAD if layer.U_v is not None else layer.r_v, at))
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
-    qp = qs = op = os_ = None
+    qp, qs, op, os_ = None, 0, None, 0
     if q is not None:
         qp, qs = _token_rows(q, "q", total, layer.Hq, D_HEAD, at)
         op, os_ = _token_rows(q_out, "q_out", total, layer.Hq, D_HEAD, at)
     B = batch.block_table.shape[0]
+    if batch.block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages_per_seq]")
     _int32(batch.block_table, "block_table", None, at)
     _int32(batch.seq_lens, "seq_lens", (B,), at)
     _int32(cu_seqlens, "cu_seqlens", (B + 1,), at)
     if positions is not None:
         _int32(positions, "positions", (total,), at)
-    _check(getattr(lib(), call)(ctypes.byref(layer.c()), ctypes.byref(batch.c()), None if rotation is None else ctypes.byref(rotation.c(at)),
-                                qp, qs or 0, *kv, total, cu_seqlens.data_ptr(), _ptr(positions), 1 if ends_at_len else 0, op, os_ or 0,
-                                _status(status, at), _raw_stream(at)), call)
+    turn = None if rotation is None else rotation.c(at)
+    structs = layer.c(), batch.c(), turn                      # kept by the references below
+    return (ctypes.byref(structs[0]), ctypes.byref(structs[1]), None if turn is None else ctypes.byref(turn), qp, qs, *kv, total,
+            cu_seqlens.data_ptr(), _ptr(positions), 1 if ends_at_len else 0, op, os_)
 
 
 def stief_rope_append(layer: Layer, batch: Batch, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
@@ -745,21 +773,41 @@ def stief_rope_append(layer: Layer, batch: Batch, k: torch.Tensor, v: torch.Tens
     """Packed new tokens into the bf16 cache, rotated on the way: k, v [total, Hkv, 128 (r on a side without basis)], q, q_out
     [total, Hq, 128] bf16 (strides over tokens free), cu_seqlens [B + 1] int32; positions [total] int32 where tokens are rotated
     by other positions than they are stored at.  q_out may be q."""
-    _append_rows("stief_rope_append", _cache_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
+    _append_rows("stief_rope_append", Layer, _cache_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
 
 
 def stief_f8_append(layer: F8Layer, batch: Batch, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor,
                     rotation: Optional[Rotation] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                     positions: Optional[torch.Tensor] = None, ends_at_len: bool = False, status: Optional[torch.Tensor] = None):
     """stief_rope_append into the 8-bit cache."""
-    _append_rows("stief_f8_append", _f8_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
+    _append_rows("stief_f8_append", F8Layer, _f8_tensors, layer, batch, k, v, cu_seqlens, rotation, q, q_out, positions, ends_at_len, status)
 
 
 def stief_f8_decode_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor, num_parts: int = 0,
                               out_lse: Optional[torch.Tensor] = None, len_add: int = 0, status: Optional[torch.Tensor] = None, flags: int = 0):
     """One query token per sequence over the 8-bit cache: q [B, Hq, 128 (r_k without key basis)] -> out [B, Hq, 128 (r_v without
     value basis)] bf16, contiguous; workspace as for stief_decode_attention."""
-    at = _here(q, "q")
+    if not isinstance(layer, F8Layer):
+        raise ValueError("an F8Layer is expected")
+    at, d = _here(q, "q"), layer.__dict__
+    tensors = (q, out, out_lse, workspace, batch.block_table, batch.seq_lens, layer.U_k, layer.U_v, layer.k_codes, layer.v_codes, layer.scales)
+    sig = _signature(tensors, (at, layer.Hq, layer.Hkv, layer.r_k, layer.r_v))
+    kept = d.get("_decode")
+    if kept is None or kept[0] != sig:
+        kept = d["_decode"] = (sig, *_f8_decode_args(layer, batch, q, workspace, out, out_lse, at))
+    cl, cb, qp, ws, ws_bytes, op, lse = kept[1:]
+    _check(lib().stief_f8_decode_attention(cl, cb, qp, len_add, ws, ws_bytes, num_parts, op, lse, flags, _status(status, at), _raw_stream(at)),
+           "stief_f8_decode_attention")
+
+
+def _f8_batch(batch, B: int, device: int):
+    if batch.block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_pages_per_seq]")
+    _int32(batch.block_table, "block_table", None, device)
+    _int32(batch.seq_lens, "seq_lens", (B,), device)
+
+
+def _f8_decode_args(layer, batch, q, workspace, out, out_lse, at: int) -> tuple:
     _f8_tensors(layer, at)
     B, Hq = batch.block_table.shape[0], layer.Hq
     d_q, d_out = D_HEAD if layer.U_k is not None else layer.r_k, D_HEAD if layer.U_v is not None else layer.r_v
@@ -774,11 +822,9 @@ def stief_f8_decode_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, wor
     if not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     _here(workspace, "workspace", at)
-    _int32(batch.block_table, "block_table", None, at)
-    _int32(batch.seq_lens, "seq_lens", (B,), at)
-    _check(lib().stief_f8_decode_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), len_add, workspace.data_ptr(),
-                                           workspace.numel() * workspace.element_size(), num_parts, out.data_ptr(), _ptr(out_lse), flags,
-                                           _status(status, at), _raw_stream(at)), "stief_f8_decode_attention")
+    _f8_batch(batch, B, at)
+    return (ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            out.data_ptr(), _ptr(out_lse))
 
 
 def stief_f8_mq_num_splits(B: int, n_q: int, Hq: int, Hkv: int, max_pages_per_seq: int) -> int:
@@ -795,9 +841,22 @@ def stief_f8_mq_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, out: to
     """Several causal query rows per head over the 8-bit cache: q [B, n_q, Hq, d_q] -> out [B, n_q, Hq, d_out] bf16 (strides over b
     and t free), the queries being the last q_lens[b] (default n_q) tokens of each cached sequence.  num_splits > 1 needs a
     workspace tensor of stief_f8_mq_workspace_bytes(...) bytes."""
+    if not isinstance(layer, F8Layer):
+        raise ValueError("an F8Layer is expected")
+    at, d = _here(q, "q"), layer.__dict__
+    tensors = (q, out, q_lens, out_lse, workspace, batch.block_table, batch.seq_lens, layer.U_k, layer.U_v, layer.k_codes, layer.v_codes, layer.scales)
+    sig = _signature(tensors, (at, layer.Hq, layer.Hkv, layer.r_k, layer.r_v))
+    kept = d.get("_mq")
+    if kept is None or kept[0] != sig:
+        kept = d["_mq"] = (sig, *_f8_mq_args(layer, batch, q, out, q_lens, out_lse, workspace, at))
+    cl, cb, q_args, ws, ws_bytes, out_args = kept[1:]
+    _check(lib().stief_f8_mq_attention(cl, cb, *q_args, ws, ws_bytes, num_splits, *out_args, flags, _status(status, at), _raw_stream(at)),
+           "stief_f8_mq_attention")
+
+
+def _f8_mq_args(layer, batch, q, out, q_lens, out_lse, workspace, at: int) -> tuple:
     if q.dtype is not torch.bfloat16 or out.dtype is not torch.bfloat16 or q.dim() != 4 or out.dim() != 4:
         raise ValueError("q and out must be bf16 [B, n_q, Hq, d]")
-    at = _here(q, "q")
     _f8_tensors(layer, at)
     B, n_q, Hq, d_q = q.shape
     d_out = D_HEAD if layer.U_v is not None else layer.r_v
@@ -819,13 +878,11 @@ def stief_f8_mq_attention(layer: F8Layer, batch: Batch, q: torch.Tensor, out: to
             raise ValueError("workspace must be contiguous")
         _here(workspace, "workspace", at)
         ws_bytes = workspace.numel() * workspace.element_size()
-    _int32(batch.block_table, "block_table", None, at)
-    _int32(batch.seq_lens, "seq_lens", (B,), at)
+    _f8_batch(batch, B, at)
     q_t, o_t = (qs[1], os_[1]) if n_q > 1 else (Hq * d_q, Hq * d_out)        # an extent of 1 may carry any stride: the call gets one that fits
     q_b, o_b = (qs[0], os_[0]) if B > 1 else (q_t, o_t)
-    _check(lib().stief_f8_mq_attention(ctypes.byref(layer.c()), ctypes.byref(batch.c()), q.data_ptr(), q_b, q_t, n_q, _ptr(q_lens),
-                                       _ptr(workspace), ws_bytes, num_splits, out.data_ptr(), o_b, o_t, _ptr(out_lse), flags,
-                                       _status(status, at), _raw_stream(at)), "stief_f8_mq_attention")
+    return (ctypes.byref(layer.c()), ctypes.byref(batch.c()), (q.data_ptr(), q_b, q_t, n_q, _ptr(q_lens)), _ptr(workspace), ws_bytes,
+            (out.data_ptr(), o_b, o_t, _ptr(out_lse)))
 
 
 def _page_tensors(layer):
