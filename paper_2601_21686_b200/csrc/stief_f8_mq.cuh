@@ -39,7 +39,8 @@ using namespace tc;
 constexpr int kThreads = 512;
 constexpr int kRows = mq::kRows;
 constexpr int kBlock = 2 * kPage;                // positions per step
-constexpr int kCtrlBytes = 1024;
+constexpr int kCtrlBytes = 1408, kListOffset = 768;
+constexpr int kListed = 96;                      // sequences whose units can be listed (see Work)
 constexpr int kMinStages = 4, kMaxStages = 8, kMinCodeSlots = 4, kMaxCodeSlots = 16;
 constexpr int kScaleSlots = 8;                   // blocks whose scales are kept: more than the operand ring holds
 constexpr int kPacePolls = 64, kPacedBlocks = 8;
@@ -80,6 +81,68 @@ __device__ __forceinline__ Unit block_unit(const mq::Args& a, int u, int TT) {
   }
   return w;
 }
+
+// The units that hold work, longest sequences first and the latest query tokens of each first, so that CTAs get equal numbers of
+// them: in a ragged batch many of the units that n_q allows for are empty.  Kept in shared memory for up to kListed sequences;
+// beyond, units are taken as they are numbered, empty ones among them.
+struct Work {
+  const int* first;              // [B + 1], by place in the order: pairs of tiles before it
+  const uint16_t* order;         // [B]: the sequence at a place
+  int B, pairs;                  // pairs < 0: no list
+  __device__ __forceinline__ int count(const mq::Args& a, int n_units) const { return pairs < 0 ? n_units : pairs * a.L.Hkv * a.n_split; }
+  __device__ __forceinline__ int unit(const mq::Args& a, int v, int TT) const {      // the number that decode_unit knows it by
+    if (pairs < 0) return v;
+    const int r = v / a.n_split, p = r / a.L.Hkv;
+    int lo = 0, hi = B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (first[mid] <= p) lo = mid;
+      else hi = mid;
+    }
+    const int n_t2 = (a.n_q + 2 * TT - 1) / (2 * TT), t2 = first[lo + 1] - 1 - p;
+    return (((n_t2 - 1 - t2) * B + order[lo]) * a.L.Hkv + r % a.L.Hkv) * a.n_split + v % a.n_split;
+  }
+};
+// Called by all threads; `scratch`: 2 kListed words.  Ends with a barrier.
+__device__ __forceinline__ Work list_work(const mq::Args& a, int TT, int* first, uint16_t* order, int* scratch) {
+  Work w{first, order, a.Bt.B, -1};
+  const int B = a.Bt.B, tid = threadIdx.x;
+  if (B > kListed) return w;
+  int *lens = scratch, *tiles = scratch + kListed;
+  int len = 0, nt = 0;
+  if (tid < B) {
+    const int ql = min(max(a.q_lens ? a.q_lens[tid] : a.n_q, 0), a.n_q);
+    len = a.Bt.seq_lens[tid];
+    if (ql > 0 && (len < ql || (len - 1) / kPage + 1 > a.Bt.max_pages)) {   // fewer cached tokens than query rows, or a table too short
+      if (blockIdx.x == 0) report(a.status, STIEF_ERR_BOUNDS);
+    } else {
+      nt = (ql + 2 * TT - 1) / (2 * TT);
+    }
+    lens[tid] = len;
+  }
+  __syncthreads();
+  if (tid < B) {
+    int rank = 0;
+    for (int i = 0; i < B; ++i) rank += lens[i] > len || (lens[i] == len && i < tid);
+    order[rank] = (uint16_t)tid;
+    tiles[rank] = nt;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int sum = 0;
+    for (int i = 0; i < B; ++i) {
+      first[i] = sum;
+      sum += tiles[i];
+    }
+    first[B] = sum;
+  }
+  fence_proxy_async_smem();                      // the scratch becomes a target of asynchronous copies
+  __syncthreads();
+  w.pairs = first[B];
+  return w;
+}
+
+static_assert((72 + 2) * 8 + kScaleSlots * 16 <= kListOffset && kListOffset + (kListed + 1) * 4 + kListed * 2 <= kCtrlBytes, "control words");
 
 template <int RK, int RV>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -147,6 +210,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   grid_dependency_wait();                                       // the setup above ran beside the kernel before; everything below reads its results
+  const Work work = list_work(a, TT, reinterpret_cast<int*>(ctrl_ptr + kListOffset), reinterpret_cast<uint16_t*>(ctrl_ptr + kListOffset + (kListed + 1) * 4),
+                              reinterpret_cast<int*>(codes_ptr));
+  const int n_work = work.count(a, n_units);
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");       // 512 x 128 registers at launch = 256 x 176 + 128 x 80 + 128 x 80
@@ -164,8 +230,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           ++use;
         }
       };
-      for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-        const Unit w = block_unit(a, u, TT);
+      for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+        const Unit w = block_unit(a, work.unit(a, u, TT), TT);
         if (!w.valid) continue;
         const int* bt = a.Bt.block_table + (size_t)w.b * a.Bt.max_pages;
         int ids = lane < w.cnt ? bt[w.p_lo + lane] : 0;
@@ -232,8 +298,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           __syncwarp();
         }
       };
-      for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-        const Unit w = block_unit(a, u, TT);
+      for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+        const Unit w = block_unit(a, work.unit(a, u, TT), TT);
         if (uniform((int)w.valid) == 0) continue;
         const int nb0 = uniform(w.nb[0]), nb1 = uniform(w.nb[1]), blocks = uniform(w.blocks);
         const int nb = mt ? nb1 : nb0;
@@ -458,8 +524,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       }
       if (backproj) tma_prefetch_desc(&tmUv);
     }
-    for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-      const Unit w = block_unit(a, u, TT);
+    for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+      const Unit w = block_unit(a, work.unit(a, u, TT), TT);
       if (!w.valid) continue;
       if (!fold_k) {
         for (int t = 0; t < 2; ++t) {
@@ -502,8 +568,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-      const Unit w = block_unit(a, u, TT);
+    for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+      const Unit w = block_unit(a, work.unit(a, u, TT), TT);
       if (!w.valid) continue;
       const int blk0 = blk;
       blk += w.blocks;
