@@ -33,7 +33,10 @@ constexpr int kRowBytes = kD * 2;                 // a row in shared memory: 16 
 constexpr int kTermBytes = kPage * kRowBytes;
 constexpr int kTokQ = kThreads / 8, kHeadsQ = 8;            // tokens and heads of a query unit
 constexpr int kRotateUnroll = 2;
-constexpr double kKeyShare = 0.45, kValueShare = 0.3, kValueShareLow = 0.25;      // of the CTAs; measured on 16000 prompt tokens
+constexpr int kResident = 2;                      // CTAs of an SM
+// Of the CTAs that are resident together: for rows of the cache; the others turn queries (17600 prompt tokens, 0.7 / 0.75 / 0.8 / 0.85:
+// bf16 64/64 97 / 98 / 104 / 120 us, 8-bit 96/128 170 / 162 / 144 / 151)
+constexpr double kRowsShare = 0.75, kRowsShareF8 = 0.8;
 constexpr int kMaxPlace = 1 << 30;                // places in the cache end here
 
 // raw rows and up to three terms (8-bit cache), or two
@@ -189,41 +192,39 @@ __device__ __forceinline__ void turn_queries(const Args& a, const Sequences& s, 
   for (long long u = cta; u < units; u += n_cta) {
     const int tok = (int)(u / groups) * kTokQ + (threadIdx.x >> 3), h0 = (int)(u % groups) * kHeadsQ;
     if (tok >= a.total) continue;
+    // all rows of the unit are on their way while the token's sequence is looked for and its angles are fetched
+    const uint4* src = reinterpret_cast<const uint4*>(a.q + (size_t)tok * a.q_stride) + h0 * 16;
+    uint4* dst = reinterpret_cast<uint4*>(a.q_out + (size_t)tok * a.qo_stride) + h0 * 16;
+    uint4 w0[kHeadsQ], w1[kHeadsQ];
+#pragma unroll
+    for (int i = 0; i < kHeadsQ; ++i) {
+      if (h0 + i < a.L.Hq) {
+        w0[i] = src[i * 16 + e.c0];
+        w1[i] = src[i * 16 + e.c1];
+      }
+    }
     const int b = last_at_most(s.cu, a.Bt.B, tok);
     if (tok < s.cu[b] || tok - s.cu[b] >= s.n[b]) continue;          // a token of no sequence
     const int pos = a.positions ? a.positions[tok] : s.start[b] + tok - s.cu[b];
-    if (a.rot && (pos < 0 || pos >= a.max_pos)) {
+    if (pos < 0 || pos >= a.max_pos) {
       report(a.status, STIEF_ERR_BOUNDS);
       continue;
     }
     float cs[8], sn[8];
     if (e.turned) load_angles(a, pos, j, cs, sn);
-    const uint4* src = reinterpret_cast<const uint4*>(a.q + (size_t)tok * a.q_stride);
-    uint4* dst = reinterpret_cast<uint4*>(a.q_out + (size_t)tok * a.qo_stride);
 #pragma unroll
-    for (int g = 0; g < kHeadsQ; g += 4) {
-      uint4 w0[4], w1[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (h0 + g + i < a.L.Hq) {
-          w0[i] = src[(h0 + g + i) * 16 + e.c0];
-          w1[i] = src[(h0 + g + i) * 16 + e.c1];
+    for (int i = 0; i < kHeadsQ; ++i) {
+      if (h0 + i < a.L.Hq) {
+        if (e.turned) {
+          float x[8], y[8];
+          unpack8(w0[i], x);
+          unpack8(w1[i], y);
+          turn_eighth(x, y, cs, sn, a.interleaved);
+          w0[i] = pack8(x);
+          w1[i] = pack8(y);
         }
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (h0 + g + i < a.L.Hq) {
-          if (e.turned) {
-            float x[8], y[8];
-            unpack8(w0[i], x);
-            unpack8(w1[i], y);
-            turn_eighth(x, y, cs, sn, a.interleaved);
-            w0[i] = pack8(x);
-            w1[i] = pack8(y);
-          }
-          dst[(h0 + g + i) * 16 + e.c0] = w0[i];
-          dst[(h0 + g + i) * 16 + e.c1] = w1[i];
-        }
+        dst[i * 16 + e.c0] = w0[i];
+        dst[i * 16 + e.c1] = w1[i];
       }
     }
   }
@@ -604,7 +605,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
 }
 
 template <int NT, bool F8>
-__global__ void __launch_bounds__(kThreads, NT > 1 || F8 ? 2 : 3)
+__global__ void __launch_bounds__(kThreads, kResident)
 append_rotated_kernel(const Args a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ TileState ts;
@@ -631,20 +632,22 @@ cudaError_t launch(Args a, cudaStream_t st) {
   }
   // CTAs that are resident together, in shares by the time that rows of keys, values and queries take; no more than there are
   // pages to touch
-  const int resident = host::sm_count() * (NT > 1 || F8 ? 2 : 3), Hkv = a.L.Hkv;
+  const int resident = host::sm_count() * kResident, Hkv = a.L.Hkv;
   const long long few = a.total < a.Bt.B ? a.total : a.Bt.B;
   const long long pages = a.total / kPage + 2 * few < a.total ? a.total / kPage + 2 * few : a.total;
-  auto share = [&](double part) {
-    long long n = (long long)(resident * part) / Hkv;
+  // what a tile takes, by side and rank (in thousands of cycles, two CTAs on an SM): rotation and the residual terms on top of the product
+  const double key = F8 ? 16 + a.L.r_k / 10.0 : 9 + a.L.r_k / 13.0, value = F8 ? 9 + a.L.r_v / 13.0 : 5 + a.L.r_v / 16.0;
+  auto share = [&](double cost) {
+    const long long n = (long long)(resident * (F8 ? kRowsShareF8 : kRowsShare) * cost / (key + value) / Hkv);
     return (int)(n < 1 ? 1 : n > pages ? pages : n);
   };
-  a.per_key = share(kKeyShare);
-  a.per_value = share(NT > 1 ? kValueShare : kValueShareLow);
+  a.per_key = share(key);
+  a.per_value = share(value);
   const int n_kv = (a.per_key + a.per_value) * Hkv;
   long long n_q = 0;
   if (a.q) {
     n_q = (long long)((a.total + kTokQ - 1) / kTokQ) * ((a.L.Hq + kHeadsQ - 1) / kHeadsQ);
-    const long long left = resident - n_kv > resident / 4 ? resident - n_kv : resident / 4;
+    const long long left = resident - n_kv > resident / 16 ? resident - n_kv : resident / 16;      // (many heads: more CTAs than are resident)
     if (n_q > left) n_q = left;
   }
   cudaLaunchAttribute attr[1];
