@@ -186,7 +186,7 @@ __device__ __forceinline__ void turn_eighth(float (&x)[8], float (&y)[8], const 
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ void turn_queries(const Args& a, const Sequences& s, int cta, int n_cta) {
   const int groups = (a.L.Hq + kHeadsQ - 1) / kHeadsQ;
-  const long long units = (long long)((a.total + kTokQ - 1) / kTokQ) * groups;
+  const long long units = ((long long)a.total + kTokQ - 1) / kTokQ * groups;
   const int j = threadIdx.x & 7;
   const Eighth e = eighth_of(j, a.rot, a.interleaved);
   for (long long u = cta; u < units; u += n_cta) {
@@ -646,7 +646,7 @@ cudaError_t launch(Args a, cudaStream_t st) {
   const int n_kv = (a.per_key + a.per_value) * Hkv;
   long long n_q = 0;
   if (a.q) {
-    n_q = (long long)((a.total + kTokQ - 1) / kTokQ) * ((a.L.Hq + kHeadsQ - 1) / kHeadsQ);
+    n_q = ((long long)a.total + kTokQ - 1) / kTokQ * ((a.L.Hq + kHeadsQ - 1) / kHeadsQ);
     const long long left = resident - n_kv > resident / 16 ? resident - n_kv : resident / 16;      // (many heads: more CTAs than are resident)
     if (n_q > left) n_q = left;
   }

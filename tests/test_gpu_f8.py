@@ -296,6 +296,74 @@ def test_runs_on_two_streams_and_captured():
     assert (a.out.float() - first.float()).abs().max() <= 2 ** -6 * first.float().abs().max()
 
 
+def test_runs_of_many_sequences():
+    """More sequences than the kernel lists the work of, many without a query."""
+    lens = [(53 * i) % 400 + 1 for i in range(130)]
+    counts = [0 if i % 3 == 0 else min(n, (7 * i) % 90) for i, n in enumerate(lens)]
+    Case(37, lens, n=90, counts=counts, Hq=4, Hkv=1, r_k=48, r_v=32).attend(splits=1).check()
+    Case(38, lens[:96], n=90, counts=counts[:96], Hq=4, Hkv=1).attend(splits=1).check()
+    Case(39, lens, n=4, counts=[min(c, 4) for c in counts], Hq=8, Hkv=2).attend(splits=2).check()
+    Case(40, [500, 90], n=3, counts=[0, 0]).attend(splits=1).check()
+
+
+def test_nan_codes_stay_nan_where_they_are_attended():
+    c = Case(41, [200, 200])
+    page = int(c.batch.block_table[0, 1])
+    c.layer.v_codes[page, :, 5, 7] = 0x7F
+    c.decode()
+    good = Case(41, [200, 200]).decode()
+    torch.cuda.synchronize()
+    assert torch.isnan(c.out[0]).all() and torch.equal(c.out[1], good.out[1])      # one NaN channel reaches all through the basis
+    d = Case(42, [200, 200], n=4)
+    d.layer.k_codes[int(d.batch.block_table[1, 0]), 0, 9, 3] = 0xFF
+    d.attend(splits=1)
+    torch.cuda.synchronize()
+    assert torch.isnan(d.out[1, :, :4]).all() and torch.isfinite(d.out[1, :, 4:]).all() and torch.isfinite(d.out[0]).all()
+
+
+def test_pages_far_into_large_pools():
+    """Byte offsets beyond 2^32, all three kernels."""
+    Hkv, r = 8, 128
+    P = 2 ** 32 // (Hkv * 64 * r) + 9
+    for n, splits in ((None, 1), (6, 4), (40, 1)):
+        c = Case(43, [500, 300], n=n, Hq=8, Hkv=Hkv, r_k=r, r_v=r)
+        (c.decode() if n is None else c.attend(splits=splits)).check()
+        first, L = c.out.clone(), c.layer
+        small = L.k_codes.shape[0]
+        far = lambda t: torch.empty(P, *t.shape[1:], dtype=t.dtype, device="cuda")  # noqa: E731
+        for name in ("k_codes", "v_codes", "scales"):
+            t = getattr(L, name)
+            big = far(t)
+            big[P - small:] = t
+            setattr(L, name, big)
+        c.batch.block_table.add_(P - small)
+        c.out.fill_(NAN)
+        (c.decode() if n is None else c.attend(splits=splits)).check()
+        assert torch.equal(c.out, first)
+        del L, c
+
+
+def test_two_captured_graphs_share_a_workspace():
+    """One after the other on one stream, replayed in turn."""
+    cases = [Case(44 + i, [3000, 700], n=8, r_k=64, r_v=rv) for i, rv in enumerate((64, 128))]
+    ws = torch.zeros(S.stief_f8_mq_workspace_bytes(2, 8, 8, 128, 4), dtype=torch.uint8, device="cuda")
+    graphs, side = [], torch.cuda.Stream()
+    for c in cases:
+        call = lambda: S.stief_f8_mq_attention(c.layer, c.batch, c.q, c.out, out_lse=c.lse, workspace=ws, num_splits=4)  # noqa: E731
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call()
+        graphs.append(g)
+    for _ in range(3):
+        for c, g in zip(cases, graphs):
+            c.out.fill_(NAN)
+            g.replay()
+    for c in cases:
+        c.check()
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then

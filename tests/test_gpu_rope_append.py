@@ -259,10 +259,10 @@ def test_bad_pages_and_positions_are_skipped(f8):
         assert kept == (bad == (0, 9, 21))                                  # the second ranges (9, 20) and (3, 20) are in order
         page = int(c.table[0, 0])
         assert torch.equal(c.pools()[0][page].view(torch.uint8), c.before[0][page].view(torch.uint8)) == (bad != (0, 9, 21))
-    for lens in (-1, 2 ** 31 - 1):
+    for lens, ends in ((-1, False), (2 ** 31 - 1, False), (2 ** 31 - 1, True), (8, True), (-5, True)):
         c = Case(14, [5], [9], f8=f8)
-        c.batch.seq_lens.fill_(lens)
-        c.call()
+        c.batch.seq_lens.fill_(lens)                                        # (8 tokens in all cannot end with 9 new ones)
+        c.call(ends_at_len=ends)
         torch.cuda.synchronize()
         assert c.status.item() == S.STIEF_ERR_BOUNDS
         assert all(torch.equal(p.view(torch.uint8), w.view(torch.uint8)) for p, w in zip(c.pools(), c.before))
@@ -365,6 +365,17 @@ def test_captured_and_replayed(f8):
             assert torch.equal(a, b)
     if f8:
         assert torch.equal(one.layer.scales, many.layer.scales)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_many_sequences_of_a_few_tokens(f8):
+    """Tiles of several pages each, pages without a valid token among them."""
+    counts = [(5 * i) % 4 for i in range(600)]
+    c = Case(19, [(11 * i) % 70 for i in range(600)], counts, f8=f8, Hq=4, Hkv=1, r_k=48, r_v=32, positions=True)
+    for b in range(0, 600, 7):
+        c.positions[c.cu_list[b]:c.cu_list[b + 1]] = -3
+    c.call().check(status=S.STIEF_ERR_BOUNDS)
+    Case(20, [3] * 300, [20] * 300, f8=f8, Hq=2, Hkv=2, r_k=96, r_v=96, rot=32).call().check()
 
 
 def test_two_streams_at_once():
