@@ -238,12 +238,13 @@ struct Touch {
   int tok0, m;                   // first packed token, rows (0: nothing to do)
   int place0;                    // place of the first row in the sequence
   int page;
+  float old;                     // 8-bit cache: the page's scale, if it holds older rows (else 0)
 };
 struct TileState {
   Touch touch[3][kPage];         // of this tile, of the next, and of the one before, whose rows may still be on their way out
   int row_ok[kPage];
-  float tops[kWarps][kPage];          // largest magnitude of each row, by warp
-  float scale[kPage], inverse[kPage], half_top[2];
+  alignas(16) float tops[kWarps][kPage];          // largest magnitude of each row, by warp
+  float top[kPage], inverse[kPage], half_top[2];
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
@@ -280,7 +281,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
 
   auto find_touches = [&](int tile, int buf) {                             // threads 0 .. group - 1
     if (tid >= group) return;
-    Touch t = {0, 0, 0, -1};
+    Touch t = {0, 0, 0, -1, 0.f};
     const int it = tile * group + tid;
     if (it < touches) {
       const int b = last_at_most(s.pref, a.Bt.B, it);                      // empty sequences repeat a prefix: the last one is meant
@@ -293,6 +294,8 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       if (t.page < 0 || t.page >= a.L.num_pages) {
         report(a.status, STIEF_ERR_BOUNDS);
         t.m = 0;
+      } else if (F8 && (t.place0 & (kPage - 1)) != 0) {
+        t.old = a.P.scales[((size_t)t.page * a.L.Hkv + h) * f8::kScalesPerTile + side];
       }
     }
     ts.touch[buf][tid] = t;
@@ -461,6 +464,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
 
     // ---- scales of the pages
     bool odd = false;                                                      // NaN or infinities among this thread's values
+    float whole_inverse = 1.f;
     if constexpr (F8) {
       float row_top[kPage / 16][2], most = 0.f;
       const int last = single ? touch[0].m : kPage;
@@ -490,15 +494,35 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
           row_top[mt][e] = top;
           if (16 * mt + gid + 8 * e < last) most = fmaxf(most, top);
         }
-      if (whole) {
+      // the larger of the new rows' scale and the one of the page's older rows, which move to it when it grows: a warp per page
+      auto settle = [&](const Touch& t, float scale) {
+        const int held = t.place0 & (kPage - 1);
+        if (held > 0 && scale != t.old) {
+          const float ratio = t.old / scale;
+          uint4* codes = reinterpret_cast<uint4*>(pool + ((size_t)t.page * a.L.Hkv + h) * kPage * R);
+          for (int i = lane; i < held * R / 16; i += 32) {
+            uint4 w = codes[i];
+            uint32_t* p = reinterpret_cast<uint32_t*>(&w);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              const float2 x = f8::e4m3x2_to_float2(p[c] & 0xffffu), y = f8::e4m3x2_to_float2(p[c] >> 16);
+              p[c] = f8::pack_e4m3(x.x * ratio, x.y * ratio, y.x * ratio, y.y * ratio);
+            }
+            codes[i] = w;
+          }
+        }
+        if (lane == 0) a.P.scales[((size_t)t.page * a.L.Hkv + h) * f8::kScalesPerTile + side] = scale;
+      };
+      if (whole) {                                                         // one exchange; every thread then knows the scale
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         if (lane == 0) ts.tops[0][warp] = most;
         __syncthreads();                                                   // also: every warp has read its operands
-        if (tid == 0) {
-          for (int w = 1; w < kWarps; ++w) most = fmaxf(most, ts.tops[0][w]);
-          ts.scale[0] = f8::scale_for(most);
-        }
+        const float4 t0 = *reinterpret_cast<const float4*>(&ts.tops[0][0]), t1 = *reinterpret_cast<const float4*>(&ts.tops[0][4]);
+        most = fmaxf(fmaxf(fmaxf(t0.x, t0.y), fmaxf(t0.z, t0.w)), fmaxf(fmaxf(t1.x, t1.y), fmaxf(t1.z, t1.w)));
+        const float scale = fmaxf(f8::scale_for(most), touch[0].old);
+        whole_inverse = 1.f / scale;                                       // exact for a power of two
+        if (warp == kWarps - 1) settle(touch[0], scale);
       } else {
 #pragma unroll
         for (int mt = 0; mt < kPage / 16; ++mt)
@@ -517,51 +541,34 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
           if (cap == kPage) {
             if (lane == 0) ts.half_top[warp] = top;
           } else if ((tid & (cap - 1)) == 0) {
-            ts.scale[tid >> lg] = top < 0.f ? 0.f : f8::scale_for(top);
+            ts.top[tid >> lg] = top;
           }
         }
         __syncthreads();
-        if (cap == kPage && tid == 0) {
-          const float top = fmaxf(ts.half_top[0], ts.half_top[1]);
-          ts.scale[0] = top < 0.f ? 0.f : f8::scale_for(top);
+        for (int g = warp; g < group; g += kWarps) {
+          const float top = cap == kPage ? fmaxf(ts.half_top[0], ts.half_top[1]) : ts.top[g];
+          if (touch[g].m == 0 || top < 0.f) continue;
+          const float scale = fmaxf(f8::scale_for(top), touch[g].old);
+          if (lane == 0) ts.inverse[g] = 1.f / scale;
+          settle(touch[g], scale);
         }
+        __syncthreads();
       }
-      __syncwarp();
-      // the larger of the new rows' scale and the one of the page's older rows, which move to it when it grows: a warp per page
-      for (int g = warp; g < group; g += kWarps) {
-        const Touch& t = touch[g];
-        const float need = ts.scale[g];
-        if (t.m == 0 || need == 0.f) continue;
-        float* where = a.P.scales + ((size_t)t.page * a.L.Hkv + h) * f8::kScalesPerTile + side;
-        const int held = t.place0 & (kPage - 1);
-        const float old = held > 0 ? *where : 0.f;
-        const float scale = fmaxf(need, old);
-        __syncwarp();
-        if (held > 0 && scale != old) {
-          const float ratio = old / scale;
-          uint4* codes = reinterpret_cast<uint4*>(pool + ((size_t)t.page * a.L.Hkv + h) * kPage * R);
-          for (int i = lane; i < held * R / 16; i += 32) {
-            uint4 w = codes[i];
-            uint32_t* p = reinterpret_cast<uint32_t*>(&w);
+      if (odd) {                                                           // infinities become NaN, as which they are stored
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const float2 x = f8::e4m3x2_to_float2(p[c] & 0xffffu), y = f8::e4m3x2_to_float2(p[c] >> 16);
-              p[c] = f8::pack_e4m3(x.x * ratio, x.y * ratio, y.x * ratio, y.y * ratio);
-            }
-            codes[i] = w;
-          }
-        }
-        if (lane == 0) {
-          *where = scale;
-          ts.inverse[g] = 1.f / scale;                                     // exact for a power of two
-        }
+        for (int mt = 0; mt < kPage / 16; ++mt)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (!(fabsf(acc[mt][i][c]) <= 3.402823466e38f)) acc[mt][i][c] = __uint_as_float(0x7fc00000u);
       }
+    } else {
+      __syncthreads();
     }
-    __syncthreads();
 
     // ---- results through shared memory: rows back to back, as they lie in their page
     uint8_t* stage = smem + operand;
-    const bool plain = !__any_sync(0xffffffffu, odd);
 #pragma unroll
     for (int mt = 0; mt < kPage / 16; ++mt) {
       if (mt * 16 >= rows) break;
@@ -569,13 +576,13 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
       for (int e = 0; e < 2; ++e) {
         const int row = 16 * mt + gid + 8 * e;
         float inv = 1.f;
-        if constexpr (F8) inv = ts.inverse[row >> lg];                     // (of pages without rows: not used)
+        if constexpr (F8) inv = whole ? whole_inverse : ts.inverse[row >> lg];       // (of pages without rows: not used)
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           if (warp + kWarps * i < R / 8) {
             const float x = acc[mt][i][2 * e] * inv, y = acc[mt][i][2 * e + 1] * inv;
             if constexpr (F8) {
-              const uint32_t w = plain ? (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3) : f8::pack_e4m3(x, y, 0.f, 0.f);
+              const uint32_t w = __nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3);
               *reinterpret_cast<uint16_t*>(stage + staged(row, 8 * (warp + kWarps * i) + 2 * tid4)) = (uint16_t)w;
             } else {
               *reinterpret_cast<uint32_t*>(stage + staged(row, 16 * (warp + kWarps * i) + 4 * tid4)) = pack_bf16(x, y);
