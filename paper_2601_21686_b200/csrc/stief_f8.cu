@@ -101,6 +101,18 @@ extern "C" size_t stief_f8_mq_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq
   return stief_mq_workspace_bytes(B, n_q, Hq, r_v, num_splits);
 }
 
+// Joins the parts of a call.  Tiles of fewer than 16 rows where those would leave SMs without work; blocks for four to an SM.
+template <int RV>
+static cudaError_t launch_combine(const mq::Args& a, cudaStream_t st) {
+  const long long rows = (long long)a.n_q * a.L.G, heads = (long long)a.L.Hkv * a.Bt.B;
+  int tile = f8mq::kCombineRows;
+  while (tile > 4 && (rows + tile - 1) / tile * heads < 2 * sm_count()) tile /= 2;
+  const long long tiles = (rows + tile - 1) / tile, most = (4ll * sm_count() + heads - 1) / heads;
+  cudaLaunchAttribute attr[1];
+  const cudaLaunchConfig_t cfg = after_previous(attr, dim3((unsigned)(tiles < most ? tiles : most), a.L.Hkv, a.Bt.B), f8mq::kCombineThreads, 0, st);
+  return cudaLaunchKernelEx(&cfg, f8mq::f8_mq_combine_kernel<RV>, a, tile);
+}
+
 extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b,
                                      int64_t q_stride_t, int32_t n_q, const int32_t* q_lens, void* workspace, size_t workspace_bytes,
                                      int32_t num_splits, uint16_t* out, int64_t out_stride_b, int64_t out_stride_t, float* out_lse,
@@ -184,9 +196,13 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
     case 128: e = few ? launch_f8_rows_rk128(L.a, st) : launch_f8_mq_rk128(L, st); break;
   }
   if (e == cudaSuccess && num_splits > 1) {
-    cudaLaunchAttribute attr[1];
-    const cudaLaunchConfig_t cfg = after_previous(attr, dim3(n_q, layer->Hkv, batch->B), f8mq::kCombineThreads, 0, st);
-    e = cudaLaunchKernelEx(&cfg, f8mq::f8_mq_combine_kernel<0>, a);
+    switch (RV) {
+      case 32: e = launch_combine<32>(a, st); break;
+      case 48: e = launch_combine<48>(a, st); break;
+      case 64: e = launch_combine<64>(a, st); break;
+      case 96: e = launch_combine<96>(a, st); break;
+      case 128: e = launch_combine<128>(a, st); break;
+    }
   }
   return e == cudaSuccess ? STIEF_OK : STIEF_ERR_CUDA;
 }

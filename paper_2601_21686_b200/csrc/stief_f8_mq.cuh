@@ -212,7 +212,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   grid_dependency_wait();                                       // the setup above ran beside the kernel before; everything below reads its results
   const Work work = list_work(a, TT, reinterpret_cast<int*>(ctrl_ptr + kListOffset), reinterpret_cast<uint16_t*>(ctrl_ptr + kListOffset + (kListed + 1) * 4),
                               reinterpret_cast<int*>(codes_ptr));
-  const int n_work = work.count(a, n_units);
+  const int n_work = work.count(a, n_units), grid = gridDim.x;
+  // Units of CTA c: there and back, so that who had a longest unit of one round gets a shortest of the next
+  auto taken = [&](int r) { return r * grid + (r & 1 ? grid - 1 - (int)blockIdx.x : (int)blockIdx.x); };
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");       // 512 x 128 registers at launch = 256 x 176 + 128 x 80 + 128 x 80
@@ -230,7 +232,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           ++use;
         }
       };
-      for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+      for (int r = 0; r * grid < n_work; ++r) {
+        const int u = taken(r);
+        if (u >= n_work) continue;
         const Unit w = block_unit(a, work.unit(a, u, TT), TT);
         if (!w.valid) continue;
         const int* bt = a.Bt.block_table + (size_t)w.b * a.Bt.max_pages;
@@ -298,7 +302,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           __syncwarp();
         }
       };
-      for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+      for (int r = 0; r * grid < n_work; ++r) {
+        const int u = taken(r);
+        if (u >= n_work) continue;
         const Unit w = block_unit(a, work.unit(a, u, TT), TT);
         if (uniform((int)w.valid) == 0) continue;
         const int nb0 = uniform(w.nb[0]), nb1 = uniform(w.nb[1]), blocks = uniform(w.blocks);
@@ -524,7 +530,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       }
       if (backproj) tma_prefetch_desc(&tmUv);
     }
-    for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+    for (int r = 0; r * grid < n_work; ++r) {
+      const int u = taken(r);
+      if (u >= n_work) continue;
       const Unit w = block_unit(a, work.unit(a, u, TT), TT);
       if (!w.valid) continue;
       if (!fold_k) {
@@ -568,7 +576,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    for (int u = blockIdx.x; u < n_work; u += gridDim.x) {
+    for (int r = 0; r * grid < n_work; ++r) {
+      const int u = taken(r);
+      if (u >= n_work) continue;
       const Unit w = block_unit(a, work.unit(a, u, TT), TT);
       if (!w.valid) continue;
       const int blk0 = blk;
@@ -677,23 +687,18 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             }
           }
         };
+        float r = 1.f;                                          // what a moved reference leaves of the sum and the accumulator
+        bool moved = false;                                     // for a row of the warp
         if (jo == 0) {
           m_ref = mx;                                           // -inf when a part of a split range begins behind the row's position
-        } else if (__any_sync(0xffffffffu, mx - m_ref > kRescaleLog2)) {
-          mixed();
+        } else {
           const bool grown = mx - m_ref > kRescaleLog2;         // a row's bits do not depend on its neighbours
-          const float r = grown ? fast_exp2(m_ref - mx) : 1.f;
-          l *= r;
-          if (grown) m_ref = mx;
-          for (int c0 = 0; c0 < RV; c0 += 16) {
-            uint32_t v[16];
-            tmem_ld16(t_o + c0, v);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * r);
-            tmem_st16(t_o + c0, v);
+          moved = __any_sync(0xffffffffu, grown);
+          if (grown) {
+            r = fast_exp2(m_ref - mx);
+            l *= r;
+            m_ref = mx;
           }
-          tmem_st_wait();
         }
         const float ref = m_ref > -INFINITY ? m_ref - kHeadroomLog2 : 0.f;
         // Exponents x - ref as one fma with e - ref where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
@@ -720,6 +725,17 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             if (h == 0) mixed();
             tmem_st16(t_p + 32 * h, *reinterpret_cast<uint32_t(*)[16]>(&pk[0]));
             tmem_st16(t_p + 32 * h + 16, *reinterpret_cast<uint32_t(*)[16]>(&pk[16]));
+            if (h == 0 && moved) {                              // as late as the weights allow: P V of the block before has to be through
+#pragma unroll 1
+              for (int c0 = 0; c0 < RV; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld16(t_o + c0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * r);
+                tmem_st16(t_o + c0, v);
+              }
+            }
             float a0, a1;
             unpack2(sum2, a0, a1);
             l = fmaf(a0 + a1, f8::pow2(h ? -e1 : -e0), l);
@@ -812,116 +828,165 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
   if (warp == 1) tmem_dealloc(tmem_base, mq::kTmemCols);
 }
 
-// Merges the parts of a split page range (by their references), normalises, back-projects and writes the rows.  One block per
-// (token, KV head, sequence): its G query rows share U_v, eight at a time.  A part that had no block for the row's tile was
-// never written and is left out by redoing the range arithmetic of decode_unit.
-constexpr int kCombineThreads = 128, kCombineRows = 8, kMaxParts = 64;
-template <int kInstance>                                        // a template only so that the header can be included by several units
+// Merges the parts of a split page range (by their references), normalises, back-projects and writes the rows.  The rows of a
+// (sequence, KV head), token by token and its G heads in turn, are taken in tiles of `tile_rows` <= 16; a block keeps U_v as operands
+// of mma.sync in registers and goes through every gridDim.x-th tile.  Rows go to the product as bf16(x) and bf16(x - bf16(x)), as
+// without parts.  A part that had no block for the row's tile was never written and is left out by redoing the range arithmetic of
+// decode_unit.
+constexpr int kCombineThreads = 128, kCombineRows = 16, kMaxParts = 64;
+template <int RV>
 __global__ void __launch_bounds__(kCombineThreads)
-f8_mq_combine_kernel(const mq::Args a) {
-  __shared__ float od[kCombineRows][kD], weight[kCombineRows][kMaxParts], total[kCombineRows];
+f8_mq_combine_kernel(const mq::Args a, int tile_rows) {
+  constexpr int kPitch = RV + 8, NK = RV / 16;                    // rows 16 (odd) bytes apart: conflict-free ldmatrix
+  __shared__ __align__(16) __nv_bfloat16 terms[2][kCombineRows][kPitch];
+  __shared__ float weight[kCombineRows][kMaxParts + 1];
   launch_dependents();
   grid_dependency_wait();
-  const int tok = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int G = a.L.G, RV = a.L.r_v, TT = kRows / G, NP = a.n_parts;
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.L.G, TT = kRows / G, NP = a.n_parts;
   int ql = a.q_lens ? a.q_lens[b] : a.n_q;
   ql = min(max(ql, 0), a.n_q);
   const int sl = a.Bt.seq_lens[b], q_start = sl - ql;
-  if (tok >= ql || q_start < 0 || (sl - 1) / kPage + 1 > a.Bt.max_pages) return;
-  // pages of the row's tile and of the unit (both tiles), as decode_unit derives them
-  const int t2 = tok / (2 * TT), first = t2 * 2 * TT;
-  int full[2] = {0, 0};
-  for (int t = 0; t < 2; ++t)
-    if (first + t * TT < ql) full[t] = (q_start + min(first + (t + 1) * TT, ql) - 1) / kPage + 1;
-  const int all = max(full[0], full[1]), mine = full[(tok - first) / TT];
-  auto exists = [&](int i) {
-    const int sp = a.dual ? i >> 1 : i;
-    const int lo = (int)((long long)sp * all / a.n_split), hi = min((int)((long long)(sp + 1) * all / a.n_split), mine);
-    return a.dual ? (i & 1) < (hi - lo + 1) >> 1 : hi > lo;
-  };
+  if (q_start < 0 || (sl - 1) / kPage + 1 > a.Bt.max_pages) return;
+  const int rows = ql * G;
+  if ((int)blockIdx.x * tile_rows >= rows) return;
   const bool fold_v = a.L.U_v == nullptr;
-  const int d_out = fold_v ? RV : kD;
-  const __nv_bfloat16* Uv = fold_v ? nullptr : a.L.U_v + (size_t)h * a.L.uv_stride;
-  for (int g0 = 0; g0 < G; g0 += kCombineRows) {
-    const int ng = min(kCombineRows, G - g0);
-    const size_t row0 = ((size_t)b * a.n_q + tok) * a.L.Hq + h * G + g0;
-    __syncthreads();
-    for (int g = warp; g < ng; g += kCombineThreads / 32) {      // weights of the row's parts, two to a lane
-      const size_t prow = (row0 + g) * NP;
-      float m[2], l[2];
+  // Output channels of the warp: 32 warp + 8 (column / 2) + 2 j + column % 2 for column 0 .. 7 of its j-th product, so that a thread's
+  // share of a row is 8 neighbours.
+  uint32_t u[NK][4][2];
+  if (!fold_v) {
+    const __nv_bfloat16* Uv = a.L.U_v + (size_t)h * a.L.uv_stride;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int p = lane + 32 * i;
+    for (int j = 0; j < 4; ++j) {
+      const int col = lane >> 2;
+      const __nv_bfloat16* src = Uv + (32 * warp + 8 * (col >> 1) + 2 * j + (col & 1)) * RV + 2 * (lane & 3);
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        u[k][j][0] = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * k));
+        u[k][j][1] = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * k + 8));
+      }
+    }
+  }
+  for (int r0 = blockIdx.x * tile_rows; r0 < rows; r0 += gridDim.x * tile_rows) {
+    const int nr = min(tile_rows, rows - r0);
+    {                                                           // weights of the rows' parts over the row sum: eight threads a row
+      const int r = tid >> 3, p8 = tid & 7;
+      const bool live = r < nr;
+      const int tok = (r0 + min(r, nr - 1)) / G, g = r0 + min(r, nr - 1) - tok * G;
+      // pages of the row's tile and of the unit (both tiles), as decode_unit derives them
+      const int t2 = tok / (2 * TT), first = t2 * 2 * TT;
+      int full[2] = {0, 0};
+      for (int t = 0; t < 2; ++t)
+        if (first + t * TT < ql) full[t] = (q_start + min(first + (t + 1) * TT, ql) - 1) / kPage + 1;
+      const uint32_t all = max(full[0], full[1]);               // times 32 parts below 2^31
+      const int mine = full[(tok - first) / TT];
+      auto exists = [&](int i) {
+        const uint32_t sp = a.dual ? i >> 1 : i;
+        const int lo = (int)(sp * all / (uint32_t)a.n_split), hi = min((int)((sp + 1) * all / (uint32_t)a.n_split), mine);
+        return a.dual ? (i & 1) < (hi - lo + 1) >> 1 : hi > lo;
+      };
+      const size_t row = ((size_t)b * a.n_q + tok) * a.L.Hq + h * G + g;
+      float m[kMaxParts / 8], l[kMaxParts / 8], M = -INFINITY, den = 0.f;
+#pragma unroll
+      for (int i = 0; i < kMaxParts / 8; ++i) {
+        const int p = p8 + 8 * i;
         m[i] = -INFINITY;
         l[i] = 0.f;
-        if (p < NP && exists(p)) {
-          const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (prow + p) * 2);
+        if (live && p < NP && exists(p)) {
+          const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (row * NP + p) * 2);
           m[i] = ml.x;
           l[i] = ml.y;
         }
-      }
-      float M = fmaxf(m[0], m[1]);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      float den = 0.f;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float wgt = l[i] > 0.f || l[i] != l[i] ? fast_exp2(m[i] - M) : 0.f;        // a part that the row attends nothing of has l = 0
-        den += l[i] > 0.f || l[i] != l[i] ? l[i] * wgt : 0.f;
-        if (lane + 32 * i < NP) weight[g][lane + 32 * i] = wgt;
+        M = fmaxf(M, m[i]);
       }
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-      if (lane == 0) {
-        total[g] = den;
-        if (a.out_lse) a.out_lse[row0 + g] = kLn2 * (M + log2f(den));
+      for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+#pragma unroll
+      for (int i = 0; i < kMaxParts / 8; ++i) {
+        const bool some = l[i] > 0.f || l[i] != l[i];           // a part that the row attends nothing of has l = 0
+        m[i] = some ? fast_exp2(m[i] - M) : 0.f;
+        den += some ? l[i] * m[i] : 0.f;
       }
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+      const float inv = 1.f / den;
+#pragma unroll
+      for (int i = 0; i < kMaxParts / 8; ++i)
+        if (live && p8 + 8 * i < NP) weight[r][p8 + 8 * i] = m[i] == 0.f ? 0.f : m[i] * inv;
+      if (live && p8 == 0 && a.out_lse) a.out_lse[row] = kLn2 * (M + log2f(den));
     }
     __syncthreads();
-    for (int e = tid; e < ng * RV / 4; e += kCombineThreads) {
-      const int g = e / (RV / 4), c = e % (RV / 4);
-      const float4* src = reinterpret_cast<const float4*>(a.part_o + (row0 + g) * NP * RV) + c;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int i = 0; i < NP; ++i) {
-        const float wgt = weight[g][i];
-        if (wgt != 0.f) {
-          const float4 v = src[(size_t)i * (RV / 4)];
-          x.x = fmaf(v.x, wgt, x.x);
-          x.y = fmaf(v.y, wgt, x.y);
-          x.z = fmaf(v.z, wgt, x.z);
-          x.w = fmaf(v.w, wgt, x.w);
-        }
-      }
-      const float inv = 1.f / total[g];
-      *reinterpret_cast<float4*>(&od[g][4 * c]) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+    const size_t row0 = ((size_t)b * a.n_q * a.L.Hq + h * G);
+    auto part_row = [&](int r) {                                // the row among all: rows of a token are Hq apart
+      const int tok = (r0 + r) / G;
+      return row0 + (size_t)tok * a.L.Hq + (r0 + r - tok * G);
+    };
+    constexpr int NE = (kCombineRows * RV / 4 + kCombineThreads - 1) / kCombineThreads;
+    const float4* src[NE];
+    float4 x[NE];
+    int er[NE];
+#pragma unroll
+    for (int i = 0; i < NE; ++i) {
+      const int e = tid + kCombineThreads * i;
+      er[i] = e / (RV / 4) < nr ? e / (RV / 4) : -1;
+      src[i] = reinterpret_cast<const float4*>(a.part_o + part_row(max(er[i], 0)) * NP * RV) + e % (RV / 4);
+      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    __syncthreads();
-    __nv_bfloat16* orow = a.out + (size_t)b * a.out_stride_b + (size_t)tok * a.out_stride_t + (size_t)(h * G + g0) * d_out;
+#pragma unroll 2
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        const float wgt = er[i] >= 0 ? weight[er[i]][p] : 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (wgt != 0.f) v = __ldcs(src[i] + (size_t)p * (RV / 4));
+        x[i].x = fmaf(v.x, wgt, x[i].x);
+        x[i].y = fmaf(v.y, wgt, x[i].y);
+        x[i].z = fmaf(v.z, wgt, x[i].z);
+        x[i].w = fmaf(v.w, wgt, x[i].w);
+      }
+    auto out_row = [&](int r, int d_out) {
+      const int tok = (r0 + r) / G;
+      return a.out + (size_t)b * a.out_stride_b + (size_t)tok * a.out_stride_t + (size_t)(h * G + r0 + r - tok * G) * d_out;
+    };
     if (fold_v) {
-      for (int e = tid; e < ng * RV; e += kCombineThreads) orow[e] = __float2bfloat16_rn(od[e / RV][e % RV]);
-    } else {                                                    // one output element per thread and row: row `tid` of U_v
-      const uint4* urow = reinterpret_cast<const uint4*>(Uv + (size_t)tid * RV);
-      float acc[kCombineRows] = {};
-#pragma unroll 4
-      for (int c8 = 0; c8 < RV / 8; ++c8) {
-        const uint4 u = urow[c8];
-        const uint32_t wv[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int g = 0; g < kCombineRows; ++g) {
-          if (g < ng) {
+      for (int i = 0; i < NE; ++i)
+        if (er[i] >= 0)
+          *reinterpret_cast<uint2*>(out_row(er[i], RV) + (tid + kCombineThreads * i) % (RV / 4) * 4) = make_uint2(pack_bf16(x[i].x, x[i].y), pack_bf16(x[i].z, x[i].w));
+    } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[g] = fmaf(od[g][c8 * 8 + 2 * i], bf16_lo(wv[i]), acc[g]);
-              acc[g] = fmaf(od[g][c8 * 8 + 2 * i + 1], bf16_hi(wv[i]), acc[g]);
-            }
-          }
+      for (int i = 0; i < NE; ++i) {
+        const int e = tid + kCombineThreads * i;
+        if (e < kCombineRows * RV / 4) {                        // rows that the tile does not have are zeros
+          uint32_t hi[2], lo[2];
+          split_bf16(x[i].x, x[i].y, hi[0], lo[0]);
+          split_bf16(x[i].z, x[i].w, hi[1], lo[1]);
+          *reinterpret_cast<uint2*>(&terms[0][e / (RV / 4)][e % (RV / 4) * 4]) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2*>(&terms[1][e / (RV / 4)][e % (RV / 4) * 4]) = make_uint2(lo[0], lo[1]);
         }
       }
+      __syncthreads();
+      float acc[4][4] = {};
+      const uint32_t at = smem_u32(&terms[0][lane & 15][(lane >> 4) * 8]);
 #pragma unroll
-      for (int g = 0; g < kCombineRows; ++g)
-        if (g < ng) orow[(size_t)g * kD + tid] = __float2bfloat16_rn(acc[g]);
+      for (int k = 0; k < NK; ++k)
+#pragma unroll
+        for (int term = 0; term < 2; ++term) {
+          uint32_t f[4];
+          ldsm_x4(at + term * (kCombineRows * kPitch * 2) + 32 * k, f[0], f[1], f[2], f[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mma_bf16(acc[j], f, u[k][j][0], u[k][j][1]);
+        }
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int r = (lane >> 2) + 8 * half;
+        if (r < nr)
+          *reinterpret_cast<uint4*>(out_row(r, kD) + 32 * warp + 8 * (lane & 3)) =
+              make_uint4(pack_bf16(acc[0][2 * half], acc[0][2 * half + 1]), pack_bf16(acc[1][2 * half], acc[1][2 * half + 1]),
+                         pack_bf16(acc[2][2 * half], acc[2][2 * half + 1]), pack_bf16(acc[3][2 * half], acc[3][2 * half + 1]));
+      }
     }
+    __syncthreads();                                            // weights and terms are free
   }
 }
 
