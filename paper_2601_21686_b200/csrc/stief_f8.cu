@@ -1,5 +1,7 @@
 // Attention over the compressed cache in 8-bit floating point: argument checks and launches of stief_f8_decode_attention and
 // stief_f8_mq_attention.
+#include <algorithm>
+
 #include "stief_f8_decode.cuh"
 #include "stief_f8_mq.cuh"
 #include "stief_f8_rows.cuh"
@@ -88,26 +90,39 @@ extern "C" int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, in
   if (B <= 0 || n_q <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_pages_per_seq <= 0) return 0;
   const int G = Hq / Hkv;
   if (G > kMqRows) return 0;
+  if (n_q > 65535) return 1;                                                            // calls of more rows are not split
   const int TT = kMqRows / G;
   const long long base = ((long long)n_q + 2 * TT - 1) / (2 * TT) * B * Hkv;            // units without splitting
-  long long s = sm_count() / base;                                                      // parts so that the units about fill the GPU
-  if (s < 2 && (long long)n_q * G <= f8rows::kMaxRows) s = 2;                           // few rows have a kernel of their own for split ranges
-  if (s > 32) s = 32;
-  if (s > max_pages_per_seq / 4) s = max_pages_per_seq / 4;                             // at least a few pages per part
-  return (int32_t)(s < 1 ? 1 : s);
+  const long long most = std::min(32ll, std::max(1ll, (long long)max_pages_per_seq / 4));   // at least a few pages per part
+  if ((long long)n_q * G <= f8rows::kMaxRows)                                           // few rows have a kernel of their own for split ranges
+    return (int32_t)std::min(most, std::max(2ll, sm_count() / base));
+  // Microseconds as measured, within a fifth: a round of units costs 10 and 2.25 for two pages (tiles of the same rows share a unit's
+  // pages); joined parts cost 12, 0.4 per thousand rows and part and 0.3 for each part of a row.  One sequence, ranks 64/64, 1 / 2 / 4
+  // parts: 512 tokens over 8192 130 / 92 / 106, 2048 over 4096 126 / 185 / -, 256 over 4096 74 / 55 / 43.
+  double best = 0.;
+  long long s = 1;
+  for (long long i = 1; i <= most; ++i) {
+    const double parts = (double)(i > 1 && n_q <= TT ? 2 * i : i), rounds = (double)((base * i + sm_count() - 1) / sm_count());
+    const double us = rounds * (10. + 2.25 * (max_pages_per_seq / 2 + max_pages_per_seq % 2) / parts) + (i > 1 ? 12. + (4e-4 * B * n_q * Hq + 0.3) * parts : 0.);
+    if (i == 1 || us < best) {
+      best = us;
+      s = i;
+    }
+  }
+  return (int32_t)s;
 }
 
 extern "C" size_t stief_f8_mq_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t r_v, int32_t num_splits) {
   return stief_mq_workspace_bytes(B, n_q, Hq, r_v, num_splits);
 }
 
-// Joins the parts of a call.  Tiles of fewer than 16 rows where those would leave SMs without work; blocks for four to an SM.
+// Joins the parts of a call.  Tiles of fewer than 16 rows where those would leave SMs without work.
 template <int RV>
 static cudaError_t launch_combine(const mq::Args& a, cudaStream_t st) {
   const long long rows = (long long)a.n_q * a.L.G, heads = (long long)a.L.Hkv * a.Bt.B;
   int tile = f8mq::kCombineRows;
   while (tile > 4 && (rows + tile - 1) / tile * heads < 2 * sm_count()) tile /= 2;
-  const long long tiles = (rows + tile - 1) / tile, most = (4ll * sm_count() + heads - 1) / heads;
+  const long long tiles = (rows + tile - 1) / tile, most = std::max(1ll, 4ll * sm_count() / heads);     // one wave, four to an SM
   cudaLaunchAttribute attr[1];
   const cudaLaunchConfig_t cfg = after_previous(attr, dim3((unsigned)(tiles < most ? tiles : most), a.L.Hkv, a.Bt.B), f8mq::kCombineThreads, 0, st);
   return cudaLaunchKernelEx(&cfg, f8mq::f8_mq_combine_kernel<RV>, a, tile);
