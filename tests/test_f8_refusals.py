@@ -71,6 +71,7 @@ def test_run_attention_refuses_and_plans(lib):
     need = S.stief_f8_mq_workspace_bytes(2, 8, 8, 64, 4)
     assert need >= 2 * 8 * 8 * 2 * 4 * 66 * 4 and S.stief_f8_mq_workspace_bytes(2, 8, 8, 64, 1) == 0 == S.stief_f8_mq_workspace_bytes(2, 8, 8, 64, 0)
     assert S.stief_f8_mq_num_splits(1, 4, 10, 2, 1000) >= 1 and S.stief_f8_mq_num_splits(1, 4, 129, 1, 10) == 0 == S.stief_f8_mq_num_splits(1, 0, 8, 2, 10)
+    assert S.stief_f8_mq_num_splits(1, 65536, 1, 1, 2 ** 31 - 1) == 1 and 1 <= S.stief_f8_mq_num_splits(1, 65535, 1, 1, 2 ** 31 - 1) <= 32
     assert S.stief_f8_mq_num_splits(8, 4096, 32, 8, 1000) == 1 and S.stief_f8_mq_num_splits(1, 2 ** 31 - 1, 32, 8, 1000) == 1
 
     def call(bt=S._CBatch(2, 4, P, P), q=P, sb=8 * 1024, st=1024, n=8, w=P, wb=need - 1, splits=4, out=P, ob=8 * 1024, ot=1024, flags=0, **kw):

@@ -252,6 +252,26 @@ def test_runs_split(splits, n, lens):
     Case(splits, lens, n=n).attend(splits=splits).check()
 
 
+@pytest.mark.parametrize("r_k,r_v", PAIRS)
+def test_parts_joined(r_k, r_v):
+    """Sequences of unequal numbers of rows, and more tiles of rows than blocks that join them."""
+    Case(r_k + 7 * r_v, [1, 700, 64, 300, 129], n=90, counts=[1, 90, 0, 77, 13], r_k=r_k, r_v=r_v).attend(splits=3).check()
+    if r_k == r_v:
+        Case(r_v, [900], n=700, Hq=16, Hkv=1, r_k=r_k, r_v=r_v).attend(splits=2).check()
+
+
+@pytest.mark.parametrize("r_k,r_v", [(64, 64), (64, 128), (48, 48), (96, 96)])
+@pytest.mark.parametrize("splits", [1, 2])
+def test_runs_whose_largest_score_grows(r_k, r_v, splits):
+    """The scale of the keys doubles every second page, so that every step moves the references of most rows."""
+    c = Case(27, [1300, 500], n=200, r_k=r_k, r_v=r_v)
+    pages = torch.arange(c.batch.block_table.shape[1], device="cuda")
+    for b, t in enumerate(c.lens):
+        c.layer.scales[c.batch.block_table[b, : (t + 63) // 64].long(), :, 0] = torch.exp2(-14.0 + pages[: (t + 63) // 64] // 2)[:, None]
+    c.K = _values(c, 0)
+    c.attend(splits=splits).check()
+
+
 def test_runs_long():
     Case(30, [9000], n=2048, Hq=4, Hkv=1).attend().check()
     c = Case(31, [500, 400], n=6)
