@@ -514,7 +514,11 @@ int stief_f8_decode_attention(const stief_f8layer* layer, const stief_batch* bat
 
 /* Several causal query rows per head over the 8-bit cache: arguments as stief_mq_attention, for any number of query heads per
  * KV head up to 128, and strides in either order (a batch stride below the token stride).  num_splits: 1 .. 32, from
- * stief_f8_mq_num_splits.  q' = q U_k and the probabilities pass through f16, each row scaled by a power of two of its own. */
+ * stief_f8_mq_num_splits, which weighs rounds of the GPU's SMs against what joining parts costs; with more than one part, up to
+ * 64 rows per KV head (n_q Hq / Hkv) take a kernel of their own, and at least two are proposed for them.  The workspace may
+ * hold anything and is used by one call at a time.  q' = q U_k and the probabilities pass through f16, each row scaled by a
+ * power of two of its own.  A NaN among a sequence's cached values reaches rows that attend its position, and may reach rows of
+ * the call up to 127 positions before it; rows behind seq_lens do not count, whatever they hold. */
 int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t max_pages_per_seq);
 size_t stief_f8_mq_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t r_v, int32_t num_splits);
 int stief_f8_mq_attention(const stief_f8layer* layer, const stief_batch* batch, const uint16_t* q, int64_t q_stride_b,
