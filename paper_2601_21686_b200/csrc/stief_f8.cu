@@ -151,7 +151,7 @@ extern "C" int stief_f8_mq_attention(const stief_f8layer* layer, const stief_bat
   const int RK = layer->r_k, RV = layer->r_v, TT = kMqRows / G;
   const bool fold_k = !layer->U_k, fold_v = !layer->U_v;
   const long long n_units = ((long long)n_q + 2 * TT - 1) / (2 * TT) * batch->B * layer->Hkv * num_splits;
-  if (n_q > (1 << 30) || n_units >= (1ll << 31)) return STIEF_ERR_INVALID_ARG;
+  if (n_q > (1 << 30) || n_units >= (1ll << 31) - 65536) return STIEF_ERR_INVALID_ARG;      // a CTA counts past the last by a grid's worth
   f8mq::Launch L = {};
   const tc::Blocks bk = tc::blocks_of(RK), bv = tc::blocks_of(RV);
   const unsigned long long nq = n_q, Hq = layer->Hq, B = batch->B;
