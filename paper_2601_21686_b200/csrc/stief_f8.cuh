@@ -10,7 +10,6 @@
 namespace stief {
 namespace f8 {
 
-constexpr float kTop = 448.f;                    // the largest e4m3 value
 constexpr int kLowest = -100, kHighest = 119;    // exponents of a scale: codes times scales stay within fp32's and bf16's range
 constexpr int kScalesPerTile = 4;                // floats of a (page, head): key scale, value scale, two unused (16 bytes, one bulk copy)
 
