@@ -419,7 +419,8 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
         }
       }
     }
-    const bool whole = single && !__syncthreads_or(missing);               // one page, all of its rows: the common case of prompts
+    // one page, all of its rows: the common case of prompts (a page outside the pool has no rows, and nothing of it is addressed)
+    const bool whole = single && !__syncthreads_or(missing || touch[0].m == 0);
     if (!single) __syncthreads();
     fetch(next, raw_at(n + 1));
 
@@ -599,7 +600,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Sequences& s, u
     __syncthreads();
     const int per_row = row_bytes / 16;
     const uint32_t recip = 65536u / per_row + 1;                           // i / per_row of i < 1024
-    uint4* whole_dst = reinterpret_cast<uint4*>(pool + (((size_t)touch[0].page * a.L.Hkv + h) * kPage + (touch[0].place0 & (kPage - 1))) * row_bytes);
+    uint4* whole_dst = whole ? reinterpret_cast<uint4*>(pool + (((size_t)touch[0].page * a.L.Hkv + h) * kPage + (touch[0].place0 & (kPage - 1))) * row_bytes) : nullptr;
     for (int i = tid; i < rows * per_row; i += kThreads) {
       const int slot = (i * recip) >> 16, piece = i - slot * per_row;
       const uint4 w = *reinterpret_cast<const uint4*>(stage + staged(slot, piece * 16));

@@ -388,3 +388,32 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     a.check()
     b.check()
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("where", ["behind the pool", "before the pool", "behind the table"])
+@pytest.mark.parametrize("lens,counts", [([100], [9]), ([100, 70], [9, 300]), ([64 * (i % 4) + 5 * (i % 3) for i in range(300)], [1 + i % 4 for i in range(300)])])
+def test_memory_around_the_pools_is_left_alone(f8, where, lens, counts):
+    """Pages outside the pool, one page to a tile and several, with older rows in front of the new ones and without.  The pools lie in
+    the middle of larger buffers."""
+    c = Case(21, lens, counts, f8=f8, Hq=4, Hkv=2, r_k=64, r_v=48)
+    L, around = c.layer, []
+    for name in ("k_codes", "v_codes", "scales") if f8 else ("k_pool", "v_pool"):
+        t = getattr(L, name)
+        big = torch.randint(0, 256, (t.shape[0] + 4, t[0].numel() * t.element_size()), dtype=torch.uint8, device="cuda")
+        big[2:-2] = t.view(torch.uint8).view(t.shape[0], -1)
+        setattr(L, name, big[2:-2].view(t.dtype).view(t.shape))
+        around.append((big, big[:2].clone(), big[-2:].clone()))
+    last = [(a + n - 1) // 64 for a, n in zip(lens, counts)]
+    if where == "behind the table":
+        width = max(last)
+        gone = [int(c.table[b, i]) for b, i in enumerate(last) if i == width]
+        c.batch = S.Batch(c.batch.block_table[:, :width].contiguous(), c.batch.seq_lens)
+    else:
+        gone = [int(c.table[b, i]) for b, i in enumerate(last) if b % 2 == 0]
+        for b, i in enumerate(last):
+            if b % 2 == 0:
+                c.batch.block_table[b, i] = c.P if where == "behind the pool" else -1
+    c.call().check(status=S.STIEF_ERR_BOUNDS, skip_pages=gone)
+    for big, front, back in around:
+        assert torch.equal(big[:2], front) and torch.equal(big[-2:], back)
