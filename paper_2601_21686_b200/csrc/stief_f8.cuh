@@ -11,6 +11,14 @@ namespace stief {
 namespace f8 {
 
 constexpr int kLowest = -100, kHighest = 119;    // exponents of a scale: codes times scales stay within fp32's and bf16's range
+// Row sums of the attention kernels.  A weight is 2^(x + e - ref), x the score and 2^e the page's value scale; the sum of a row wants
+// 2^x, and e may differ by 219 from page to page, so the sum l has a reference of its own, N, that goes by scores alone: l counts 2^(x - N).
+// N is set to a page's largest score where that lies more than kSumGrown above it, so with weights of up to 2^15 and pages of 64 rows l
+// stays below 2^(6 + 40) a page.  A page adds its sum of weights times 2^(ref - e - N).  Where its largest weight lies below 2^kSumLow,
+// they may vanish in the sum: it then takes exponentials that go by the page's own largest instead of ref (in the mix, whose f16 weights
+// end at 2^-24, the page is nothing).
+constexpr float kSumGrown = 40.f, kSumLow = -80.f;
+
 constexpr int kScalesPerTile = 4;                // floats of a (page, head): key scale, value scale, two unused (16 bytes, one bulk copy)
 
 // The layer as the attention kernels see it: LayerDev's pool pointers are unused.

@@ -10,7 +10,8 @@
 //           e4m3x2 -> f16x2 (exact) make them B fragments, the channels being contracted in that order on both sides.
 //   softmax base 2, in registers.  The page's value scale is a power of two 2^e, so it joins the exponent: the weight of a
 //           token is w = 2^(x + e - ref), x its score, ref the running maximum of x + e.  Weights of any two pages are thus
-//           right relative to each other's contribution, however far their scales lie apart, and the row sum takes w 2^-e.
+//           right relative to each other's contribution, however far their scales lie apart.  The row sum takes w 2^-e under a
+//           reference of its own (kSumGrown in stief_f8.cuh).
 //   mix     O^T = V^T P^T: the 16 channels of a 16-byte chunk are the 16 rows of A (ldmatrix.trans and a byte permutation
 //           bring two tokens of one channel together; even channels in rows 0-7, odd ones in rows 8-15), B = the weights, in
 //           the very registers that computed them.  Weights are rounded to f16 once, scaled by 2^15 so that the
@@ -91,7 +92,7 @@ struct DecodeCfg8 {
   static constexpr int SMEM_BYTES = 1024 + RING_BYTES + MISC;
   static_assert(K_BYTES % 1024 == 0 && V_BYTES % 1024 == 0, "both tiles keep the swizzle alignment");
   static_assert(SPW >= 1 && NS <= 32, "ring shape");
-  static_assert((NW * 8 * RV + 2 * NW * 8) * 4 <= UNION_BYTES, "merge scratch must fit");
+  static_assert((NW * 8 * RV + 3 * NW * 8) * 4 <= UNION_BYTES, "merge scratch must fit");
   static_assert(kCombineScratchFloats * 4 <= UNION_BYTES, "combine scratch must fit");
   static_assert(SMEM_BYTES <= 232448, "exceeds the 227 KiB shared memory of an SM");
 };
@@ -302,7 +303,8 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
     }
 
-    float m = -INFINITY, l = 0.f;                          // row gid: reference, and this thread's share of the sum
+    // row gid: reference of the mix, this thread's share of the sum, the sum's reference, m - n (-inf: nothing seen)
+    float m = -INFINITY, l = 0.f, n = -INFINITY, apart = -INFINITY;
     float o[NCV][4];                                       // channels 16 i + 2 gid, + 1 (o[.][0], [1] and [2], [3]) of queries 2 tid4, 2 tid4 + 1
 #pragma unroll
     for (int i = 0; i < NCV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -363,9 +365,11 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const float m_new = fmaxf(m, top - 15.f);            // weights reach 2^15
-      if (__any_sync(0xffffffffu, m_new > m)) {            // the reference seldom grows after a sequence's first pages
+      const float x_top = top - evf;
+      float share = apart - evf;                           // log2 of what the page's weights count for in the sum
+      // seldom after a sequence's first pages: the references grow, or the page's weights may vanish in the sum
+      if (__any_sync(0xffffffffu, m_new > m || x_top > n + kSumGrown || top < m + kSumLow)) {
         const float alpha = fast_exp2(m - m_new);
-        l *= alpha;
         const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * tid4), a1 = __shfl_sync(0xffffffffu, alpha, 8 * tid4 + 4);
 #pragma unroll
         for (int i = 0; i < NCV; ++i) {
@@ -375,6 +379,21 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           o[i][3] *= a1;
         }
         m = m_new;
+        if (x_top > n + kSumGrown) {
+          l *= fast_exp2(n - x_top);
+          n = x_top;
+        }
+        apart = m > -INFINITY ? m - n : -INFINITY;
+        share = apart - evf;
+        if (top < m + kSumLow) {
+          share = -INFINITY;
+          if (top > -INFINITY) {
+            float own = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) own += fast_exp2(x[i] - top);
+            l = fmaf(own, fast_exp2(x_top - n), l);
+          }
+        }
       }
       float sum = 0.f;
 #pragma unroll
@@ -382,7 +401,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         x[i] = fast_exp2(x[i] - m);
         sum += x[i];
       }
-      l = fmaf(sum, pow2(-ev), l);
+      l = fmaf(sum, fast_exp2(share), l);
 
       // ---- mix
 #pragma unroll
@@ -421,6 +440,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     float* wo = un;                      // [NW][8][RV]
     float* wm = wo + NW * 8 * RV;        // [NW][8]
     float* wl = wm + NW * 8;             // [NW][8]
+    float* wn = wl + NW * 8;             // [NW][8]
 #pragma unroll
     for (int i = 0; i < NCV; ++i) {
       *reinterpret_cast<float2*>(wo + (warp * 8 + 2 * tid4) * RV + 16 * i + 2 * gid) = make_float2(o[i][0], o[i][2]);
@@ -429,6 +449,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     if (tid4 == 0) {
       wm[warp * 8 + gid] = m;
       wl[warp * 8 + gid] = l;
+      wn[warp * 8 + gid] = n;
     }
     // Everything up to here only read inputs.  This section of the workspace may still be in use by its previous user when the
     // launch overlaps earlier kernels.  Thread 0 settles the question for the CTA before the barrier: yes if producer 0 saw
@@ -450,18 +471,21 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     if (*gate == 0) grid_dependency_wait();
     for (int idx = tid; idx < ng * RV; idx += NT) {
       const int gg = idx / RV, j = idx % RV;
-      float M = wm[gg];
+      float M = wm[gg], N = wn[gg];
 #pragma unroll
-      for (int w = 1; w < NW; ++w) M = fmaxf(M, wm[w * 8 + gg]);
+      for (int w = 1; w < NW; ++w) {
+        M = fmaxf(M, wm[w * 8 + gg]);
+        N = fmaxf(N, wn[w * 8 + gg]);
+      }
       float num = 0.f, den = 0.f;
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float e = fast_exp2(wm[w * 8 + gg] - M);
-        num += e * wo[(w * 8 + gg) * RV + j];
-        den += e * wl[w * 8 + gg];
+        num += fast_exp2(wm[w * 8 + gg] - M) * wo[(w * 8 + gg) * RV + j];
+        den += fast_exp2(wn[w * 8 + gg] - N) * wl[w * 8 + gg];
       }
-      __stcg(a.partial_o + ((size_t)slot_id * kGroupTile + gg) * RV + j, num / den);
-      if (j == 0) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, (M + log2f(den)) * kLn2);
+      const float half = fast_exp2(0.5f * (M - N));        // in two steps: M - N reaches beyond fp32's exponents where scales lie far apart
+      __stcg(a.partial_o + ((size_t)slot_id * kGroupTile + gg) * RV + j, num / den * half * half);
+      if (j == 0) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, (N + log2f(den)) * kLn2);
     }
 
     // ------------------------------------------------------------------ the unit's last partial triggers the combine

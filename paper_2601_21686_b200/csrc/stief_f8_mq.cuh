@@ -11,7 +11,8 @@
 //              2^11 .. 2^12: f16's range is no limit, and a row's factor goes into its exponents.
 //   scales     powers of two.  The key scale joins a page's exponent factor.  The value scale 2^e joins the exponent itself: the
 //              weight of a position is w = 2^(x + e - ref), ref going by the largest x + e of the row, so weights of pages
-//              whose scales lie far apart keep their precision; the row sum takes w 2^-e.
+//              whose scales lie far apart keep their precision; the row sum takes w 2^-e under a reference of its own (kSumGrown in
+//              stief_f8.cuh).
 //   weights    f16 (11 bits, where bf16 would leave 8), at most 2^15: the reference is moved when a row's largest has grown by
 //              more than 2^8, and w = 2^7 at the reference.
 // A step is a block of two pages, 128 positions: waits, TMEM round trips and reductions are paid once per 128 scores of a row.
@@ -645,7 +646,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         arrive_warp(bar_at(kQReady + t));
       }
 
-      float m_ref = -INFINITY, l = 0.f;                         // the largest exponent when the reference was last set; row sum
+      float m_ref = -INFINITY, l = 0.f, n_ref = -INFINITY;      // the largest exponent when the reference was last set; row sum and its reference
       for (int jo = 0; jo < nb; ++jo, ++n) {
         const int j = a.dual ? 2 * jo + t : jo;                 // the block within the unit's range
         mbar_wait(bar_at(kSFull + t), n & 1, abort_flag, status);
@@ -671,7 +672,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         // exponents x = s f + e of the two pages; f is above zero, so that masked scores stay -inf
         const float f0 = fmaxf(c_row * sc.x, 1e-37f), f1 = fmaxf(c_row * sc.z, 1e-37f);
         const int e0 = min(max((int)((__float_as_uint(sc.y) >> 23) & 255u) - 127, -126), 126), e1 = min(max((int)((__float_as_uint(sc.w) >> 23) & 255u) - 127, -126), 126);
-        float mx;
+        float mx, top0, top1;                                   // largest exponent of both pages, largest scores of each
         {
           float m[4] = {s[0], s[1], s[64], s[65]};
 #pragma unroll
@@ -681,7 +682,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
               m[2 * h] = max3(m[2 * h], s[64 * h + i], s[64 * h + i + 1]);
               m[2 * h + 1] = max3(m[2 * h + 1], s[64 * h + i + 2], s[64 * h + i + 3]);
             }
-          mx = fmaxf(fmaf(fmaxf(max3(m[0], s[62], s[63]), m[1]), f0, (float)e0), fmaf(fmaxf(max3(m[2], s[126], s[127]), m[3]), f1, (float)e1));
+          top0 = fmaxf(max3(m[0], s[62], s[63]), m[1]);
+          top1 = fmaxf(max3(m[2], s[126], s[127]), m[3]);
+          mx = fmaxf(fmaf(top0, f0, (float)e0), fmaf(top1, f1, (float)e1));
         }
         // P and the accumulator are idle once the block before is mixed (with P over the scores, these scores came after that)
         auto mixed = [&]() {
@@ -701,19 +704,38 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
           moved = __any_sync(0xffffffffu, grown);
           if (grown) {
             r = fast_exp2(m_ref - mx);
-            l *= r;
             m_ref = mx;
           }
         }
         const float ref = m_ref > -INFINITY ? m_ref - kHeadroomLog2 : 0.f;
+        // The row sum: what the exponentials of the two pages go by, and what they count for
+        const float x_page[2] = {top0 * f0, top1 * f1};
+        float share[2];
+        bool vanish[2];
+        {
+          const float x_top = fmaxf(x_page[0], x_page[1]);
+          if (x_top > n_ref + f8::kSumGrown) {
+            l *= fast_exp2(n_ref - x_top);
+            n_ref = x_top;
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float e = (float)(h ? e1 : e0), y = x_page[h] + e;
+            vanish[h] = y - ref < f8::kSumLow && y > -INFINITY;
+            // (with an end, so that a page of which the row attends nothing, sum 0, meets no infinity)
+            share[h] = fast_exp2(fminf((vanish[h] ? y : ref) - e - n_ref, 126.f));
+          }
+        }
         // Exponents x - ref as one fma with e - ref where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
-        // rounded x is what counts, less the reference.  A page at a time: its weights are mixed while the next one's are made.
+        // rounded x is what counts, less the reference.  That form also serves pages whose weights vanish: exponentials by the page's own
+        // largest score, for the sum alone.  A page at a time: its weights are mixed while the next one's are made.
         auto weights = [&](auto far_tag) {
           constexpr bool kFar = decltype(far_tag)::value;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float f = h ? f1 : f0, e = (float)(h ? e1 : e0), shift = kFar ? e : e - ref;
-            const uint64_t f2 = pack2(f, f), e2 = pack2(shift, shift), ref2 = pack2(-ref, -ref);
+            const float f = h ? f1 : f0, e = (float)(h ? e1 : e0), shift = kFar ? (vanish[h] ? -x_page[h] : e) : e - ref;
+            const float less = kFar && vanish[h] ? 0.f : -ref, mix = vanish[h] ? 0.f : 1.f;
+            const uint64_t f2 = pack2(f, f), e2 = pack2(shift, shift), ref2 = pack2(less, less);
             uint64_t sum2 = pack2(0.f, 0.f);
             uint32_t pk[32];
 #pragma unroll
@@ -725,7 +747,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
               x0 = fast_exp2(x0);
               x1 = fast_exp2(x1);
               sum2 = add2(sum2, pack2(x0, x1));
-              pk[i] = f8::pack_f16(x0, x1);
+              pk[i] = kFar ? f8::pack_f16(x0 * mix, x1 * mix) : f8::pack_f16(x0, x1);
             }
             if (h == 0) mixed();
             tmem_st16(t_p + 32 * h, *reinterpret_cast<uint32_t(*)[16]>(&pk[0]));
@@ -743,24 +765,24 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             }
             float a0, a1;
             unpack2(sum2, a0, a1);
-            l = fmaf(a0 + a1, f8::pow2(h ? -e1 : -e0), l);
+            l = fmaf(a0 + a1, share[h], l);
             tmem_st_wait();
             tc_fence_before();
             arrive_warp(bar_at(kPFull + 2 * t + h));
           }
         };
-        if (__any_sync(0xffffffffu, fabsf(ref) > kFarReference)) weights(std::true_type{});
+        if (__any_sync(0xffffffffu, fabsf(ref) > kFarReference || vanish[0] || vanish[1])) weights(std::true_type{});
         else weights(std::false_type{});
       }
 
       // ---- epilogue of the unit
       mbar_wait(bar_at(kOFull + t), kt & 1, abort_flag, status);
       tc_fence_after();
-      const float ref = m_ref - kHeadroomLog2;
-      const float inv = 1.0f / l;
+      const float half = fast_exp2(0.5f * (m_ref - kHeadroomLog2 - n_ref));      // in two steps: beyond fp32's exponents where scales lie far apart
+      const float inv = half / l;
       __nv_bfloat16* orow = a.out + (size_t)w.b * a.out_stride_b + (size_t)tok * a.out_stride_t + (size_t)(w.h * G + g) * d_out;
       if (a.n_split > 1) {
-        // partial result of this part of the page range: unnormalised mix, reference (base-2 units) and row sum
+        // partial result of this part of the page range: its mix, and its row sum with the reference (base-2 units)
         const size_t prow = (((size_t)w.b * a.n_q + tok) * a.L.Hq + w.h * G + g) * a.n_parts + (a.dual ? 2 * w.split + t : w.split);
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16];
@@ -770,15 +792,18 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             float4* dst = reinterpret_cast<float4*>(a.part_o + prow * RV + c0);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              dst[i] = make_float4(__uint_as_float(v[4 * i]), __uint_as_float(v[4 * i + 1]), __uint_as_float(v[4 * i + 2]), __uint_as_float(v[4 * i + 3]));
+              dst[i] = make_float4(__uint_as_float(v[4 * i]) * half * inv, __uint_as_float(v[4 * i + 1]) * half * inv,
+                                   __uint_as_float(v[4 * i + 2]) * half * inv, __uint_as_float(v[4 * i + 3]) * half * inv);
           }
         }
-        if (row_valid) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(ref, l);
+        if (row_valid) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(n_ref, l);
       } else if (fold_v) {
         for (int c0 = 0; c0 < RV; c0 += 16) {
           uint32_t v[16], pk[8];
           tmem_ld16(t_o + c0, v);
           tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * half);
           pack16(v, inv, pk);
           if (row_valid) {
             *reinterpret_cast<uint4*>(orow + c0) = make_uint4(pk[0], pk[1], pk[2], pk[3]);
@@ -795,7 +820,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const float x0 = __uint_as_float(v[2 * i]) * inv, x1 = __uint_as_float(v[2 * i + 1]) * inv;
+              const float x0 = __uint_as_float(v[2 * i]) * half * inv, x1 = __uint_as_float(v[2 * i + 1]) * half * inv;
               uint32_t hi, lo;
               split_bf16(x0, x1, hi, lo);
               pk[i] = pass ? lo : hi;
@@ -821,7 +846,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         }
       }
       if (row_valid && a.out_lse && a.n_split == 1)
-        a.out_lse[((size_t)w.b * a.n_q + tok) * a.L.Hq + w.h * G + g] = kLn2 * (ref + log2f(l));
+        a.out_lse[((size_t)w.b * a.n_q + tok) * a.L.Hq + w.h * G + g] = kLn2 * (n_ref + log2f(l));
       tc_fence_before();
       arrive_warp(bar_at(kUnitDone + t));                       // the tile's TMEM columns and operand region are free
       ++kt;
@@ -835,7 +860,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
 
 // Measured: 0.25 (r_v 32, 64) to 0.5 us (128) for a thousand rows of two parts, on top of 10 us for a launch that waits for
 // another; a block of 256 threads that fetches the next tile's references early took as long.
-// Merges the parts of a split page range (by their references), normalises, back-projects and writes the rows.  The rows of a
+// Merges the parts of a split page range (by their sums and references), back-projects and writes the rows.  The rows of a
 // (sequence, KV head), token by token and its G heads in turn, are taken in tiles of `tile_rows` <= 16; a block keeps U_v as operands
 // of mma.sync in registers and goes through every gridDim.x-th tile.  Rows go to the product as bf16(x) and bf16(x - bf16(x)), as
 // without parts.  A part that had no block for the row's tile was never written and is left out by redoing the range arithmetic of
@@ -911,8 +936,8 @@ f8_mq_combine_kernel(const mq::Args a, int tile_rows) {
 #pragma unroll
       for (int i = 0; i < kMaxParts / 8; ++i) {
         const bool some = l[i] > 0.f || l[i] != l[i];           // a part that the row attends nothing of has l = 0
-        m[i] = some ? fast_exp2(m[i] - M) : 0.f;
-        den += some ? l[i] * m[i] : 0.f;
+        m[i] = some ? l[i] * fast_exp2(m[i] - M) : 0.f;
+        den += m[i];
       }
 #pragma unroll
       for (int o = 4; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);

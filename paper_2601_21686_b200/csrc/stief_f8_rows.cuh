@@ -9,7 +9,7 @@
 //            by the power of two that brings its largest element to 2^11 .. 2^12
 //   pages    as in the decode kernel: codes to f16 in registers, weights 2^(x + e - ref) with the value scale 2^e in the exponent,
 //            O^T = V^T P^T with two groups of 8 rows as the columns of P^T
-// The parts' unnormalised mixes, references and sums are merged by f8_mq_combine_kernel.
+// The parts' mixes, sums and references are merged by f8_mq_combine_kernel.
 //
 // Measured with that kernel (4 x 32768 tokens, 32 query heads over 8): ranks 64/64 4 / 8 / 16 tokens 41 / 61 / 102 us, 128/128 8 tokens 104.  Two
 // warps that read the same page convert it twice, which sets the pace from 32 rows on; 32 rows in one warp ran at 75 us where 16 in two ran
@@ -35,6 +35,7 @@ struct Cfg {
   static constexpr int STAGE_BYTES = (TX_BYTES + 1023) / 1024 * 1024;
   static constexpr int CTRL_BYTES = 1024;
   static constexpr int U_PITCH = RK * 2 + 16;              // bytes of a basis row in shared memory: ldmatrix reads eight of them without conflicts
+  static_assert(3 * kWarps * 16 <= kMaxRows * (RK + 4), "the warps' references and sums fit where the queries were");
   static constexpr int Q_PITCH = RK + 4;                   // floats of a projected row
   static constexpr int MISC = CTRL_BYTES + kD * U_PITCH + kMaxRows * Q_PITCH * 4;
   static constexpr int BUDGET = 232448 - 1024 - MISC;
@@ -227,7 +228,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     voff[i] = TV::chunk(8 * (n & 1) + l7, n >> 1);
   }
 
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, n[2] = {-INFINITY, -INFINITY}, apart[2] = {-INFINITY, -INFINITY};      // as in the decode kernel
   float o[NCV][2][4];                                           // channels 16 i + 2 gid (+ 1) of rows 2 tid4, + 1, and of those 8 further
 #pragma unroll
   for (int i = 0; i < NCV; ++i)
@@ -271,8 +272,9 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         }
     }
     const int ev = min(max((int)((__float_as_uint(vs) >> 23) & 255u) - 127, -126), 126);
-    const float evf = (float)ev, inv_vs = f8::pow2(-ev);
-    float m_new[2];
+    const float evf = (float)ev;
+    float m_new[2], tops[2], share[2];
+    bool seldom = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const float f = fac[e] * ks;
@@ -288,13 +290,15 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       for (int t = 1; t < 16; ++t) top = fmaxf(top, x[e][t]);
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      tops[e] = top;
       m_new[e] = fmaxf(m[e], top - 15.f);                       // weights reach 2^15
+      share[e] = apart[e] - evf;
+      seldom |= m_new[e] > m[e] || top - evf > n[e] + f8::kSumGrown || top < m[e] + f8::kSumLow;
     }
-    if (__any_sync(0xffffffffu, m_new[0] > m[0] || m_new[1] > m[1])) {
+    if (__any_sync(0xffffffffu, seldom)) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float alpha = m_new[e] > m[e] ? fast_exp2(m[e] - m_new[e]) : 1.f;          // (a row that has seen nothing keeps -inf)
-        l[e] *= alpha;
         m[e] = m_new[e];
         const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * tid4), a1 = __shfl_sync(0xffffffffu, alpha, 8 * tid4 + 4);
 #pragma unroll
@@ -303,6 +307,22 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           o[c][e][1] *= a1;
           o[c][e][2] *= a0;
           o[c][e][3] *= a1;
+        }
+        const float x_top = tops[e] - evf;
+        if (x_top > n[e] + f8::kSumGrown) {
+          l[e] *= fast_exp2(n[e] - x_top);
+          n[e] = x_top;
+        }
+        apart[e] = m[e] > -INFINITY ? m[e] - n[e] : -INFINITY;
+        share[e] = apart[e] - evf;
+        if (tops[e] < m[e] + f8::kSumLow) {
+          share[e] = -INFINITY;
+          if (tops[e] > -INFINITY) {
+            float own = 0.f;
+#pragma unroll
+            for (int t = 0; t < 16; ++t) own += fast_exp2(x[e][t] - tops[e]);
+            l[e] = fmaf(own, fast_exp2(x_top - n[e]), l[e]);
+          }
         }
       }
     }
@@ -315,7 +335,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         x[e][t] = fast_exp2(x[e][t] - ref);
         sum += x[e][t];
       }
-      l[e] = fmaf(sum, inv_vs, l[e]);
+      l[e] = fmaf(sum, fast_exp2(share[e]), l[e]);
     }
 
     // ---- mix
@@ -363,8 +383,8 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   bar1(kConsumers);                                             // every page has been consumed
   constexpr int WP = RV + 4;
   float* wo = reinterpret_cast<float*>(ring_ptr);               // [warp][16][WP]
-  float* wm = qp;                                               // [warp][16], then the sums
-  float* wl = qp + kWarps * 16;
+  float* wm = qp;                                               // [warp][16], then the sums and their references
+  float *wl = wm + kWarps * 16, *wn = wl + kWarps * 16;
 #pragma unroll
   for (int c = 0; c < NCV; ++c)
 #pragma unroll
@@ -377,13 +397,17 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     for (int e = 0; e < 2; ++e) {
       wm[warp * 16 + gid + 8 * e] = m[e];
       wl[warp * 16 + gid + 8 * e] = l[e];
+      wn[warp * 16 + gid + 8 * e] = n[e];
     }
   }
   bar1(kConsumers);
   for (int idx = tid; idx < n_rows * (RV / 4); idx += kConsumers) {
     const int row = idx / (RV / 4), c = idx % (RV / 4), g = row >> 4, r = row & 15;
-    float M = -INFINITY;
-    for (int p = 0; p < lanes; ++p) M = fmaxf(M, wm[((p << lg) + g) * 16 + r]);
+    float M = -INFINITY, N = -INFINITY;
+    for (int p = 0; p < lanes; ++p) {
+      M = fmaxf(M, wm[((p << lg) + g) * 16 + r]);
+      N = fmaxf(N, wn[((p << lg) + g) * 16 + r]);
+    }
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
     float den = 0.f;
     for (int p = 0; p < lanes; ++p) {
@@ -396,11 +420,12 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       num.y = fmaf(v.y, f, num.y);
       num.z = fmaf(v.z, f, num.z);
       num.w = fmaf(v.w, f, num.w);
-      den = fmaf(wl[w * 16 + r], f, den);
+      den = fmaf(wl[w * 16 + r], fast_exp2(wn[w * 16 + r] - N), den);
     }
+    const float half = fast_exp2(0.5f * (M - N)), over = half / den;
     const size_t prow = (((size_t)b * a.n_q + row / G) * a.L.Hq + h * G + row % G) * a.n_parts + split;
-    *reinterpret_cast<float4*>(a.part_o + prow * RV + 4 * c) = num;
-    if (c == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(M, den);
+    *reinterpret_cast<float4*>(a.part_o + prow * RV + 4 * c) = make_float4(num.x * half * over, num.y * half * over, num.z * half * over, num.w * half * over);
+    if (c == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(N, den);
   }
 }
 

@@ -384,6 +384,72 @@ def test_two_captured_graphs_share_a_workspace():
         c.check()
 
 
+def _forms(seed, lens, **kw):
+    """The three kernels: one token in one part and in many, a few rows (the kernel for them from two parts on), tiles of rows."""
+    yield Case(seed, lens, **kw), lambda c: c.decode(parts=1)
+    yield Case(seed, lens, **kw), lambda c: c.decode()
+    for n, splits in ((3, 1), (3, 2), (3, None), (70, 1), (70, 3)):
+        yield Case(seed, lens, n=n, **kw), lambda c, splits=splits: c.attend(splits=splits)
+
+
+def _fill(c, side, pages, scale, code=None):
+    """Pages (a mask over the places of each sequence's table) get one scale, and one code where it is given."""
+    codes = (c.layer.k_codes, c.layer.v_codes)[side]
+    for b, t in enumerate(c.lens):
+        ids = c.batch.block_table[b, :(t + 63) // 64].long()
+        ids = ids[pages(torch.arange(ids.numel(), device="cuda"))]
+        c.layer.scales[ids, :, side] = scale
+        if code is not None:
+            codes[ids] = code
+    if side:
+        c.V = _values(c, 1)
+    else:
+        c.K = _values(c, 0)
+
+
+@pytest.mark.parametrize("code", [0x00, 0x01, 0x7E])
+def test_long_sequences_of_zeros_and_tiny_values(code):
+    """Rows of zeros and of the smallest scale: each page's share of a row's sum is 2^100 times its weights."""
+    for c, call in _forms(50, [16384] * 4, Hq=4, Hkv=1, r_k=32, r_v=32, spare=0):
+        _fill(c, 0, lambda i: i >= 0, 2.0 ** -100, 0x00)
+        _fill(c, 1, lambda i: i >= 0, 2.0 ** -100, code)
+        call(c).check()
+
+
+def test_zeros_over_the_longest_batches():
+    """16 x 16384 in a decode step, 4 x 32768 in runs: zeros, and the logarithm of the length."""
+    for n, lens, splits in ((None, [16384] * 16, None), (8, [32768] * 4, None), (8, [32768] * 4, 1), (40, [32768] * 4, 1)):
+        c = Case(51, lens, n=n, Hq=32, Hkv=8, r_k=32, r_v=32, spare=0)
+        for side in (0, 1):
+            _fill(c, side, lambda i: i >= 0, 2.0 ** -100, 0x00)
+        (c.decode() if n is None else c.attend(splits=splits))
+        torch.cuda.synchronize()
+        assert c.status.item() == 0 and (c.out == 0).all()
+        seen = torch.full_like(c.lse, lens[0])
+        if n is not None:
+            seen -= torch.arange(n - 1, -1, -1, device="cuda")[:, None]
+        assert ((c.lse - seen.log()).abs() <= 1e-4 + 2.0 ** -22 * 11).all()
+
+
+@pytest.mark.parametrize("low,high", [(-100, 119), (-100, 20), (-100, -6), (-60, 40)])
+def test_pages_of_scales_as_far_apart_as_they_can_be(low, high):
+    """Every third page of the lower scale, scores of the same range in all: those pages are part of the sum, whatever their weights."""
+    for c, call in _forms(52, [1500, 130, 40], r_k=48, r_v=64):
+        _fill(c, 0, lambda i: i >= 0, 2.0 ** -7)
+        _fill(c, 1, lambda i: i % 3 != 1, 2.0 ** (high - 10))
+        _fill(c, 1, lambda i: i % 3 == 1, 2.0 ** low)
+        call(c).check()
+
+
+def test_zero_pages_between_ordinary_ones():
+    """... with scores that grow from page to page on top."""
+    for c, call in _forms(53, [2500, 700], r_k=64, r_v=48):
+        _fill(c, 1, lambda i: i % 2 == 0, 2.0 ** -100, 0x00)
+        for k in range(12):
+            _fill(c, 0, lambda i, k=k: i // 4 == k, 2.0 ** (k - 12))
+        call(c).check()
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then
