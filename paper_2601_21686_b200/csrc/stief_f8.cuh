@@ -11,13 +11,22 @@ namespace stief {
 namespace f8 {
 
 constexpr int kLowest = -100, kHighest = 119;    // exponents of a scale: codes times scales stay within fp32's and bf16's range
-// Row sums of the attention kernels.  A weight is 2^(x + e - ref), x the score and 2^e the page's value scale; the sum of a row wants
-// 2^x, and e may differ by 219 from page to page, so the sum l has a reference of its own, N, that goes by scores alone: l counts 2^(x - N).
-// N is set to a page's largest score where that lies more than kSumGrown above it, so with weights of up to 2^15 and pages of 64 rows l
-// stays below 2^(6 + 40) a page.  A page adds its sum of weights times 2^(ref - e - N).  Where its largest weight lies below 2^kSumLow,
-// they may vanish in the sum: it then takes exponentials that go by the page's own largest instead of ref (in the mix, whose f16 weights
-// end at 2^-24, the page is nothing).
-constexpr float kSumGrown = 40.f, kSumLow = -80.f;
+// Weights and row sums of the attention kernels.  A weight is w = 2^((x - M) + (e - E)), x the score and 2^e the page's value scale.  The
+// reference stays in two parts, M a score and E by the exponent of a scale: with far scores (beyond 2^24 fp32 holds not even all
+// integers) a sum of both would lose e and the headroom, where x - M is exact next to the largest.  (M, E) is moved when a weight would
+// exceed 2^kTopWeight, which is in the range of f16.
+// The sum of a row wants 2^x, and e may differ by 219 from page to page, so the sum l has a reference of its own, N, that goes by
+// scores alone: l counts 2^(x - N).  N is set to a page's largest score where that lies more than kSumGrown above it, so with pages of
+// 64 rows l stays below 2^(6 + 40) a page.  A page adds its sum of weights times 2^((M - N) + (E - e)).  Where its largest weight lies below 2^kSumLow,
+// they may vanish in the sum: it then takes exponentials that go by the page's own largest (in the mix, whose f16 weights end at 2^-24,
+// the page is nothing).
+constexpr float kNoSum = -3.402823466e38f;       // N before anything was seen
+constexpr float kTopWeight = 15.f, kSumGrown = 40.f, kSumLow = -80.f;
+// e of a scale 2^e, as a float and without a conversion, which would take a turn on the pipe of the exponentials
+__device__ __forceinline__ float scale_exponent(float scale) { return __uint_as_float(0x4b000000u | ((__float_as_uint(scale) >> 23) & 255u)) - 8388735.f; }
+// What turns a product of normalised queries and codes into a score.  Large queries over large scales leave fp32's range: a score is
+// then infinite, but that of a row of zeros stays zero.
+__device__ __forceinline__ float score_factor(float row, float scale) { return fminf(row * scale, 3.402823466e38f); }
 
 constexpr int kScalesPerTile = 4;                // floats of a (page, head): key scale, value scale, two unused (16 bytes, one bulk copy)
 

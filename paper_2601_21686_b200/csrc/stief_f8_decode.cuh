@@ -9,9 +9,9 @@
 //           codes.  ldmatrix leaves a thread four consecutive channels of one token in a register: two conversions
 //           e4m3x2 -> f16x2 (exact) make them B fragments, the channels being contracted in that order on both sides.
 //   softmax base 2, in registers.  The page's value scale is a power of two 2^e, so it joins the exponent: the weight of a
-//           token is w = 2^(x + e - ref), x its score, ref the running maximum of x + e.  Weights of any two pages are thus
-//           right relative to each other's contribution, however far their scales lie apart.  The row sum takes w 2^-e under a
-//           reference of its own (kSumGrown in stief_f8.cuh).
+//           token is w = 2^(x + e - ref), x its score, ref the running maximum of x + e, in two parts (kTopWeight in stief_f8.cuh).
+//           Weights of any two pages are thus right relative to each other's contribution, however far their scales lie
+//           apart.  The row sum takes w 2^-e under a reference of its own.
 //   mix     O^T = V^T P^T: the 16 channels of a 16-byte chunk are the 16 rows of A (ldmatrix.trans and a byte permutation
 //           bring two tokens of one channel together; even channels in rows 0-7, odd ones in rows 8-15), B = the weights, in
 //           the very registers that computed them.  Weights are rounded to f16 once, scaled by 2^15 so that the
@@ -92,7 +92,7 @@ struct DecodeCfg8 {
   static constexpr int SMEM_BYTES = 1024 + RING_BYTES + MISC;
   static_assert(K_BYTES % 1024 == 0 && V_BYTES % 1024 == 0, "both tiles keep the swizzle alignment");
   static_assert(SPW >= 1 && NS <= 32, "ring shape");
-  static_assert((NW * 8 * RV + 3 * NW * 8) * 4 <= UNION_BYTES, "merge scratch must fit");
+  static_assert((NW * 8 * RV + 4 * NW * 8) * 4 <= UNION_BYTES, "merge scratch must fit");
   static_assert(kCombineScratchFloats * 4 <= UNION_BYTES, "combine scratch must fit");
   static_assert(SMEM_BYTES <= 232448, "exceeds the 227 KiB shared memory of an SM");
 };
@@ -303,8 +303,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
     }
 
-    // row gid: reference of the mix, this thread's share of the sum, the sum's reference, m - n (-inf: nothing seen)
-    float m = -INFINITY, l = 0.f, n = -INFINITY, apart = -INFINITY;
+    float m = -INFINITY, em = 0.f, l = 0.f, n = kNoSum;    // row gid: both parts of the reference, this thread's share of the sum, the sum's reference
     float o[NCV][4];                                       // channels 16 i + 2 gid, + 1 (o[.][0], [1] and [2], [3]) of queries 2 tid4, 2 tid4 + 1
 #pragma unroll
     for (int i = 0; i < NCV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -344,11 +343,10 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           x[4 * j + 2 * u + 1] = s4[u][1] + s4[u][3];
         }
       }
-      const float f = fac * ks;
-      const int ev = min(max((int)((__float_as_uint(vs) >> 23) & 255u) - 127, -126), 126);
-      const float evf = (float)ev;
+      const float f = score_factor(fac, ks);
+      const float evf = scale_exponent(vs);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = __fadd_rn(__fmul_rn(x[i], f), evf);      // the rounded product is what the reference goes by
+      for (int i = 0; i < 16; ++i) x[i] = __fmul_rn(x[i], f);               // the rounded product is what the reference goes by
       if (tail) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -364,12 +362,11 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const float m_new = fmaxf(m, top - 15.f);            // weights reach 2^15
-      const float x_top = top - evf;
-      float share = apart - evf;                           // log2 of what the page's weights count for in the sum
+      const float above = (top - m) + (evf - em);          // log2 of the page's largest weight (infinity: nothing seen before)
       // seldom after a sequence's first pages: the references grow, or the page's weights may vanish in the sum
-      if (__any_sync(0xffffffffu, m_new > m || x_top > n + kSumGrown || top < m + kSumLow)) {
-        const float alpha = fast_exp2(m - m_new);
+      if (__any_sync(0xffffffffu, above > kTopWeight || above < kSumLow || top > n + kSumGrown)) {
+        const bool grown = above > kTopWeight;
+        const float alpha = grown ? fast_exp2(kTopWeight - above) : 1.f;
         const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * tid4), a1 = __shfl_sync(0xffffffffu, alpha, 8 * tid4 + 4);
 #pragma unroll
         for (int i = 0; i < NCV; ++i) {
@@ -378,30 +375,29 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           o[i][2] *= a0;
           o[i][3] *= a1;
         }
-        m = m_new;
-        if (x_top > n + kSumGrown) {
-          l *= fast_exp2(n - x_top);
-          n = x_top;
+        if (grown) {
+          m = top;
+          em = evf - kTopWeight;
         }
-        apart = m > -INFINITY ? m - n : -INFINITY;
-        share = apart - evf;
-        if (top < m + kSumLow) {
-          share = -INFINITY;
-          if (top > -INFINITY) {
-            float own = 0.f;
+        if (top > n + kSumGrown) {
+          l *= fast_exp2(n - top);
+          n = top;
+        }
+        if (above < kSumLow && top > -INFINITY) {
+          float own = 0.f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) own += fast_exp2(x[i] - top);
-            l = fmaf(own, fast_exp2(x_top - n), l);
-          }
+          for (int i = 0; i < 16; ++i) own += fast_exp2(x[i] - top);
+          l = fmaf(own, fast_exp2(top - n), l);
         }
       }
+      const float ref = m > -INFINITY ? m : 0.f, shift = evf - em;
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        x[i] = fast_exp2(x[i] - m);
+        x[i] = fast_exp2((x[i] - ref) + shift);
         sum += x[i];
       }
-      l = fmaf(sum, fast_exp2(share), l);
+      l = fmaf(sum, above < kSumLow ? 0.f : fast_exp2((m - n) - shift), l);
 
       // ---- mix
 #pragma unroll
@@ -441,6 +437,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     float* wm = wo + NW * 8 * RV;        // [NW][8]
     float* wl = wm + NW * 8;             // [NW][8]
     float* wn = wl + NW * 8;             // [NW][8]
+    float* we = wn + NW * 8;             // [NW][8]
 #pragma unroll
     for (int i = 0; i < NCV; ++i) {
       *reinterpret_cast<float2*>(wo + (warp * 8 + 2 * tid4) * RV + 16 * i + 2 * gid) = make_float2(o[i][0], o[i][2]);
@@ -450,6 +447,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       wm[warp * 8 + gid] = m;
       wl[warp * 8 + gid] = l;
       wn[warp * 8 + gid] = n;
+      we[warp * 8 + gid] = em;
     }
     // Everything up to here only read inputs.  This section of the workspace may still be in use by its previous user when the
     // launch overlaps earlier kernels.  Thread 0 settles the question for the CTA before the barrier: yes if producer 0 saw
@@ -469,23 +467,36 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     const int u = b * upb + seg.j;
     const int slot_id = c + u;
     if (*gate == 0) grid_dependency_wait();
+    // what each warp's mix counts for (in place of its reference) and what the row's is multiplied by: eight threads a row
+    if (tid < 64) {
+      const int w = tid & 7, gg = tid >> 3;
+      const float mw = wm[w * 8 + gg], ew = we[w * 8 + gg], nw = wn[w * 8 + gg];
+      float M = mw, E = ew, N = nw;
+#pragma unroll
+      for (int o1 = 1; o1 < 8; o1 <<= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, M, o1), e2 = __shfl_xor_sync(0xffffffffu, E, o1);
+        const bool larger = (m2 - M) + (e2 - E) > 0.f;
+        M = larger ? m2 : M;
+        E = larger ? e2 : E;
+        N = fmaxf(N, __shfl_xor_sync(0xffffffffu, N, o1));
+      }
+      float den = fast_exp2(nw - N) * wl[w * 8 + gg];
+#pragma unroll
+      for (int o1 = 1; o1 < 8; o1 <<= 1) den += __shfl_xor_sync(0xffffffffu, den, o1);
+      const float half = fast_exp2(0.5f * ((M - N) + E));  // in two steps: it reaches beyond fp32's exponents where scales lie far apart
+      wm[w * 8 + gg] = fast_exp2((mw - M) + (ew - E)) * half;
+      if (w == 0) {
+        wl[gg] = half / den;
+        if (gg < ng) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, (N + log2f(den)) * kLn2);
+      }
+    }
+    bar1(NT);
     for (int idx = tid; idx < ng * RV; idx += NT) {
       const int gg = idx / RV, j = idx % RV;
-      float M = wm[gg], N = wn[gg];
+      float num = 0.f;
 #pragma unroll
-      for (int w = 1; w < NW; ++w) {
-        M = fmaxf(M, wm[w * 8 + gg]);
-        N = fmaxf(N, wn[w * 8 + gg]);
-      }
-      float num = 0.f, den = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        num += fast_exp2(wm[w * 8 + gg] - M) * wo[(w * 8 + gg) * RV + j];
-        den += fast_exp2(wn[w * 8 + gg] - N) * wl[w * 8 + gg];
-      }
-      const float half = fast_exp2(0.5f * (M - N));        // in two steps: M - N reaches beyond fp32's exponents where scales lie far apart
-      __stcg(a.partial_o + ((size_t)slot_id * kGroupTile + gg) * RV + j, num / den * half * half);
-      if (j == 0) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, (N + log2f(den)) * kLn2);
+      for (int w = 0; w < NW; ++w) num = fmaf(wm[w * 8 + gg], wo[(w * 8 + gg) * RV + j], num);
+      __stcg(a.partial_o + ((size_t)slot_id * kGroupTile + gg) * RV + j, num * wl[gg]);
     }
 
     // ------------------------------------------------------------------ the unit's last partial triggers the combine

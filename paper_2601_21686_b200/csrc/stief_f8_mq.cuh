@@ -11,8 +11,8 @@
 //              2^11 .. 2^12: f16's range is no limit, and a row's factor goes into its exponents.
 //   scales     powers of two.  The key scale joins a page's exponent factor.  The value scale 2^e joins the exponent itself: the
 //              weight of a position is w = 2^(x + e - ref), ref going by the largest x + e of the row, so weights of pages
-//              whose scales lie far apart keep their precision; the row sum takes w 2^-e under a reference of its own (kSumGrown in
-//              stief_f8.cuh).
+//              whose scales lie far apart keep their precision; the row sum takes w 2^-e under a reference of its own (both
+//              references: kTopWeight in stief_f8.cuh).
 //   weights    f16 (11 bits, where bf16 would leave 8), at most 2^15: the reference is moved when a row's largest has grown by
 //              more than 2^8, and w = 2^7 at the reference.
 // A step is a block of two pages, 128 positions: waits, TMEM round trips and reductions are paid once per 128 scores of a row.
@@ -50,9 +50,8 @@ constexpr int kListed = 96;                      // sequences whose units can be
 constexpr int kMinStages = 4, kMaxStages = 8, kMinCodeSlots = 4, kMaxCodeSlots = 16;
 constexpr int kScaleSlots = 8;                   // blocks whose scales are kept: more than the operand ring holds
 constexpr int kPacePolls = 64, kPacedBlocks = 8;           // looks at the other tile; blocks from which on turns pay (2048 over 16384, 128/128: 795 us without, 644 with)
-constexpr float kRescaleLog2 = 8.0f;             // move a row's reference when its largest exponent grew by more
 constexpr float kFarReference = 1024.f;
-constexpr float kHeadroomLog2 = 7.0f;            // weights are 2^7 at the reference: at most 2^15 in f16
+constexpr float kHeadroomLog2 = 7.0f;            // weights are 2^7 at the reference; it is moved when one would exceed 2^kTopWeight
 
 struct Args {
   mq::Args m;                    // layer, batch, rows, outputs, parts; m.nst and m.qp_bytes as there, the pools in m.L are unused
@@ -646,7 +645,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         arrive_warp(bar_at(kQReady + t));
       }
 
-      float m_ref = -INFINITY, l = 0.f, n_ref = -INFINITY;      // the largest exponent when the reference was last set; row sum and its reference
+      float m = -INFINITY, em = 0.f, l = 0.f, n_ref = f8::kNoSum;      // both parts of the reference; row sum and its reference
       for (int jo = 0; jo < nb; ++jo, ++n) {
         const int j = a.dual ? 2 * jo + t : jo;                 // the block within the unit's range
         mbar_wait(bar_at(kSFull + t), n & 1, abort_flag, status);
@@ -670,9 +669,9 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             if (p0 + i >= end) s[i] = -INFINITY;
         }
         // exponents x = s f + e of the two pages; f is above zero, so that masked scores stay -inf
-        const float f0 = fmaxf(c_row * sc.x, 1e-37f), f1 = fmaxf(c_row * sc.z, 1e-37f);
-        const int e0 = min(max((int)((__float_as_uint(sc.y) >> 23) & 255u) - 127, -126), 126), e1 = min(max((int)((__float_as_uint(sc.w) >> 23) & 255u) - 127, -126), 126);
-        float mx, top0, top1;                                   // largest exponent of both pages, largest scores of each
+        const float f0 = fmaxf(f8::score_factor(c_row, sc.x), 1e-37f), f1 = fmaxf(f8::score_factor(c_row, sc.z), 1e-37f);
+        const float e0 = f8::scale_exponent(sc.y), e1 = f8::scale_exponent(sc.w);
+        float x_page[2];                                        // largest score of each page
         {
           float m[4] = {s[0], s[1], s[64], s[65]};
 #pragma unroll
@@ -682,9 +681,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
               m[2 * h] = max3(m[2 * h], s[64 * h + i], s[64 * h + i + 1]);
               m[2 * h + 1] = max3(m[2 * h + 1], s[64 * h + i + 2], s[64 * h + i + 3]);
             }
-          top0 = fmaxf(max3(m[0], s[62], s[63]), m[1]);
-          top1 = fmaxf(max3(m[2], s[126], s[127]), m[3]);
-          mx = fmaxf(fmaf(top0, f0, (float)e0), fmaf(top1, f1, (float)e1));
+          x_page[0] = __fmul_rn(fmaxf(max3(m[0], s[62], s[63]), m[1]), f0);
+          x_page[1] = __fmul_rn(fmaxf(max3(m[2], s[126], s[127]), m[3]), f1);
         }
         // P and the accumulator are idle once the block before is mixed (with P over the scores, these scores came after that)
         auto mixed = [&]() {
@@ -695,53 +693,48 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             }
           }
         };
-        float r = 1.f;                                          // what a moved reference leaves of the sum and the accumulator
+        float r = 1.f;                                          // what a moved reference leaves of the accumulator
         bool moved = false;                                     // for a row of the warp
-        if (jo == 0) {
-          m_ref = mx;                                           // -inf when a part of a split range begins behind the row's position
-        } else {
-          const bool grown = mx - m_ref > kRescaleLog2;         // a row's bits do not depend on its neighbours
-          moved = __any_sync(0xffffffffu, grown);
-          if (grown) {
-            r = fast_exp2(m_ref - mx);
-            m_ref = mx;
-          }
-        }
-        const float ref = m_ref > -INFINITY ? m_ref - kHeadroomLog2 : 0.f;
-        // The row sum: what the exponentials of the two pages go by, and what they count for
-        const float x_page[2] = {top0 * f0, top1 * f1};
-        float share[2];
         bool vanish[2];
         {
-          const float x_top = fmaxf(x_page[0], x_page[1]);
-          if (x_top > n_ref + f8::kSumGrown) {
-            l *= fast_exp2(n_ref - x_top);
-            n_ref = x_top;
+          // log2 of each page's largest weight (infinity: the row has attended nothing before)
+          float above[2] = {(x_page[0] - m) + (e0 - em), (x_page[1] - m) + (e1 - em)};
+          const float most = fmaxf(above[0], above[1]);
+          const bool grown = jo == 0 || most > f8::kTopWeight;
+          if (jo > 0) moved = __any_sync(0xffffffffu, grown);
+          if (grown) {
+            const bool second = (x_page[1] - x_page[0]) + (e1 - e0) > 0.f;
+            r = fast_exp2(kHeadroomLog2 - most);
+            m = second ? x_page[1] : x_page[0];                 // -inf when a part of a split range begins behind the row's position
+            em = (second ? e1 : e0) - kHeadroomLog2;
+            above[0] = (x_page[0] - m) + (e0 - em);
+            above[1] = (x_page[1] - m) + (e1 - em);
           }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float e = (float)(h ? e1 : e0), y = x_page[h] + e;
-            vanish[h] = y - ref < f8::kSumLow && y > -INFINITY;
-            // (with an end, so that a page of which the row attends nothing, sum 0, meets no infinity)
-            share[h] = fast_exp2(fminf((vanish[h] ? y : ref) - e - n_ref, 126.f));
-          }
+          for (int h = 0; h < 2; ++h) vanish[h] = above[h] < f8::kSumLow && x_page[h] > -INFINITY;
         }
-        // Exponents x - ref as one fma with e - ref where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
-        // rounded x is what counts, less the reference.  That form also serves pages whose weights vanish: exponentials by the page's own
-        // largest score, for the sum alone.  A page at a time: its weights are mixed while the next one's are made.
+        const float ref = m > -INFINITY ? m : 0.f;
+        const float x_top = fmaxf(x_page[0], x_page[1]);
+        if (x_top > n_ref + f8::kSumGrown) {
+          l *= fast_exp2(n_ref - x_top);
+          n_ref = x_top;
+        }
+        // Exponents as one fma with (e - E) - M where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
+        // rounded x is what counts, less M, then the scales.  That form also serves pages whose weights vanish: exponentials by the page's
+        // own largest score, for the sum alone.  A page at a time: its weights are mixed while the next one's are made.
         auto weights = [&](auto far_tag) {
           constexpr bool kFar = decltype(far_tag)::value;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float f = h ? f1 : f0, e = (float)(h ? e1 : e0), shift = kFar ? (vanish[h] ? -x_page[h] : e) : e - ref;
-            const float less = kFar && vanish[h] ? 0.f : -ref, mix = vanish[h] ? 0.f : 1.f;
-            const uint64_t f2 = pack2(f, f), e2 = pack2(shift, shift), ref2 = pack2(less, less);
+            const float f = h ? f1 : f0, shift = (h ? e1 : e0) - em, mix = vanish[h] ? 0.f : 1.f;
+            const float first = kFar ? 0.f : shift - ref, less = vanish[h] ? -x_page[h] : -ref, rest = vanish[h] ? 0.f : shift;
+            const uint64_t f2 = pack2(f, f), first2 = pack2(first, first), less2 = pack2(less, less), rest2 = pack2(rest, rest);
             uint64_t sum2 = pack2(0.f, 0.f);
             uint32_t pk[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
-              uint64_t x2 = fma2(pack2(s[64 * h + 2 * i], s[64 * h + 2 * i + 1]), f2, e2);
-              if constexpr (kFar) x2 = add2(x2, ref2);
+              uint64_t x2 = fma2(pack2(s[64 * h + 2 * i], s[64 * h + 2 * i + 1]), f2, first2);
+              if constexpr (kFar) x2 = add2(add2(x2, less2), rest2);
               float x0, x1;
               unpack2(x2, x0, x1);
               x0 = fast_exp2(x0);
@@ -765,7 +758,8 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             }
             float a0, a1;
             unpack2(sum2, a0, a1);
-            l = fmaf(a0 + a1, share[h], l);
+            // what the sum counts for (with an end, so that a page of which the row attends nothing, sum 0, meets no infinity)
+            l = fmaf(a0 + a1, fast_exp2(kFar && vanish[h] ? x_page[h] - n_ref : fminf((m - n_ref) - shift, 126.f)), l);
             tmem_st_wait();
             tc_fence_before();
             arrive_warp(bar_at(kPFull + 2 * t + h));
@@ -778,7 +772,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
       // ---- epilogue of the unit
       mbar_wait(bar_at(kOFull + t), kt & 1, abort_flag, status);
       tc_fence_after();
-      const float half = fast_exp2(0.5f * (m_ref - kHeadroomLog2 - n_ref));      // in two steps: beyond fp32's exponents where scales lie far apart
+      const float half = fast_exp2(0.5f * ((m - n_ref) + em));      // in two steps: beyond fp32's exponents where scales lie far apart
       const float inv = half / l;
       __nv_bfloat16* orow = a.out + (size_t)w.b * a.out_stride_b + (size_t)tok * a.out_stride_t + (size_t)(w.h * G + g) * d_out;
       if (a.n_split > 1) {

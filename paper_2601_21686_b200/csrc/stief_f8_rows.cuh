@@ -35,7 +35,7 @@ struct Cfg {
   static constexpr int STAGE_BYTES = (TX_BYTES + 1023) / 1024 * 1024;
   static constexpr int CTRL_BYTES = 1024;
   static constexpr int U_PITCH = RK * 2 + 16;              // bytes of a basis row in shared memory: ldmatrix reads eight of them without conflicts
-  static_assert(3 * kWarps * 16 <= kMaxRows * (RK + 4), "the warps' references and sums fit where the queries were");
+  static_assert(4 * kWarps * 16 <= kMaxRows * (RK + 4), "the warps' references and sums fit where the queries were");
   static constexpr int Q_PITCH = RK + 4;                   // floats of a projected row
   static constexpr int MISC = CTRL_BYTES + kD * U_PITCH + kMaxRows * Q_PITCH * 4;
   static constexpr int BUDGET = 232448 - 1024 - MISC;
@@ -228,7 +228,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     voff[i] = TV::chunk(8 * (n & 1) + l7, n >> 1);
   }
 
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, n[2] = {-INFINITY, -INFINITY}, apart[2] = {-INFINITY, -INFINITY};      // as in the decode kernel
+  float m[2] = {-INFINITY, -INFINITY}, em[2] = {0.f, 0.f}, l[2] = {0.f, 0.f}, n[2] = {f8::kNoSum, f8::kNoSum};      // as in the decode kernel
   float o[NCV][2][4];                                           // channels 16 i + 2 gid (+ 1) of rows 2 tid4, + 1, and of those 8 further
 #pragma unroll
   for (int i = 0; i < NCV; ++i)
@@ -271,15 +271,14 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           x[1][4 * j + 2 * u + c] = s4[u][2 + c];
         }
     }
-    const int ev = min(max((int)((__float_as_uint(vs) >> 23) & 255u) - 127, -126), 126);
-    const float evf = (float)ev;
-    float m_new[2], tops[2], share[2];
+    const float evf = f8::scale_exponent(vs);
+    float above[2], tops[2];
     bool seldom = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const float f = fac[e] * ks;
+      const float f = f8::score_factor(fac[e], ks);
 #pragma unroll
-      for (int t = 0; t < 16; ++t) x[e][t] = __fadd_rn(__fmul_rn(x[e][t], f), evf);      // the rounded product is what the reference goes by
+      for (int t = 0; t < 16; ++t) x[e][t] = __fmul_rn(x[e][t], f);      // the rounded product is what the reference goes by
       if (p0 + kPage > first_end) {
 #pragma unroll
         for (int t = 0; t < 16; ++t)
@@ -291,15 +290,14 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       tops[e] = top;
-      m_new[e] = fmaxf(m[e], top - 15.f);                       // weights reach 2^15
-      share[e] = apart[e] - evf;
-      seldom |= m_new[e] > m[e] || top - evf > n[e] + f8::kSumGrown || top < m[e] + f8::kSumLow;
+      above[e] = (top - m[e]) + (evf - em[e]);
+      seldom |= above[e] > f8::kTopWeight || above[e] < f8::kSumLow || top > n[e] + f8::kSumGrown;
     }
     if (__any_sync(0xffffffffu, seldom)) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float alpha = m_new[e] > m[e] ? fast_exp2(m[e] - m_new[e]) : 1.f;          // (a row that has seen nothing keeps -inf)
-        m[e] = m_new[e];
+        const bool grown = above[e] > f8::kTopWeight;           // (a row that has seen nothing keeps -inf)
+        const float alpha = grown ? fast_exp2(f8::kTopWeight - above[e]) : 1.f;
         const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * tid4), a1 = __shfl_sync(0xffffffffu, alpha, 8 * tid4 + 4);
 #pragma unroll
         for (int c = 0; c < NCV; ++c) {
@@ -308,34 +306,32 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           o[c][e][2] *= a0;
           o[c][e][3] *= a1;
         }
-        const float x_top = tops[e] - evf;
-        if (x_top > n[e] + f8::kSumGrown) {
-          l[e] *= fast_exp2(n[e] - x_top);
-          n[e] = x_top;
+        if (grown) {
+          m[e] = tops[e];
+          em[e] = evf - f8::kTopWeight;
         }
-        apart[e] = m[e] > -INFINITY ? m[e] - n[e] : -INFINITY;
-        share[e] = apart[e] - evf;
-        if (tops[e] < m[e] + f8::kSumLow) {
-          share[e] = -INFINITY;
-          if (tops[e] > -INFINITY) {
-            float own = 0.f;
+        if (tops[e] > n[e] + f8::kSumGrown) {
+          l[e] *= fast_exp2(n[e] - tops[e]);
+          n[e] = tops[e];
+        }
+        if (above[e] < f8::kSumLow && tops[e] > -INFINITY) {
+          float own = 0.f;
 #pragma unroll
-            for (int t = 0; t < 16; ++t) own += fast_exp2(x[e][t] - tops[e]);
-            l[e] = fmaf(own, fast_exp2(x_top - n[e]), l[e]);
-          }
+          for (int t = 0; t < 16; ++t) own += fast_exp2(x[e][t] - tops[e]);
+          l[e] = fmaf(own, fast_exp2(tops[e] - n[e]), l[e]);
         }
       }
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const float ref = m[e] > -INFINITY ? m[e] : 0.f;
+      const float ref = m[e] > -INFINITY ? m[e] : 0.f, shift = evf - em[e];
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 16; ++t) {
-        x[e][t] = fast_exp2(x[e][t] - ref);
+        x[e][t] = fast_exp2((x[e][t] - ref) + shift);
         sum += x[e][t];
       }
-      l[e] = fmaf(sum, fast_exp2(share[e]), l[e]);
+      l[e] = fmaf(sum, above[e] < f8::kSumLow ? 0.f : fast_exp2((m[e] - n[e]) - shift), l[e]);
     }
 
     // ---- mix
@@ -384,7 +380,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
   constexpr int WP = RV + 4;
   float* wo = reinterpret_cast<float*>(ring_ptr);               // [warp][16][WP]
   float* wm = qp;                                               // [warp][16], then the sums and their references
-  float *wl = wm + kWarps * 16, *wn = wl + kWarps * 16;
+  float *wl = wm + kWarps * 16, *wn = wl + kWarps * 16, *we = wn + kWarps * 16;
 #pragma unroll
   for (int c = 0; c < NCV; ++c)
 #pragma unroll
@@ -398,15 +394,20 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       wm[warp * 16 + gid + 8 * e] = m[e];
       wl[warp * 16 + gid + 8 * e] = l[e];
       wn[warp * 16 + gid + 8 * e] = n[e];
+      we[warp * 16 + gid + 8 * e] = em[e];
     }
   }
   bar1(kConsumers);
   for (int idx = tid; idx < n_rows * (RV / 4); idx += kConsumers) {
     const int row = idx / (RV / 4), c = idx % (RV / 4), g = row >> 4, r = row & 15;
-    float M = -INFINITY, N = -INFINITY;
+    float M = -INFINITY, E = 0.f, N = f8::kNoSum;
     for (int p = 0; p < lanes; ++p) {
-      M = fmaxf(M, wm[((p << lg) + g) * 16 + r]);
-      N = fmaxf(N, wn[((p << lg) + g) * 16 + r]);
+      const int w = (p << lg) + g;
+      if ((wm[w * 16 + r] - M) + (we[w * 16 + r] - E) > 0.f) {
+        M = wm[w * 16 + r];
+        E = we[w * 16 + r];
+      }
+      N = fmaxf(N, wn[w * 16 + r]);
     }
     float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
     float den = 0.f;
@@ -414,7 +415,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       const int w = (p << lg) + g;
       const float mw = wm[w * 16 + r];
       if (mw == -INFINITY) continue;                            // a lane that the row attends nothing of
-      const float f = fast_exp2(mw - M);
+      const float f = fast_exp2((mw - M) + (we[w * 16 + r] - E));
       const float4 v = *reinterpret_cast<const float4*>(wo + (w * 16 + r) * WP + 4 * c);
       num.x = fmaf(v.x, f, num.x);
       num.y = fmaf(v.y, f, num.y);
@@ -422,7 +423,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       num.w = fmaf(v.w, f, num.w);
       den = fmaf(wl[w * 16 + r], fast_exp2(wn[w * 16 + r] - N), den);
     }
-    const float half = fast_exp2(0.5f * (M - N)), over = half / den;
+    const float half = fast_exp2(0.5f * ((M - N) + E)), over = half / den;
     const size_t prow = (((size_t)b * a.n_q + row / G) * a.L.Hq + h * G + row % G) * a.n_parts + split;
     *reinterpret_cast<float4*>(a.part_o + prow * RV + 4 * c) = make_float4(num.x * half * over, num.y * half * over, num.z * half * over, num.w * half * over);
     if (c == 0) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(N, den);

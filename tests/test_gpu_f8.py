@@ -450,6 +450,51 @@ def test_zero_pages_between_ordinary_ones():
         call(c).check()
 
 
+@pytest.mark.parametrize("q_scale", [3e4, 1e6, 4e6, 1e7, 3e7, 1e8, 1e12, 1e25])
+def test_scores_far_from_zero(q_scale):
+    """References whose steps are as wide as the headroom of the weights (2^24 to 2^28 in base 2) and wider."""
+    for c, call in _forms(54, [900, 33], q_scale=q_scale):
+        call(c).check()
+
+
+@pytest.mark.parametrize("q_scale", [1.0, 3e4, 1e6, 1e7, 1e8, 1e12])
+def test_far_scores_of_equal_rows(q_scale):
+    """One key for every token: the mean of the values, whose scales differ from page to page.  (Decode in one part: the parts of a
+    decode step are joined by their log-sum-exps, which far scores leave no room for.)"""
+    for n, splits in ((None, None), (3, 1), (3, 4), (70, 1), (70, 3)):
+        c = Case(55, [700, 130], n=n, q_scale=q_scale, exponents=(-9, -4))
+        _fill(c, 0, lambda i: i >= 0, 2.0 ** -3, 0x38)
+        c.decode(parts=1) if n is None else c.attend(splits=splits)
+        torch.cuda.synchronize()
+        assert c.status.item() == 0
+        Uv, G = c.layer.U_v.double(), c.layer.Hq // c.layer.Hkv
+        for b, t in enumerate(c.lens):
+            for i in range(c.counts[b]):
+                V = c.V[b][:t - c.counts[b] + 1 + i]
+                o, size = (torch.einsum("hr,hdr->hd", x.mean(0), y).repeat_interleave(G, 0) for x, y in ((V, Uv), (V.abs(), Uv.abs())))
+                assert ((c.out[b, i].double() - o).abs() <= (HALF16 + 1e-4 + HALF * HALF) * size + HALF * o.abs()).all(), f"sequence {b}, token {i}"
+
+
+def test_scores_beyond_the_range():
+    """Queries and keys whose products leave fp32's range downwards, but for the rows of zeros, whose score is zero: their mean."""
+    for n, splits in ((None, None), (3, 1), (3, 4), (70, 1), (70, 3)):
+        c = Case(56, [700, 130], n=n, fold_k=True, exponents=(-6, -6))
+        _fill(c, 0, lambda i: i >= 0, 2.0 ** 60, 0xFE)                      # -448
+        for b, t in enumerate(c.lens):
+            c.layer.k_codes[c.batch.block_table[b, :(t + 63) // 64].long(), :, ::7] = 0
+        c.q.fill_(2.0 ** 80)
+        c.decode(parts=1) if n is None else c.attend(splits=splits)
+        torch.cuda.synchronize()
+        assert c.status.item() == 0
+        Uv, G = c.layer.U_v.double(), c.layer.Hq // c.layer.Hkv
+        for b, t in enumerate(c.lens):
+            for i in range(c.counts[b]):
+                seen = t - c.counts[b] + 1 + i
+                V = c.V[b][:seen][(torch.arange(seen, device="cuda") % 64) % 7 == 0]
+                o, size = (torch.einsum("hr,hdr->hd", x.mean(0), y).repeat_interleave(G, 0) for x, y in ((V, Uv), (V.abs(), Uv.abs())))
+                assert ((c.out[b, i].double() - o).abs() <= (HALF16 + 1e-4 + HALF * HALF) * size + HALF * o.abs()).all(), f"sequence {b}, token {i}"
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then
