@@ -630,7 +630,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         }
         const int e = top > 0.f ? min(max((int)(__float_as_uint(top) >> 23) - 127, -112), 126) - 11 : 0;
         const float norm = f8::pow2(-e);
-        c_row = f8::pow2(e) * c;
+        c_row = row_valid ? f8::pow2(e) * c : 0.f;              // rows of no token (what stands there may be anything) do not ask for the form for far scores
         for (int c0 = 0; c0 < RK; c0 += 16) {
           float x[16];
           piece(c0, x);
@@ -721,13 +721,21 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         }
         // Exponents as one fma with (e - E) - M where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
         // rounded x is what counts, less M, then the scales.  That form also serves pages whose weights vanish: exponentials by the page's
-        // own largest score, for the sum alone.  A page at a time: its weights are mixed while the next one's are made.
+        // own largest score, for the sum alone.  A warp takes it if a row of it needs it; the other rows then add zeros to the first form, so
+        // that a row's bits do not depend on its neighbours.  A page at a time: its weights are mixed while the next one's are made.
         auto weights = [&](auto far_tag) {
           constexpr bool kFar = decltype(far_tag)::value;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const float f = h ? f1 : f0, shift = (h ? e1 : e0) - em, mix = vanish[h] ? 0.f : 1.f;
-            const float first = kFar ? 0.f : shift - ref, less = vanish[h] ? -x_page[h] : -ref, rest = vanish[h] ? 0.f : shift;
+            float first = shift - ref, less = 0.f, rest = 0.f;
+            if constexpr (kFar) {
+              if (vanish[h] || fabsf(ref) > kFarReference) {
+                first = 0.f;
+                less = vanish[h] ? -x_page[h] : -ref;
+                rest = vanish[h] ? 0.f : shift;
+              }
+            }
             const uint64_t f2 = pack2(f, f), first2 = pack2(first, first), less2 = pack2(less, less), rest2 = pack2(rest, rest);
             uint64_t sum2 = pack2(0.f, 0.f);
             uint32_t pk[32];
@@ -765,7 +773,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             arrive_warp(bar_at(kPFull + 2 * t + h));
           }
         };
-        if (__any_sync(0xffffffffu, fabsf(ref) > kFarReference || vanish[0] || vanish[1])) weights(std::true_type{});
+        if (__any_sync(0xffffffffu, (fabsf(ref) > kFarReference || vanish[0] || vanish[1]))) weights(std::true_type{});
         else weights(std::false_type{});
       }
 

@@ -495,6 +495,24 @@ def test_scores_beyond_the_range():
                 assert ((c.out[b, i].double() - o).abs() <= (HALF16 + 1e-4 + HALF * HALF) * size + HALF * o.abs()).all(), f"sequence {b}, token {i}"
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (10, 2), (6, 2)])
+@pytest.mark.parametrize("other", [1e4, 1e7, 1e30, NAN])
+def test_rows_do_not_depend_on_their_neighbours(Hq, Hkv, other):
+    """Queries behind a sequence's last, and other rows of the tile, of any size: the same bits."""
+    def outputs(scale, first):
+        c = Case(57, [700, 90], n=30, counts=[17, 30], Hq=Hq, Hkv=Hkv, r_k=48, r_v=64, exponents=(-9, -4))
+        c.q[0, 17:] *= scale
+        c.q[1, :first] *= scale
+        c.attend(splits=1)
+        torch.cuda.synchronize()
+        assert c.status.item() == 0
+        return c.out[0, :17], c.lse[0, :17], c.out[1, 3:], c.lse[1, 3:]
+
+    for first in (0, 3):
+        for x, y in zip(outputs(1.0, 0), outputs(other, first)):
+            assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then
