@@ -487,7 +487,8 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       wm[w * 8 + gg] = fast_exp2((mw - M) + (ew - E)) * half;
       if (w == 0) {
         wl[gg] = half / den;
-        if (gg < ng) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, (N + log2f(den)) * kLn2);
+        // a sum that is not a number weighs more than any other, so that it is not passed over where parts are joined
+        if (gg < ng) __stcg(a.partial_lse + (size_t)slot_id * kGroupTile + gg, den == den ? (N + log2f(den)) * kLn2 : INFINITY);
       }
     }
     bar1(NT);

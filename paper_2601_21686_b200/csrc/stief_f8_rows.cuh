@@ -414,7 +414,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     for (int p = 0; p < lanes; ++p) {
       const int w = (p << lg) + g;
       const float mw = wm[w * 16 + r];
-      if (mw == -INFINITY) continue;                            // a lane that the row attends nothing of
+      if (mw == -INFINITY && wl[w * 16 + r] == 0.f) continue;   // a lane that the row attends nothing of (with scores that are all NaN the sum is NaN)
       const float f = fast_exp2((mw - M) + (we[w * 16 + r] - E));
       const float4 v = *reinterpret_cast<const float4*>(wo + (w * 16 + r) * WP + 4 * c);
       num.x = fmaf(v.x, f, num.x);

@@ -513,6 +513,24 @@ def test_rows_do_not_depend_on_their_neighbours(Hq, Hkv, other):
             assert torch.equal(x, y)
 
 
+def test_nan_queries_and_pages_of_nan_keys_are_not_passed_over():
+    """A query of NaN, or a page whose keys are NaN throughout, leaves no score to go by: the rows are NaN, the others what they were."""
+    for what in ("query", "page"):
+        for (c, call), (good, _) in zip(_forms(58, [700, 90]), _forms(58, [700, 90])):
+            call(good).check()
+            if what == "query":
+                c.q[0, -1, 1] = NAN
+            else:
+                c.layer.k_codes[int(c.batch.block_table[0, 3]), 0] = 0x7F
+            call(c)
+            torch.cuda.synchronize()
+            assert c.status.item() == 0 and torch.equal(c.out[1], good.out[1])
+            if what == "query":
+                assert torch.isnan(c.out[0, -1, 1]).all() and torch.equal(c.out[0, -1, 2:], good.out[0, -1, 2:]) and torch.equal(c.out[0, -1, 0], good.out[0, -1, 0])
+            else:
+                assert torch.isnan(c.out[0, :, :4]).all() and torch.equal(c.out[0, :, 4:], good.out[0, :, 4:])
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then
