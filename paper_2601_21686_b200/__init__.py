@@ -747,12 +747,17 @@ def _append_args(check, layer, batch, k, v, cu_seqlens, rotation, q, q_out, posi
     total, Hkv = k.shape[0], layer.Hkv
     kv = (*_token_rows(k, "k", total, Hkv, D_HEAD if layer.U_k is not None else layer.r_k, at),
           *_token_rows(v, "v", total, Hkv, D_HEAD if layer.U_v is not None else layer.r_v, at))
+    if total == 0:                                            # tensors of no tokens have no address, and the library wants one that it does not use
+        anywhere = _page_tensors(layer)[0].data_ptr()
+        kv = anywhere, kv[1], anywhere, kv[3]
     if (q is None) != (q_out is None):
         raise ValueError("q and q_out go together")
     qp, qs, op, os_ = None, 0, None, 0
     if q is not None:
         qp, qs = _token_rows(q, "q", total, layer.Hq, D_HEAD, at)
         op, os_ = _token_rows(q_out, "q_out", total, layer.Hq, D_HEAD, at)
+        if total == 0:
+            qp = op = anywhere
     B = batch.block_table.shape[0]
     if batch.block_table.dim() != 2:
         raise ValueError("block_table must be [B, max_pages_per_seq]")

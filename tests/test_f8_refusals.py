@@ -130,6 +130,22 @@ def append(layer, batch=None, k=None, v=None, cu=None, **kw):
 
 
 @pytest.mark.parametrize("make", [f8, plain])
+def test_append_binding_of_no_tokens(lib, calls, make):
+    """A step without new tokens: empty tensors have no address, which the entry points refuse.  What the binding hands over is taken."""
+    for kw in (dict(), dict(q=bf(0, 8, 128), q_out=bf(0, 8, 128)), dict(rotation=None)):
+        l = make()
+        append(l, k=bf(0, 2, 128), v=bf(0, 2, 128), **kw)
+        name, args = calls[-1]
+        assert args[9] == 0 and args[5] and args[7] and bool(args[3]) == bool(args[13]) == ("q" in kw)
+        c = args[0]._obj
+        for field in ("U_k", "U_v", "k_pool", "v_pool", "k_codes", "v_codes", "scales"):
+            if hasattr(c, field):
+                setattr(c, field, P)                             # (host memory need not be aligned)
+        aligned = lambda x: P if x else None  # noqa: E731
+        assert getattr(lib, name)(*args[:3], aligned(args[3]), args[4], aligned(args[5]), args[6], aligned(args[7]), *args[8:13], aligned(args[13]), *args[14:]) == S.STIEF_OK
+
+
+@pytest.mark.parametrize("make", [f8, plain])
 def test_append_binding(calls, make):
     wide = bf(5, 12, 128)
     append(make(), k=wide[:, 8:10], v=wide[:, 10:], q=wide[:, :8], q_out=bf(5, 8, 128), positions=i32(5))

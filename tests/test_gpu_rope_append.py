@@ -417,3 +417,9 @@ def test_memory_around_the_pools_is_left_alone(f8, where, lens, counts):
     c.call().check(status=S.STIEF_ERR_BOUNDS, skip_pages=gone)
     for big, front, back in around:
         assert torch.equal(big[:2], front) and torch.equal(big[-2:], back)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_no_tokens_at_all(f8):
+    Case(22, [5, 0, 70], [0, 0, 0], f8=f8).call().check()
+    Case(23, [5], [0], f8=f8, queries=False, rot=0).call().check()
