@@ -17,11 +17,14 @@ constexpr int kLowest = -100, kHighest = 119;    // exponents of a scale: codes 
 // exceed 2^kTopWeight, which is in the range of f16.
 // The sum of a row wants 2^x, and e may differ by 219 from page to page, so the sum l has a reference of its own, N, that goes by
 // scores alone: l counts 2^(x - N).  N is set to a page's largest score where that lies more than kSumGrown above it, so with pages of
-// 64 rows l stays below 2^(6 + 40) a page.  A page adds its sum of weights times 2^((M - N) + (E - e)).  Where its largest weight lies below 2^kSumLow,
+// 64 rows l stays below 2^(6 + 16) a page.  A page adds its sum of weights times 2^((M - N) + (E - e)).  Where its largest weight lies below 2^kSumLow,
 // they may vanish in the sum: it then takes exponentials that go by the page's own largest (in the mix, whose f16 weights end at 2^-24,
-// the page is nothing).
+// the page is nothing), unless its scores lie kSumSeen below M, which is in the sum: even 2^25 positions are nothing to that.  So scores
+// alone, however far apart, do not lead there.
 constexpr float kNoSum = -3.402823466e38f;       // N before anything was seen
-constexpr float kTopWeight = 15.f, kSumGrown = 40.f, kSumLow = -80.f;
+constexpr float kTopWeight = 15.f, kSumGrown = 16.f, kSumLow = -80.f, kSumSeen = -72.f;
+__device__ __forceinline__ bool may_vanish(float beyond, float above) { return above < kSumLow && beyond > kSumSeen; }       // x - M, log2 of a weight
+
 // e of a scale 2^e, as a float and without a conversion, which would take a turn on the pipe of the exponentials
 __device__ __forceinline__ float scale_exponent(float scale) { return __uint_as_float(0x4b000000u | ((__float_as_uint(scale) >> 23) & 255u)) - 8388735.f; }
 // What turns a product of normalised queries and codes into a score.  Large queries over large scales leave fp32's range: a score is

@@ -362,9 +362,10 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const float above = (top - m) + (evf - em);          // log2 of the page's largest weight (infinity: nothing seen before)
+      const float beyond = top - m, above = beyond + (evf - em);       // (above: log2 of the page's largest weight; infinity: nothing seen before)
+      const bool vanish = may_vanish(beyond, above);
       // seldom after a sequence's first pages: the references grow, or the page's weights may vanish in the sum
-      if (__any_sync(0xffffffffu, above > kTopWeight || above < kSumLow || top > n + kSumGrown)) {
+      if (__any_sync(0xffffffffu, above > kTopWeight || vanish || top > n + kSumGrown)) {
         const bool grown = above > kTopWeight;
         const float alpha = grown ? fast_exp2(kTopWeight - above) : 1.f;
         const float a0 = __shfl_sync(0xffffffffu, alpha, 8 * tid4), a1 = __shfl_sync(0xffffffffu, alpha, 8 * tid4 + 4);
@@ -383,7 +384,7 @@ decode_f8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           l *= fast_exp2(n - top);
           n = top;
         }
-        if (above < kSumLow && top > -INFINITY) {
+        if (vanish) {
           float own = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) own += fast_exp2(x[i] - top);

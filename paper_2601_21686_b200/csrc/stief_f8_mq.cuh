@@ -698,7 +698,7 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
         bool vanish[2];
         {
           // log2 of each page's largest weight (infinity: the row has attended nothing before)
-          float above[2] = {(x_page[0] - m) + (e0 - em), (x_page[1] - m) + (e1 - em)};
+          float beyond[2] = {x_page[0] - m, x_page[1] - m}, above[2] = {beyond[0] + (e0 - em), beyond[1] + (e1 - em)};
           const float most = fmaxf(above[0], above[1]);
           const bool grown = jo == 0 || most > f8::kTopWeight;
           if (jo > 0) moved = __any_sync(0xffffffffu, grown);
@@ -707,17 +707,19 @@ f8_mq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CU
             r = fast_exp2(kHeadroomLog2 - most);
             m = second ? x_page[1] : x_page[0];                 // -inf when a part of a split range begins behind the row's position
             em = (second ? e1 : e0) - kHeadroomLog2;
-            above[0] = (x_page[0] - m) + (e0 - em);
-            above[1] = (x_page[1] - m) + (e1 - em);
+            beyond[0] = x_page[0] - m;
+            beyond[1] = x_page[1] - m;
+            above[0] = beyond[0] + (e0 - em);
+            above[1] = beyond[1] + (e1 - em);
           }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) vanish[h] = above[h] < f8::kSumLow && x_page[h] > -INFINITY;
+          for (int h = 0; h < 2; ++h) vanish[h] = f8::may_vanish(beyond[h], above[h]);
         }
         const float ref = m > -INFINITY ? m : 0.f;
-        const float x_top = fmaxf(x_page[0], x_page[1]);
-        if (x_top > n_ref + f8::kSumGrown) {
-          l *= fast_exp2(n_ref - x_top);
-          n_ref = x_top;
+        {
+          const float x_top = fmaxf(x_page[0], x_page[1]), n_old = n_ref;
+          n_ref = x_top > n_ref + f8::kSumGrown ? x_top : n_ref;
+          l *= fast_exp2(n_old - n_ref);
         }
         // Exponents as one fma with (e - E) - M where that is good to 2^-14; with scores far from zero (references beyond 2^10) the
         // rounded x is what counts, less M, then the scales.  That form also serves pages whose weights vanish: exponentials by the page's

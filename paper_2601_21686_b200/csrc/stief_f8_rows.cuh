@@ -273,7 +273,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     }
     const float evf = f8::scale_exponent(vs);
     float above[2], tops[2];
-    bool seldom = false;
+    bool vanish[2], seldom = false;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const float f = f8::score_factor(fac[e], ks);
@@ -290,8 +290,10 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       tops[e] = top;
-      above[e] = (top - m[e]) + (evf - em[e]);
-      seldom |= above[e] > f8::kTopWeight || above[e] < f8::kSumLow || top > n[e] + f8::kSumGrown;
+      const float beyond = top - m[e];
+      above[e] = beyond + (evf - em[e]);
+      vanish[e] = f8::may_vanish(beyond, above[e]);
+      seldom |= above[e] > f8::kTopWeight || vanish[e] || top > n[e] + f8::kSumGrown;
     }
     if (__any_sync(0xffffffffu, seldom)) {
 #pragma unroll
@@ -314,7 +316,7 @@ f8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
           l[e] *= fast_exp2(n[e] - tops[e]);
           n[e] = tops[e];
         }
-        if (above[e] < f8::kSumLow && tops[e] > -INFINITY) {
+        if (vanish[e]) {
           float own = 0.f;
 #pragma unroll
           for (int t = 0; t < 16; ++t) own += fast_exp2(x[e][t] - tops[e]);
