@@ -531,6 +531,22 @@ def test_nan_queries_and_pages_of_nan_keys_are_not_passed_over():
                 assert torch.isnan(c.out[0, :, :4]).all() and torch.equal(c.out[0, :, 4:], good.out[0, :, 4:])
 
 
+@pytest.mark.parametrize("splits", [1, 2, 4])
+@pytest.mark.parametrize("other", [1e4, 1e30, NAN])
+def test_few_rows_do_not_depend_on_their_neighbours(splits, other):
+    def outputs(scale):
+        c = Case(59, [700, 90], n=8, counts=[5, 8], exponents=(-9, -4))
+        c.q[0, 5:] *= scale
+        c.q[1, :3] *= scale
+        c.attend(splits=splits)
+        torch.cuda.synchronize()
+        assert c.status.item() == 0
+        return c.out[0, :5], c.lse[0, :5], c.out[1, 3:], c.lse[1, 3:]
+
+    for x, y in zip(outputs(1.0), outputs(other)):
+        assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------------------------------------- together
 def test_prompt_chunks_and_decode_in_one_run():
     """What a server does with one layer: prompts appended (rotated) and attended in chunks, pages reserved, a sequence forked, then
