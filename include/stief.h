@@ -478,8 +478,9 @@ int stief_rope_append(const stief_layer* layer, const stief_batch* batch, const 
 /* ---- compressed cache in 8-bit floating point, one scale for each page and KV head -------------------------------
  * k_codes [num_pages][Hkv][64][r_k] and v_codes [num_pages][Hkv][64][r_v] hold e4m3 values, indexed like the bf16 pools;
  * scales [num_pages][Hkv][4] fp32 holds for each page and KV head (key scale, value scale, unused, unused); a code c stands for
- * c * scale.  Scales are powers of two, 2^e with e in -100 .. 119: the least that brings the block's largest magnitude to
- * at most 448.  An element then keeps 4 significant bits whatever its channel's share of the block (down to 2^-13 of the
+ * c * scale.  Scales are powers of two, 2^e with e in -100 .. 119: the least that brings the largest magnitude that the block has
+ * held since its row 0 was written to at most 448 (rows that were taken back, as those of a rejected draft, leave it raised, and
+ * the older rows rounded as it left them).  An element then keeps 4 significant bits whatever its channel's share of the block (down to 2^-13 of the
  * block's largest magnitude), and a page whose scale has to grow when a larger row joins it has its older rows moved to
  * the new scale by their exponents alone (only values below 2^-6 of the new scale are rounded again).  NaN and infinities
  * are stored as NaN and leave the scale alone.
@@ -499,7 +500,7 @@ typedef struct stief_f8layer {
 
 /* stief_rope_append into the 8-bit cache (rotation NULL: a plain append).  The rows are quantised from fp32, not rounded to
  * bf16 first.  A page whose row 0 is written starts a new scale; otherwise rows 0 .. up to the first new one are the page's
- * older rows. */
+ * older rows.  (Nothing attends a tree in this cache, nor moves its accepted rows: drafts are verified as runs.) */
 int stief_f8_append(const stief_f8layer* layer, const stief_batch* batch, const stief_rotation* rotation, const uint16_t* q,
                     int64_t q_stride_t, const uint16_t* k, int64_t k_stride_t, const uint16_t* v, int64_t v_stride_t,
                     int32_t total_tokens, const int32_t* cu_seqlens, const int32_t* positions, int32_t ends_at_len,
@@ -507,17 +508,25 @@ int stief_f8_append(const stief_f8layer* layer, const stief_batch* batch, const 
 
 /* Decode attention over the 8-bit cache, one query token per sequence: arguments, workspace (stief_decode_workspace_bytes
  * with the same r_v), flags and empty sequences as in stief_decode_attention; out must not be NULL.  With U_k NULL q has r_k
- * elements per head, with U_v NULL out has r_v. */
+ * elements per head, with U_v NULL out has r_v.  q' = q U_k passes through f16 as two terms (22 bits of the row's largest), the
+ * weights once: with its page's value scale a weight keeps 11 bits down to 2^-29 of the row's largest and is nothing in the mix below
+ * 2^-40; the row's sum counts every weight in fp32, whatever scales the pages have.  Scores (scaled, base 2) may be as large as
+ * fp32 holds; parts are joined through their log-sum-exps in fp32, which from 2^20 on say less and less about how many tokens a
+ * part has.  A query of NaN gives a row of NaN (its log-sum-exp is -infinity). */
 int stief_f8_decode_attention(const stief_f8layer* layer, const stief_batch* batch, const uint16_t* q, int32_t len_add,
                               void* workspace, size_t workspace_bytes, int32_t num_parts, uint16_t* out, float* out_lse,
                               uint32_t flags, int32_t* status, void* stream);
 
 /* Several causal query rows per head over the 8-bit cache: arguments as stief_mq_attention, for any number of query heads per
  * KV head up to 128, and strides in either order (a batch stride below the token stride).  num_splits: 1 .. 32, from
- * stief_f8_mq_num_splits, which weighs rounds of the GPU's SMs against what joining parts costs; with more than one part, up to
- * 64 rows per KV head (n_q Hq / Hkv) take a kernel of their own, and at least two are proposed for them.  The workspace may
- * hold anything and is used by one call at a time.  q' = q U_k and the probabilities pass through f16, each row scaled by a
- * power of two of its own.  A NaN among a sequence's cached values reaches rows that attend its position, and may reach rows of
+ * stief_f8_mq_num_splits, which weighs rounds of the GPU's SMs against what joining parts costs for sequences of
+ * max_pages_per_seq pages: where the table is wider than the longest sequence, that sequence's pages say more.  With more than
+ * one part, up to 64 rows per KV head (n_q Hq / Hkv) take a kernel of their own, and from 8 pages on at least two are proposed for
+ * them; in one part a call of few rows over long sequences leaves most SMs idle (8 tokens over 4 x 32768: 394 us in one part, 59
+ * in the proposed four).  The workspace may hold anything and is used by one call at a time.  q' = q U_k and the probabilities
+ * pass through f16 once, each row scaled by a power of two of its own: 11 bits of an element of q', and of a weight (with its
+ * page's value scale) down to 2^-21 of the row's largest at least; below 2^-32 one may be nothing in the mix, but is part of the
+ * row's sum.  A row's bits do not depend on what the other rows hold.  A NaN among a sequence's cached values reaches rows that attend its position, and may reach rows of
  * the call up to 127 positions before it; rows behind seq_lens do not count, whatever they hold. */
 int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, int32_t Hkv, int32_t max_pages_per_seq);
 size_t stief_f8_mq_workspace_bytes(int32_t B, int32_t n_q, int32_t Hq, int32_t r_v, int32_t num_splits);

@@ -98,7 +98,8 @@ extern "C" int32_t stief_f8_mq_num_splits(int32_t B, int32_t n_q, int32_t Hq, in
     return (int32_t)std::min(most, std::max(2ll, sm_count() / base));
   // Microseconds as measured, within a fifth: a round of units costs 10 and 2.25 for two pages (tiles of the same rows share a unit's
   // pages); joined parts cost 12, 0.4 per thousand rows and part and 0.3 for each part of a row.  One sequence, ranks 64/64, 1 / 2 / 4
-  // parts: 512 tokens over 8192 130 / 92 / 106, 2048 over 4096 126 / 185 / -, 256 over 4096 74 / 55 / 43.
+  // parts: 512 tokens over 8192 136 / 94 / 107, 2048 over 4096 132 / 190 / -, 256 over 4096 72 / 53 / 41.  The constants are those of 64/64
+  // for all ranks, and every sequence counts as long as the longest that the caller names.
   double best = 0.;
   long long s = 1;
   for (long long i = 1; i <= most; ++i) {

@@ -19,9 +19,9 @@
 // With 64 tokens per warp and page a page's chain of dependent steps (load, product, maximum, exponential, product) is
 // paid once per 8 KiB at ranks 64/64 and hidden behind seven other warps.
 //
-// Measured (32 query heads over 8): 4 x 32768 tokens 24 us at ranks 32/32, 27 at 48/64, 32 at 64/64 (4.1 TB/s; 27 where calls may overlap),
-// 51 at 96/128, 59 at 128/128.  Every further 134 MB take 19 to 20 us (6.7 to 7 TB/s): what is left is 12 us from launch to the end
-// of the combine, of which overlapped calls hide half.  1 x 1021 tokens: 10.6 us, 4.8 overlapped.
+// Measured (32 query heads over 8): 4 x 32768 tokens 24 us at ranks 32/32, 28 at 48/64, 31 at 64/64 (4.4 TB/s; 26 where calls may overlap),
+// 52 at 96/128, 60 at 128/128.  Every further 134 MB take 19 to 21 us (6.4 to 7.1 TB/s): what is left is 12 us from launch to the end
+// of the combine, of which overlapped calls hide half.  1 x 1021 tokens: 10.3 us, 4.7 overlapped.
 #pragma once
 
 #include "stief_decode.cuh"

@@ -1,5 +1,5 @@
-// Instantiations of the decode kernel, and of the one for a few query rows, over the 8-bit floating-point cache for one key rank (STIEF_RK, given on the command line)
-// and every value rank.  Compiled once per key rank so the build parallelises.
+// Instantiations of the decode kernel, and of the one for a few query rows, over the 8-bit floating-point cache for one key
+// rank (STIEF_RK, given on the command line) and every value rank.  Compiled once per key rank so the build parallelises.
 #include "stief_f8_decode.cuh"
 #include "stief_f8_rows.cuh"
 #include "stief_host_util.h"

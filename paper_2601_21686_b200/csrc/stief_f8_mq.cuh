@@ -24,11 +24,12 @@
 //   warps 4-11    softmax and epilogue, four per tile; thread = row = TMEM lane
 //   warps 12-15   fill the ring of operands: expand the pages; raw queries, U_k and U_v come straight into it by TMA
 // TMEM, per tile 256 columns: scores 0-127 (also Q' at the start of a unit and OUT at its end), P 128-191 and O 192-255, or O 128-255.
-// Measured (32 query heads over 8): 2048 tokens over 16384 at ranks 64/64 541 us with scales that vary from page to page and 522 with one
-// (480 and 500 TFLOP/s), 96/128 553, 128/128 560 (930); 512 over 8192 93 (two parts), 256 over 4096 44 (four).  A step of two pages
-// for both tiles takes 2.1 to 2.3 us: the softmax of 2 x 128 x 128 scores, half of it on the special-function units, then the waits
-// between the roles; the tensor pipe is busy for a fifth (64/64) to two fifths of it.  A unit costs another 8 to 10 us for its queries,
-// its first page and its epilogue.
+// Measured (32 query heads over 8): 2048 tokens over 16384 at ranks 64/64 553 to 563 us with scales that vary from page to page and 525
+// with one (465 and 495 TFLOP/s), 96/128 592 and 558, 128/128 617 and 582 (893); 512 over 8192 94 (two parts), 256 over 4096 41 (four).
+// A step of two pages for both tiles takes 2.1 to 2.4 us: the softmax of 2 x 128 x 128 scores, half of it on the special-function units,
+// then the waits between the roles; the tensor pipe is busy for a fifth (64/64) to two fifths of it.  A unit costs another 8 to 10 us for its
+// queries, its first page and its epilogue.  (Scores with a standard deviation of 72 in base 2 move the accumulators in most steps: 580,
+// 694 and 886 us.)
 // Every wait is bounded (see mbar_wait): on a timeout the status word says so, later waits return at once, every role walks
 // to the end of its loops and TMEM is released.
 #pragma once

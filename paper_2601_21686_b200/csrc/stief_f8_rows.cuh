@@ -11,9 +11,9 @@
 //            O^T = V^T P^T with two groups of 8 rows as the columns of P^T
 // The parts' mixes, sums and references are merged by f8_mq_combine_kernel.
 //
-// Measured with that kernel (4 x 32768 tokens, 32 query heads over 8): ranks 64/64 4 / 8 / 16 tokens 41 / 61 / 102 us, 128/128 8 tokens 104.  Two
-// warps that read the same page convert it twice, which sets the pace from 32 rows on; 32 rows in one warp ran at 75 us where 16 in two ran
-// at 68 (registers, half the warps to hide a page's chain), and the tensor-core kernel at 127.
+// Measured with that kernel (4 x 32768 tokens, 32 query heads over 8, four parts): ranks 64/64 4 / 8 / 16 tokens 38 / 59 / 100 us, 128/128
+// 8 tokens 100.  Two warps that read the same page convert it twice, which sets the pace from 32 rows on; 32 rows in one warp ran at 75 us where
+// 16 in two ran at 68 (registers, half the warps to hide a page's chain), and the tensor-core kernel at 127.
 #pragma once
 
 #include "stief_f8_decode.cuh"

@@ -22,7 +22,7 @@
 // grows, the same CTA moves the older rows' codes.
 //
 // Measured (32 query heads over 8; 17600 tokens of 8 prompts): bf16 64/64 98 us (3.9 TB/s of inputs and outputs), 128/128 118;
-// 8-bit 32/32 116, 64/64 118, 96/128 144, 128/32 152.  One token 5.5 to 6.2 us, 64 sequences of one token 6.7 and (8-bit) 8.8.  What
+// 8-bit 32/32 117, 64/64 118, 96/128 144, 128/32 156.  One token 5.5 to 6.2 us, 64 sequences of one token 6.7 and (8-bit) 8.8.  What
 // bounds the large calls is the chain of a tile (rotate, multiply, settle the scale, stage) with two CTAs per SM to hide it, not the
 // memory; its rounds of a 96-channel 8-bit key tile take 1300 (raw rows), 2700, 5600, 1800 and 2400 cycles.
 #include <type_traits>
