@@ -90,7 +90,8 @@ __device__ __forceinline__ Unit block_unit(const mq::Args& a, int u, int TT) {
 
 // The units that hold work, longest sequences first and the latest query tokens of each first, so that CTAs get equal numbers of
 // them: in a ragged batch many of the units that n_q allows for are empty.  Kept in shared memory for up to kListed sequences;
-// beyond, units are taken as they are numbered, empty ones among them.
+// beyond, units are taken as they are numbered, empty ones among them (up to 512 query tokens in every 16th sequence of up to 2048, up to
+// 30 in the others: 96 sequences 250 us, 97 323).
 struct Work {
   const int* first;              // [B + 1], by place in the order: pairs of tiles before it
   const uint16_t* order;         // [B]: the sequence at a place
